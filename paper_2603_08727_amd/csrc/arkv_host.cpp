@@ -23,6 +23,7 @@ static int hip_fail(hipError_t e, const char* what) {
   (void)hipGetLastError();
   return ARKV_EHIP;
 }
+namespace arkv { int hip_failure(hipError_t e, const char* what) { return hip_fail(e, what); } }
 #define HIP_TRY(expr)                                   \
   do {                                                  \
     hipError_t e_ = (expr);                             \

@@ -1,0 +1,422 @@
+"""GPU tests of the operators around a paged cache against plain 64-bit forms (tests/paged_ref.py)."""
+import math
+
+import pytest
+import torch
+
+from paper_2603_08727_amd import paged as P
+import paged_ref as R
+
+pytestmark = pytest.mark.gpu
+BF, FP = torch.bfloat16, torch.float16
+
+
+def handles(s, max_q=None, max_kv=None):
+    pages = P.arkv_pages(s.k, s.v, s.pos, s.weight)
+    batch = P.arkv_page_batch(s.cu_q, s.kv_len, s.table, s.n, s.max_q if max_q is None else max_q, s.max_kv if max_kv is None else max_kv)
+    return pages, batch, P.arkv_paged_workspace(pages, batch, s.hq)
+
+
+def attend(s, **kw):
+    pages, batch, ws = handles(s)
+    ws.fill_(0xFF)                                     # what a workspace holds does not matter
+    out = torch.full((s.n, s.hq, s.d), 7.0, dtype=s.dtype, device="cuda")
+    lse = torch.full((s.n, s.hq), 7.0, device="cuda")
+    P.arkv_paged_attention(pages, batch, s.q, s.scale, out, lse=lse, workspace=ws, **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def check_attention(s, **kw):
+    out, lse = attend(s, **kw)
+    ref, rl, tol, ltol = R.attention(s, **kw)
+    n = sum(s.q_len)
+    R.close(out[:n], ref[:n], tol[:n], "out")
+    R.close(lse[:n], rl[:n], ltol[:n], "lse")
+    assert (out[n:] == 7).all() and (lse[n:] == 7).all()      # rows of no sequence are left alone
+    return out, lse
+
+
+def slopes_of(s):
+    sl = 2.0 ** (-8.0 * (torch.arange(s.hq, device="cuda", dtype=torch.float32) + 1) / s.hq)
+    qp = torch.cat([torch.arange(t - a, t, device="cuda", dtype=torch.int32) * 2 + 1 for a, t in zip(s.q_len, s.kv_len_list)] +
+                   [torch.zeros(s.n - sum(s.q_len), device="cuda", dtype=torch.int32)])
+    return sl, qp
+
+
+STEPS = [((1,), (1,)), ((1,), (2,)), ((1,), (15,)), ((1,), (16,)), ((1,), (17,)), ((1, 1, 1), (63, 64, 65)), ((1, 1), (1000, 31)),
+         ((1, 0, 1, 1), (129, 0, 513, 2)), ((1,) * 9, (5, 700, 33, 1, 2049, 64, 96, 128, 300))]
+CHUNKS = [((2,), (2,)), ((3,), (50,)), ((16, 1), (16, 40)), ((17,), (17,)), ((33, 0, 5), (64, 0, 5)), ((64,), (1000,)), ((129, 1, 77), (300, 1025, 77)),
+          ((300,), (2100,)), ((5, 1, 1, 40), (900, 3, 700, 41)), ((257,), (257,))]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("hq,hkv,d,page", [(8, 2, 64, 16), (8, 2, 128, 32), (3, 3, 128, 16), (12, 4, 64, 64), (16, 1, 64, 128), (10, 2, 128, 16),
+                                           (16, 2, 128, 256)])
+@pytest.mark.parametrize("i", range(len(STEPS)))
+def test_steps_of_single_tokens(i, hq, hkv, d, page, dtype):
+    q, kv = STEPS[i]
+    check_attention(R.problem("cuda", dtype, hq, hkv, d, page, q, kv, seed=i, fused=bool(i & 1)))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("hq,hkv,d,page", [(8, 2, 64, 16), (4, 1, 128, 32), (3, 3, 128, 16), (12, 4, 64, 64), (16, 1, 64, 1024), (7, 1, 128, 16)])
+@pytest.mark.parametrize("i", range(len(CHUNKS)))
+def test_chunks(i, hq, hkv, d, page, dtype):
+    q, kv = CHUNKS[i]
+    check_attention(R.problem("cuda", dtype, hq, hkv, d, page, q, kv, seed=i, fused=bool(i & 1), extra_tokens=i % 3))
+
+
+@pytest.mark.parametrize("kind", ["cap", "distance", "prefix", "cap+distance", "cap+prefix", "distance+prefix", "all"])
+@pytest.mark.parametrize("i,q,kv", [(0, (1, 1, 1), (40, 700, 1)), (1, (60, 1, 130), (61, 800, 400)), (2, (200,), (1500,))])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(BF, 8, 2, 128), (FP, 12, 4, 64), (FP, 4, 4, 128), (BF, 8, 1, 64)])
+def test_scores(kind, i, q, kv, dtype, hq, hkv, d):
+    s = R.problem("cuda", dtype, hq, hkv, d, 16, q, kv, seed=10 + i, hot=6.0)
+    kw = {}
+    if "cap" in kind or kind == "all":
+        kw["cap"] = 3.5
+    if "distance" in kind or kind == "all":
+        kw["slopes"], kw["q_pos"] = slopes_of(s)
+    if "prefix" in kind or kind == "all":
+        pre = [min(t, t - a + (2 * a) // 3) for a, t in zip(q, kv)]
+        pre[0] = kv[0] + 9                              # longer than what is cached: cut
+        if len(pre) > 1:
+            pre[1] = -4 if i else 3                     # nothing beyond the causal ones
+        kw["prefix"] = torch.tensor(pre, dtype=torch.int32, device="cuda")
+    check_attention(s, **kw)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("q,kv", [((4,), (1,)), ((1, 3, 40), (0, 1, 7)), ((100, 2), (30, 0)), ((200, 1), (90, 600))])
+def test_rows_that_see_nothing(q, kv, dtype):
+    """More new tokens than slots: the first have none and see nothing (or the prefix alone)."""
+    s = R.problem("cuda", dtype, 8, 2, 64, 16, q, kv, seed=3)
+    out, lse = check_attention(s)
+    lost = max(0, q[0] - kv[0])
+    assert (out[:lost] == 0).all() and (lse[:lost] == -math.inf).all()
+    s = R.problem("cuda", dtype, 8, 2, 64, 16, q, kv, seed=3)
+    check_attention(s, prefix=torch.tensor([1] * len(q), dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (FP, 128), (BF, 128)])
+@pytest.mark.parametrize("q", [1, 5, 150])
+def test_absent_pages(q, dtype, d):
+    s = R.problem("cuda", dtype, 8, 2, d, 16, (q, min(q, 20)), (700, 90), seed=4)
+    s.table[0, 0], s.table[0, 5], s.table[0, 6], s.table[1, 2] = -1, s.n_pages, 2 ** 31 - 1, -2 ** 31
+    check_attention(s)
+    s.table[1, :] = -1                                 # a sequence whose pages are all gone
+    out, lse = check_attention(s)
+    assert (lse[q:] == -math.inf).all() and (out[q:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("q,kv", [((40,), (100,)), ((150,), (333,)), ((2,), (70,))])
+def test_unseen_rows_have_no_influence(q, kv, what, dtype):
+    """Keys and values of the last new token are no numbers: only its own row, which sees them, may show it."""
+    s = R.problem("cuda", dtype, 8, 2, 64, 16, q, kv, seed=5)
+    clean, clean_lse = attend(s)
+    last = kv[0] - 1
+    page = int(s.table[0, last // 16])
+    s.v[page, :, last % 16, 3] = what
+    s.v[page, 0, last % 16, 40] = what
+    out, lse = check_attention(s)
+    assert torch.equal(out[:-1], clean[:-1]) and torch.equal(lse, clean_lse)
+    s.k[page, :, last % 16] = math.nan
+    out, lse = attend(s)
+    assert torch.equal(out[:-1], clean[:-1]) and torch.equal(lse[:-1], clean_lse[:-1])
+    assert torch.isnan(out[-1]).all() and torch.isnan(lse[-1]).all()
+
+
+@pytest.mark.parametrize("q,kv", [((1,), (5000,)), ((70,), (3000,))])
+def test_values_that_are_seen_but_no_numbers_reach_their_channel_alone(q, kv):
+    s = R.problem("cuda", BF, 8, 2, 128, 16, q, kv, seed=6)
+    page = int(s.table[0, 10])
+    s.v[page, 1, 3, 77] = math.inf
+    out, _ = attend(s)
+    bad = ~torch.isfinite(out.float())
+    want = torch.zeros_like(bad)
+    want[:, 4:, 77] = True
+    assert torch.equal(bad, want)
+
+
+@pytest.mark.parametrize("q", [1, 90])
+def test_extreme_logits(q):
+    """Rows whose logits reach thousands, and rows of equal logits."""
+    s = R.problem("cuda", BF, 8, 2, 128, 16, (q, q), (900, 333), seed=7, hot=300.0)
+    check_attention(s)
+    s.q.zero_()
+    check_attention(s)
+    s = R.problem("cuda", BF, 8, 2, 128, 16, (q,), (900,), seed=8, hot=200.0)
+    s.scale = -s.scale
+    check_attention(s)
+
+
+@pytest.mark.parametrize("q,kv,hq,hkv", [((1, 1), (20001, 70001), 8, 1), ((500,), (9000,), 8, 2), ((1, 600, 1), (40000, 4001, 7), 4, 2)])
+def test_long_caches(q, kv, hq, hkv):
+    check_attention(R.problem("cuda", BF, hq, hkv, 128, 64, q, kv, seed=9))
+    s = R.problem("cuda", FP, hq, hkv, 64, 64, q, kv, seed=9)
+    sl, qp = slopes_of(s)
+    check_attention(s, slopes=sl, q_pos=qp)
+
+
+def test_offsets_beyond_32_bits():
+    """A pool of more than 4 GiB, its last pages in use."""
+    n_pages, hkv, page, d = 40000, 8, 64, 128
+    small = R.problem("cuda", BF, 16, hkv, d, page, (3, 1), (200, 130), seed=11)
+    k = torch.empty((n_pages, hkv, page, d), dtype=BF, device="cuda")
+    v = torch.empty_like(k)
+    base = n_pages - small.n_pages
+    k[base:], v[base:] = small.k, small.v
+    out, lse = attend(small)
+    pos = torch.zeros((n_pages, hkv, page), dtype=torch.int32, device="cuda")
+    weight = torch.zeros((n_pages, hkv, page), device="cuda")
+    pos[base:], weight[base:] = small.pos, small.weight
+    big = R.problem("cuda", BF, 16, hkv, d, page, (3, 1), (200, 130), seed=11)
+    big.k, big.v, big.pos, big.weight, big.n_pages = k, v, pos, weight, n_pages
+    big.table = torch.where(small.table >= 0, small.table + base, small.table)
+    o2, l2 = attend(big)
+    assert torch.equal(out, o2) and torch.equal(lse, l2)
+    for s in (small, big):
+        pages, batch, ws = handles(s)
+        P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=0.5, workspace=ws)
+        new = torch.randn(s.n, hkv, d, generator=torch.Generator().manual_seed(1)).to(BF).cuda()
+        P.arkv_paged_append(pages, batch, P.arkv_rotary(None), None, new, new, torch.arange(s.n, dtype=torch.int32, device="cuda")[None], None)
+    assert torch.equal(big.weight[base:].nan_to_num(9.0), small.weight.nan_to_num(9.0))
+    assert torch.equal(big.k[base:].float().nan_to_num(9.0), small.k.float().nan_to_num(9.0))
+    dst = torch.tensor([[0, 1], [2, 3]], dtype=torch.int32, device="cuda")
+    kept, lens = torch.empty((2, hkv, 100), dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    P.arkv_paged_evict(P.arkv_pages(big.k, big.v, big.pos, big.weight), handles(big)[1], torch.tensor([100, 100], dtype=torch.int32, device="cuda"),
+                       dst, kept, lens)
+    ref, _ = R.evict(big, [100, 100], 4, 32, 100)
+    assert torch.equal(kept.cpu(), ref)
+    old = R.rows(big, big.k, 0, 7)[0]
+    assert torch.equal(big.k[0, 7], old[kept[0, 7, :64].long()])
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("hq,hkv,d,page", [(8, 2, 64, 16), (8, 2, 128, 64), (3, 3, 128, 16), (12, 4, 64, 32), (16, 1, 128, 16)])
+@pytest.mark.parametrize("i", range(6))
+def test_weights(i, hq, hkv, d, page, dtype):
+    q, kv = [((1,), (1,)), ((1, 1, 0, 1), (64, 700, 0, 33)), ((33, 1, 90), (400, 1025, 90)), ((300,), (2100,)), ((40, 3), (7, 0)), ((130,), (130,))][i]
+    s = R.problem("cuda", dtype, hq, hkv, d, page, q, kv, seed=20 + i, fused=bool(i & 1), extra_tokens=i % 2)
+    _, lse = attend(s)
+    pages, batch, ws = handles(s)
+    ws.fill_(0xFF)
+    for decay, other in [(1.0, False), (0.0, False), (0.75, True)]:
+        carried = torch.rand_like(s.weight) if other else s.weight.clone()
+        ref, tol = R.weights(s, lse, decay, carried)
+        P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=decay, carried=carried if other else None, workspace=ws)
+        R.close(s.weight, ref, tol, "weight")
+
+
+@pytest.mark.parametrize("kind", ["cap", "distance", "prefix", "all"])
+@pytest.mark.parametrize("q,kv", [((1, 1), (40, 700)), ((60, 1, 130), (61, 800, 400))])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(BF, 8, 2, 128), (FP, 12, 4, 64), (BF, 8, 1, 64)])
+def test_weights_of_scores(kind, q, kv, dtype, hq, hkv, d):
+    s = R.problem("cuda", dtype, hq, hkv, d, 16, q, kv, seed=30, hot=4.0)
+    kw = {}
+    if kind in ("cap", "all"):
+        kw["cap"] = 3.5
+    if kind in ("distance", "all"):
+        kw["slopes"], kw["q_pos"] = slopes_of(s)
+    if kind in ("prefix", "all"):
+        kw["prefix"] = torch.tensor([min(t, t - a + (2 * a) // 3) for a, t in zip(q, kv)], dtype=torch.int32, device="cuda")
+    _, lse = attend(s, **kw)
+    pages, batch, ws = handles(s)
+    ref, tol = R.weights(s, lse, 1.0, s.weight, **kw)
+    P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, workspace=ws, **kw)
+    R.close(s.weight, ref, tol, "weight")
+
+
+def test_weights_of_a_step_sum_to_the_tokens_and_heads():
+    s = R.problem("cuda", BF, 8, 2, 128, 16, (50, 1), (333, 1000), seed=31)
+    _, lse = attend(s)
+    pages, batch, ws = handles(s)
+    P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=0.0, workspace=ws)
+    for b, q in enumerate((50, 1)):
+        for h in range(2):
+            assert abs(float(R.rows(s, s.weight, b, h)[0].double().sum()) - 4 * q) < 1e-3 * q
+
+
+def test_absent_pages_and_unseen_rows_in_weights():
+    s = R.problem("cuda", BF, 8, 2, 64, 16, (5,), (300,), seed=32)
+    s.table[0, 3] = -1
+    _, lse = attend(s)
+    pages, batch, ws = handles(s)
+    page = int(s.table[0, 299 // 16])
+    s.k[page, :, 299 % 16] = math.nan                  # the last token's key: the rows before it do not see it
+    ref, tol = R.weights(s, lse, 1.0, s.weight)
+    P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, workspace=ws)
+    assert torch.isnan(s.weight[page, :, 299 % 16]).all()
+    ref[page, :, 299 % 16] = math.nan
+    R.close(s.weight, ref, tol, "weight")
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (FP, 64)])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("axes,rot", [(1, None), (3, None), (2, 32), (4, 48), (1, 0)])
+@pytest.mark.parametrize("q,kv", [((1,), (1,)), ((1, 0, 1), (17, 0, 300)), ((33, 5, 100), (40, 5, 250))])
+def test_append(q, kv, axes, rot, adjacent, dtype, d):
+    s = R.problem("cuda", dtype, 6, 3, d, 16, q, kv, seed=40, extra_tokens=2, fused=True)
+    rot = d if rot is None else rot
+    half = rot // 2
+    g = torch.Generator().manual_seed(1)
+    freq = (500000.0 ** (-torch.arange(half, dtype=torch.float64) / max(half, 1))).cuda()
+    axis = [i % axes for i in range(half)]
+    positions = torch.randint(0, 200000, (axes, s.n), generator=g, dtype=torch.int32)
+    positions[0, 0] = 2 ** 31 - 1
+    positions = positions.cuda()
+    kv_new = torch.randn(s.n, 9, d, generator=g).to(dtype).cuda()
+    kn, vn = kv_new[:, 1:7:2], kv_new[:, 6:]           # strided heads
+    pages, batch, _ = handles(s)
+    before = {n: getattr(s, n).clone() for n in ("k", "v", "pos", "weight")}
+    q_out = torch.full((s.n, 6, d), 7.0, dtype=dtype, device="cuda")
+    P.arkv_paged_append(pages, batch, P.arkv_rotary(freq if half else None, axis, axes, adjacent), s.q, kn, vn, positions, q_out)
+    n = sum(q)
+    (rq, tq), (rk, tk) = (R.rotate(x, positions, freq, axis, adjacent) for x in (s.q, kn))
+    R.close(q_out[:n], rq[:n], tq[:n], "q")
+    assert (q_out[n:] == 7).all()
+    assert torch.equal(q_out[:n, :, rot:], s.q[:n, :, rot:])
+    at = 0
+    for b, (a, t) in enumerate(zip(q, kv)):
+        for i in range(a):
+            slot = t - a + i
+            page, off = int(s.table[b, slot // 16]), slot % 16
+            R.close(s.k[page, :, off], rk[at + i], tk[at + i], "k")
+            assert torch.equal(s.v[page, :, off], vn[at + i])
+            assert (s.pos[page, :, off] == positions[0, at + i]).all() and (s.weight[page, :, off] == 0).all()
+            for name in before:                        # put back: what is left must be untouched
+                getattr(s, name)[page, :, off] = before[name][page, :, off]
+        at += a
+    for name in before:
+        assert torch.equal(getattr(s, name).view(torch.uint8), before[name].view(torch.uint8)), name
+
+
+def test_append_in_place_without_queries_and_without_slots():
+    s = R.problem("cuda", BF, 4, 2, 64, 16, (5, 2), (3, 40), seed=41)
+    s.table[1, 2] = -1                                 # the second sequence's new tokens have no page
+    freq = (10000.0 ** (-torch.arange(32, dtype=torch.float64) / 32)).cuda()
+    pos = torch.arange(7, dtype=torch.int32, device="cuda")[None].contiguous()
+    kn, vn = torch.randn(7, 2, 64, device="cuda").to(BF), torch.randn(7, 2, 64, device="cuda").to(BF)
+    pages, batch, _ = handles(s)
+    rot = P.arkv_rotary(freq)
+    q_out = torch.empty_like(s.q)
+    P.arkv_paged_append(pages, batch, rot, s.q, kn, vn, pos, q_out)
+    q2 = s.q.clone()
+    P.arkv_paged_append(pages, batch, rot, q2, kn, vn, pos, q2)
+    assert torch.equal(q2, q_out)
+    v0 = s.v.clone()
+    s.v[int(s.table[0, 0]), :, :3] = 0
+    P.arkv_paged_append(pages, batch, rot, None, kn, vn, pos, None)
+    assert torch.equal(s.v.nan_to_num(5.0), v0.nan_to_num(5.0))
+    assert torch.equal(s.v[int(s.table[0, 0]), :, :3], vn[2:5].transpose(0, 1))       # tokens 0 and 1 have no slot
+    s.weight = None
+    P.arkv_paged_append(P.arkv_pages(s.k, s.v, s.pos), batch, rot, None, kn, vn, pos, None)
+
+
+@pytest.mark.parametrize("seed", range(3))
+@pytest.mark.parametrize("kv,keep,sink,recent", [
+    ((1,), (1,), 4, 32), ((40, 7), (36, 36), 4, 32), ((300, 0, 1000), (100, 100, 100), 4, 32), ((2500, 1024, 1025), (700, 1024, 1), 0, 0),
+    ((999, 333), (0, 50), 4, 8), ((500, 500), (20, -3), 30, 30), ((5000, 3000), (2500, 2999), 1, 7), ((9000,), (4500,), 4, 32)])
+def test_evict(kv, keep, sink, recent, seed):
+    s = R.problem("cuda", [BF, FP][seed % 2], 4, 2, [64, 128][seed % 2], [16, 64, 32][seed], (0,) * len(kv), kv, seed=50 + seed,
+                  spare_pages=400)
+    if seed == 1:                                      # few different weights: ties everywhere, signs, zeros, infinities, NaN
+        pick = torch.tensor([0.0, -0.0, 1.0, -1.0, math.inf, -math.inf, math.nan, 1e-40], device="cuda")
+        s.weight = pick[torch.randint(0, 8, s.weight.shape, generator=torch.Generator().manual_seed(2)).cuda()].contiguous()
+    if seed == 2:
+        s.weight.zero_()
+    max_keep = max(max(keep), 1)
+    need = -(-max_keep // s.page)
+    dst = torch.tensor(s.spare[:need * len(kv)], dtype=torch.int32, device="cuda").reshape(len(kv), need)
+    ref, lens = R.evict(s, keep, sink, recent, max_keep)
+    before = {n: getattr(s, n).clone() for n in ("k", "v", "pos", "weight")}
+    pages, batch, ws = handles(s)
+    ws.fill_(0xFF)
+    kept = torch.full((len(kv), 2, max_keep), 99, dtype=torch.int32, device="cuda")
+    new_len = torch.full((len(kv),), 99, dtype=torch.int32, device="cuda")
+    P.arkv_paged_evict(pages, batch, torch.tensor(keep, dtype=torch.int32, device="cuda"), dst, kept, new_len, sink=sink, recent=recent, workspace=ws)
+    assert new_len.tolist() == lens
+    assert torch.equal(kept.cpu(), ref)
+    for name, old in before.items():
+        want = old.clone()
+        for b, m in enumerate(lens):
+            for h in range(2):
+                j = ref[b, h, :m].long().cuda()
+                to = torch.arange(m, device="cuda")
+                want[dst[b].long()[to // s.page], h, to % s.page] = old[s.table[b].long()[j // s.page], h, j % s.page]
+        assert torch.equal(getattr(s, name).view(torch.uint8), want.view(torch.uint8)), name
+
+
+def test_evict_around_absent_pages():
+    s = R.problem("cuda", BF, 4, 2, 64, 16, (0,), (200,), seed=60, spare_pages=9)
+    s.table[0, 2] = -1
+    dst = torch.tensor([s.spare[:7]], dtype=torch.int32, device="cuda")
+    dst[0, 1] = s.n_pages                              # nothing is written there
+    k0 = s.k.clone()
+    pages, batch, ws = handles(s)
+    kept, lens = torch.empty((1, 2, 100), dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+    P.arkv_paged_evict(pages, batch, torch.tensor([100], dtype=torch.int32, device="cuda"), dst, kept, lens, workspace=ws)
+    ref, _ = R.evict(s, [100], 4, 32, 100)
+    assert torch.equal(kept.cpu(), ref) and not ((ref >= 32) & (ref < 48)).any()
+    assert torch.equal(s.k[s.spare[0], 1], k0[s.table[0].long()[ref[0, 1, :16].cuda() // 16], 1, ref[0, 1, :16].long().cuda() % 16])
+
+
+def test_other_streams_and_bitwise_repeats():
+    s = R.problem("cuda", BF, 8, 2, 128, 16, (70, 1, 1), (3000, 5000, 10), seed=70)
+    o1, l1 = attend(s)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        o2, l2 = attend(s)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(o1, o2) and torch.equal(l1, l2)
+    pages, batch, ws = handles(s)
+    w = []
+    for _ in range(2):
+        P.arkv_paged_weights(pages, batch, s.q, s.scale, l1, decay=0.0, workspace=ws)
+        w.append(s.weight.clone())
+    assert torch.equal(w[0].nan_to_num(5.0), w[1].nan_to_num(5.0))
+
+
+def test_a_captured_step_follows_lengths_and_tables():
+    """append, attention, weights, eviction in one graph, replayed with other lengths, pages and rows in the same arrays."""
+    q, kv = (1, 40, 1), (500, 90, 33)
+    s = R.problem("cuda", BF, 8, 2, 64, 16, q, kv, seed=71, spare_pages=60)
+    pages = P.arkv_pages(s.k, s.v, s.pos, s.weight)
+    batch = P.arkv_page_batch(s.cu_q, s.kv_len, s.table, s.n, 40, 512)
+    ws = P.arkv_paged_workspace(pages, batch, s.hq)
+    dst = torch.tensor(s.spare[:12], dtype=torch.int32, device="cuda").reshape(3, 4)
+    keep = torch.tensor([60, 50, 64], dtype=torch.int32, device="cuda")
+    kept, lens = torch.empty((3, 2, 64), dtype=torch.int32, device="cuda"), torch.empty(3, dtype=torch.int32, device="cuda")
+    freq = (10000.0 ** (-torch.arange(32, dtype=torch.float64) / 32)).cuda()
+    rot = P.arkv_rotary(freq)
+    new = torch.randn(s.n, 12, 64, device="cuda").to(BF)
+    positions = torch.arange(s.n, dtype=torch.int32, device="cuda")[None].contiguous()
+    q_rot, out, lse = torch.empty(s.n, 8, 64, dtype=BF, device="cuda"), torch.empty(s.n, 8, 64, dtype=BF, device="cuda"), torch.empty(s.n, 8, device="cuda")
+
+    def step():
+        P.arkv_paged_append(pages, batch, rot, new[:, :8], new[:, 8:10], new[:, 10:], positions, q_rot)
+        P.arkv_paged_attention(pages, batch, q_rot, s.scale, out, lse=lse, workspace=ws)
+        P.arkv_paged_weights(pages, batch, q_rot, s.scale, lse, workspace=ws)
+        P.arkv_paged_evict(pages, batch, keep, dst, kept, lens, workspace=ws)
+
+    state = {n: getattr(s, n).clone() for n in ("k", "v", "pos", "weight")}
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i, (cu, kvl) in enumerate([((0, 1, 41, 42), (500, 90, 33)), ((0, 0, 30, 42), (0, 64, 33)), ((0, 12, 13, 42), (499, 1, 31)), ((0, 1, 41, 42), (500, 90, 33))]):
+        s.cu_q.copy_(torch.tensor(cu, dtype=torch.int32)); s.kv_len.copy_(torch.tensor(kvl, dtype=torch.int32))
+        new.copy_(torch.randn(s.n, 12, 64, device="cuda"))
+        got = []
+        for run in (graph.replay, step):
+            for name in state:
+                getattr(s, name).copy_(state[name])
+            run()
+            torch.cuda.synchronize()
+            got.append([x.clone() for x in (out, lse, kept, lens, s.k, s.weight, s.pos)])
+        for a, b in zip(*got):
+            assert torch.equal(a.float().nan_to_num(3.0), b.float().nan_to_num(3.0)), i

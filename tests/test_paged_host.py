@@ -1,0 +1,187 @@
+"""CPU checks of the paged operators' entry points: exports, refusals before anything is launched, slots of pages."""
+import ctypes as C
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_08727_amd import binding as A
+from paper_2603_08727_amd import paged as P
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_header_binding_and_library_agree():
+    hdr = open(os.path.join(ROOT, "include", "arkv_paged.h")).read()
+    hdr = re.sub(r"/\*.*?\*/", "", hdr, flags=re.S)
+    declared = set(re.findall(r"\b(arkv_[a-z0-9_]+)\s*\(", hdr))
+    assert declared == set(P.EXPORTED)
+    lib = P.load()
+    for name in declared:
+        assert hasattr(lib, name), name
+
+
+@pytest.mark.parametrize("page,hkv", [(16, 1), (16, 3), (64, 8), (1024, 2)])
+def test_slots_of_pages(page, hkv):
+    rng = np.random.default_rng(page + hkv)
+    n_pages, width = 50, 7
+    table = rng.permutation(n_pages)[:width].astype(np.int32)
+    table[2], table[4] = -1, n_pages
+    length = width * page - 5
+    for slot in [-2**31, -1, 0, 1, page - 1, page, 2 * page, 3 * page - 1, 4 * page, length - 1, length, width * page, 2**31 - 1]:
+        for h in (0, hkv - 1):
+            got = P.arkv_debug_paged_row(table, n_pages, page, hkv, h, length, slot)
+            if not 0 <= slot < length or slot // page in (2, 4):
+                assert got == -1
+            else:
+                assert got == (int(table[slot // page]) * hkv + h) * page + slot % page
+
+
+def test_slot_hook_refusals():
+    t = np.zeros(4, np.int32)
+    for bad in [dict(n_pages=0), dict(page=8), dict(page=24), dict(page=2048), dict(hkv=0), dict(h=1), dict(h=-1), dict(length=-1),
+                dict(length=65)]:
+        kw = dict(n_pages=4, page=16, hkv=1, h=0, length=64)
+        kw.update(bad)
+        with pytest.raises(A.ArkvError) as e:
+            P.arkv_debug_paged_row(t, kw["n_pages"], kw["page"], kw["hkv"], kw["h"], kw["length"], 0)
+        assert e.value.code == A.EINVAL
+    assert P.load().arkv_debug_paged_row(None, 4, 4, 16, 1, 0, 4, 0, None) == A.EINVAL
+
+
+# Addresses that are never followed: every call below is refused on the host.
+ADDR = 0x1000
+
+
+def _args():
+    pages = P._Pages(0, 100, 16, 2, 64, ADDR, ADDR, ADDR, ADDR)
+    batch = P._Batch(2, 10, 5, 64, 4, ADDR, ADDR, ADDR)
+    rows = P._Rows(ADDR, 512, 64)
+    rot = P._Rotary(64, 1, 0, (C.c_uint8 * 64)(), ADDR)
+    sc = P._Scores(0.125, 0.0, None, None, None)
+    return pages, batch, rows, rot, sc
+
+
+def _call(name, pages, batch, rows, rot, sc, hq=8, ws=ADDR, size=1 << 40, **kw):
+    lib = P.load()
+    r = C.byref
+    if name == "append":
+        return lib.arkv_paged_append(r(pages), r(batch), r(rot), hq, r(rows), r(rows), r(rows), kw.get("positions", ADDR), kw.get("out", ADDR), None)
+    if name == "workspace":
+        return lib.arkv_paged_workspace(r(pages), r(batch), hq, r(C.c_size_t()))
+    if name == "attention":
+        return lib.arkv_paged_attention(r(pages), r(batch), r(sc), hq, r(rows), kw.get("out", ADDR), None, ws, size, None)
+    if name == "weights":
+        return lib.arkv_paged_weights(r(pages), r(batch), r(sc), hq, r(rows), kw.get("lse", ADDR), kw.get("decay", 1.0), None, ws, size, None)
+    return lib.arkv_paged_evict(r(pages), r(batch), kw.get("keep", ADDR), kw.get("max_keep", 32), kw.get("sink", 4), kw.get("recent", 8),
+                                kw.get("dst", ADDR), kw.get("dst_width", 2), kw.get("kept", ADDR), kw.get("new_len", ADDR), ws, size, None)
+
+
+ALL = ["append", "workspace", "attention", "weights", "evict"]
+
+
+@pytest.mark.parametrize("name", ALL)
+@pytest.mark.parametrize("where,field,value,code", [
+    ("pages", "k", None, A.EINVAL), ("pages", "v", None, A.EINVAL), ("pages", "pos", None, A.EINVAL), ("pages", "n_pages", 0, A.EINVAL),
+    ("pages", "n_pages", -3, A.EINVAL), ("pages", "page_size", 0, A.EINVAL), ("pages", "page_size", 24, A.EINVAL),
+    ("pages", "page_size", 8, A.EUNSUPPORTED), ("pages", "page_size", 2048, A.EUNSUPPORTED), ("pages", "n_kv_heads", 0, A.EINVAL),
+    ("pages", "head_dim", 96, A.EUNSUPPORTED), ("pages", "head_dim", 0, A.EINVAL), ("pages", "dtype", 2, A.EUNSUPPORTED),
+    ("pages", "dtype", -1, A.EUNSUPPORTED), ("pages", "n_pages", 1 << 27, A.EUNSUPPORTED), ("pages", "k", ADDR + 8, A.EINVAL),
+    ("pages", "v", ADDR + 2, A.EINVAL), ("batch", "batch", 0, A.EINVAL), ("batch", "batch", 65536, A.EUNSUPPORTED),
+    ("batch", "n_tokens", -1, A.EINVAL), ("batch", "max_q", -1, A.EINVAL), ("batch", "max_q", 11, A.EINVAL), ("batch", "max_kv", -1, A.EINVAL),
+    ("batch", "max_kv", 65, A.EINVAL), ("batch", "table_width", 0, A.EINVAL), ("batch", "cu_q", None, A.EINVAL),
+    ("batch", "kv_len", None, A.EINVAL), ("batch", "table", None, A.EINVAL),
+])
+def test_pages_and_batch_are_checked(name, where, field, value, code):
+    pages, batch, rows, rot, sc = _args()
+    setattr(pages if where == "pages" else batch, field, value)
+    assert _call(name, pages, batch, rows, rot, sc) == code
+
+
+@pytest.mark.parametrize("field,value", [("p", None), ("p", ADDR + 2), ("token_stride", 511), ("token_stride", -512), ("head_stride", 4),
+                                         ("head_stride", -64)])
+@pytest.mark.parametrize("name", ["append", "attention", "weights"])
+def test_rows_are_checked(name, field, value):
+    pages, batch, rows, rot, sc = _args()
+    setattr(rows, field, value)
+    assert _call(name, pages, batch, rows, rot, sc) == A.EINVAL
+
+
+@pytest.mark.parametrize("name", ["workspace", "attention", "weights"])
+def test_heads_are_checked(name):
+    a = _args()
+    assert _call(name, *a, hq=7) == A.EINVAL and _call(name, *a, hq=0) == A.EINVAL and _call(name, *a, hq=-2) == A.EINVAL
+    assert _call(name, *a, hq=34) == A.EUNSUPPORTED       # 17 query heads per kv-head
+
+
+@pytest.mark.parametrize("field,value", [("rot_dim", 8), ("rot_dim", -16), ("rot_dim", 80), ("n_axes", 0), ("n_axes", 5), ("adjacent", 2),
+                                         ("freq", None)])
+def test_rotary_is_checked(field, value):
+    pages, batch, rows, rot, sc = _args()
+    setattr(rot, field, value)
+    assert _call("append", pages, batch, rows, rot, sc) == A.EINVAL
+
+
+def test_append_refusals():
+    pages, batch, rows, rot, sc = _args()
+    rot.axis[31] = 1
+    assert _call("append", pages, batch, rows, rot, sc) == A.EINVAL
+    rot.axis[31] = 0
+    assert _call("append", pages, batch, rows, rot, sc, positions=None) == A.EINVAL
+    assert _call("append", pages, batch, rows, rot, sc, out=None) == A.EINVAL          # q without q_out
+    assert _call("append", pages, batch, rows, rot, sc, out=ADDR + 4) == A.EINVAL
+    assert _call("append", pages, batch, rows, rot, sc, hq=0) == A.EINVAL
+    assert P.load().arkv_paged_append(None, None, None, 8, None, None, None, None, None, None) == A.EINVAL
+
+
+@pytest.mark.parametrize("name", ["attention", "weights"])
+def test_scores_are_checked(name):
+    for field, value in [("scale", float("nan")), ("scale", float("inf")), ("cap", -1.0), ("cap", float("nan")), ("cap", float("inf")),
+                         ("slopes", ADDR)]:                # slopes without q_pos
+        pages, batch, rows, rot, sc = _args()
+        setattr(sc, field, value)
+        assert _call(name, pages, batch, rows, rot, sc) == A.EINVAL, field
+
+
+def test_attention_and_weights_refusals():
+    a = _args()
+    assert _call("attention", *a, out=None) == A.EINVAL and _call("attention", *a, out=ADDR + 8) == A.EINVAL
+    assert _call("weights", *a, lse=None) == A.EINVAL and _call("weights", *a, decay=float("nan")) == A.EINVAL
+    a[0].weight = None
+    assert _call("weights", *a) == A.EINVAL and _call("evict", *a) == A.EINVAL
+
+
+def test_workspaces_that_are_too_small_are_refused():
+    pages, batch, rows, rot, sc = _args()
+    n = C.c_size_t()
+    lib = P.load()
+    assert lib.arkv_paged_workspace(C.byref(pages), C.byref(batch), 8, None) == A.EINVAL
+    assert lib.arkv_paged_workspace(C.byref(pages), C.byref(batch), 8, C.byref(n)) == A.OK
+    if n.value:
+        for name in ("attention", "weights"):
+            assert _call(name, pages, batch, rows, rot, sc, ws=None) == A.EINVAL
+            assert _call(name, pages, batch, rows, rot, sc, size=n.value - 1) == A.EINVAL
+            assert _call(name, pages, batch, rows, rot, sc, ws=ADDR + 4) == A.EINVAL
+
+
+def test_evict_refusals():
+    a = _args()
+    for kw in [dict(keep=None), dict(dst=None), dict(kept=None), dict(new_len=None), dict(max_keep=0), dict(max_keep=33), dict(sink=-1),
+               dict(recent=-1), dict(dst_width=0)]:
+        assert _call("evict", *a, **kw) == A.EINVAL, kw
+
+
+def test_the_binding_takes_gpu_tensors_of_the_right_kind():
+    z = torch.zeros
+    with pytest.raises(ValueError):
+        P.arkv_pages(z(4, 2, 16, 64, dtype=torch.bfloat16), z(4, 2, 16, 64, dtype=torch.bfloat16), z(4, 2, 16, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        P.arkv_pages(z(4, 2, 16, 64), z(4, 2, 16, 64), z(4, 2, 16, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        P.arkv_page_batch(z(3, dtype=torch.int32), z(2, dtype=torch.int32), z(2, 4, dtype=torch.int32), 4, 1, 64)
+    with pytest.raises(ValueError):
+        P.arkv_page_batch(z(3, dtype=torch.int32), z(2, dtype=torch.int32), z(2, 4, dtype=torch.int32), 4)
+    with pytest.raises(ValueError):
+        P.arkv_rotary(z(32, dtype=torch.float64))
