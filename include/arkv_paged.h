@@ -35,7 +35,7 @@ extern "C" {
 
 /* One layer's pages.  k, v DEVICE [n_pages][H_kv][page_size][d] of dtype; pos DEVICE int32, weight DEVICE float
  * [n_pages][H_kv][page_size]: a row's position and the attention weight it collected (weight may be NULL where no
- * weights are kept).  page_size: a power of two from 16 to 1024.  head_dim 64 or 128.  n_pages H_kv page_size < 2^31.  k and v 16-byte aligned. */
+ * weights are kept).  page_size: a power of two from 16 to 1024.  head_dim 64 or 128.  n_pages H_kv page_size < 2^31.  k, v and pos 16-byte aligned. */
 typedef struct {
   int32_t dtype, n_pages, page_size, n_kv_heads, head_dim;
   void* k;

@@ -1,26 +1,733 @@
 // Attention of new tokens over a paged cache, and the weight that the cached rows collect from them.
+//
+// The rows of a (sequence, kv-head) are its new tokens times the G query heads of the group: row r is token r / G, head
+// r % G, so the heads of a group share every key and value that is fetched.  Two kernels divide the sequences between them:
+//   k_paged_step   up to 16 rows (a generated token, a few drafted ones): bound by reading the pages
+//   k_paged_chunk  more rows: bound by the matrix cores
+// Both split a sequence's keys over workgroups where that fills the chip; k_paged_merge joins the pieces.
+//
+// In both, keys are on the M side of the logits MFMA (S^T = K Q^T), which leaves one row per lane, and the lane's
+// probabilities are, as they lie, the B operand of O^T = V^T P^T once the contraction index is read in their order; the
+// matching A operand comes out of row-major values in LDS by transposing reads (ds_read_b64_tr_b16: sixteen lanes read a
+// 4 x 16 block, four lanes a row, and get a column each).
+// The softmax reference of a row is lazy: probabilities are taken against the row's present reference, which moves to the
+// tile's maximum only when a lane's sum shows that they grew large (or when it is unset).
+// Pages are at least 16 slots, so the 16 rows from a multiple of 16 on (a granule) lie in one page, whose id is uniform.
+#include <algorithm>
+
 #include "arkv_dev.h"
 #include "arkv_paged_dev.h"
 
 namespace arkv {
 
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+typedef uint32_t u32x4g __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2g __attribute__((ext_vector_type(2)));
+typedef float f32x4g __attribute__((ext_vector_type(4)));
+typedef float f32x16g __attribute__((ext_vector_type(16)));
+typedef short s16x4g __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8g __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2g __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8g __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2g __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s16x4g* lds_s16x4;
 
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-  return x;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kUnset = -1.0e30f;      // softmax reference of a row that has seen nothing
+constexpr float kSumLimit = 16384.0f;   // a lane's probabilities of a tile may sum to this before the reference moves
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <typename T> struct Mfma;
+template <> struct Mfma<__bf16> {
+  static constexpr uint32_t kExp = 0x7F80u;      // exponent bits: all set = not finite
+  static __device__ __forceinline__ f32x4g m16(u32x4g a, u32x4g b, f32x4g c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8g, a), __builtin_bit_cast(bf16x8g, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x16g m32(u32x4g a, u32x4g b, f32x16g c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8g, a), __builtin_bit_cast(bf16x8g, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) { bf16x2g h; h[0] = (__bf16)a; h[1] = (__bf16)b; return __builtin_bit_cast(uint32_t, h); }
+  static __device__ __forceinline__ float get(uint32_t w, int hi) { return __uint_as_float(hi ? w & 0xFFFF0000u : w << 16); }
+};
+template <> struct Mfma<_Float16> {
+  static constexpr uint32_t kExp = 0x7C00u;
+  static __device__ __forceinline__ f32x4g m16(u32x4g a, u32x4g b, f32x4g c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8g, a), __builtin_bit_cast(f16x8g, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x16g m32(u32x4g a, u32x4g b, f32x16g c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8g, a), __builtin_bit_cast(f16x8g, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) { f16x2g h; h[0] = (_Float16)a; h[1] = (_Float16)b; return __builtin_bit_cast(uint32_t, h); }
+  static __device__ __forceinline__ float get(uint32_t w, int hi) { return (float)__builtin_bit_cast(f16x2g, w)[hi]; }
+};
+
+// halves of w that are not finite, as a mask of whole halves
+template <typename T> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  return ((w & Mfma<T>::kExp) == Mfma<T>::kExp ? 0xFFFFu : 0u) | ((w >> 16 & Mfma<T>::kExp) == Mfma<T>::kExp ? 0xFFFF0000u : 0u);
 }
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  return x;
+
+// logit, times log2(e), of a raw dot product (MODE 1: whatever the scores say)
+struct Logit {
+  float mul, inv_cap2, cap2;     // scale log2(e); 2 log2(e) scale / cap; cap log2(e)
+  __device__ __forceinline__ Logit(const Scores& S) {
+    mul = S.scale * kLog2e;
+    cap2 = S.cap * kLog2e;
+    inv_cap2 = S.cap > 0.f ? 2.f * kLog2e * (S.scale / S.cap) : 0.f;
+  }
+  // tanh x = 1 - 2 / (1 + e^2x): off by a few 2^-24 of 1, for logits up to the cap in absolute terms
+  __device__ __forceinline__ float plain(float dot) const {
+    if (cap2 > 0.f) return cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_hw(dot * inv_cap2)));
+    return dot * mul;
+  }
+};
+
+__device__ __forceinline__ Seq seq_of(const Paged& P, int b) {
+  return clamp_seq(P.cu_q[b], P.cu_q[b + 1], P.kv_len[b], P.N, P.max_q, P.max_kv);
 }
+// slots that new token i of a sequence sees are those below this (0: none)
+__device__ __forceinline__ int row_end(const Seq& s, int i, int prefix) { return max(0, min(s.kv, max(s.kv - s.nq + i + 1, prefix))); }
+
+constexpr int kStepRows = 16;           // rows of a sequence that k_paged_step takes
+constexpr int kStepWaves = 4;
+constexpr int kStepMaxPiece = 4096;     // a lane holds the page of one granule: 64 granules per wave
+constexpr int kChunkRows = 128, kChunkKeys = 64;
+
+// How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
+struct Cut { int step_piece, n_step, chunk_piece, n_chunk; bool step, chunk; };
+
+static Cut cut_of(const Paged& P, int Hq) {
+  Cut c = {};
+  const int G = Hq / P.H;
+  const long long units = (long long)P.B * P.H;
+  c.chunk = P.max_q * G > kStepRows;
+  c.step = !c.chunk || (long long)P.B * P.max_q != P.N;      // all sequences have max_q new tokens: none has few rows
+  auto pieces = [&](long long have, int least, int most, int unit, int& piece, int& n) {
+    const long long want = std::max(1ll, 512 / std::max(1ll, have));
+    long long p = (P.max_kv + want - 1) / want;
+    p = std::min<long long>(most, std::max<long long>(least, (p + unit - 1) / unit * unit));
+    piece = (int)p;
+    n = std::max(1, (int)((P.max_kv + p - 1) / p));
+  };
+  pieces(units, 256, kStepMaxPiece, 128, c.step_piece, c.n_step);
+  const long long blocks = ((long long)P.N * G + kChunkRows - 1) / kChunkRows * P.H;
+  pieces(blocks, 512, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
+  return c;
+}
+
+// Pieces' results: sums [row][D] and (reference, denominator) [row].  Rows of k_paged_step: ((unit * n_step + piece) * 16 +
+// row), behind them rows of k_paged_chunk: (piece * N + token) * Hq + head.
+struct Parts { float* acc; float2* ml; size_t chunk0; };
+
+static size_t part_rows(const Paged& P, int Hq, const Cut& c, size_t& chunk0) {
+  chunk0 = c.step && c.n_step > 1 ? (size_t)P.B * P.H * c.n_step * kStepRows : 0;
+  return chunk0 + (c.chunk && c.n_chunk > 1 ? (size_t)c.n_chunk * P.N * Hq : 0);
+}
+
+size_t paged_attention_floats(const Paged& P, int D, int Hq) {
+  size_t chunk0;
+  return part_rows(P, Hq, cut_of(P, Hq), chunk0) * (D + 2);
+}
+
+// four adjacent channels of a finished row
+template <typename T> __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
+  *reinterpret_cast<u32x2g*>(p) = u32x2g{Mfma<T>::pack(a, b), Mfma<T>::pack(c, d)};
+}
+
+// ---- few rows -----------------------------------------------------------------------------------------
+
+// One workgroup = one piece of a (sequence, kv-head); its waves take a quarter of the piece each, 32 keys at a time, with
+// 16x16x32 MFMAs (lane: row lane % 16, keys 4 (lane / 16) .. + 3 of each granule).  Keys come from memory in operand
+// layout; values in whole rows, through LDS of the wave's own.  A tile's loads are in flight while the tile before it
+// is worked on.
+template <typename T, int D, int MODE>
+__global__ __launch_bounds__(64 * kStepWaves, 2) void k_paged_step(PagedAttnArgs A, int piece_keys, int n_pieces, Parts parts) {
+  constexpr int KK = D / 32, CB = D / 16, VI = 32 * D * 2 / 1024;   // k-steps, channel blocks, 1 KB loads of a value tile
+  constexpr int RPI = 1024 / (2 * D), CPR = D / 8;                 // rows per load, 16-byte chunks per row
+  constexpr int VP = D + 16;                                       // halves per value row: transposing reads of 16 rows meet each bank twice
+  __shared__ __align__(16) uint16_t sv[kStepWaves][32][VP];
+  __shared__ float s_acc[kStepWaves][kStepRows][D + 4];
+  __shared__ float2 s_ml[kStepWaves][kStepRows];
+  const Paged& P = A.P;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, gq = lane >> 4;
+  const int h = blockIdx.x % P.H, b = blockIdx.x / P.H, piece = blockIdx.y;
+  const Seq s = seq_of(P, b);
+  const int R = s.nq * A.G;
+  if (R == 0 || R > kStepRows) return;
+  const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
+  const int end = row_end(s, s.nq - 1, prefix);                    // what the last token sees is what any sees
+  const int np = max(1, (end + piece_keys - 1) / piece_keys);
+  if (piece >= np) return;
+  const int row = n < R ? n : 0;
+  const int my_end = n < R ? row_end(s, row / A.G, prefix) : 0;
+  const int all_end = row_end(s, 0, prefix);                       // every row sees the slots below
+  const int hq = h * A.G + row % A.G, tok = s.q0 + row / A.G;
+  const Logit lg(A.S);
+  const float slope = MODE && A.S.slopes ? A.S.slopes[hq] * kLog2e : 0.f;
+  const int qp = MODE && A.S.slopes ? A.S.q_pos[tok] : 0;
+
+  u32x4g q[KK];
+  {
+    const T* p = (const T*)A.q.p + (size_t)tok * A.q.ts + (size_t)hq * A.q.hs + 8 * gq;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) q[kk] = *reinterpret_cast<const u32x4g*>(p + 32 * kk);
+  }
+  // this wave's keys: [w0, w1), whole tiles
+  const int p0 = piece * piece_keys, p1 = min(p0 + piece_keys, end);
+  const int tiles = (p1 - p0 + 31) / 32, per = (tiles + kStepWaves - 1) / kStepWaves;
+  const int t0 = min(per * wave, tiles), t1 = min(t0 + per, tiles);
+  const int w0 = p0 + 32 * t0;
+  // lane i holds the page id of granule i from w0 on; one that is not there becomes page 0, whose rows nobody sees
+  int my_page;
+  bool page_ok;
+  {
+    const int j = w0 + 16 * lane;
+    my_page = j < p1 ? P.table[(size_t)b * P.width + (j >> P.lg_page)] : 0;
+    page_ok = (unsigned)my_page < (unsigned)P.n_pages;
+    if (!page_ok) my_page = 0;
+  }
+  const uint64_t ok_mask = __ballot(page_ok);
+  const int in_page = (1 << P.lg_page) - 1;
+  auto granule_row = [&](int g) {                                  // first row of granule g
+    const int page = __builtin_amdgcn_readlane(my_page, g);
+    return (size_t)(unsigned)(((page * P.H + h) << P.lg_page) + ((w0 + 16 * g) & in_page));
+  };
+
+  u32x4g kb[2][2][KK], vb[VI];
+  auto load_k = [&](int t, u32x4g (&to)[2][KK]) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const T* p = (const T*)P.k + granule_row(2 * t + g) * D + n * D + 8 * gq;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) to[g][kk] = *reinterpret_cast<const u32x4g*>(p + 32 * kk);
+    }
+  };
+  auto load_v = [&](int t) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const T* p = (const T*)P.v + granule_row(2 * t + g) * D + (lane / CPR) * D + 8 * (lane % CPR);
+#pragma unroll
+      for (int i = 0; i < VI / 2; ++i) vb[g * (VI / 2) + i] = *reinterpret_cast<const u32x4g*>(p + i * RPI * D);
+    }
+  };
+  f32x4g acc[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c) acc[c] = f32x4g{0.f, 0.f, 0.f, 0.f};
+  float m = kUnset, l = 0.f;
+  const int nt = t1 - t0;
+
+  auto tile = [&](int t, const u32x4g (&kc)[2][KK]) {
+    const int j0 = w0 + 32 * t;
+    f32x4g x[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      x[g] = f32x4g{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) x[g] = Mfma<T>::m16(kc[g][kk], q[kk], x[g]);
+    }
+    const bool masked = j0 + 32 > all_end || (ok_mask >> (2 * t) & 3) != 3;
+    float mul = lg.mul;
+    if (MODE) {
+      mul = 1.f;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[g][i] = lg.plain(x[g][i]);
+        if (A.S.slopes) {
+          const int4 kp = *reinterpret_cast<const int4*>(P.pos + granule_row(2 * t + g) + 4 * gq);
+          x[g][0] -= slope * fabsf((float)(qp - kp.x));
+          x[g][1] -= slope * fabsf((float)(qp - kp.y));
+          x[g][2] -= slope * fabsf((float)(qp - kp.z));
+          x[g][3] -= slope * fabsf((float)(qp - kp.w));
+        }
+      }
+    }
+    uint32_t odd = 0;                                              // keys of this tile whose values are not all finite
+    if (masked) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          x[g][i] = j0 + 16 * g + 4 * gq + i < my_end && (ok_mask >> (2 * t + g) & 1) ? x[g][i] * mul : -INFINITY;
+      mul = 1.f;
+      // a value that is not finite would spoil the rows that do not see it: it leaves the product, and is added below
+#pragma unroll
+      for (int i = 0; i < VI; ++i) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t f = not_finite<T>(vb[i][e]);
+          vb[i][e] &= ~f;
+          any |= f;
+        }
+        const uint64_t who = __ballot(any != 0);
+#pragma unroll
+        for (int r = 0; r < RPI; ++r)
+          if (who >> (CPR * r) & ((1ull << CPR) - 1)) odd |= 1u << (RPI * i + r);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VI; ++i)
+      *reinterpret_cast<u32x4g*>(&sv[wave][RPI * i + lane / CPR][8 * (lane % CPR)]) = vb[i];
+    if (t + 1 < nt) load_v(t + 1);
+    float p[8];
+    auto probs = [&]() {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = exp2_hw(fmaf(x[i >> 2][i & 3], mul, -m));
+        sum += p[i];
+      }
+      return sum;
+    };
+    float sum = probs();
+    if (__any(!(sum <= kSumLimit))) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i >> 2][i & 3] * mul);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(m, top), f = exp2_hw(m - mn);         // every lane of a row moves alike
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < CB; ++c) acc[c] *= f;
+      sum = probs();
+    }
+    l += sum;
+    const u32x4g pb = {Mfma<T>::pack(p[0], p[1]), Mfma<T>::pack(p[2], p[3]), Mfma<T>::pack(p[4], p[5]), Mfma<T>::pack(p[6], p[7])};
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+      const s16x4g a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sv[wave][4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
+      const s16x4g a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sv[wave][16 + 4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
+      const u32x2g w0_ = __builtin_bit_cast(u32x2g, a0), w1_ = __builtin_bit_cast(u32x2g, a1);
+      acc[c] = Mfma<T>::m16(u32x4g{w0_[0], w0_[1], w1_[0], w1_[1]}, pb, acc[c]);
+    }
+    while (odd) {                                                  // (uniform; hardly ever)
+      const int j = __builtin_ctz(odd);
+      odd &= odd - 1;
+      const int g = j >> 4, i = j & 3, from = (j & 12) >> 2;
+      float pj = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e == 4 * g + i) pj = Mfma<T>::get(pb[e / 2], e & 1);
+      pj = __shfl(pj, n + 16 * from);
+      const bool seen = j0 + j < my_end && (ok_mask >> (2 * t + g) & 1);
+      const T* v = (const T*)P.v + (granule_row(2 * t + g) + (j & 15)) * D + 4 * gq;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float w = (float)v[16 * c + e];
+          if (seen && !(fabsf(w) < INFINITY)) acc[c][e] += pj * w;
+        }
+    }
+  };
+  if (nt > 0) {
+    load_k(0, kb[0]);
+    load_v(0);
+    for (int t = 0; t < nt; t += 2) {
+      if (t + 1 < nt) load_k(t + 1, kb[1]);
+      tile(t, kb[0]);
+      if (t + 1 < nt) {
+        if (t + 2 < nt) load_k(t + 2, kb[0]);
+        tile(t + 1, kb[1]);
+      }
+    }
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+#pragma unroll
+  for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4g*>(&s_acc[wave][n][16 * c + 4 * gq]) = acc[c];
+  if (gq == 0) s_ml[wave][n] = make_float2(m, l);
+  __syncthreads();
+  // the waves' parts: thread = four channels of a row
+  for (int it = threadIdx.x; it < R * (D / 4); it += 64 * kStepWaves) {
+    const int r = it / (D / 4), c = 4 * (it % (D / 4));
+    float mm = kUnset, ll = 0.f;
+#pragma unroll
+    for (int w = 0; w < kStepWaves; ++w) mm = fmaxf(mm, s_ml[w][r].x);
+    f32x4g o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kStepWaves; ++w) {
+      const float f = exp2_hw(s_ml[w][r].x - mm);
+      ll += f * s_ml[w][r].y;
+      o += f * *reinterpret_cast<const f32x4g*>(&s_acc[w][r][c]);
+    }
+    if (np > 1) {
+      const size_t pr = ((size_t)blockIdx.x * n_pieces + piece) * kStepRows + r;
+      *reinterpret_cast<f32x4g*>(parts.acc + pr * D + c) = o;
+      if (c == 0) parts.ml[pr] = make_float2(mm, ll);
+    } else {
+      const size_t orow = (size_t)(s.q0 + r / A.G) * A.Hq + h * A.G + r % A.G;
+      const float inv = ll == 0.f ? 0.f : 1.f / ll;                // (NaN stays)
+      store4((T*)A.out + orow * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+      if (c == 0 && A.lse) A.lse[orow] = ll == 0.f ? -INFINITY : kLn2 * (mm + log2f(ll));
+    }
+  }
+}
+
+// ---- many rows ----------------------------------------------------------------------------------------
+
+// Blocks of kChunkRows rows that k_paged_chunk makes of a sequence.
+__host__ __device__ __forceinline__ int chunk_blocks(int nq, int G) { return nq * G <= kStepRows ? 0 : (nq * G + kChunkRows - 1) / kChunkRows; }
+
+// Sequence and block of the rank-th block of a launch; the lanes of a wave look at 64 sequences at a time.
+__device__ __forceinline__ bool find_block(const Paged& P, int G, int rank, int lane, int& b, int& blk) {
+  for (int i = 0; i < P.B; i += 64) {
+    const int mine = i + lane < P.B ? chunk_blocks(seq_of(P, i + lane).nq, G) : 0;
+    int sum = mine;                                                // blocks up to and with this lane's sequence
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int below = __shfl_up(sum, o);
+      if (lane >= o) sum += below;
+    }
+    const uint64_t hit = __ballot(sum > rank);
+    if (hit) {
+      const int first = __builtin_ctzll(hit);
+      b = i + first;
+      const int n = __builtin_amdgcn_readlane(mine, first);
+      blk = n - 1 - (rank - (__builtin_amdgcn_readlane(sum, first) - n));   // the block that sees most comes first
+      return true;
+    }
+    rank -= __builtin_amdgcn_readlane(sum, 63);
+  }
+  return false;
+}
+
+// 1 KB from memory to LDS, 16 bytes per lane, in lane order from `lds` on, without a register in between.  The caller waits
+// (vm_wait) and synchronises before anyone reads.  Inline assembly, because the compiler would wait for every such load in
+// front of any LDS read; it has no output register.
+__device__ __forceinline__ void load_lds(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(base), "v"(off), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void vm_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// One workgroup = 128 rows of a (sequence, kv-head) and a piece of the keys they see; a wave takes 32 rows with 32x32x16
+// MFMAs (lane: row lane % 32, keys 8 (i / 4) + 4 (lane / 32) + i % 4 of each half of a 64-key tile).  Keys and values of
+// a tile go to LDS as they lie in the pages, sixteen rows per wave, while the tile before is worked on: two buffers, one
+// barrier a tile.  The rows' 16-byte chunks are stored in an order in which neither the keys' reads (one chunk of 32
+// rows) nor the values' transposing reads (64 bytes of 8 rows) meet in a bank more often than they must.
+template <int D> struct ChunkLds {
+  uint16_t k[2][kChunkKeys * D];
+  uint16_t v[2][kChunkKeys * D];
+  uint32_t odd[2];
+};
+template <int D> __device__ __forceinline__ int k_chunk(int row, int c) { return D == 128 ? c ^ (row & 15) : c ^ (row >> 1 & 7); }
+template <int D> __device__ __forceinline__ int v_chunk(int row, int c) { return D == 128 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; }
+
+template <typename T, int D, int MODE>
+__global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs A, int piece_keys, int n_pieces, Parts parts) {
+  constexpr int KK = D / 16, CB = D / 32, CPR = D / 8, RPI = 64 / CPR, LPG = 16 / RPI;   // LPG: 1 KB loads of a granule
+  __shared__ __align__(16) ChunkLds<D> sm;
+  const Paged& P = A.P;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int h = blockIdx.x % P.H, piece = blockIdx.y;
+  int b, blk;
+  if (!find_block(P, A.G, blockIdx.x / P.H, lane, b, blk)) return;
+  const Seq s = seq_of(P, b);
+  const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
+  const int R = s.nq * A.G, r0 = blk * kChunkRows;
+  const int end = row_end(s, min(R - 1, r0 + kChunkRows - 1) / A.G, prefix);
+  const int np = max(1, (end + piece_keys - 1) / piece_keys);
+  if (piece >= np) return;
+  const int r = r0 + 32 * wave + n;
+  const int rc = min(r, R - 1);
+  const int my_end = r < R ? row_end(s, rc / A.G, prefix) : 0;
+  const int all_end = row_end(s, r0 / A.G, prefix);                // every row of the workgroup sees the slots below
+  const int hq = h * A.G + rc % A.G, tok = s.q0 + rc / A.G;
+  const Logit lg(A.S);
+  const float slope = MODE && A.S.slopes ? A.S.slopes[hq] * kLog2e : 0.f;
+  const int qp = MODE && A.S.slopes ? A.S.q_pos[tok] : 0;
+
+  u32x4g q[KK];
+  {
+    const T* p = (const T*)A.q.p + (size_t)tok * A.q.ts + (size_t)hq * A.q.hs + 8 * hh;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) q[kk] = *reinterpret_cast<const u32x4g*>(p + 16 * kk);
+  }
+  const int p0 = piece * piece_keys, p1 = min(p0 + piece_keys, end), nt = (p1 - p0 + kChunkKeys - 1) / kChunkKeys;
+  const int32_t* table = P.table + (size_t)b * P.width;
+  const int in_page = (1 << P.lg_page) - 1;
+
+  // where this lane's chunk of a 1 KB load lies in a granule: row RPI i + lane / CPR
+  uint32_t koff[LPG], voff[LPG];
+#pragma unroll
+  for (int i = 0; i < LPG; ++i) {
+    const int rr = RPI * i + lane / CPR;
+    koff[i] = 2 * (rr * D + 8 * k_chunk<D>(rr, lane % CPR));
+    voff[i] = 2 * (rr * D + 8 * v_chunk<D>(rr, lane % CPR));
+  }
+  const uint32_t lds_k = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.k;
+  const uint32_t lds_v = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.v;
+  // Lane i holds the page of granule i of a group of sixteen tiles, this one and the next one; one that is not there becomes
+  // page 0, whose rows nobody sees.
+  int pages[2];
+  uint64_t there[2];
+  auto load_pages = [&](int group, int which) {
+    const int j = p0 + 16 * (64 * group + lane);
+    int page = j < p1 ? table[j >> P.lg_page] : -1;
+    const bool ok = (unsigned)page < (unsigned)P.n_pages;
+    there[which] = __ballot(ok);
+    pages[which] = ok ? page : 0;
+  };
+  auto granule_row = [&](int which, int t, int g) {                // first row of granule g of tile t
+    const int page = __builtin_amdgcn_readlane(which ? pages[1] : pages[0], 4 * (t & 15) + g);
+    return (size_t)(unsigned)(((page * P.H + h) << P.lg_page) + ((p0 + kChunkKeys * t + 16 * g) & in_page));
+  };
+  auto fetch = [&](int which, int t, int buf) {                    // this wave's granule of tile t
+    const size_t row = granule_row(which, t, wave);
+    const T* kp = (const T*)P.k + row * D;
+    const T* vp = (const T*)P.v + row * D;
+    const uint32_t at = (uint32_t)(buf * kChunkKeys * D * 2 + wave * 16 * D * 2);
+#pragma unroll
+    for (int i = 0; i < LPG; ++i) load_lds(kp, koff[i], lds_k + at + 1024 * i);
+#pragma unroll
+    for (int i = 0; i < LPG; ++i) load_lds(vp, voff[i], lds_v + at + 1024 * i);
+  };
+
+  f32x16g acc[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
+  float m = kUnset, l = 0.f;
+  load_pages(0, 0);
+  if (nt > 0) fetch(0, 0, 0);
+  for (int t = 0; t < nt; ++t) {
+    const int buf = t & 1, j0 = p0 + kChunkKeys * t;
+    if ((t & 15) == 0) {
+      if (t) { pages[0] = pages[1]; there[0] = there[1]; }
+      load_pages((t >> 4) + 1, 1);
+    }
+    vm_wait();                                                     // this wave's part of tile t is in LDS,
+    __syncthreads();                                               // everyone's is, and the other buffer's readers are done
+    if (t + 1 < nt) fetch((t & 15) == 15, t + 1, buf ^ 1);
+    const uint32_t ok = (uint32_t)(there[0] >> (4 * (t & 15))) & 15;   // granules that are there
+    const bool masked = j0 + kChunkKeys > all_end || ok != 15;
+    uint64_t odd = 0;
+    if (masked) {
+      // Values that are not finite would spoil the rows that do not see them: they leave the product, and are added below.
+      if (tid < 2) sm.odd[tid] = 0;
+      __syncthreads();
+      constexpr int PT = kChunkKeys * CPR / 256;                   // chunks per thread
+#pragma unroll
+      for (int i = 0; i < PT; ++i) {
+        const int at = tid + 256 * i, rr = at / CPR;
+        u32x4g* p = reinterpret_cast<u32x4g*>(&sm.v[buf][8 * at]);
+        u32x4g w = *p;
+        uint32_t any = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t f = not_finite<T>(w[e]);
+          w[e] &= ~f;
+          any |= f;
+        }
+        if (any) {
+          *p = w;
+          if (j0 + rr < end && (ok >> (rr >> 4) & 1)) atomicOr(&sm.odd[rr >> 5], 1u << (rr & 31));
+        }
+      }
+      __syncthreads();
+      odd = (uint64_t)sm.odd[1] << 32 | sm.odd[0];
+    }
+    f32x16g x[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[g][i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const u32x4g a = *reinterpret_cast<const u32x4g*>(&sm.k[buf][(32 * g + n) * D + 8 * k_chunk<D>(n, 2 * kk + hh)]);
+        x[g] = Mfma<T>::m32(a, q[kk], x[g]);
+      }
+    float mul = lg.mul;
+    if (MODE) {
+      mul = 1.f;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[g][i] = lg.plain(x[g][i]);
+        if (A.S.slopes) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int4 kp = *reinterpret_cast<const int4*>(P.pos + granule_row(0, t, 2 * g + (e >> 1)) + 8 * (e & 1) + 4 * hh);
+            x[g][4 * e] -= slope * fabsf((float)(qp - kp.x));
+            x[g][4 * e + 1] -= slope * fabsf((float)(qp - kp.y));
+            x[g][4 * e + 2] -= slope * fabsf((float)(qp - kp.z));
+            x[g][4 * e + 3] -= slope * fabsf((float)(qp - kp.w));
+          }
+        }
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = 32 * g + 8 * (i >> 2) + 4 * hh + (i & 3);
+          x[g][i] = j0 + j < my_end && (ok >> (j >> 4) & 1) ? x[g][i] * mul : -INFINITY;
+        }
+      mul = 1.f;
+    }
+    u32x4g pb[4];                                                  // probabilities of keys 16 i .. 16 i + 15, eight per lane
+    auto probs = [&]() {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; i += 2) {
+        const float a = exp2_hw(fmaf(x[i >> 4][i & 15], mul, -m)), e = exp2_hw(fmaf(x[i >> 4][(i & 15) + 1], mul, -m));
+        sum += a + e;
+        pb[i >> 3][(i & 7) >> 1] = Mfma<T>::pack(a, e);
+      }
+      return sum;
+    };
+    float sum = probs();
+    if (__any(!(sum <= kSumLimit))) {                              // rare after the first tile
+      const bool move = !(fmaxf(sum, __shfl_xor(sum, 32)) <= kSumLimit);   // (a NaN beside a small sum: stays, and so does the NaN)
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i >> 4][i & 15] * mul);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = move ? fmaxf(m, top) : m, f = exp2_hw(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[c][i] *= f;
+      sum = probs();
+    }
+    l += sum;
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        const int r4 = 16 * jj + 4 * hh + (lane >> 2 & 3), ch = 32 * c + 16 * (lane >> 4 & 1) + 4 * (lane & 3);
+        const s16x4g a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.v[buf][r4 * D + 8 * v_chunk<D>(r4, ch >> 3) + (ch & 7)]);
+        const s16x4g a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.v[buf][(r4 + 8) * D + 8 * v_chunk<D>(r4, ch >> 3) + (ch & 7)]);
+        const u32x2g w0 = __builtin_bit_cast(u32x2g, a0), w1 = __builtin_bit_cast(u32x2g, a1);
+        acc[c] = Mfma<T>::m32(u32x4g{w0[0], w0[1], w1[0], w1[1]}, pb[jj], acc[c]);
+      }
+    while (odd) {                                                  // (uniform; hardly ever)
+      const int j = __builtin_ctzll(odd);
+      odd &= odd - 1;
+      float pj = 0.f;
+#pragma unroll
+      for (int e = 0; e < 32; ++e)
+        if (e == 16 * (j >> 5) + 4 * (j >> 3 & 3) + (j & 3)) pj = Mfma<T>::get(pb[e >> 3][(e & 7) >> 1], e & 1);
+      pj = __shfl(pj, n + 32 * (j >> 2 & 1));
+      const bool seen = j0 + j < my_end;
+      const T* v = (const T*)P.v + (granule_row(0, t, j >> 4) + (j & 15)) * D + 4 * hh;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float w = (float)v[32 * c + 8 * (i >> 2) + (i & 3)];
+          if (seen && !(fabsf(w) < INFINITY)) acc[c][i] += pj * w;
+        }
+    }
+  }
+  l += __shfl_xor(l, 32);
+  if (r >= R) return;
+  const size_t orow = (size_t)tok * A.Hq + hq;
+  if (np > 1) {
+    const size_t pr = parts.chunk0 + (size_t)piece * P.N * A.Hq + orow;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4g*>(parts.acc + pr * D + 32 * c + 8 * e + 4 * hh) =
+            f32x4g{acc[c][4 * e], acc[c][4 * e + 1], acc[c][4 * e + 2], acc[c][4 * e + 3]};
+    if (hh == 0) parts.ml[pr] = make_float2(m, l);
+  } else {
+    const float inv = l == 0.f ? 0.f : 1.f / l;                    // (NaN stays)
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        store4((T*)A.out + orow * D + 32 * c + 8 * e + 4 * hh, acc[c][4 * e] * inv, acc[c][4 * e + 1] * inv, acc[c][4 * e + 2] * inv,
+               acc[c][4 * e + 3] * inv);
+    if (hh == 0 && A.lse) A.lse[orow] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+  }
+}
+
+// ---- joining the pieces -------------------------------------------------------------------------------
+
 __device__ __forceinline__ int find_seq(const int32_t* cu_q, int B, int t, int lane) {
   int b = 0;
   for (int i = 0; i < B; i += 64) b += __popcll(__ballot(i + lane < B && cu_q[min(i + lane, B - 1) + 1] <= t));
   return b;
 }
+
+// One wave per row whose keys were split; rows that one workgroup finished are left alone.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs A, Cut cut, Parts parts) {
+  const Paged& P = A.P;
+  const int lane = threadIdx.x & 63;
+  const int id = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (id >= P.N * A.Hq) return;
+  const int t = id / A.Hq, hq = id % A.Hq;
+  const int b = find_seq(P.cu_q, P.B, t, lane);
+  if (b >= P.B) return;
+  const Seq s = seq_of(P, b);
+  const int i = t - s.q0;
+  if (i < 0 || i >= s.nq) return;
+  const int prefix = A.S.prefix ? A.S.prefix[b] : 0, R = s.nq * A.G, r = i * A.G + hq % A.G;
+  const bool step = R <= kStepRows;
+  const int last = step ? s.nq - 1 : min(R - 1, r / kChunkRows * kChunkRows + kChunkRows - 1) / A.G;
+  const int piece = step ? cut.step_piece : cut.chunk_piece;
+  const int np = (row_end(s, last, prefix) + piece - 1) / piece;
+  if (np <= 1) return;
+  const size_t first = step ? (size_t)(b * P.H + hq / A.G) * cut.n_step * kStepRows + r : parts.chunk0 + (size_t)t * A.Hq + hq;
+  const size_t stride = step ? kStepRows : (size_t)P.N * A.Hq;
+  float m = kUnset, l = 0.f;
+  for (int p = lane; p < np; p += 64) m = fmaxf(m, parts.ml[first + p * stride].x);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  float acc[D / 64] = {};
+  for (int p = 0; p < np; ++p) {
+    const float2 ml = parts.ml[first + p * stride];
+    const float f = exp2_hw(ml.x - m);
+    l += f * ml.y;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) acc[e] += f * parts.acc[(first + p * stride) * D + D / 64 * lane + e];
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* out = (T*)A.out + (size_t)id * D + D / 64 * lane;
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) out[e] = (T)(acc[e] * inv);
+  if (lane == 0 && A.lse) A.lse[id] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+}
+
+template <typename T, int D, int MODE>
+static hipError_t launch_attention(const PagedAttnArgs& A, hipStream_t st) {
+  const Paged& P = A.P;
+  const Cut c = cut_of(P, A.Hq);
+  Parts parts = {};
+  const size_t rows = part_rows(P, A.Hq, c, parts.chunk0);
+  parts.acc = A.ws;
+  parts.ml = (float2*)(A.ws + rows * D);
+  if (c.chunk) {
+    const int blocks = (int)(((long long)P.N * A.G) / kChunkRows + P.B);     // sum over sequences of blocks, at most
+    k_paged_chunk<T, D, MODE><<<dim3(blocks * P.H, c.n_chunk), 256, 0, st>>>(A, c.chunk_piece, c.n_chunk, parts);
+  }
+  if (c.step) k_paged_step<T, D, MODE><<<dim3(P.B * P.H, c.n_step), 64 * kStepWaves, 0, st>>>(A, c.step_piece, c.n_step, parts);
+  if (rows) k_paged_merge<T, D><<<(P.N * A.Hq + 3) / 4, 256, 0, st>>>(A, c, parts);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_attention(int dtype, int D, const PagedAttnArgs& A, hipStream_t st) {
+  const bool plain = !(A.S.cap > 0.f) && !A.S.slopes;
+#define GO(T, D) return plain ? launch_attention<T, D, 0>(A, st) : launch_attention<T, D, 1>(A, st)
+  if (dtype == ARKV_DTYPE_BF16) { if (D == 64) GO(__bf16, 64); else GO(__bf16, 128); }
+  else { if (D == 64) GO(_Float16, 64); else GO(_Float16, 128); }
+#undef GO
+}
+
+// ---- weights ------------------------------------------------------------------------------------------
 
 // logit of a raw dot product (natural units)
 __device__ __forceinline__ float logit_of(const Scores& S, float dot, float slope, int qp, int kp) {
@@ -30,60 +737,12 @@ __device__ __forceinline__ float logit_of(const Scores& S, float dot, float slop
   return x;
 }
 
-// One wave per (new token, query head): a lane per key, then a lane per channel.
-template <typename T, int D>
-__global__ __launch_bounds__(64) void k_paged_attn(PagedAttnArgs A) {
-  __shared__ float qs[D];
-  const Paged& P = A.P;
-  const int lane = threadIdx.x, t = blockIdx.x, hq = blockIdx.y, h = hq / A.G;
-  const int b = find_seq(P.cu_q, P.B, t, lane);
-  if (b >= P.B) return;
-  const Seq s = clamp_seq(P.cu_q[b], P.cu_q[b + 1], P.kv_len[b], P.N, P.max_q, P.max_kv);
-  if (t < s.q0 || t >= s.q0 + s.nq) return;
-  const T* q = (const T*)A.q.p + (size_t)t * A.q.ts + (size_t)hq * A.q.hs;
-  for (int c = lane; c < D; c += 64) qs[c] = (float)q[c];
-  __syncthreads();
-  int end = s.kv - s.nq + t - s.q0 + 1;
-  if (A.S.prefix) end = max(end, A.S.prefix[b]);
-  end = min(end, s.kv);
-  const float slope = A.S.slopes ? A.S.slopes[hq] : 0.f;
-  const int qp = A.S.slopes ? A.S.q_pos[t] : 0;
-  const int32_t* table = P.table + (size_t)b * P.width;
-  float m = -INFINITY, l = 0.f, acc[D / 64] = {};
-  for (int j0 = 0; j0 < end; j0 += 64) {
-    const int j = j0 + lane;
-    const int row = j < end ? slot_row(table, P.n_pages, P.H, h, P.lg_page, s.kv, j) : -1;
-    float x = -INFINITY;
-    if (row >= 0) {
-      const T* k = (const T*)P.k + (size_t)row * D;
-      float dot = 0.f;
-      for (int c = 0; c < D; ++c) dot += qs[c] * (float)k[c];
-      x = logit_of(A.S, dot, slope, qp, A.S.slopes ? P.pos[row] : 0);
-    }
-    const float mn = fmaxf(m, wave_max(x));
-    const float ref = mn == -INFINITY ? 0.f : mn;
-    const float f = __expf(m - ref), p = row >= 0 ? __expf(x - ref) : 0.f;
-    m = mn;
-    l = l * f + wave_sum(p);
-    for (int e = 0; e < D / 64; ++e) acc[e] *= f;
-    for (int i = 0; i < 64; ++i) {
-      const int r = __shfl(row, i);
-      const float w = __shfl(p, i);
-      if (r < 0) continue;
-      for (int e = 0; e < D / 64; ++e) acc[e] += w * (float)((const T*)P.v)[(size_t)r * D + 64 * e + lane];
-    }
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;          // (NaN stays)
-  for (int e = 0; e < D / 64; ++e) ((T*)A.out)[((size_t)t * A.Hq + hq) * D + 64 * e + lane] = (T)(acc[e] * inv);
-  if (A.lse && lane == 0) A.lse[(size_t)t * A.Hq + hq] = l == 0.f ? -INFINITY : m + __logf(l);
-}
-
 // One wave per 64 slots of a (sequence, kv-head): a lane per key, all query rows of the group in turn.
 template <typename T, int D>
 __global__ __launch_bounds__(64) void k_paged_weights(PagedAttnArgs A) {
   const Paged& P = A.P;
   const int h = blockIdx.y, b = blockIdx.z, j = blockIdx.x * 64 + threadIdx.x;
-  const Seq s = clamp_seq(P.cu_q[b], P.cu_q[b + 1], P.kv_len[b], P.N, P.max_q, P.max_kv);
+  const Seq s = seq_of(P, b);
   const int row = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, s.kv, j);
   if (row < 0) return;
   const T* k = (const T*)P.k + (size_t)row * D;
@@ -102,20 +761,6 @@ __global__ __launch_bounds__(64) void k_paged_weights(PagedAttnArgs A) {
     }
   }
   P.weight[row] = (A.decay == 0.f ? 0.f : A.decay * A.carried[row]) + sum;
-}
-
-size_t paged_attention_floats(const Paged&, int, int) { return 0; }
-
-hipError_t launch_paged_attention(int dtype, int D, const PagedAttnArgs& A, hipStream_t st) {
-  const dim3 grid(A.P.N, A.Hq);
-  if (dtype == ARKV_DTYPE_BF16) {
-    if (D == 64) k_paged_attn<__bf16, 64><<<grid, 64, 0, st>>>(A);
-    else k_paged_attn<__bf16, 128><<<grid, 64, 0, st>>>(A);
-  } else {
-    if (D == 64) k_paged_attn<_Float16, 64><<<grid, 64, 0, st>>>(A);
-    else k_paged_attn<_Float16, 128><<<grid, 64, 0, st>>>(A);
-  }
-  return hipGetLastError();
 }
 
 hipError_t launch_paged_weights(int dtype, int D, const PagedAttnArgs& A, hipStream_t st) {

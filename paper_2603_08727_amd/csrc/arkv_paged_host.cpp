@@ -13,7 +13,7 @@ static int check(const arkv_pages* p, const arkv_page_batch* b, Paged& P) {
   if (!p || !b || !p->k || !p->v || !p->pos || !b->cu_q || !b->kv_len || !b->table) return ARKV_EINVAL;
   if (p->n_pages < 1 || p->n_kv_heads < 1 || p->head_dim < 1 || p->page_size < 1) return ARKV_EINVAL;
   if (b->batch < 1 || b->n_tokens < 0 || b->max_q < 0 || b->max_kv < 0 || b->table_width < 1) return ARKV_EINVAL;
-  if ((p->page_size & (p->page_size - 1)) || !aligned16(p->k) || !aligned16(p->v)) return ARKV_EINVAL;
+  if ((p->page_size & (p->page_size - 1)) || !aligned16(p->k) || !aligned16(p->v) || !aligned16(p->pos)) return ARKV_EINVAL;
   if (p->dtype != ARKV_DTYPE_BF16 && p->dtype != ARKV_DTYPE_FP16) return ARKV_EUNSUPPORTED;
   if ((p->head_dim != 64 && p->head_dim != 128) || p->page_size < 16 || p->page_size > 1024) return ARKV_EUNSUPPORTED;
   if ((int64_t)p->n_pages * p->n_kv_heads >= (int64_t)(1u << 31) / p->page_size) return ARKV_EUNSUPPORTED;
