@@ -92,15 +92,17 @@ constexpr int kStepWaves = 4;
 constexpr int kStepMaxPiece = 4096;     // a lane holds the page of one granule: 64 granules per wave
 constexpr int kChunkRows = 128, kChunkKeys = 64;
 
-// How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
-struct Cut { int step_piece, n_step, chunk_piece, n_chunk; bool step, chunk; };
+// How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.  few: sequences of
+// up to so many rows are the step kernel's; -1 where only the other one is launched, which then takes all of them.
+struct Cut { int step_piece, n_step, chunk_piece, n_chunk, few; bool step, chunk; };
 
 static Cut cut_of(const Paged& P, int Hq) {
   Cut c = {};
   const int G = Hq / P.H;
   const long long units = (long long)P.B * P.H;
   c.chunk = P.max_q * G > kStepRows;
-  c.step = !c.chunk || (long long)P.B * P.max_q != P.N;      // all sequences have max_q new tokens: none has few rows
+  c.step = !c.chunk || (long long)P.B * P.max_q != P.N;      // else all sequences have max_q new tokens: one launch will do
+  c.few = c.step ? kStepRows : -1;
   auto pieces = [&](long long have, int least, int most, int unit, int& piece, int& n) {
     const long long want = std::max(1ll, 512 / std::max(1ll, have));
     long long p = (P.max_kv + want - 1) / want;
@@ -370,12 +372,12 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void k_paged_step(PagedAttnArgs
 // ---- many rows ----------------------------------------------------------------------------------------
 
 // Blocks of kChunkRows rows that k_paged_chunk makes of a sequence.
-__host__ __device__ __forceinline__ int chunk_blocks(int nq, int G) { return nq * G <= kStepRows ? 0 : (nq * G + kChunkRows - 1) / kChunkRows; }
+__host__ __device__ __forceinline__ int chunk_blocks(int nq, int G, int few) { return nq * G <= few ? 0 : (nq * G + kChunkRows - 1) / kChunkRows; }
 
 // Sequence and block of the rank-th block of a launch; the lanes of a wave look at 64 sequences at a time.
-__device__ __forceinline__ bool find_block(const Paged& P, int G, int rank, int lane, int& b, int& blk) {
+__device__ __forceinline__ bool find_block(const Paged& P, int G, int few, int rank, int lane, int& b, int& blk) {
   for (int i = 0; i < P.B; i += 64) {
-    const int mine = i + lane < P.B ? chunk_blocks(seq_of(P, i + lane).nq, G) : 0;
+    const int mine = i + lane < P.B ? chunk_blocks(seq_of(P, i + lane).nq, G, few) : 0;
     int sum = mine;                                                // blocks up to and with this lane's sequence
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -417,7 +419,7 @@ template <int D> __device__ __forceinline__ int k_chunk(int row, int c) { return
 template <int D> __device__ __forceinline__ int v_chunk(int row, int c) { return D == 128 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; }
 
 template <typename T, int D, int MODE>
-__global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs A, int piece_keys, int n_pieces, Parts parts) {
+__global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs A, int few, int piece_keys, Parts parts) {
   constexpr int KK = D / 16, CB = D / 32, CPR = D / 8, RPI = 64 / CPR, LPG = 16 / RPI;   // LPG: 1 KB loads of a granule
   __shared__ __align__(16) ChunkLds<D> sm;
   const Paged& P = A.P;
@@ -425,7 +427,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs A, int pie
   const int n = lane & 31, hh = lane >> 5;
   const int h = blockIdx.x % P.H, piece = blockIdx.y;
   int b, blk;
-  if (!find_block(P, A.G, blockIdx.x / P.H, lane, b, blk)) return;
+  if (!find_block(P, A.G, few, blockIdx.x / P.H, lane, b, blk)) return;
   const Seq s = seq_of(P, b);
   const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
   const int R = s.nq * A.G, r0 = blk * kChunkRows;
@@ -676,7 +678,7 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs A, Cut cut, P
   const int i = t - s.q0;
   if (i < 0 || i >= s.nq) return;
   const int prefix = A.S.prefix ? A.S.prefix[b] : 0, R = s.nq * A.G, r = i * A.G + hq % A.G;
-  const bool step = R <= kStepRows;
+  const bool step = R <= cut.few;
   const int last = step ? s.nq - 1 : min(R - 1, r / kChunkRows * kChunkRows + kChunkRows - 1) / A.G;
   const int piece = step ? cut.step_piece : cut.chunk_piece;
   const int np = (row_end(s, last, prefix) + piece - 1) / piece;
@@ -712,7 +714,7 @@ static hipError_t launch_attention(const PagedAttnArgs& A, hipStream_t st) {
   parts.ml = (float2*)(A.ws + rows * D);
   if (c.chunk) {
     const int blocks = (int)(((long long)P.N * A.G) / kChunkRows + P.B);     // sum over sequences of blocks, at most
-    k_paged_chunk<T, D, MODE><<<dim3(blocks * P.H, c.n_chunk), 256, 0, st>>>(A, c.chunk_piece, c.n_chunk, parts);
+    k_paged_chunk<T, D, MODE><<<dim3(blocks * P.H, c.n_chunk), 256, 0, st>>>(A, c.few, c.chunk_piece, parts);
   }
   if (c.step) k_paged_step<T, D, MODE><<<dim3(P.B * P.H, c.n_step), 64 * kStepWaves, 0, st>>>(A, c.step_piece, c.n_step, parts);
   if (rows) k_paged_merge<T, D><<<(P.N * A.Hq + 3) / 4, 256, 0, st>>>(A, c, parts);
@@ -729,50 +731,271 @@ hipError_t launch_paged_attention(int dtype, int D, const PagedAttnArgs& A, hipS
 
 // ---- weights ------------------------------------------------------------------------------------------
 
-// logit of a raw dot product (natural units)
-__device__ __forceinline__ float logit_of(const Scores& S, float dot, float slope, int qp, int kp) {
-  float x = dot * S.scale;
-  if (S.cap > 0.f) x = S.cap * tanhf(x / S.cap);
-  if (S.slopes) x -= slope * fabsf((float)(qp - kp));
-  return x;
+// Here query rows are on the M side (S = Q K^T), which leaves one key per lane: a lane adds up its rows' probabilities, and
+// the lanes that share a key add theirs in a fixed order at the end.  As above, few rows and many have a kernel each.
+constexpr int kWeighStepKeys = 128;     // keys per wave of k_weigh_step
+constexpr int kWeighKeys = 256, kWeighRows = 64;   // keys per workgroup and rows per tile of k_weigh_chunk
+
+__device__ __forceinline__ void store_weight(const PagedAttnArgs& A, int row, float sum) {
+  A.P.weight[row] = (A.decay == 0.f ? 0.f : A.decay * A.carried[row]) + sum;
 }
 
-// One wave per 64 slots of a (sequence, kv-head): a lane per key, all query rows of the group in turn.
-template <typename T, int D>
-__global__ __launch_bounds__(64) void k_paged_weights(PagedAttnArgs A) {
+// Few rows: bound by reading the keys.  A wave takes 128 keys, 32 at a time (two granules), the next 32 in flight.
+template <typename T, int D, int MODE>
+__global__ __launch_bounds__(256) void k_weigh_step(PagedAttnArgs A) {
+  constexpr int KK = D / 32, NT = kWeighStepKeys / 32;
   const Paged& P = A.P;
-  const int h = blockIdx.y, b = blockIdx.z, j = blockIdx.x * 64 + threadIdx.x;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, gq = lane >> 4;
+  const int h = blockIdx.y, b = blockIdx.z;
+  const int w0 = (blockIdx.x * 4 + wave) * kWeighStepKeys;
   const Seq s = seq_of(P, b);
-  const int row = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, s.kv, j);
-  if (row < 0) return;
-  const T* k = (const T*)P.k + (size_t)row * D;
-  const int ctx = s.kv - s.nq, prefix = A.S.prefix ? A.S.prefix[b] : 0;
-  const int kp = A.S.slopes ? P.pos[row] : 0;
-  float sum = 0.f;
-  for (int i = j < prefix ? 0 : max(0, j - ctx); i < s.nq; ++i) {
-    const int t = s.q0 + i;
-    for (int g = 0; g < A.G; ++g) {
-      const int hq = h * A.G + g;
-      const T* q = (const T*)A.q.p + (size_t)t * A.q.ts + (size_t)hq * A.q.hs;
-      float dot = 0.f;
-      for (int c = 0; c < D; ++c) dot += (float)q[c] * (float)k[c];
-      const float x = logit_of(A.S, dot, A.S.slopes ? A.S.slopes[hq] : 0.f, A.S.slopes ? A.S.q_pos[t] : 0, kp);
-      sum += expf(x - A.lse[(size_t)t * A.Hq + hq]);
+  const int R = s.nq * A.G;
+  if (w0 >= s.kv || R > kStepRows) return;
+  const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
+  // lane i holds the page of granule i; one that is not there becomes page 0, whose rows get nothing
+  int my_page = w0 + 16 * lane < s.kv && lane < 2 * NT ? P.table[(size_t)b * P.width + ((w0 + 16 * lane) >> P.lg_page)] : -1;
+  const bool page_ok = (unsigned)my_page < (unsigned)P.n_pages;
+  if (!page_ok) my_page = 0;
+  const uint64_t ok_mask = __ballot(page_ok);
+  const int in_page = (1 << P.lg_page) - 1;
+  auto granule_row = [&](int g) {
+    const int page = __builtin_amdgcn_readlane(my_page, g);
+    return ((page * P.H + h) << P.lg_page) + ((w0 + 16 * g) & in_page);
+  };
+  u32x4g q[KK];
+  float lse[4], slope[4];
+  int qp[4], end[4];
+  {
+    const int row = n < R ? n : 0;                                 // (rows from R on see nothing)
+    const T* p = (const T*)A.q.p + (size_t)(s.q0 + row / A.G) * A.q.ts + (size_t)(h * A.G + row % A.G) * A.q.hs + 8 * gq;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) q[kk] = R ? *reinterpret_cast<const u32x4g*>(p + 32 * kk) : u32x4g{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 4 * gq + i, rc = row < R ? row : 0;
+    const int tok = s.q0 + rc / A.G, hq = h * A.G + rc % A.G;
+    end[i] = row < R ? row_end(s, rc / A.G, prefix) : 0;
+    lse[i] = R ? A.lse[(size_t)tok * A.Hq + hq] * kLog2e : 0.f;
+    slope[i] = MODE && R && A.S.slopes ? A.S.slopes[hq] * kLog2e : 0.f;
+    qp[i] = MODE && R && A.S.slopes ? A.S.q_pos[tok] : 0;
+  }
+  const Logit lg(A.S);
+  u32x4g kb[2][2][KK];
+  auto load_k = [&](int t, u32x4g (&to)[2][KK]) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const T* p = (const T*)P.k + (size_t)(unsigned)granule_row(2 * t + g) * D + n * D + 8 * gq;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) to[g][kk] = *reinterpret_cast<const u32x4g*>(p + 32 * kk);
+    }
+  };
+  load_k(0, kb[0]);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (w0 + 32 * t >= s.kv) break;
+    if (t + 1 < NT) load_k(t + 1, kb[(t + 1) & 1]);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      f32x4g x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) x = Mfma<T>::m16(q[kk], kb[t & 1][g][kk], x);
+      const int j = w0 + 32 * t + 16 * g + n, row = granule_row(2 * t + g) + n;
+      const bool there = j < s.kv && (ok_mask >> (2 * t + g) & 1);
+      const int kp = MODE && A.S.slopes ? P.pos[row] : 0;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float y = MODE ? lg.plain(x[i]) : x[i] * lg.mul;
+        if (MODE && A.S.slopes) y -= slope[i] * fabsf((float)(qp[i] - kp));
+        sum += j < end[i] ? exp2_hw(y - lse[i]) : 0.f;
+      }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (there && gq == 0) store_weight(A, row, sum);
     }
   }
-  P.weight[row] = (A.decay == 0.f ? 0.f : A.decay * A.carried[row]) + sum;
+}
+
+// Many rows: bound by the matrix cores and the exponentials.  One workgroup = 256 keys of a (sequence, kv-head), 64 per wave,
+// held in registers as B operands, and a share of the rows that see them; rows come through LDS, 64 at a time, the next 64
+// on their way.
+template <int D> struct WeighLds {
+  uint16_t q[2][kWeighRows * D];
+  float lse[2][kWeighRows], slope[2][kWeighRows];
+  int qp[2][kWeighRows];
+};
+
+// 4 bytes per lane from memory to LDS, in lane order; as load_lds
+__device__ __forceinline__ void load_lds4(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(p), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void load_lds16(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
+}
+
+template <typename T, int D, int MODE>
+__global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few, int n_shares) {
+  constexpr int KK = D / 16, CPR = D / 8, RPI = 64 / CPR, LPW = kWeighRows / RPI / 4;    // LPW: 1 KB loads of a tile per wave
+  __shared__ __align__(16) WeighLds<D> sm;
+  const Paged& P = A.P;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int share = blockIdx.x % n_shares, blk = blockIdx.x / n_shares, h = blockIdx.y, b = blockIdx.z;
+  const Seq s = seq_of(P, b);
+  const int R = s.nq * A.G, j00 = blk * kWeighKeys;
+  if (R <= few || j00 >= s.kv) return;
+  const int prefix = A.S.prefix ? A.S.prefix[b] : 0, ctx = s.kv - s.nq;
+  const int w0 = j00 + 64 * wave;                                  // this wave's keys
+  const int32_t* table = P.table + (size_t)b * P.width;
+  // rows that see key j start here
+  auto first_row = [&](int j) { return j < prefix ? 0 : max(0, j - ctx) * A.G; };
+  const int start = first_row(j00) / kWeighRows, tiles = (R + kWeighRows - 1) / kWeighRows;
+  const int per = (max(0, tiles - start) + n_shares - 1) / n_shares;
+  const int t0 = min(start + share * per, tiles), t1 = min(t0 + per, tiles);
+  const int wave_lo = first_row(min(w0 + 63, s.kv - 1));           // rows from here on see all keys of the wave (prefixes grow with no key)
+  u32x4g k[2][KK];
+  int krow[2], lo[2], kp[2];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const int j = w0 + 32 * g + n;
+    krow[g] = slot_row(table, P.n_pages, P.H, h, P.lg_page, s.kv, j);
+    lo[g] = krow[g] < 0 ? 0x7FFFFFFF : first_row(j);
+    const T* p = (const T*)P.k + (size_t)max(krow[g], 0) * D + 8 * hh;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) k[g][kk] = *reinterpret_cast<const u32x4g*>(p + 16 * kk);
+    kp[g] = MODE && A.S.slopes ? P.pos[max(krow[g], 0)] : 0;
+  }
+  const bool all_there = !__any(krow[0] < 0 || krow[1] < 0);
+  const uint32_t lds_q = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.q;
+  const uint32_t lds_lse = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.lse;
+  const uint32_t lds_slope = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.slope;
+  const uint32_t lds_qp = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.qp;
+  auto fetch = [&](int t, int buf) {
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+      const int lr = 16 * wave + RPI * i + lane / CPR, r = min(kWeighRows * t + lr, R - 1);   // (rows from R on: masked)
+      const T* p = (const T*)A.q.p + (size_t)(s.q0 + r / A.G) * A.q.ts + (size_t)(h * A.G + r % A.G) * A.q.hs + 8 * k_chunk<D>(lr, lane % CPR);
+      load_lds16(p, lds_q + 2 * (buf * kWeighRows * D + (16 * wave + RPI * i) * D));
+    }
+    const int r = min(kWeighRows * t + lane, R - 1), tok = s.q0 + r / A.G, hq = h * A.G + r % A.G;
+    if (wave == 0) load_lds4(A.lse + (size_t)tok * A.Hq + hq, lds_lse + 4 * buf * kWeighRows);
+    if (MODE && A.S.slopes) {
+      if (wave == 1) load_lds4(A.S.slopes + hq, lds_slope + 4 * buf * kWeighRows);
+      if (wave == 2) load_lds4(A.S.q_pos + tok, lds_qp + 4 * buf * kWeighRows);
+    }
+  };
+  const Logit lg(A.S);
+  float sum[2] = {0.f, 0.f};
+  if (t0 < t1) fetch(t0, 0);
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    vm_wait();
+    __syncthreads();
+    if (t + 1 < t1) fetch(t + 1, buf ^ 1);
+    const bool full = all_there && kWeighRows * t >= wave_lo && kWeighRows * (t + 1) <= R;
+#pragma unroll
+    for (int rb = 0; rb < kWeighRows / 32; ++rb) {
+      f32x16g x[2];
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[g][i] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const u32x4g a = *reinterpret_cast<const u32x4g*>(&sm.q[buf][(32 * rb + n) * D + 8 * k_chunk<D>(n, 2 * kk + hh)]);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) x[g] = Mfma<T>::m32(a, k[g][kk], x[g]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int lr = 32 * rb + 8 * e + 4 * hh;
+        const f32x4g z = *reinterpret_cast<const f32x4g*>(&sm.lse[buf][lr]) * kLog2e;
+        f32x4g sl = {0.f, 0.f, 0.f, 0.f};
+        int4 qp = make_int4(0, 0, 0, 0);
+        if (MODE && A.S.slopes) {
+          sl = *reinterpret_cast<const f32x4g*>(&sm.slope[buf][lr]) * kLog2e;
+          qp = *reinterpret_cast<const int4*>(&sm.qp[buf][lr]);
+        }
+        const int qpv[4] = {qp.x, qp.y, qp.z, qp.w};
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float y;
+            if (MODE) {
+              y = lg.plain(x[g][4 * e + i]) - z[i];
+              if (A.S.slopes) y -= sl[i] * fabsf((float)(qpv[i] - kp[g]));
+            } else {
+              y = fmaf(x[g][4 * e + i], lg.mul, -z[i]);
+            }
+            const float p = exp2_hw(y);
+            const int r = kWeighRows * t + lr + i;
+            sum[g] += full || (r >= lo[g] && r < R) ? p : 0.f;
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    sum[g] += __shfl_xor(sum[g], 32);
+    if (hh == 0 && krow[g] >= 0) {
+      if (n_shares == 1) store_weight(A, krow[g], sum[g]);
+      else A.ws[((size_t)share * P.B * P.H + (size_t)b * P.H + h) * P.max_kv + w0 + 32 * g + n] = sum[g];
+    }
+  }
+}
+
+// Adds the shares' sums, in order.
+__global__ __launch_bounds__(256) void k_weigh_join(PagedAttnArgs A, int few, int n_shares) {
+  const Paged& P = A.P;
+  const int h = blockIdx.y, b = blockIdx.z, j = blockIdx.x * 256 + threadIdx.x;
+  const Seq s = seq_of(P, b);
+  if (s.nq * A.G <= few) return;
+  const int row = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, s.kv, j);
+  if (row < 0) return;
+  float sum = 0.f;
+  for (int i = 0; i < n_shares; ++i) sum += A.ws[((size_t)i * P.B * P.H + (size_t)b * P.H + h) * P.max_kv + j];
+  store_weight(A, row, sum);
+}
+
+// Shares into which the rows that see a block of keys are dealt, where the blocks alone do not fill the chip; at least four
+// tiles each.
+static int weigh_shares(const Paged& P, int Hq) {
+  const long long rows = (long long)P.max_q * (Hq / P.H), blocks = (long long)P.B * P.H * ((P.max_kv + kWeighKeys - 1) / kWeighKeys);
+  if (rows <= kStepRows || blocks == 0) return 1;
+  return (int)std::max(1ll, std::min(512 / blocks, rows / (4 * kWeighRows)));
+}
+
+size_t paged_weights_floats(const Paged& P, int Hq) {
+  const int n = weigh_shares(P, Hq);
+  return n == 1 ? 0 : (size_t)n * P.B * P.H * P.max_kv;
+}
+
+template <typename T, int D, int MODE>
+static hipError_t launch_weights(const PagedAttnArgs& A, hipStream_t st) {
+  const Paged& P = A.P;
+  const Cut c = cut_of(P, A.Hq);
+  const int shares = weigh_shares(P, A.Hq);
+  if (c.chunk) {
+    const int blocks = (P.max_kv + kWeighKeys - 1) / kWeighKeys;
+    k_weigh_chunk<T, D, MODE><<<dim3(blocks * shares, P.H, P.B), 256, 0, st>>>(A, c.few, shares);
+    if (shares > 1) k_weigh_join<<<dim3((P.max_kv + 255) / 256, P.H, P.B), 256, 0, st>>>(A, c.few, shares);
+  }
+  if (c.step) {
+    const int per = 4 * kWeighStepKeys;
+    k_weigh_step<T, D, MODE><<<dim3((P.max_kv + per - 1) / per, P.H, P.B), 256, 0, st>>>(A);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_paged_weights(int dtype, int D, const PagedAttnArgs& A, hipStream_t st) {
-  const dim3 grid((A.P.max_kv + 63) / 64, A.P.H, A.P.B);
-  if (dtype == ARKV_DTYPE_BF16) {
-    if (D == 64) k_paged_weights<__bf16, 64><<<grid, 64, 0, st>>>(A);
-    else k_paged_weights<__bf16, 128><<<grid, 64, 0, st>>>(A);
-  } else {
-    if (D == 64) k_paged_weights<_Float16, 64><<<grid, 64, 0, st>>>(A);
-    else k_paged_weights<_Float16, 128><<<grid, 64, 0, st>>>(A);
-  }
-  return hipGetLastError();
+  const bool plain = !(A.S.cap > 0.f) && !A.S.slopes;
+#define GO(T, D) return plain ? launch_weights<T, D, 0>(A, st) : launch_weights<T, D, 1>(A, st)
+  if (dtype == ARKV_DTYPE_BF16) { if (D == 64) GO(__bf16, 64); else GO(__bf16, 128); }
+  else { if (D == 64) GO(_Float16, 64); else GO(_Float16, 128); }
+#undef GO
 }
 
 }  // namespace arkv

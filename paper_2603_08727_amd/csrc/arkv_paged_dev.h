@@ -65,6 +65,7 @@ struct PagedAttnArgs {
   float* ws;
 };
 size_t paged_attention_floats(const Paged& P, int D, int Hq);
+size_t paged_weights_floats(const Paged& P, int Hq);
 hipError_t launch_paged_attention(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
 hipError_t launch_paged_weights(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
 

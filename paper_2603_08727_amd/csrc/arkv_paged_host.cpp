@@ -2,6 +2,8 @@
 // here or cut to the announced bounds in the kernel (clamp_seq, page_row).
 #include <math.h>
 
+#include <algorithm>
+
 #include "arkv_paged_dev.h"
 
 using namespace arkv;
@@ -40,6 +42,11 @@ static int check_heads(int n_q_heads, int H, int& G) {
   if (n_q_heads < 1 || n_q_heads % H) return ARKV_EINVAL;
   G = n_q_heads / H;
   return G > 16 ? ARKV_EUNSUPPORTED : ARKV_OK;
+}
+
+// One size for all calls, so that a workspace serves every one of them.
+static size_t workspace_bytes(const Paged& P, int D, int Hq) {
+  return 4 * std::max(paged_attention_floats(P, D, Hq), paged_weights_floats(P, Hq));
 }
 
 static int check_scores(const arkv_scores* s, Scores& out) {
@@ -86,7 +93,7 @@ int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, 
   if (!bytes) return ARKV_EINVAL;
   TRY(check(pages, batch, P));
   TRY(check_heads(n_q_heads, P.H, G));
-  *bytes = 4 * paged_attention_floats(P, pages->head_dim, n_q_heads);
+  *bytes = workspace_bytes(P, pages->head_dim, n_q_heads);
   return ARKV_OK;
 }
 
@@ -97,7 +104,7 @@ static int attn_args(const arkv_pages* pages, const arkv_page_batch* batch, cons
   TRY(check_scores(scores, A.S));
   TRY(check_rows(q, A.q));
   A.Hq = n_q_heads;
-  const size_t need = 4 * paged_attention_floats(A.P, pages->head_dim, n_q_heads);
+  const size_t need = workspace_bytes(A.P, pages->head_dim, n_q_heads);
   if (need && (!workspace || !aligned16(workspace) || bytes < need)) return ARKV_EINVAL;
   A.ws = (float*)workspace;
   return ARKV_OK;

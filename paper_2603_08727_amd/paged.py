@@ -7,6 +7,7 @@ refuses raises binding.ArkvError.  Calls run on torch's current stream, allocate
 from __future__ import annotations
 
 import ctypes as C
+import threading
 
 from . import binding as _b
 from .binding import ArkvError, EINVAL, EUNSUPPORTED, EHIP, OK  # noqa: F401
@@ -80,10 +81,14 @@ def _need(ok, what):
 
 
 def _dense(t, shape, dtype, what, device=None):
-    _need(t.is_cuda and t.is_contiguous(), f"{what}: a contiguous GPU tensor is needed")
-    _need(t.dtype == dtype, f"{what}: expected {dtype}, got {t.dtype}")
-    _need(tuple(t.shape) == tuple(shape), f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    _need(device is None or t.device == device, f"{what}: on {t.device}, the pages are on {device}")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous GPU tensor is needed")
+    if t.dtype != dtype:
+        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{what}: on {t.device}, the pages are on {device}")
     return t.data_ptr()
 
 
@@ -96,7 +101,7 @@ class arkv_pages:
         _need(k.dim() == 4, "k: [n_pages][H_kv][page_size][d]")
         _need(k.dtype in (torch.bfloat16, torch.float16), f"k: bf16 or fp16, got {k.dtype}")
         self.k, self.v, self.pos, self.weight = k, v, pos, weight
-        self.device, self.dtype = k.device, k.dtype
+        self.device, self.dtype, self.index = k.device, k.dtype, k.device.index
         self.n_pages, self.H, self.page_size, self.d = k.shape
         dev = k.device
         self.c = _Pages(0 if k.dtype == torch.bfloat16 else 1, self.n_pages, self.page_size, self.H, self.d,
@@ -139,24 +144,42 @@ class arkv_rotary:
         self.ref = C.byref(self.c)
 
 
-def _rows(t, n, pages, what):
+# A call's own structs.  Making one costs a microsecond, so every thread keeps its set and fills it anew in each call (the C
+# side reads them before it returns).
+class _Own(threading.local):
+    def __init__(self):
+        self.q, self.k, self.v, self.s = _Rows(), _Rows(), _Rows(), _Scores()
+        self.rq, self.rk, self.rv, self.rs = (C.byref(x) for x in (self.q, self.k, self.v, self.s))
+
+
+_own = _Own()
+
+
+def _rows(to, t, n, pages, what):
     """[n][heads][d] with any token and head stride; the channels are adjacent."""
-    _need(t.is_cuda and t.dim() == 3 and t.shape[0] == n and t.shape[2] == pages.d, f"{what}: expected [{n}][heads][{pages.d}] on the GPU, got {tuple(t.shape)}")
-    _need(t.dtype == pages.dtype and t.device == pages.device, f"{what}: expected {pages.dtype} on {pages.device}")
-    _need(t.stride(2) == 1, f"{what}: channels must be adjacent")
-    return C.byref(_Rows(t.data_ptr(), t.stride(0), t.stride(1)))
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != n or shape[2] != pages.d or not t.is_cuda:
+        raise ValueError(f"{what}: expected [{n}][heads][{pages.d}] on the GPU, got {tuple(shape)}")
+    if t.dtype != pages.dtype or t.device != pages.device:
+        raise ValueError(f"{what}: expected {pages.dtype} on {pages.device}")
+    if stride[2] != 1:
+        raise ValueError(f"{what}: channels must be adjacent")
+    to.p, to.token_stride, to.head_stride = t.data_ptr(), stride[0], stride[1]
 
 
 def _current(pages, batch):
-    _need(batch.device == pages.device, "pages and batch are on different devices")
-    _need(pages.device.index == _b._device(), f"the pages are on {pages.device}, which is not the current device")
+    if batch.device != pages.device:
+        raise ValueError("pages and batch are on different devices")
+    if pages.index != _b._device():
+        raise ValueError(f"the pages are on {pages.device}, which is not the current device")
 
 
 def _workspace(ws, pages):
     if ws is None:
         return None, 0
-    _need(ws.is_cuda and ws.is_contiguous() and ws.device == pages.device, "workspace: a contiguous tensor on the pages' device")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    if not ws.is_contiguous() or ws.device != pages.device:
+        raise ValueError("workspace: a contiguous tensor on the pages' device")
+    return ws.data_ptr(), ws.nbytes
 
 
 def _call(name, *args):
@@ -179,39 +202,47 @@ def arkv_paged_append(pages, batch, rotary, q, k, v, positions, q_out):
     """q [n][H_q][d], k, v [n][H_kv][d] (strided), positions int32 [n_axes][n]; q and q_out may both be None."""
     torch = _TORCH or _torch()
     _current(pages, batch)
-    n, H = batch.n_tokens, pages.H
-    _need(k.shape[1] == H and v.shape[1] == H, f"k, v: expected {H} heads")
-    _need(rotary.freq is None or rotary.freq.device == pages.device, "freq: on another device than the pages")
+    n, H, o = batch.n_tokens, pages.H, _own
+    if k.dim() != 3 or v.dim() != 3 or k.shape[1] != H or v.shape[1] != H:
+        raise ValueError(f"k, v: expected [{n}][{H}][{pages.d}]")
+    if rotary.freq is not None and rotary.freq.device != pages.device:
+        raise ValueError("freq: on another device than the pages")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    _rows(o.k, k, n, pages, "k")
+    _rows(o.v, v, n, pages, "v")
     hq = 0
-    if q is not None or q_out is not None:
-        _need(q is not None and q_out is not None, "q and q_out go together")
+    if q is not None:
+        _rows(o.q, q, n, pages, "q")
         hq = q.shape[1]
-    _call("arkv_paged_append", pages.ref, batch.ref, rotary.ref, hq, None if q is None else _rows(q, n, pages, "q"),
-          _rows(k, n, pages, "k"), _rows(v, n, pages, "v"),
+    _call("arkv_paged_append", pages.ref, batch.ref, rotary.ref, hq, None if q is None else o.rq, o.rk, o.rv,
           _dense(positions, (rotary.n_axes, n), torch.int32, "positions", pages.device),
           None if q is None else _dense(q_out, (n, hq, pages.d), pages.dtype, "q_out", pages.device), _b._stream())
 
 
 def _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix):
-    torch = _TORCH
-    s = _Scores(scale, cap, None, None, None)
+    torch, s = _TORCH, _own.s
+    s.scale, s.cap, s.slopes, s.q_pos, s.prefix = scale, cap, None, None, None
     if slopes is not None:
-        _need(q_pos is not None, "slopes need q_pos")
+        if q_pos is None:
+            raise ValueError("slopes need q_pos")
         s.slopes = _dense(slopes, (hq,), torch.float32, "slopes", pages.device)
         s.q_pos = _dense(q_pos, (batch.n_tokens,), torch.int32, "q_pos", pages.device)
     if prefix is not None:
         s.prefix = _dense(prefix, (batch.B,), torch.int32, "prefix", pages.device)
-    return C.byref(s)
+    return _own.rs
 
 
 def arkv_paged_attention(pages, batch, q, scale, out, lse=None, cap=0.0, slopes=None, q_pos=None, prefix=None, workspace=None):
     """q [n][H_q][d] (strided), out [n][H_q][d], lse fp32 [n][H_q] or None; the other arguments as arkv_scores."""
     torch = _TORCH or _torch()
     _current(pages, batch)
-    n, hq = batch.n_tokens, q.shape[1]
+    n, o = batch.n_tokens, _own
+    _rows(o.q, q, n, pages, "q")
+    hq = q.shape[1]
     ws, size = _workspace(workspace, pages)
-    _call("arkv_paged_attention", pages.ref, batch.ref, _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix), hq,
-          _rows(q, n, pages, "q"), _dense(out, (n, hq, pages.d), pages.dtype, "out", pages.device),
+    _call("arkv_paged_attention", pages.ref, batch.ref, _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix), hq, o.rq,
+          _dense(out, (n, hq, pages.d), pages.dtype, "out", pages.device),
           None if lse is None else _dense(lse, (n, hq), torch.float32, "lse", pages.device), ws, size, _b._stream())
 
 
@@ -220,11 +251,13 @@ def arkv_paged_weights(pages, batch, q, scale, lse, decay=1.0, carried=None, cap
     """Adds the tokens' probabilities to pages.weight (decay * carried + sum); carried None: pages.weight itself."""
     torch = _TORCH or _torch()
     _current(pages, batch)
-    n, hq = batch.n_tokens, q.shape[1]
+    n, o = batch.n_tokens, _own
+    _rows(o.q, q, n, pages, "q")
+    hq = q.shape[1]
     ws, size = _workspace(workspace, pages)
-    _call("arkv_paged_weights", pages.ref, batch.ref, _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix), hq,
-          _rows(q, n, pages, "q"), _dense(lse, (n, hq), torch.float32, "lse", pages.device), decay,
-          None if carried is None else _dense(carried, (pages.n_pages, pages.H, pages.page_size), torch.float32, "carried", pages.device),
+    _call("arkv_paged_weights", pages.ref, batch.ref, _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix), hq, o.rq,
+          _dense(lse, (n, hq), torch.float32, "lse", pages.device), decay,
+          None if carried is None else _dense(carried, pages.k.shape[:3], torch.float32, "carried", pages.device),
           ws, size, _b._stream())
 
 

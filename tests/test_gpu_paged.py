@@ -229,6 +229,18 @@ def test_weights_of_scores(kind, q, kv, dtype, hq, hkv, d):
     R.close(s.weight, ref, tol, "weight")
 
 
+@pytest.mark.parametrize("lens", [(0, 0), (1, 0), (3, 40), (0, 64)])
+def test_sequences_shorter_than_announced(lens):
+    """Bounds that say 64 new tokens each for all sequences, lengths that say less: nobody is left out."""
+    s = R.problem("cuda", BF, 8, 2, 64, 16, lens, (300, 90), seed=33, extra_tokens=128 - sum(lens))
+    s.max_q = 64
+    _, lse = check_attention(s)
+    pages, batch, ws = handles(s)
+    ref, tol = R.weights(s, lse, 0.5, s.weight)
+    P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=0.5, workspace=ws)
+    R.close(s.weight, ref, tol, "weight")
+
+
 def test_weights_of_a_step_sum_to_the_tokens_and_heads():
     s = R.problem("cuda", BF, 8, 2, 128, 16, (50, 1), (333, 1000), seed=31)
     _, lse = attend(s)
