@@ -21,84 +21,112 @@ template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b
   return __builtin_bit_cast(uint32_t, h);
 }
 
-// Sequence of token t: how many sequences end at or before it.  Lanes look at 64 ends at a time.
-__device__ __forceinline__ int find_seq(const int32_t* cu_q, int B, int t, int lane) {
-  int b = 0;
-  for (int i = 0; i < B; i += 64) b += __popcll(__ballot(i + lane < B && cu_q[min(i + lane, B - 1) + 1] <= t));
-  return b;
-}
-
-constexpr int kAppendWaves = 4;
+constexpr int kAppendWaves = 4, kAppendItems = 4;
 
 // One wave per new token.  The wave's lanes form the token's angles (position times frequency in turns, in 64 bits: at
 // position 2^17 a 32-bit product is off by up to 2^-8 turns; the fraction that is left fits 32), then walk its heads'
-// 16-byte chunks in pairs: item i of a row is the pair of chunks whose channels turn together.
+// 16-byte chunks in pairs: item i of a row is the pair of chunks whose channels turn together.  A generated token is bound by
+// round trips to memory: its lengths, angles and rows are requested together, the page behind them, then it stores.
 template <typename T, int D>
 __global__ __launch_bounds__(64 * kAppendWaves) void k_paged_append(AppendArgs A) {
   __shared__ float2 turn[kAppendWaves][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = blockIdx.x * kAppendWaves + wave;
   const Paged& P = A.P;
-  if (t < P.N && lane < A.half) {
-    const double turns = (double)A.positions[(size_t)A.axis[lane] * P.N + t] * (A.freq[lane] * 0.15915494309189533577);
-    const float f = (float)(turns - rint(turns));
-    float s, c;
-    sincospif(2.0f * f, &s, &c);
-    turn[wave][lane] = make_float2(c, s);
-  }
-  __syncthreads();
   if (t >= P.N) return;
-  const int b = find_seq(P.cu_q, P.B, t, lane);
-  if (b >= P.B) return;
-  const Seq s = clamp_seq(P.cu_q[b], P.cu_q[b + 1], P.kv_len[b], P.N, P.max_q, P.max_kv);
-  if (t < s.q0 || t >= s.q0 + s.nq) return;
+  constexpr int IPR = D / 16;                                      // items of a row
+  const int Hr = A.Hq + P.H, rot = A.half / 8;                     // heads that turn; items that turn
+  const int n_items = (A.Hq + 2 * P.H) * IPR;
+  struct Item { int h, hs, c0, c1; bool turns; };
+  auto item = [&](int it) {
+    Item o;
+    o.h = it / IPR;
+    const int i = it % IPR;
+    o.hs = o.h < A.Hq ? o.h : o.h < Hr ? o.h - A.Hq : o.h - Hr;
+    o.turns = i < rot && o.h < Hr;
+    // with halves, chunk i turns with chunk i + rot; else (and behind rot_dim) two adjacent ones
+    const bool halves = i < rot && !A.adjacent;
+    o.c0 = halves ? i : 2 * i;
+    o.c1 = halves ? i + rot : 2 * i + 1;
+    return o;
+  };
+  u32x4p x[kAppendItems], y[kAppendItems];
+  auto load = [&](int it0) {
+#pragma unroll
+    for (int u = 0; u < kAppendItems; ++u) {
+      const int it = it0 + 64 * u + lane;
+      if (it >= n_items) continue;
+      const Item o = item(it);
+      const Rows& src = o.h < A.Hq ? A.q : o.h < Hr ? A.k : A.v;
+      const T* from = (const T*)src.p + (size_t)t * src.ts + (size_t)o.hs * src.hs;
+      x[u] = *reinterpret_cast<const u32x4p*>(from + 8 * o.c0);
+      y[u] = *reinterpret_cast<const u32x4p*>(from + 8 * o.c1);
+    }
+  };
+  load(0);
+  const int position = A.positions[t];
+  double angle_pos = 0, angle_freq = 0;
+  if (lane < A.half) {
+    angle_pos = (double)A.positions[(size_t)A.axis[lane] * P.N + t];
+    angle_freq = A.freq[lane];
+  }
+  // the token's sequence: the first that ends behind it; the lanes look at 64 at a time
+  int b = -1;
+  Seq s = {0, 0, 0};
+  for (int i = 0; i < P.B && b < 0; i += 64) {
+    const int at = min(i + lane, P.B - 1);
+    const int q0 = P.cu_q[at], q1 = P.cu_q[at + 1], kv = P.kv_len[at];
+    const uint64_t hit = __ballot(i + lane < P.B && q1 > t);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      b = i + l;
+      s = clamp_seq(__builtin_amdgcn_readlane(q0, l), __builtin_amdgcn_readlane(q1, l), __builtin_amdgcn_readlane(kv, l), P.N, P.max_q, P.max_kv);
+    }
+  }
+  if (b < 0 || t < s.q0 || t >= s.q0 + s.nq) return;               // a row of no sequence
   const int slot = s.kv - s.nq + t - s.q0;
   const int row0 = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, 0, P.lg_page, s.kv, slot);
+  if (lane < A.half) {
+    const double turns = angle_pos * (angle_freq * 0.15915494309189533577);
+    float sn, cs;
+    sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+    turn[wave][lane] = make_float2(cs, sn);                        // (read by this wave alone)
+  }
   if (row0 >= 0)
     for (int h = lane; h < P.H; h += 64) {
-      P.pos[(size_t)row0 + ((size_t)h << P.lg_page)] = A.positions[t];
+      P.pos[(size_t)row0 + ((size_t)h << P.lg_page)] = position;
       if (P.weight) P.weight[(size_t)row0 + ((size_t)h << P.lg_page)] = 0.f;
     }
-  constexpr int IPR = D / 16;                       // items of a row
-  const int Hr = A.Hq + P.H, rot = A.half / 8;      // heads that turn; items that turn
-  const int n_items = (A.Hq + 2 * P.H) * IPR;
-  for (int it = lane; it < n_items; it += 64) {
-    const int h = it / IPR, i = it % IPR;
-    const Rows& src = h < A.Hq ? A.q : h < Hr ? A.k : A.v;
-    const int hs = h < A.Hq ? h : h < Hr ? h - A.Hq : h - Hr;
-    T* to;
-    if (h < A.Hq) to = (T*)A.q_out + ((size_t)t * A.Hq + h) * D;
-    else {
-      if (row0 < 0) continue;
-      to = (T*)(h < Hr ? P.k : P.v) + ((size_t)row0 + ((size_t)hs << P.lg_page)) * D;
-    }
-    const T* from = (const T*)src.p + (size_t)t * src.ts + (size_t)hs * src.hs;
-    // chunks of this item: with halves, chunk i turns with chunk i + rot; else (and behind rot_dim) two adjacent ones
-    const bool turns = i < rot && h < Hr;
-    const bool halves = i < rot && !A.adjacent;
-    const int c0 = halves ? i : 2 * i, c1 = halves ? i + rot : 2 * i + 1;
-    u32x4p x = *reinterpret_cast<const u32x4p*>(from + 8 * c0), y = *reinterpret_cast<const u32x4p*>(from + 8 * c1);
-    if (turns) {
-      if (!A.adjacent) {
+  for (int it0 = 0; it0 < n_items; it0 += 64 * kAppendItems) {
+    if (it0) load(it0);
+#pragma unroll
+    for (int u = 0; u < kAppendItems; ++u) {
+      const int it = it0 + 64 * u + lane;
+      if (it >= n_items) continue;
+      const Item o = item(it);
+      if (o.turns) {
+        const int i = o.c0;                                        // (halves: the pairs 8 i ..; adjacent: chunk c0 = 2 i holds 4 pairs)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float2 a = unpack2<T>(x[e]), o = unpack2<T>(y[e]);
-          const float2 t0 = turn[wave][8 * i + 2 * e], t1 = turn[wave][8 * i + 2 * e + 1];
-          x[e] = pack2<T>(a.x * t0.x - o.x * t0.y, a.y * t1.x - o.y * t1.y);
-          y[e] = pack2<T>(o.x * t0.x + a.x * t0.y, o.y * t1.x + a.y * t1.y);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 a = unpack2<T>(x[e]), o = unpack2<T>(y[e]);
-          const float2 t0 = turn[wave][8 * i + e], t1 = turn[wave][8 * i + 4 + e];
-          x[e] = pack2<T>(a.x * t0.x - a.y * t0.y, a.y * t0.x + a.x * t0.y);
-          y[e] = pack2<T>(o.x * t1.x - o.y * t1.y, o.y * t1.x + o.x * t1.y);
+          const float2 a = unpack2<T>(x[u][e]), z = unpack2<T>(y[u][e]);
+          if (!A.adjacent) {
+            const float2 t0 = turn[wave][8 * i + 2 * e], t1 = turn[wave][8 * i + 2 * e + 1];
+            x[u][e] = pack2<T>(a.x * t0.x - z.x * t0.y, a.y * t1.x - z.y * t1.y);
+            y[u][e] = pack2<T>(z.x * t0.x + a.x * t0.y, z.y * t1.x + a.y * t1.y);
+          } else {
+            const float2 t0 = turn[wave][4 * i + e], t1 = turn[wave][4 * i + 4 + e];
+            x[u][e] = pack2<T>(a.x * t0.x - a.y * t0.y, a.y * t0.x + a.x * t0.y);
+            y[u][e] = pack2<T>(z.x * t1.x - z.y * t1.y, z.y * t1.x + z.x * t1.y);
+          }
         }
       }
+      T* to;
+      if (o.h < A.Hq) to = (T*)A.q_out + ((size_t)t * A.Hq + o.h) * D;
+      else if (row0 < 0) continue;
+      else to = (T*)(o.h < Hr ? P.k : P.v) + ((size_t)row0 + ((size_t)o.hs << P.lg_page)) * D;
+      *reinterpret_cast<u32x4p*>(to + 8 * o.c0) = x[u];
+      *reinterpret_cast<u32x4p*>(to + 8 * o.c1) = y[u];
     }
-    *reinterpret_cast<u32x4p*>(to + 8 * c0) = x;
-    *reinterpret_cast<u32x4p*>(to + 8 * c1) = y;
   }
 }
 
@@ -136,110 +164,190 @@ __device__ __forceinline__ Kept kept_of(const EvictArgs& A, int b) {
   return k;
 }
 
-// Which rows of a (sequence, kv-head) stay: one workgroup finds the weight of the last one by four passes over the
-// weights, eight bits of their order each, then writes the survivors' slots in order.
+// Adds one to hist[bin] for every lane with `on`; the lanes that share the first one's bin (equal weights, such as those of
+// rows that nobody looked at) add once: 64 additions to one word would queue.
+__device__ __forceinline__ void count_bin(int* hist, bool on, int bin, int lane) {
+  const uint64_t live = __ballot(on);
+  if (!live) return;
+  const int first = __builtin_ctzll(live), shared = __builtin_amdgcn_readlane(bin, first);
+  const uint64_t same = __ballot(on && bin == shared);
+  if (lane == first) atomicAdd(&hist[shared], __popcll(same));
+  else if (on && bin != shared) atomicAdd(&hist[bin], 1);
+}
+
+constexpr int kEvictBins = 2048;        // eleven bits of a key
+constexpr int kEvictLdsRows = 36 << 10; // keys that fit LDS beside the bins
+
+// Which rows of a (sequence, kv-head) stay.  One workgroup finds the key of the last one digit by digit, from the top: how
+// many rows have which digit, and the digit at which the rows to keep run out; a digit whose rows all stay ends the search.
+// Then every wave writes its share's survivors, behind those of the shares before.  IN_LDS: the keys are read from memory
+// once; else (more rows than LDS holds) in every pass.
+template <bool IN_LDS>
 __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
-  __shared__ int hist[256];
-  __shared__ int sums[2][kEvictThreads / 64];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_need;
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  extern __shared__ uint32_t keys[];
+  constexpr int NW = kEvictThreads / 64, BPT = kEvictBins / kEvictThreads;
+  __shared__ int hist[kEvictBins];
+  __shared__ int sums[NW], gts[NW], ties_in[NW];
+  __shared__ int s_bin, s_left, s_count;
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Kept K = kept_of(A, b);
   const int32_t* table = A.P.table + (size_t)b * A.P.width;
   int32_t* kept = A.kept + ((size_t)b * A.P.H + h) * A.max_keep;
   if (h == 0 && tid == 0) A.new_len[b] = K.m;
-  const int lo = K.front, hi = K.n - K.back;          // ranked slots
-  int need = K.m - K.front - K.back;
-  auto key = [&](int j) {
+  const int lo = K.front, hi = K.n - K.back;                       // ranked slots
+  const int ranked = K.m - K.front - K.back;
+  const bool all = ranked >= hi - lo, none = ranked <= 0;
+  auto fetch = [&](int j) {
     const int r = slot_row(table, A.P.n_pages, A.P.H, h, A.P.lg_page, K.n, j);
     return r < 0 ? 0u : weight_key(A.P.weight[r]);
   };
-  uint32_t prefix = 0;                                 // the key of the last row that stays, digit by digit
-  if (need > 0 && need < hi - lo) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int j = lo + tid; j < hi; j += kEvictThreads) {
-        const uint32_t x = key(j);
-        if (shift == 24 || x >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[x >> shift & 255], 1);
+  auto key = [&](int j) { return IN_LDS ? keys[j] : fetch(j); };
+  // survivors: keys above `last`, and of those equal to it the first `need`
+  uint32_t last = 0;
+  int need = 0;
+  if (!all && !none) {
+    for (int i = tid; i < kEvictBins; i += kEvictThreads) hist[i] = 0;
+    if (IN_LDS) {
+#pragma unroll 4
+      for (int j = lo + tid; j < hi; j += kEvictThreads) keys[j] = fetch(j);
+    }
+    __syncthreads();
+    need = ranked;
+    uint32_t prefix = 0;
+    for (int shift = 21; ; shift = shift == 21 ? 10 : 0) {
+      const int bits = shift ? 11 : 10;
+      for (int j0 = lo; j0 < hi; j0 += kEvictThreads) {
+        const int j = j0 + tid;
+        const uint32_t x = j < hi ? key(j) : 0;
+        const bool on = j < hi && (shift == 21 || x >> (shift + bits) == prefix >> (shift + bits));
+        count_bin(hist, on, x >> shift & ((1 << bits) - 1), lane);
       }
       __syncthreads();
-      if (tid == 0) {
-        int left = need, d = 255;
-        for (; d > 0 && hist[d] < left; --d) left -= hist[d];
-        s_prefix = prefix | (uint32_t)d << shift;
-        s_need = left;
+      // thread t: the bins at BPT t from the top
+      int c[BPT], mine = 0;
+#pragma unroll
+      for (int i = 0; i < BPT; ++i) {
+        c[i] = hist[kEvictBins - 1 - (BPT * tid + i)];
+        hist[kEvictBins - 1 - (BPT * tid + i)] = 0;
+        mine += c[i];
+      }
+      int upto = mine;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(upto, o);
+        if (lane >= o) upto += v;
+      }
+      if (lane == 63) sums[wave] = upto;
+      __syncthreads();
+      int before = upto - mine;
+      for (int w = 0; w < wave; ++w) before += sums[w];
+#pragma unroll
+      for (int i = 0; i < BPT; ++i) {
+        if (before < need && need <= before + c[i]) {
+          s_bin = kEvictBins - 1 - (BPT * tid + i);
+          s_left = need - before;
+          s_count = c[i];
+        }
+        before += c[i];
       }
       __syncthreads();
-      prefix = s_prefix;
-      need = s_need;                                   // rows of the prefix's digits that stay
-      __syncthreads();
+      prefix |= (uint32_t)s_bin << shift;
+      need = s_left;
+      if (s_count == need && prefix) {                             // the whole digit stays: everything from its lowest key on
+        last = prefix - 1;
+        need = 0;
+        break;
+      }
+      last = prefix;
+      if (!shift) break;
     }
   }
-  const bool all = K.m - K.front - K.back >= hi - lo, none = K.m - K.front - K.back <= 0;
-  int at = 0, ties = 0;                                // survivors and equal keys in front of this block of slots
-  for (int j0 = 0; j0 < K.n; j0 += kEvictThreads) {
-    const int j = j0 + tid;
-    bool take = false, tie = false;
-    if (j < K.n) {
-      if (j < lo || j >= hi || all) take = true;
-      else if (!none) {
-        const uint32_t x = key(j);
-        take = x > prefix;
-        tie = x == prefix;
-      }
-    }
-    const uint64_t below = (1ull << lane) - 1;
+  // every wave takes a share of the slots, whole blocks of 64
+  const int per = ((K.n + 63) / 64 + NW - 1) / NW * 64, b0 = min(wave * per, K.n), b1 = min(b0 + per, K.n);
+  auto fate = [&](int j, bool& tie) {                              // 0 leaves, 1 stays; tie: by rank among the equal ones
+    tie = false;
+    if (j >= b1) return false;
+    if (j < lo || j >= hi || all) return true;
+    if (none) return false;
+    const uint32_t x = key(j);
+    tie = x == last && need > 0;
+    return x > last;
+  };
+  int n_gt = 0, n_tie = 0;
+  for (int j0 = b0; j0 < b1; j0 += 64) {
+    bool tie;
+    n_gt += __popcll(__ballot(fate(j0 + lane, tie)));
+    n_tie += __popcll(__ballot(tie));
+  }
+  if (lane == 0) { gts[wave] = n_gt; ties_in[wave] = n_tie; }
+  __syncthreads();
+  int at = 0, tied = 0;                                            // survivors and equal keys in front of this share
+  for (int w = 0; w < wave; ++w) { at += gts[w]; tied += ties_in[w]; }
+  at += min(tied, need);
+  const uint64_t below = (1ull << lane) - 1;
+  for (int j0 = b0; j0 < b1; j0 += 64) {
+    bool tie;
+    bool take = fate(j0 + lane, tie);
     const uint64_t tb = __ballot(tie);
-    if (lane == 0) sums[0][wave] = __popcll(tb);
-    __syncthreads();
-    int before = ties;
-    for (int w = 0; w < kEvictThreads / 64; ++w) {
-      if (w < wave) before += sums[0][w];
-      ties += sums[0][w];
-    }
-    if (tie && before + __popcll(tb & below) < need) take = true;
+    if (tie && tied + __popcll(tb & below) < need) take = true;
+    tied += __popcll(tb);
     const uint64_t kb = __ballot(take);
-    if (lane == 0) sums[1][wave] = __popcll(kb);
-    __syncthreads();
-    int mine = at;
-    for (int w = 0; w < kEvictThreads / 64; ++w) {
-      if (w < wave) mine += sums[1][w];
-      at += sums[1][w];
-    }
-    if (take) {
-      mine += __popcll(kb & below);
-      if (mine < A.max_keep) kept[mine] = j;
-    }
-    __syncthreads();
+    const int to = at + __popcll(kb & below);
+    if (take && to < A.max_keep) kept[to] = j0 + lane;
+    at += __popcll(kb);
   }
   for (int i = K.m + tid; i < A.max_keep; i += kEvictThreads) kept[i] = -1;
 }
 
-// Copies the survivors to their new slots.  D / 8 lanes per row.
+// Copies the survivors to their new slots: D / 8 lanes a row, kMoveRows rows per lane whose loads are all under way together.
+constexpr int kMoveRows = 4;
 template <int D>
 __global__ __launch_bounds__(256) void k_evict_move(EvictArgs A) {
   constexpr int LPR = D / 8, RPW = 256 / LPR;
-  const int h = blockIdx.y, b = blockIdx.z;
-  const int i = blockIdx.x * RPW + threadIdx.x / LPR, c = threadIdx.x % LPR;
-  const Kept K = kept_of(A, b);
-  if (i >= K.m) return;
+  const int h = blockIdx.y, b = blockIdx.z, c = threadIdx.x % LPR;
+  const int i0 = blockIdx.x * RPW * kMoveRows + threadIdx.x / LPR;
   const Paged& P = A.P;
-  const int j = A.kept[((size_t)b * P.H + h) * A.max_keep + i];
-  const int from = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, K.n, j);
-  const int to = slot_row(A.dst_table + (size_t)b * A.dst_width, P.n_pages, P.H, h, P.lg_page, K.m, i);
-  if (from < 0 || to < 0) return;
-  const u32x4p* k = (const u32x4p*)P.k + (size_t)from * LPR + c;
-  const u32x4p* v = (const u32x4p*)P.v + (size_t)from * LPR + c;
-  const u32x4p x = *k, y = *v;
-  ((u32x4p*)P.k)[(size_t)to * LPR + c] = x;
-  ((u32x4p*)P.v)[(size_t)to * LPR + c] = y;
-  if (c == 0) { P.pos[to] = P.pos[from]; P.weight[to] = P.weight[from]; }
+  const Kept K = kept_of(A, b);
+  const int32_t* kept = A.kept + ((size_t)b * P.H + h) * A.max_keep;
+  int from[kMoveRows], to[kMoveRows];
+#pragma unroll
+  for (int r = 0; r < kMoveRows; ++r) {
+    const int i = i0 + r * RPW;
+    from[r] = i < K.m ? kept[i] : -1;
+  }
+#pragma unroll
+  for (int r = 0; r < kMoveRows; ++r) {
+    from[r] = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, K.n, from[r]);
+    to[r] = slot_row(A.dst_table + (size_t)b * A.dst_width, P.n_pages, P.H, h, P.lg_page, K.m, i0 + r * RPW);
+  }
+  u32x4p x[kMoveRows], y[kMoveRows];
+#pragma unroll
+  for (int r = 0; r < kMoveRows; ++r) {
+    x[r] = ((const u32x4p*)P.k)[(size_t)max(from[r], 0) * LPR + c];
+    y[r] = ((const u32x4p*)P.v)[(size_t)max(from[r], 0) * LPR + c];
+  }
+#pragma unroll
+  for (int r = 0; r < kMoveRows; ++r) {
+    if (from[r] < 0 || to[r] < 0) continue;
+    ((u32x4p*)P.k)[(size_t)to[r] * LPR + c] = x[r];
+    ((u32x4p*)P.v)[(size_t)to[r] * LPR + c] = y[r];
+    if (c == 0) P.pos[to[r]] = P.pos[from[r]];
+    if (c == 1) P.weight[to[r]] = P.weight[from[r]];
+  }
 }
 
 hipError_t launch_paged_evict(int D, const EvictArgs& A, hipStream_t st) {
-  k_evict_select<<<dim3(A.P.H, A.P.B), kEvictThreads, 0, st>>>(A);
-  const int rows = std::min(A.max_keep, A.P.max_kv), rpw = 256 / (D / 8);
+  const dim3 units(A.P.H, A.P.B);
+  if (A.P.max_kv <= kEvictLdsRows) {
+    const size_t bytes = 4 * (size_t)std::max(A.P.max_kv, 1);
+    // (more than 64 KB of LDS has to be asked for, once per kernel and device)
+    const hipError_t e = hipFuncSetAttribute((const void*)k_evict_select<true>, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kEvictLdsRows);
+    if (e != hipSuccess) return e;
+    k_evict_select<true><<<units, kEvictThreads, bytes, st>>>(A);
+  } else {
+    k_evict_select<false><<<units, kEvictThreads, 0, st>>>(A);
+  }
+  const int rows = std::min(A.max_keep, A.P.max_kv), rpw = 256 / (D / 8) * kMoveRows;
   if (rows > 0) {
     const dim3 grid((rows + rpw - 1) / rpw, A.P.H, A.P.B);
     if (D == 64) k_evict_move<64><<<grid, 256, 0, st>>>(A);
