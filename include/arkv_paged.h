@@ -35,7 +35,7 @@ extern "C" {
 
 /* One layer's pages.  k, v DEVICE [n_pages][H_kv][page_size][d] of dtype; pos DEVICE int32, weight DEVICE float
  * [n_pages][H_kv][page_size]: a row's position and the attention weight it collected (weight may be NULL where no
- * weights are kept).  page_size: a power of two from 16 to 1024.  head_dim 64 or 128.  n_pages H_kv page_size < 2^31.  k, v and pos 16-byte aligned. */
+ * weights are kept).  page_size: a power of two from 16 to 1024.  head_dim 64 or 128.  n_pages H_kv page_size < 2^31.  All four 16-byte aligned. */
 typedef struct {
   int32_t dtype, n_pages, page_size, n_kv_heads, head_dim;
   void* k;
@@ -46,7 +46,8 @@ typedef struct {
 
 /* One step's sequences.  cu_q DEVICE int32 [B+1] (not decreasing), kv_len DEVICE int32 [B], table DEVICE int32
  * [B][table_width] (entries behind a sequence's last page are not read).  n_tokens: rows of the token-major arrays;
- * max_q, max_kv: bounds of q_len and kv_len (they shape the launches; tight ones are faster). */
+ * max_q, max_kv: bounds of q_len and kv_len (they shape the launches; tight ones are faster).  B H_kv <= 2^20, B H_kv max_kv <= 2^40,
+ * n_tokens H_q < 2^31. */
 typedef struct {
   int32_t batch, n_tokens, max_q, max_kv, table_width;
   const int32_t* cu_q;

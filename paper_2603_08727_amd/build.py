@@ -16,7 +16,7 @@ LIB_TRACE = os.path.join(HERE, "libarkv_trace.so")
 LIB_MEASURE = os.path.join(HERE, "libarkv_measure.so")   # bandwidth measurement kernels, not part of the product
 MEASURE_SOURCES = ["arkv_measure.hip"]
 SOURCES = ["arkv_host.cpp", "arkv_decode.hip", "arkv_tailor.hip", "arkv_prefill.hip", "arkv_attn.hip",
-           "arkv_paged_host.cpp", "arkv_paged.hip", "arkv_paged_attn.hip"]
+           "arkv_paged_host.cpp", "arkv_paged.hip", "arkv_paged_attn.hip", "arkv_paged_weigh.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

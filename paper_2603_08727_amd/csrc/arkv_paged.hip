@@ -50,6 +50,9 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_paged_append(AppendArgs A
     o.c1 = halves ? i + rot : 2 * i + 1;
     return o;
   };
+  // (values, not structs, are chosen between: a lane's own choice of a struct would be read from memory)
+  const T *qp = (const T*)A.q.p + (size_t)t * A.q.ts, *kp = (const T*)A.k.p + (size_t)t * A.k.ts, *vp = (const T*)A.v.p + (size_t)t * A.v.ts;
+  const int64_t qs = A.q.hs, ks = A.k.hs, vs = A.v.hs;
   u32x4p x[kAppendItems], y[kAppendItems];
   auto load = [&](int it0) {
 #pragma unroll
@@ -57,8 +60,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_paged_append(AppendArgs A
       const int it = it0 + 64 * u + lane;
       if (it >= n_items) continue;
       const Item o = item(it);
-      const Rows& src = o.h < A.Hq ? A.q : o.h < Hr ? A.k : A.v;
-      const T* from = (const T*)src.p + (size_t)t * src.ts + (size_t)o.hs * src.hs;
+      const T* from = (o.h < A.Hq ? qp : o.h < Hr ? kp : vp) + (o.h < A.Hq ? qs : o.h < Hr ? ks : vs) * o.hs;
       x[u] = *reinterpret_cast<const u32x4p*>(from + 8 * o.c0);
       y[u] = *reinterpret_cast<const u32x4p*>(from + 8 * o.c1);
     }
@@ -176,16 +178,17 @@ __device__ __forceinline__ void count_bin(int* hist, bool on, int bin, int lane)
 }
 
 constexpr int kEvictBins = 2048;        // eleven bits of a key
-constexpr int kEvictLdsRows = 36 << 10; // keys that fit LDS beside the bins
+constexpr int kEvictLdsBlocks = 9;      // blocks of 4 x kEvictThreads keys that fit LDS beside the bins
 
 // Which rows of a (sequence, kv-head) stay.  One workgroup finds the key of the last one digit by digit, from the top: how
 // many rows have which digit, and the digit at which the rows to keep run out; a digit whose rows all stay ends the search.
-// Then every wave writes its share's survivors, behind those of the shares before.  IN_LDS: the keys are read from memory
-// once; else (more rows than LDS holds) in every pass.
+// Then every wave writes the survivors among its slots, behind those of the waves before.  A wave's slots are adjacent,
+// four per lane and block (in one page: one look at the table and one 16-byte load).  IN_LDS: the keys are read from memory
+// once and stay in LDS; else (more rows than it holds) they are read in every pass.
 template <bool IN_LDS>
 __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
-  extern __shared__ uint32_t keys[];
   constexpr int NW = kEvictThreads / 64, BPT = kEvictBins / kEvictThreads;
+  extern __shared__ u32x4p held[];                                 // [block][thread]
   __shared__ int hist[kEvictBins];
   __shared__ int sums[NW], gts[NW], ties_in[NW];
   __shared__ int s_bin, s_left, s_count;
@@ -197,31 +200,43 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
   const int lo = K.front, hi = K.n - K.back;                       // ranked slots
   const int ranked = K.m - K.front - K.back;
   const bool all = ranked >= hi - lo, none = ranked <= 0;
-  auto fetch = [&](int j) {
+  const int nq = (K.n + 256 * NW - 1) / (256 * NW);                // blocks of 256 slots per wave
+  const int w0 = wave * nq * 256;
+  auto fetch = [&](int q) {                                        // keys of the lane's four slots of block q
+    const int j = w0 + 256 * q + 4 * lane;
+    u32x4p k = {0, 0, 0, 0};
     const int r = slot_row(table, A.P.n_pages, A.P.H, h, A.P.lg_page, K.n, j);
-    return r < 0 ? 0u : weight_key(A.P.weight[r]);
+    if (r >= 0) {
+      const float4 w = *reinterpret_cast<const float4*>(A.P.weight + r);
+      k = u32x4p{weight_key(w.x), weight_key(w.y), weight_key(w.z), weight_key(w.w)};
+    }
+    return k;
   };
-  auto key = [&](int j) { return IN_LDS ? keys[j] : fetch(j); };
+  auto key = [&](int q) { return IN_LDS ? held[q * kEvictThreads + tid] : fetch(q); };
   // survivors: keys above `last`, and of those equal to it the first `need`
   uint32_t last = 0;
   int need = 0;
   if (!all && !none) {
     for (int i = tid; i < kEvictBins; i += kEvictThreads) hist[i] = 0;
-    if (IN_LDS) {
+    if (IN_LDS) {                                                  // (a thread's own keys: nobody else reads them)
 #pragma unroll 4
-      for (int j = lo + tid; j < hi; j += kEvictThreads) keys[j] = fetch(j);
+      for (int q = 0; q < nq; ++q) held[q * kEvictThreads + tid] = fetch(q);
     }
     __syncthreads();
     need = ranked;
     uint32_t prefix = 0;
     for (int shift = 21; ; shift = shift == 21 ? 10 : 0) {
       const int bits = shift ? 11 : 10;
-      for (int j0 = lo; j0 < hi; j0 += kEvictThreads) {
-        const int j = j0 + tid;
-        const uint32_t x = j < hi ? key(j) : 0;
-        const bool on = j < hi && (shift == 21 || x >> (shift + bits) == prefix >> (shift + bits));
-        count_bin(hist, on, x >> shift & ((1 << bits) - 1), lane);
-      }
+      auto count = [&](int q) {
+        const u32x4p x = key(q);
+        const int j = w0 + 256 * q + 4 * lane;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool on = j + e >= lo && j + e < hi && (shift == 21 || x[e] >> (shift + bits) == prefix >> (shift + bits));
+          count_bin(hist, on, x[e] >> shift & ((1 << bits) - 1), lane);
+        }
+      };
+      for (int q = 0; q < nq; ++q) count(q);
       __syncthreads();
       // thread t: the bins at BPT t from the top
       int c[BPT], mine = 0;
@@ -262,40 +277,68 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
       if (!shift) break;
     }
   }
-  // every wave takes a share of the slots, whole blocks of 64
-  const int per = ((K.n + 63) / 64 + NW - 1) / NW * 64, b0 = min(wave * per, K.n), b1 = min(b0 + per, K.n);
-  auto fate = [&](int j, bool& tie) {                              // 0 leaves, 1 stays; tie: by rank among the equal ones
-    tie = false;
-    if (j >= b1) return false;
-    if (j < lo || j >= hi || all) return true;
-    if (none) return false;
-    const uint32_t x = key(j);
-    tie = x == last && need > 0;
-    return x > last;
+  // bit e: slot e of the lane's four stays for certain, bit 4 + e: it is one of the equal ones
+  auto fate = [&](int q) {
+    const u32x4p x = all || none ? u32x4p{0, 0, 0, 0} : key(q);
+    const int j = w0 + 256 * q + 4 * lane;
+    uint32_t f = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool held_ = j + e < lo || j + e >= hi || all;
+      if (j + e < K.n && (held_ || (!none && x[e] > last))) f |= 1u << e;
+      if (j + e < K.n && !held_ && !none && x[e] == last && need > 0) f |= 16u << e;
+    }
+    return f;
   };
   int n_gt = 0, n_tie = 0;
-  for (int j0 = b0; j0 < b1; j0 += 64) {
-    bool tie;
-    n_gt += __popcll(__ballot(fate(j0 + lane, tie)));
-    n_tie += __popcll(__ballot(tie));
-  }
+  auto tally = [&](int q) {
+    const uint32_t f = fate(q);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      n_gt += __popcll(__ballot(f >> e & 1));
+      n_tie += __popcll(__ballot(f >> (4 + e) & 1));
+    }
+  };
+  for (int q = 0; q < nq; ++q) tally(q);
   if (lane == 0) { gts[wave] = n_gt; ties_in[wave] = n_tie; }
   __syncthreads();
-  int at = 0, tied = 0;                                            // survivors and equal keys in front of this share
+  int at = 0, tied = 0;                                            // survivors and equal keys in front of this wave's slots
   for (int w = 0; w < wave; ++w) { at += gts[w]; tied += ties_in[w]; }
   at += min(tied, need);
   const uint64_t below = (1ull << lane) - 1;
-  for (int j0 = b0; j0 < b1; j0 += 64) {
-    bool tie;
-    bool take = fate(j0 + lane, tie);
-    const uint64_t tb = __ballot(tie);
-    if (tie && tied + __popcll(tb & below) < need) take = true;
-    tied += __popcll(tb);
-    const uint64_t kb = __ballot(take);
-    const int to = at + __popcll(kb & below);
-    if (take && to < A.max_keep) kept[to] = j0 + lane;
-    at += __popcll(kb);
-  }
+  auto write = [&](int q) {
+    const uint32_t f = fate(q);
+    int mine = 0, ties = 0;                                        // equal ones in lanes below, and in all
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint64_t tb = __ballot(f >> (4 + e) & 1);
+      mine += __popcll(tb & below);
+      ties += __popcll(tb);
+    }
+    uint32_t take = f & 15;
+    int rank = tied + mine;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (f >> (4 + e) & 1) {
+        if (rank < need) take |= 1u << e;
+        ++rank;
+      }
+    tied += ties;
+    int to = at;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint64_t kb = __ballot(take >> e & 1);
+      to += __popcll(kb & below);
+      at += __popcll(kb);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (take >> e & 1) {
+        if (to < A.max_keep) kept[to] = w0 + 256 * q + 4 * lane + e;
+        ++to;
+      }
+  };
+  for (int q = 0; q < nq; ++q) write(q);
   for (int i = K.m + tid; i < A.max_keep; i += kEvictThreads) kept[i] = -1;
 }
 
@@ -338,10 +381,10 @@ __global__ __launch_bounds__(256) void k_evict_move(EvictArgs A) {
 
 hipError_t launch_paged_evict(int D, const EvictArgs& A, hipStream_t st) {
   const dim3 units(A.P.H, A.P.B);
-  if (A.P.max_kv <= kEvictLdsRows) {
-    const size_t bytes = 4 * (size_t)std::max(A.P.max_kv, 1);
-    // (more than 64 KB of LDS has to be asked for, once per kernel and device)
-    const hipError_t e = hipFuncSetAttribute((const void*)k_evict_select<true>, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kEvictLdsRows);
+  const int blocks = (A.P.max_kv + 4 * kEvictThreads - 1) / (4 * kEvictThreads);
+  if (blocks <= kEvictLdsBlocks) {
+    const int bytes = 16 * kEvictThreads * blocks, most = 16 * kEvictThreads * kEvictLdsBlocks;
+    const hipError_t e = hipFuncSetAttribute((const void*)k_evict_select<true>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
     if (e != hipSuccess) return e;
     k_evict_select<true><<<units, kEvictThreads, bytes, st>>>(A);
   } else {

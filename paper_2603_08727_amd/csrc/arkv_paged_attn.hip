@@ -15,104 +15,30 @@
 // Pages are at least 16 slots, so the 16 rows from a multiple of 16 on (a granule) lie in one page, whose id is uniform.
 #include <algorithm>
 
-#include "arkv_dev.h"
-#include "arkv_paged_dev.h"
+#include "arkv_paged_mma.h"
 
 namespace arkv {
 
-typedef uint32_t u32x4g __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2g __attribute__((ext_vector_type(2)));
-typedef float f32x4g __attribute__((ext_vector_type(4)));
-typedef float f32x16g __attribute__((ext_vector_type(16)));
-typedef short s16x4g __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8g __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2g __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8g __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2g __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) s16x4g* lds_s16x4;
-
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr float kUnset = -1.0e30f;      // softmax reference of a row that has seen nothing
-constexpr float kSumLimit = 16384.0f;   // a lane's probabilities of a tile may sum to this before the reference moves
-
-__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-
-template <typename T> struct Mfma;
-template <> struct Mfma<__bf16> {
-  static constexpr uint32_t kExp = 0x7F80u;      // exponent bits: all set = not finite
-  static __device__ __forceinline__ f32x4g m16(u32x4g a, u32x4g b, f32x4g c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8g, a), __builtin_bit_cast(bf16x8g, b), c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ f32x16g m32(u32x4g a, u32x4g b, f32x16g c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8g, a), __builtin_bit_cast(bf16x8g, b), c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ uint32_t pack(float a, float b) { bf16x2g h; h[0] = (__bf16)a; h[1] = (__bf16)b; return __builtin_bit_cast(uint32_t, h); }
-  static __device__ __forceinline__ float get(uint32_t w, int hi) { return __uint_as_float(hi ? w & 0xFFFF0000u : w << 16); }
-};
-template <> struct Mfma<_Float16> {
-  static constexpr uint32_t kExp = 0x7C00u;
-  static __device__ __forceinline__ f32x4g m16(u32x4g a, u32x4g b, f32x4g c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8g, a), __builtin_bit_cast(f16x8g, b), c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ f32x16g m32(u32x4g a, u32x4g b, f32x16g c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8g, a), __builtin_bit_cast(f16x8g, b), c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ uint32_t pack(float a, float b) { f16x2g h; h[0] = (_Float16)a; h[1] = (_Float16)b; return __builtin_bit_cast(uint32_t, h); }
-  static __device__ __forceinline__ float get(uint32_t w, int hi) { return (float)__builtin_bit_cast(f16x2g, w)[hi]; }
-};
-
-// halves of w that are not finite, as a mask of whole halves
-template <typename T> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
-  return ((w & Mfma<T>::kExp) == Mfma<T>::kExp ? 0xFFFFu : 0u) | ((w >> 16 & Mfma<T>::kExp) == Mfma<T>::kExp ? 0xFFFF0000u : 0u);
-}
-
-// logit, times log2(e), of a raw dot product (MODE 1: whatever the scores say)
-struct Logit {
-  float mul, inv_cap2, cap2;     // scale log2(e); 2 log2(e) scale / cap; cap log2(e)
-  __device__ __forceinline__ Logit(const Scores& S) {
-    mul = S.scale * kLog2e;
-    cap2 = S.cap * kLog2e;
-    inv_cap2 = S.cap > 0.f ? 2.f * kLog2e * (S.scale / S.cap) : 0.f;
-  }
-  // tanh x = 1 - 2 / (1 + e^2x): off by a few 2^-24 of 1, for logits up to the cap in absolute terms
-  __device__ __forceinline__ float plain(float dot) const {
-    if (cap2 > 0.f) return cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_hw(dot * inv_cap2)));
-    return dot * mul;
-  }
-};
-
-__device__ __forceinline__ Seq seq_of(const Paged& P, int b) {
-  return clamp_seq(P.cu_q[b], P.cu_q[b + 1], P.kv_len[b], P.N, P.max_q, P.max_kv);
-}
-// slots that new token i of a sequence sees are those below this (0: none)
-__device__ __forceinline__ int row_end(const Seq& s, int i, int prefix) { return max(0, min(s.kv, max(s.kv - s.nq + i + 1, prefix))); }
-
-constexpr int kStepRows = 16;           // rows of a sequence that k_paged_step takes
 constexpr int kStepWaves = 4;
-constexpr int kStepMaxPiece = 4096;     // a lane holds the page of one granule: 64 granules per wave
+constexpr int kStepMaxPiece = 1024;     // (at most 4096: a lane holds the page of one granule)
 constexpr int kChunkRows = 128, kChunkKeys = 64;
 
-// How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.  few: sequences of
-// up to so many rows are the step kernel's; -1 where only the other one is launched, which then takes all of them.
-struct Cut { int step_piece, n_step, chunk_piece, n_chunk, few; bool step, chunk; };
+// How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
+struct Cut { int step_piece, n_step, chunk_piece, n_chunk; Which w; };
 
 static Cut cut_of(const Paged& P, int Hq) {
   Cut c = {};
   const int G = Hq / P.H;
-  const long long units = (long long)P.B * P.H;
-  c.chunk = P.max_q * G > kStepRows;
-  c.step = !c.chunk || (long long)P.B * P.max_q != P.N;      // else all sequences have max_q new tokens: one launch will do
-  c.few = c.step ? kStepRows : -1;
-  auto pieces = [&](long long have, int least, int most, int unit, int& piece, int& n) {
-    const long long want = std::max(1ll, 512 / std::max(1ll, have));
-    long long p = (P.max_kv + want - 1) / want;
-    p = std::min<long long>(most, std::max<long long>(least, (p + unit - 1) / unit * unit));
-    piece = (int)p;
-    n = std::max(1, (int)((P.max_kv + p - 1) / p));
+  c.w = which_kernels(P, Hq);
+  auto pieces = [&](long long have, long long want, int least, int most, int unit, int& piece, int& n) {
+    const long long p = (P.max_kv * std::max(1ll, have) + want - 1) / want;
+    piece = (int)std::min<long long>(most, std::max<long long>(least, (p + unit - 1) / unit * unit));
+    n = std::max(1, (P.max_kv + piece - 1) / piece);
   };
-  pieces(units, 256, kStepMaxPiece, 128, c.step_piece, c.n_step);
+  // Sequences differ in length, so a few rounds of small pieces: the last one ends with the others.
+  pieces((long long)P.B * P.H, 2048, 256, kStepMaxPiece, 128, c.step_piece, c.n_step);
   const long long blocks = ((long long)P.N * G + kChunkRows - 1) / kChunkRows * P.H;
-  pieces(blocks, 512, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
+  pieces(blocks, 512, 512, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
   return c;
 }
 
@@ -121,8 +47,8 @@ static Cut cut_of(const Paged& P, int Hq) {
 struct Parts { float* acc; float2* ml; size_t chunk0; };
 
 static size_t part_rows(const Paged& P, int Hq, const Cut& c, size_t& chunk0) {
-  chunk0 = c.step && c.n_step > 1 ? (size_t)P.B * P.H * c.n_step * kStepRows : 0;
-  return chunk0 + (c.chunk && c.n_chunk > 1 ? (size_t)c.n_chunk * P.N * Hq : 0);
+  chunk0 = c.w.step && c.n_step > 1 ? (size_t)P.B * P.H * c.n_step * kStepRows : 0;
+  return chunk0 + (c.w.chunk && c.n_chunk > 1 ? (size_t)c.n_chunk * P.N * Hq : 0);
 }
 
 size_t paged_attention_floats(const Paged& P, int D, int Hq) {
@@ -141,18 +67,22 @@ template <typename T> __device__ __forceinline__ void store4(T* p, float a, floa
 // 16x16x32 MFMAs (lane: row lane % 16, keys 4 (lane / 16) .. + 3 of each granule).  Keys come from memory in operand
 // layout; values in whole rows, through LDS of the wave's own.  A tile's loads are in flight while the tile before it
 // is worked on.
+template <int D> struct StepLds {
+  uint16_t v[kStepWaves][32][D + 16];     // (the pitch: transposing reads of 16 rows meet each bank twice, as they must)
+  float acc[kStepWaves][kStepRows][D + 4];
+  float2 ml[kStepWaves][kStepRows];
+};
+
 template <typename T, int D, int MODE>
-__global__ __launch_bounds__(64 * kStepWaves, 2) void k_paged_step(PagedAttnArgs A, int piece_keys, int n_pieces, Parts parts) {
+__device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, StepLds<D>& sm, int id) {
+  constexpr bool CAP = Mode<MODE>::cap, DIST = Mode<MODE>::dist;
   constexpr int KK = D / 32, CB = D / 16, VI = 32 * D * 2 / 1024;   // k-steps, channel blocks, 1 KB loads of a value tile
   constexpr int RPI = 1024 / (2 * D), CPR = D / 8;                 // rows per load, 16-byte chunks per row
-  constexpr int VP = D + 16;                                       // halves per value row: transposing reads of 16 rows meet each bank twice
-  __shared__ __align__(16) uint16_t sv[kStepWaves][32][VP];
-  __shared__ float s_acc[kStepWaves][kStepRows][D + 4];
-  __shared__ float2 s_ml[kStepWaves][kStepRows];
+  const int piece_keys = cut.step_piece, n_pieces = cut.n_step;
   const Paged& P = A.P;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, gq = lane >> 4;
-  const int h = blockIdx.x % P.H, b = blockIdx.x / P.H, piece = blockIdx.y;
+  const int unit = id % (P.B * P.H), piece = id / (P.B * P.H), h = unit % P.H, b = unit / P.H;
   const Seq s = seq_of(P, b);
   const int R = s.nq * A.G;
   if (R == 0 || R > kStepRows) return;
@@ -165,8 +95,8 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void k_paged_step(PagedAttnArgs
   const int all_end = row_end(s, 0, prefix);                       // every row sees the slots below
   const int hq = h * A.G + row % A.G, tok = s.q0 + row / A.G;
   const Logit lg(A.S);
-  const float slope = MODE && A.S.slopes ? A.S.slopes[hq] * kLog2e : 0.f;
-  const int qp = MODE && A.S.slopes ? A.S.q_pos[tok] : 0;
+  const float slope = DIST ? A.S.slopes[hq] * kLog2e : 0.f;
+  const int qp = DIST ? A.S.q_pos[tok] : 0;
 
   u32x4g q[KK];
   {
@@ -229,13 +159,13 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void k_paged_step(PagedAttnArgs
     }
     const bool masked = j0 + 32 > all_end || (ok_mask >> (2 * t) & 3) != 3;
     float mul = lg.mul;
-    if (MODE) {
+    if (CAP || DIST) {
       mul = 1.f;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[g][i] = lg.plain(x[g][i]);
-        if (A.S.slopes) {
+        for (int i = 0; i < 4; ++i) x[g][i] = lg.logit<CAP>(x[g][i]);
+        if (DIST) {
           const int4 kp = *reinterpret_cast<const int4*>(P.pos + granule_row(2 * t + g) + 4 * gq);
           x[g][0] -= slope * fabsf((float)(qp - kp.x));
           x[g][1] -= slope * fabsf((float)(qp - kp.y));
@@ -270,7 +200,7 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void k_paged_step(PagedAttnArgs
     }
 #pragma unroll
     for (int i = 0; i < VI; ++i)
-      *reinterpret_cast<u32x4g*>(&sv[wave][RPI * i + lane / CPR][8 * (lane % CPR)]) = vb[i];
+      *reinterpret_cast<u32x4g*>(&sm.v[wave][RPI * i + lane / CPR][8 * (lane % CPR)]) = vb[i];
     if (t + 1 < nt) load_v(t + 1);
     float p[8];
     auto probs = [&]() {
@@ -300,8 +230,8 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void k_paged_step(PagedAttnArgs
     const u32x4g pb = {Mfma<T>::pack(p[0], p[1]), Mfma<T>::pack(p[2], p[3]), Mfma<T>::pack(p[4], p[5]), Mfma<T>::pack(p[6], p[7])};
 #pragma unroll
     for (int c = 0; c < CB; ++c) {
-      const s16x4g a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sv[wave][4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
-      const s16x4g a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sv[wave][16 + 4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
+      const s16x4g a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.v[wave][4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
+      const s16x4g a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.v[wave][16 + 4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
       const u32x2g w0_ = __builtin_bit_cast(u32x2g, a0), w1_ = __builtin_bit_cast(u32x2g, a1);
       acc[c] = Mfma<T>::m16(u32x4g{w0_[0], w0_[1], w1_[0], w1_[1]}, pb, acc[c]);
     }
@@ -340,24 +270,24 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void k_paged_step(PagedAttnArgs
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
 #pragma unroll
-  for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4g*>(&s_acc[wave][n][16 * c + 4 * gq]) = acc[c];
-  if (gq == 0) s_ml[wave][n] = make_float2(m, l);
+  for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4g*>(&sm.acc[wave][n][16 * c + 4 * gq]) = acc[c];
+  if (gq == 0) sm.ml[wave][n] = make_float2(m, l);
   __syncthreads();
   // the waves' parts: thread = four channels of a row
   for (int it = threadIdx.x; it < R * (D / 4); it += 64 * kStepWaves) {
     const int r = it / (D / 4), c = 4 * (it % (D / 4));
     float mm = kUnset, ll = 0.f;
 #pragma unroll
-    for (int w = 0; w < kStepWaves; ++w) mm = fmaxf(mm, s_ml[w][r].x);
+    for (int w = 0; w < kStepWaves; ++w) mm = fmaxf(mm, sm.ml[w][r].x);
     f32x4g o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kStepWaves; ++w) {
-      const float f = exp2_hw(s_ml[w][r].x - mm);
-      ll += f * s_ml[w][r].y;
-      o += f * *reinterpret_cast<const f32x4g*>(&s_acc[w][r][c]);
+      const float f = exp2_hw(sm.ml[w][r].x - mm);
+      ll += f * sm.ml[w][r].y;
+      o += f * *reinterpret_cast<const f32x4g*>(&sm.acc[w][r][c]);
     }
     if (np > 1) {
-      const size_t pr = ((size_t)blockIdx.x * n_pieces + piece) * kStepRows + r;
+      const size_t pr = ((size_t)unit * n_pieces + piece) * kStepRows + r;
       *reinterpret_cast<f32x4g*>(parts.acc + pr * D + c) = o;
       if (c == 0) parts.ml[pr] = make_float2(mm, ll);
     } else {
@@ -397,14 +327,6 @@ __device__ __forceinline__ bool find_block(const Paged& P, int G, int few, int r
   return false;
 }
 
-// 1 KB from memory to LDS, 16 bytes per lane, in lane order from `lds` on, without a register in between.  The caller waits
-// (vm_wait) and synchronises before anyone reads.  Inline assembly, because the compiler would wait for every such load in
-// front of any LDS read; it has no output register.
-__device__ __forceinline__ void load_lds(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(base), "v"(off), "s"(lds) : "memory");
-}
-__device__ __forceinline__ void vm_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-
 // One workgroup = 128 rows of a (sequence, kv-head) and a piece of the keys they see; a wave takes 32 rows with 32x32x16
 // MFMAs (lane: row lane % 32, keys 8 (i / 4) + 4 (lane / 32) + i % 4 of each half of a 64-key tile).  Keys and values of
 // a tile go to LDS as they lie in the pages, sixteen rows per wave, while the tile before is worked on: two buffers, one
@@ -415,19 +337,19 @@ template <int D> struct ChunkLds {
   uint16_t v[2][kChunkKeys * D];
   uint32_t odd[2];
 };
-template <int D> __device__ __forceinline__ int k_chunk(int row, int c) { return D == 128 ? c ^ (row & 15) : c ^ (row >> 1 & 7); }
 template <int D> __device__ __forceinline__ int v_chunk(int row, int c) { return D == 128 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; }
 
 template <typename T, int D, int MODE>
-__global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs A, int few, int piece_keys, Parts parts) {
+__device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, ChunkLds<D>& sm, int id, int n_blocks) {
+  constexpr bool CAP = Mode<MODE>::cap, DIST = Mode<MODE>::dist;
+  const int piece_keys = cut.chunk_piece;
   constexpr int KK = D / 16, CB = D / 32, CPR = D / 8, RPI = 64 / CPR, LPG = 16 / RPI;   // LPG: 1 KB loads of a granule
-  __shared__ __align__(16) ChunkLds<D> sm;
   const Paged& P = A.P;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, hh = lane >> 5;
-  const int h = blockIdx.x % P.H, piece = blockIdx.y;
+  const int h = id % P.H, piece = id / (n_blocks * P.H);
   int b, blk;
-  if (!find_block(P, A.G, few, blockIdx.x / P.H, lane, b, blk)) return;
+  if (!find_block(P, A.G, cut.w.few, id / P.H % n_blocks, lane, b, blk)) return;
   const Seq s = seq_of(P, b);
   const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
   const int R = s.nq * A.G, r0 = blk * kChunkRows;
@@ -440,8 +362,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs A, int few
   const int all_end = row_end(s, r0 / A.G, prefix);                // every row of the workgroup sees the slots below
   const int hq = h * A.G + rc % A.G, tok = s.q0 + rc / A.G;
   const Logit lg(A.S);
-  const float slope = MODE && A.S.slopes ? A.S.slopes[hq] * kLog2e : 0.f;
-  const int qp = MODE && A.S.slopes ? A.S.q_pos[tok] : 0;
+  const float slope = DIST ? A.S.slopes[hq] * kLog2e : 0.f;
+  const int qp = DIST ? A.S.q_pos[tok] : 0;
 
   u32x4g q[KK];
   {
@@ -547,13 +469,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs A, int few
         x[g] = Mfma<T>::m32(a, q[kk], x[g]);
       }
     float mul = lg.mul;
-    if (MODE) {
+    if (CAP || DIST) {
       mul = 1.f;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[g][i] = lg.plain(x[g][i]);
-        if (A.S.slopes) {
+        for (int i = 0; i < 16; ++i) x[g][i] = lg.logit<CAP>(x[g][i]);
+        if (DIST) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int4 kp = *reinterpret_cast<const int4*>(P.pos + granule_row(0, t, 2 * g + (e >> 1)) + 8 * (e & 1) + 4 * hh);
@@ -656,6 +578,21 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs A, int few
   }
 }
 
+// A launch: chunk_wgs workgroups for sequences of many rows (n_blocks blocks of each kv-head, piece by piece), behind them those for
+// few (unit by unit, piece by piece).  One launch for both: a prompt's chunk and the other requests' tokens share the chip.
+// KIND: bit 0: there are the former, bit 1: the latter.
+template <typename T, int D, int MODE, int KIND>
+__global__ __launch_bounds__(256, 2) void k_paged_attn(PagedAttnArgs A, Cut cut, Parts parts, int chunk_wgs, int n_blocks) {
+  constexpr size_t kMost = sizeof(ChunkLds<D>) > sizeof(StepLds<D>) ? sizeof(ChunkLds<D>) : sizeof(StepLds<D>);
+  __shared__ __align__(16) char lds[KIND == 1 ? sizeof(ChunkLds<D>) : KIND == 2 ? sizeof(StepLds<D>) : kMost];
+  const int id = (int)blockIdx.x;
+  if ((KIND & 1) && (KIND == 1 || id < chunk_wgs)) {
+    if constexpr (KIND & 1) paged_chunk<T, D, MODE>(A, cut, parts, *reinterpret_cast<ChunkLds<D>*>(lds), id, n_blocks);
+  } else {
+    if constexpr (KIND & 2) paged_step<T, D, MODE>(A, cut, parts, *reinterpret_cast<StepLds<D>*>(lds), id - chunk_wgs);
+  }
+}
+
 // ---- joining the pieces -------------------------------------------------------------------------------
 
 __device__ __forceinline__ int find_seq(const int32_t* cu_q, int B, int t, int lane) {
@@ -664,44 +601,71 @@ __device__ __forceinline__ int find_seq(const int32_t* cu_q, int B, int t, int l
   return b;
 }
 
-// One wave per row whose keys were split; rows that one workgroup finished are left alone.
-template <typename T, int D>
+// Joins the pieces of rows whose keys were split; rows that one workgroup finished are left alone.  32 lanes hold a row's
+// channels.  MANY pieces: the eight groups of 32 share a row's pieces; else each has a row of its own.
+template <typename T, int D, bool MANY>
 __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs A, Cut cut, Parts parts) {
+  constexpr int C = D / 32;
+  typedef float chan __attribute__((ext_vector_type(C)));
+  __shared__ float s_acc[MANY ? 8 : 1][D];
+  __shared__ float s_l[8];
   const Paged& P = A.P;
-  const int lane = threadIdx.x & 63;
-  const int id = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= P.N * A.Hq) return;
+  const int lane = threadIdx.x & 63, c = threadIdx.x & 31, grp = threadIdx.x >> 5;
+  const int rows = P.N * A.Hq, want = MANY ? (int)blockIdx.x : (int)blockIdx.x * 8 + grp, id = min(want, rows - 1);
   const int t = id / A.Hq, hq = id % A.Hq;
-  const int b = find_seq(P.cu_q, P.B, t, lane);
-  if (b >= P.B) return;
-  const Seq s = seq_of(P, b);
+  int b;
+  if constexpr (MANY) b = find_seq(P.cu_q, P.B, t, lane);
+  else {                                                           // (two rows in a wave)
+    const int t0 = __builtin_amdgcn_readlane(t, 0), t1 = __builtin_amdgcn_readlane(t, 32);
+    const int b0 = find_seq(P.cu_q, P.B, t0, lane), b1 = t1 == t0 ? b0 : find_seq(P.cu_q, P.B, t1, lane);
+    b = lane < 32 ? b0 : b1;
+  }
+  const Seq s = seq_of(P, min(b, P.B - 1));
   const int i = t - s.q0;
-  if (i < 0 || i >= s.nq) return;
-  const int prefix = A.S.prefix ? A.S.prefix[b] : 0, R = s.nq * A.G, r = i * A.G + hq % A.G;
-  const bool step = R <= cut.few;
+  const int prefix = A.S.prefix ? A.S.prefix[min(b, P.B - 1)] : 0, R = s.nq * A.G, r = i * A.G + hq % A.G;
+  const bool step = R <= cut.w.few;
   const int last = step ? s.nq - 1 : min(R - 1, r / kChunkRows * kChunkRows + kChunkRows - 1) / A.G;
   const int piece = step ? cut.step_piece : cut.chunk_piece;
-  const int np = (row_end(s, last, prefix) + piece - 1) / piece;
-  if (np <= 1) return;
+  int np = (row_end(s, last, prefix) + piece - 1) / piece;
+  if (want >= rows || b >= P.B || i < 0 || i >= s.nq || np <= 1) np = 0;
+  if (MANY && np == 0) return;
   const size_t first = step ? (size_t)(b * P.H + hq / A.G) * cut.n_step * kStepRows + r : parts.chunk0 + (size_t)t * A.Hq + hq;
   const size_t stride = step ? kStepRows : (size_t)P.N * A.Hq;
   float m = kUnset, l = 0.f;
-  for (int p = lane; p < np; p += 64) m = fmaxf(m, parts.ml[first + p * stride].x);
+  for (int p = c; p < np; p += 32) m = fmaxf(m, parts.ml[first + p * stride].x);
 #pragma unroll
-  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  float acc[D / 64] = {};
-  for (int p = 0; p < np; ++p) {
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  chan acc;
+#pragma unroll
+  for (int e = 0; e < C; ++e) acc[e] = 0.f;
+#pragma unroll 4
+  for (int p = MANY ? grp : 0; p < np; p += MANY ? 8 : 1) {
     const float2 ml = parts.ml[first + p * stride];
+    const chan x = *reinterpret_cast<const chan*>(parts.acc + (first + p * stride) * D + C * c);
     const float f = exp2_hw(ml.x - m);
     l += f * ml.y;
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) acc[e] += f * parts.acc[(first + p * stride) * D + D / 64 * lane + e];
+    acc += f * x;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  T* out = (T*)A.out + (size_t)id * D + D / 64 * lane;
+  if constexpr (MANY) {
+    *reinterpret_cast<chan*>(&s_acc[grp][C * c]) = acc;
+    if (c == 0) s_l[grp] = l;
+    __syncthreads();
+    if (grp) return;
+    l = 0.f;
 #pragma unroll
-  for (int e = 0; e < D / 64; ++e) out[e] = (T)(acc[e] * inv);
-  if (lane == 0 && A.lse) A.lse[id] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+    for (int e = 0; e < C; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+      l += s_l[g];
+      acc += *reinterpret_cast<const chan*>(&s_acc[g][C * c]);
+    }
+  }
+  if (np == 0) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;                      // (NaN stays)
+  T* out = (T*)A.out + (size_t)id * D + C * c;
+#pragma unroll
+  for (int e = 0; e < C; e += 2) *reinterpret_cast<uint32_t*>(out + e) = Mfma<T>::pack(acc[e] * inv, acc[e + 1] * inv);
+  if (c == 0 && A.lse) A.lse[id] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
 }
 
 template <typename T, int D, int MODE>
@@ -709,293 +673,27 @@ static hipError_t launch_attention(const PagedAttnArgs& A, hipStream_t st) {
   const Paged& P = A.P;
   const Cut c = cut_of(P, A.Hq);
   Parts parts = {};
-  const size_t rows = part_rows(P, A.Hq, c, parts.chunk0);
+  const size_t n = part_rows(P, A.Hq, c, parts.chunk0);
   parts.acc = A.ws;
-  parts.ml = (float2*)(A.ws + rows * D);
-  if (c.chunk) {
-    const int blocks = (int)(((long long)P.N * A.G) / kChunkRows + P.B);     // sum over sequences of blocks, at most
-    k_paged_chunk<T, D, MODE><<<dim3(blocks * P.H, c.n_chunk), 256, 0, st>>>(A, c.few, c.chunk_piece, parts);
+  parts.ml = (float2*)(A.ws + n * D);
+  const int blocks = (int)((long long)P.N * A.G / kChunkRows + P.B);       // blocks of all sequences, at most
+  const int chunk = c.w.chunk ? blocks * P.H * c.n_chunk : 0, step = c.w.step ? P.B * P.H * c.n_step : 0;
+  if (chunk && step) k_paged_attn<T, D, MODE, 3><<<chunk + step, 256, 0, st>>>(A, c, parts, chunk, blocks);
+  else if (chunk) k_paged_attn<T, D, MODE, 1><<<chunk, 256, 0, st>>>(A, c, parts, chunk, blocks);
+  else k_paged_attn<T, D, MODE, 2><<<step, 256, 0, st>>>(A, c, parts, 0, blocks);
+  if (n) {
+    const int rows = P.N * A.Hq;
+    // with few pieces a row is little work, and eight fit a workgroup
+    if ((c.w.chunk ? c.n_chunk : c.n_step) >= 8) k_paged_merge<T, D, true><<<rows, 256, 0, st>>>(A, c, parts);
+    else k_paged_merge<T, D, false><<<(rows + 7) / 8, 256, 0, st>>>(A, c, parts);
   }
-  if (c.step) k_paged_step<T, D, MODE><<<dim3(P.B * P.H, c.n_step), 64 * kStepWaves, 0, st>>>(A, c.step_piece, c.n_step, parts);
-  if (rows) k_paged_merge<T, D><<<(P.N * A.Hq + 3) / 4, 256, 0, st>>>(A, c, parts);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_attention(int dtype, int D, const PagedAttnArgs& A, hipStream_t st) {
-  const bool plain = !(A.S.cap > 0.f) && !A.S.slopes;
-#define GO(T, D) return plain ? launch_attention<T, D, 0>(A, st) : launch_attention<T, D, 1>(A, st)
-  if (dtype == ARKV_DTYPE_BF16) { if (D == 64) GO(__bf16, 64); else GO(__bf16, 128); }
-  else { if (D == 64) GO(_Float16, 64); else GO(_Float16, 128); }
-#undef GO
-}
-
-// ---- weights ------------------------------------------------------------------------------------------
-
-// Here query rows are on the M side (S = Q K^T), which leaves one key per lane: a lane adds up its rows' probabilities, and
-// the lanes that share a key add theirs in a fixed order at the end.  As above, few rows and many have a kernel each.
-constexpr int kWeighStepKeys = 128;     // keys per wave of k_weigh_step
-constexpr int kWeighKeys = 256, kWeighRows = 64;   // keys per workgroup and rows per tile of k_weigh_chunk
-
-__device__ __forceinline__ void store_weight(const PagedAttnArgs& A, int row, float sum) {
-  A.P.weight[row] = (A.decay == 0.f ? 0.f : A.decay * A.carried[row]) + sum;
-}
-
-// Few rows: bound by reading the keys.  A wave takes 128 keys, 32 at a time (two granules), the next 32 in flight.
-template <typename T, int D, int MODE>
-__global__ __launch_bounds__(256) void k_weigh_step(PagedAttnArgs A) {
-  constexpr int KK = D / 32, NT = kWeighStepKeys / 32;
-  const Paged& P = A.P;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 15, gq = lane >> 4;
-  const int h = blockIdx.y, b = blockIdx.z;
-  const int w0 = (blockIdx.x * 4 + wave) * kWeighStepKeys;
-  const Seq s = seq_of(P, b);
-  const int R = s.nq * A.G;
-  if (w0 >= s.kv || R > kStepRows) return;
-  const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
-  // lane i holds the page of granule i; one that is not there becomes page 0, whose rows get nothing
-  int my_page = w0 + 16 * lane < s.kv && lane < 2 * NT ? P.table[(size_t)b * P.width + ((w0 + 16 * lane) >> P.lg_page)] : -1;
-  const bool page_ok = (unsigned)my_page < (unsigned)P.n_pages;
-  if (!page_ok) my_page = 0;
-  const uint64_t ok_mask = __ballot(page_ok);
-  const int in_page = (1 << P.lg_page) - 1;
-  auto granule_row = [&](int g) {
-    const int page = __builtin_amdgcn_readlane(my_page, g);
-    return ((page * P.H + h) << P.lg_page) + ((w0 + 16 * g) & in_page);
-  };
-  u32x4g q[KK];
-  float lse[4], slope[4];
-  int qp[4], end[4];
-  {
-    const int row = n < R ? n : 0;                                 // (rows from R on see nothing)
-    const T* p = (const T*)A.q.p + (size_t)(s.q0 + row / A.G) * A.q.ts + (size_t)(h * A.G + row % A.G) * A.q.hs + 8 * gq;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) q[kk] = R ? *reinterpret_cast<const u32x4g*>(p + 32 * kk) : u32x4g{0, 0, 0, 0};
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = 4 * gq + i, rc = row < R ? row : 0;
-    const int tok = s.q0 + rc / A.G, hq = h * A.G + rc % A.G;
-    end[i] = row < R ? row_end(s, rc / A.G, prefix) : 0;
-    lse[i] = R ? A.lse[(size_t)tok * A.Hq + hq] * kLog2e : 0.f;
-    slope[i] = MODE && R && A.S.slopes ? A.S.slopes[hq] * kLog2e : 0.f;
-    qp[i] = MODE && R && A.S.slopes ? A.S.q_pos[tok] : 0;
-  }
-  const Logit lg(A.S);
-  u32x4g kb[2][2][KK];
-  auto load_k = [&](int t, u32x4g (&to)[2][KK]) {
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const T* p = (const T*)P.k + (size_t)(unsigned)granule_row(2 * t + g) * D + n * D + 8 * gq;
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) to[g][kk] = *reinterpret_cast<const u32x4g*>(p + 32 * kk);
-    }
-  };
-  load_k(0, kb[0]);
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    if (w0 + 32 * t >= s.kv) break;
-    if (t + 1 < NT) load_k(t + 1, kb[(t + 1) & 1]);
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      f32x4g x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) x = Mfma<T>::m16(q[kk], kb[t & 1][g][kk], x);
-      const int j = w0 + 32 * t + 16 * g + n, row = granule_row(2 * t + g) + n;
-      const bool there = j < s.kv && (ok_mask >> (2 * t + g) & 1);
-      const int kp = MODE && A.S.slopes ? P.pos[row] : 0;
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float y = MODE ? lg.plain(x[i]) : x[i] * lg.mul;
-        if (MODE && A.S.slopes) y -= slope[i] * fabsf((float)(qp[i] - kp));
-        sum += j < end[i] ? exp2_hw(y - lse[i]) : 0.f;
-      }
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
-      if (there && gq == 0) store_weight(A, row, sum);
-    }
-  }
-}
-
-// Many rows: bound by the matrix cores and the exponentials.  One workgroup = 256 keys of a (sequence, kv-head), 64 per wave,
-// held in registers as B operands, and a share of the rows that see them; rows come through LDS, 64 at a time, the next 64
-// on their way.
-template <int D> struct WeighLds {
-  uint16_t q[2][kWeighRows * D];
-  float lse[2][kWeighRows], slope[2][kWeighRows];
-  int qp[2][kWeighRows];
-};
-
-// 4 bytes per lane from memory to LDS, in lane order; as load_lds
-__device__ __forceinline__ void load_lds4(const void* p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(p), "s"(lds) : "memory");
-}
-__device__ __forceinline__ void load_lds16(const void* p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
-}
-
-template <typename T, int D, int MODE>
-__global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few, int n_shares) {
-  constexpr int KK = D / 16, CPR = D / 8, RPI = 64 / CPR, LPW = kWeighRows / RPI / 4;    // LPW: 1 KB loads of a tile per wave
-  __shared__ __align__(16) WeighLds<D> sm;
-  const Paged& P = A.P;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = lane & 31, hh = lane >> 5;
-  const int share = blockIdx.x % n_shares, blk = blockIdx.x / n_shares, h = blockIdx.y, b = blockIdx.z;
-  const Seq s = seq_of(P, b);
-  const int R = s.nq * A.G, j00 = blk * kWeighKeys;
-  if (R <= few || j00 >= s.kv) return;
-  const int prefix = A.S.prefix ? A.S.prefix[b] : 0, ctx = s.kv - s.nq;
-  const int w0 = j00 + 64 * wave;                                  // this wave's keys
-  const int32_t* table = P.table + (size_t)b * P.width;
-  // rows that see key j start here
-  auto first_row = [&](int j) { return j < prefix ? 0 : max(0, j - ctx) * A.G; };
-  const int start = first_row(j00) / kWeighRows, tiles = (R + kWeighRows - 1) / kWeighRows;
-  const int per = (max(0, tiles - start) + n_shares - 1) / n_shares;
-  const int t0 = min(start + share * per, tiles), t1 = min(t0 + per, tiles);
-  const int wave_lo = first_row(min(w0 + 63, s.kv - 1));           // rows from here on see all keys of the wave (prefixes grow with no key)
-  u32x4g k[2][KK];
-  int krow[2], lo[2], kp[2];
-#pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    const int j = w0 + 32 * g + n;
-    krow[g] = slot_row(table, P.n_pages, P.H, h, P.lg_page, s.kv, j);
-    lo[g] = krow[g] < 0 ? 0x7FFFFFFF : first_row(j);
-    const T* p = (const T*)P.k + (size_t)max(krow[g], 0) * D + 8 * hh;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) k[g][kk] = *reinterpret_cast<const u32x4g*>(p + 16 * kk);
-    kp[g] = MODE && A.S.slopes ? P.pos[max(krow[g], 0)] : 0;
-  }
-  const bool all_there = !__any(krow[0] < 0 || krow[1] < 0);
-  const uint32_t lds_q = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.q;
-  const uint32_t lds_lse = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.lse;
-  const uint32_t lds_slope = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.slope;
-  const uint32_t lds_qp = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.qp;
-  auto fetch = [&](int t, int buf) {
-#pragma unroll
-    for (int i = 0; i < LPW; ++i) {
-      const int lr = 16 * wave + RPI * i + lane / CPR, r = min(kWeighRows * t + lr, R - 1);   // (rows from R on: masked)
-      const T* p = (const T*)A.q.p + (size_t)(s.q0 + r / A.G) * A.q.ts + (size_t)(h * A.G + r % A.G) * A.q.hs + 8 * k_chunk<D>(lr, lane % CPR);
-      load_lds16(p, lds_q + 2 * (buf * kWeighRows * D + (16 * wave + RPI * i) * D));
-    }
-    const int r = min(kWeighRows * t + lane, R - 1), tok = s.q0 + r / A.G, hq = h * A.G + r % A.G;
-    if (wave == 0) load_lds4(A.lse + (size_t)tok * A.Hq + hq, lds_lse + 4 * buf * kWeighRows);
-    if (MODE && A.S.slopes) {
-      if (wave == 1) load_lds4(A.S.slopes + hq, lds_slope + 4 * buf * kWeighRows);
-      if (wave == 2) load_lds4(A.S.q_pos + tok, lds_qp + 4 * buf * kWeighRows);
-    }
-  };
-  const Logit lg(A.S);
-  float sum[2] = {0.f, 0.f};
-  if (t0 < t1) fetch(t0, 0);
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
-    vm_wait();
-    __syncthreads();
-    if (t + 1 < t1) fetch(t + 1, buf ^ 1);
-    const bool full = all_there && kWeighRows * t >= wave_lo && kWeighRows * (t + 1) <= R;
-#pragma unroll
-    for (int rb = 0; rb < kWeighRows / 32; ++rb) {
-      f32x16g x[2];
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[g][i] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        const u32x4g a = *reinterpret_cast<const u32x4g*>(&sm.q[buf][(32 * rb + n) * D + 8 * k_chunk<D>(n, 2 * kk + hh)]);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) x[g] = Mfma<T>::m32(a, k[g][kk], x[g]);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int lr = 32 * rb + 8 * e + 4 * hh;
-        const f32x4g z = *reinterpret_cast<const f32x4g*>(&sm.lse[buf][lr]) * kLog2e;
-        f32x4g sl = {0.f, 0.f, 0.f, 0.f};
-        int4 qp = make_int4(0, 0, 0, 0);
-        if (MODE && A.S.slopes) {
-          sl = *reinterpret_cast<const f32x4g*>(&sm.slope[buf][lr]) * kLog2e;
-          qp = *reinterpret_cast<const int4*>(&sm.qp[buf][lr]);
-        }
-        const int qpv[4] = {qp.x, qp.y, qp.z, qp.w};
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float y;
-            if (MODE) {
-              y = lg.plain(x[g][4 * e + i]) - z[i];
-              if (A.S.slopes) y -= sl[i] * fabsf((float)(qpv[i] - kp[g]));
-            } else {
-              y = fmaf(x[g][4 * e + i], lg.mul, -z[i]);
-            }
-            const float p = exp2_hw(y);
-            const int r = kWeighRows * t + lr + i;
-            sum[g] += full || (r >= lo[g] && r < R) ? p : 0.f;
-          }
-      }
-    }
-  }
-#pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    sum[g] += __shfl_xor(sum[g], 32);
-    if (hh == 0 && krow[g] >= 0) {
-      if (n_shares == 1) store_weight(A, krow[g], sum[g]);
-      else A.ws[((size_t)share * P.B * P.H + (size_t)b * P.H + h) * P.max_kv + w0 + 32 * g + n] = sum[g];
-    }
-  }
-}
-
-// Adds the shares' sums, in order.
-__global__ __launch_bounds__(256) void k_weigh_join(PagedAttnArgs A, int few, int n_shares) {
-  const Paged& P = A.P;
-  const int h = blockIdx.y, b = blockIdx.z, j = blockIdx.x * 256 + threadIdx.x;
-  const Seq s = seq_of(P, b);
-  if (s.nq * A.G <= few) return;
-  const int row = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, s.kv, j);
-  if (row < 0) return;
-  float sum = 0.f;
-  for (int i = 0; i < n_shares; ++i) sum += A.ws[((size_t)i * P.B * P.H + (size_t)b * P.H + h) * P.max_kv + j];
-  store_weight(A, row, sum);
-}
-
-// Shares into which the rows that see a block of keys are dealt, where the blocks alone do not fill the chip; at least four
-// tiles each.
-static int weigh_shares(const Paged& P, int Hq) {
-  const long long rows = (long long)P.max_q * (Hq / P.H), blocks = (long long)P.B * P.H * ((P.max_kv + kWeighKeys - 1) / kWeighKeys);
-  if (rows <= kStepRows || blocks == 0) return 1;
-  return (int)std::max(1ll, std::min(512 / blocks, rows / (4 * kWeighRows)));
-}
-
-size_t paged_weights_floats(const Paged& P, int Hq) {
-  const int n = weigh_shares(P, Hq);
-  return n == 1 ? 0 : (size_t)n * P.B * P.H * P.max_kv;
-}
-
-template <typename T, int D, int MODE>
-static hipError_t launch_weights(const PagedAttnArgs& A, hipStream_t st) {
-  const Paged& P = A.P;
-  const Cut c = cut_of(P, A.Hq);
-  const int shares = weigh_shares(P, A.Hq);
-  if (c.chunk) {
-    const int blocks = (P.max_kv + kWeighKeys - 1) / kWeighKeys;
-    k_weigh_chunk<T, D, MODE><<<dim3(blocks * shares, P.H, P.B), 256, 0, st>>>(A, c.few, shares);
-    if (shares > 1) k_weigh_join<<<dim3((P.max_kv + 255) / 256, P.H, P.B), 256, 0, st>>>(A, c.few, shares);
-  }
-  if (c.step) {
-    const int per = 4 * kWeighStepKeys;
-    k_weigh_step<T, D, MODE><<<dim3((P.max_kv + per - 1) / per, P.H, P.B), 256, 0, st>>>(A);
-  }
-  return hipGetLastError();
-}
-
-hipError_t launch_paged_weights(int dtype, int D, const PagedAttnArgs& A, hipStream_t st) {
-  const bool plain = !(A.S.cap > 0.f) && !A.S.slopes;
-#define GO(T, D) return plain ? launch_weights<T, D, 0>(A, st) : launch_weights<T, D, 1>(A, st)
-  if (dtype == ARKV_DTYPE_BF16) { if (D == 64) GO(__bf16, 64); else GO(__bf16, 128); }
-  else { if (D == 64) GO(_Float16, 64); else GO(_Float16, 128); }
-#undef GO
+  return dispatch(dtype, D, mode_of(A.S), [&](auto t, auto d, auto m) {
+    return launch_attention<typename decltype(t)::type, decltype(d)::value, decltype(m)::value>(A, st);
+  });
 }
 
 }  // namespace arkv

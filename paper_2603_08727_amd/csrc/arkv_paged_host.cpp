@@ -15,13 +15,15 @@ static int check(const arkv_pages* p, const arkv_page_batch* b, Paged& P) {
   if (!p || !b || !p->k || !p->v || !p->pos || !b->cu_q || !b->kv_len || !b->table) return ARKV_EINVAL;
   if (p->n_pages < 1 || p->n_kv_heads < 1 || p->head_dim < 1 || p->page_size < 1) return ARKV_EINVAL;
   if (b->batch < 1 || b->n_tokens < 0 || b->max_q < 0 || b->max_kv < 0 || b->table_width < 1) return ARKV_EINVAL;
-  if ((p->page_size & (p->page_size - 1)) || !aligned16(p->k) || !aligned16(p->v) || !aligned16(p->pos)) return ARKV_EINVAL;
+  if ((p->page_size & (p->page_size - 1)) || !aligned16(p->k) || !aligned16(p->v) || !aligned16(p->pos) || !aligned16(p->weight)) return ARKV_EINVAL;
   if (p->dtype != ARKV_DTYPE_BF16 && p->dtype != ARKV_DTYPE_FP16) return ARKV_EUNSUPPORTED;
   if ((p->head_dim != 64 && p->head_dim != 128) || p->page_size < 16 || p->page_size > 1024) return ARKV_EUNSUPPORTED;
   if ((int64_t)p->n_pages * p->n_kv_heads >= (int64_t)(1u << 31) / p->page_size) return ARKV_EUNSUPPORTED;
   if (b->batch > 65535 || p->n_kv_heads > 65535 || b->n_tokens > (1 << 28)) return ARKV_EUNSUPPORTED;
   if ((int64_t)b->max_kv > (int64_t)b->table_width * p->page_size || b->max_q > b->n_tokens) return ARKV_EINVAL;
-  if (b->max_kv > (1 << 28)) return ARKV_EUNSUPPORTED;
+  // (launches have fewer than 2^31 workgroups)
+  const int64_t units = (int64_t)b->batch * p->n_kv_heads;
+  if (b->max_kv > (1 << 28) || units > (1 << 20) || units * b->max_kv > (1ll << 40)) return ARKV_EUNSUPPORTED;
   P.k = p->k; P.v = p->v; P.pos = p->pos; P.weight = p->weight;
   P.cu_q = b->cu_q; P.kv_len = b->kv_len; P.table = b->table;
   P.n_pages = p->n_pages; P.H = p->n_kv_heads; P.B = b->batch; P.N = b->n_tokens;
@@ -38,10 +40,10 @@ static int check_rows(const arkv_rows* r, Rows& out) {
   return ARKV_OK;
 }
 
-static int check_heads(int n_q_heads, int H, int& G) {
+static int check_heads(int n_q_heads, int H, int n_tokens, int& G) {
   if (n_q_heads < 1 || n_q_heads % H) return ARKV_EINVAL;
   G = n_q_heads / H;
-  return G > 16 ? ARKV_EUNSUPPORTED : ARKV_OK;
+  return G > 16 || (int64_t)n_q_heads * n_tokens >= (1ll << 31) ? ARKV_EUNSUPPORTED : ARKV_OK;
 }
 
 // One size for all calls, so that a workspace serves every one of them.
@@ -92,7 +94,7 @@ int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, 
   int G;
   if (!bytes) return ARKV_EINVAL;
   TRY(check(pages, batch, P));
-  TRY(check_heads(n_q_heads, P.H, G));
+  TRY(check_heads(n_q_heads, P.H, P.N, G));
   *bytes = workspace_bytes(P, pages->head_dim, n_q_heads);
   return ARKV_OK;
 }
@@ -100,7 +102,7 @@ int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, 
 static int attn_args(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores, int32_t n_q_heads,
                      const arkv_rows* q, void* workspace, size_t bytes, PagedAttnArgs& A) {
   TRY(check(pages, batch, A.P));
-  TRY(check_heads(n_q_heads, A.P.H, A.G));
+  TRY(check_heads(n_q_heads, A.P.H, A.P.N, A.G));
   TRY(check_scores(scores, A.S));
   TRY(check_rows(q, A.q));
   A.Hq = n_q_heads;

@@ -92,12 +92,26 @@ ALL = ["append", "workspace", "attention", "weights", "evict"]
     ("pages", "v", ADDR + 2, A.EINVAL), ("batch", "batch", 0, A.EINVAL), ("batch", "batch", 65536, A.EUNSUPPORTED),
     ("batch", "n_tokens", -1, A.EINVAL), ("batch", "max_q", -1, A.EINVAL), ("batch", "max_q", 11, A.EINVAL), ("batch", "max_kv", -1, A.EINVAL),
     ("batch", "max_kv", 65, A.EINVAL), ("batch", "table_width", 0, A.EINVAL), ("batch", "cu_q", None, A.EINVAL),
-    ("batch", "kv_len", None, A.EINVAL), ("batch", "table", None, A.EINVAL),
+    ("batch", "kv_len", None, A.EINVAL), ("batch", "table", None, A.EINVAL), ("pages", "pos", ADDR + 4, A.EINVAL),
+    ("pages", "weight", ADDR + 4, A.EINVAL), ("batch", "batch", 65535, A.OK),
 ])
 def test_pages_and_batch_are_checked(name, where, field, value, code):
     pages, batch, rows, rot, sc = _args()
+    if code == A.OK:                                   # the limit itself, in the one call that launches nothing
+        name = "workspace"
     setattr(pages if where == "pages" else batch, field, value)
     assert _call(name, pages, batch, rows, rot, sc) == code
+
+
+def test_sizes_whose_launches_would_be_too_large():
+    pages, batch, rows, rot, sc = _args()
+    batch.batch, pages.n_kv_heads = 32768, 33          # more than 2^20 sequences times heads
+    assert _call("workspace", pages, batch, rows, rot, sc, hq=33) == A.EUNSUPPORTED
+    pages.n_kv_heads, batch.max_kv, batch.table_width = 32, (1 << 20) + 1, (1 << 16) + 1
+    assert _call("workspace", pages, batch, rows, rot, sc, hq=32) == A.EUNSUPPORTED
+    pages, batch, rows, rot, sc = _args()
+    batch.n_tokens = 1 << 27
+    assert _call("workspace", pages, batch, rows, rot, sc, hq=16) == A.EUNSUPPORTED
 
 
 @pytest.mark.parametrize("field,value", [("p", None), ("p", ADDR + 2), ("token_stride", 511), ("token_stride", -512), ("head_stride", 4),
