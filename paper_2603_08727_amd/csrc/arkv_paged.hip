@@ -21,14 +21,14 @@ template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b
   return __builtin_bit_cast(uint32_t, h);
 }
 
-constexpr int kAppendWaves = 4, kAppendItems = 4;
+constexpr int kAppendWaves = 4, kAppendItems = 3;
 
-// One wave per new token.  The wave's lanes form the token's angles (position times frequency in turns, in 64 bits: at
+// One wave per new token (or a share of its heads).  The wave's lanes form the token's angles (position times frequency in turns, in 64 bits: at
 // position 2^17 a 32-bit product is off by up to 2^-8 turns; the fraction that is left fits 32), then walk its heads'
 // 16-byte chunks in pairs: item i of a row is the pair of chunks whose channels turn together.  A generated token is bound by
 // round trips to memory: its lengths, angles and rows are requested together, the page behind them, then it stores.
 template <typename T, int D>
-__global__ __launch_bounds__(64 * kAppendWaves) void k_paged_append(AppendArgs A) {
+__global__ __launch_bounds__(64 * kAppendWaves) void k_paged_append(AppendArgs A, int per_wave) {
   __shared__ float2 turn[kAppendWaves][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = blockIdx.x * kAppendWaves + wave;
@@ -36,7 +36,8 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_paged_append(AppendArgs A
   if (t >= P.N) return;
   constexpr int IPR = D / 16;                                      // items of a row
   const int Hr = A.Hq + P.H, rot = A.half / 8;                     // heads that turn; items that turn
-  const int n_items = (A.Hq + 2 * P.H) * IPR;
+  const int n_all = (A.Hq + 2 * P.H) * IPR;
+  const int it00 = (int)blockIdx.y * per_wave, n_items = min(it00 + per_wave, n_all);     // this wave's share of the token
   struct Item { int h, hs, c0, c1; bool turns; };
   auto item = [&](int it) {
     Item o;
@@ -50,57 +51,63 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_paged_append(AppendArgs A
     o.c1 = halves ? i + rot : 2 * i + 1;
     return o;
   };
-  // (values, not structs, are chosen between: a lane's own choice of a struct would be read from memory)
+  // The first 64 sequences, the token's positions and the lane's frequency ...
+  const int32_t* positions = A.positions + t;
+  const int at0 = min(lane, P.B - 1);
+  int sq0 = P.cu_q[at0], sq1 = P.cu_q[at0 + 1], skv = P.kv_len[at0];
+  const int axis = A.axis[lane];
+  const double freq = A.freq[min(lane, max(A.half, 1) - 1)];
+  int pos[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) pos[i] = positions[(size_t)min(i, A.n_axes - 1) * P.N];
+  // ... and its rows.  (Values, not structs, are chosen between: a lane's own choice of a struct would be read from memory.)
   const T *qp = (const T*)A.q.p + (size_t)t * A.q.ts, *kp = (const T*)A.k.p + (size_t)t * A.k.ts, *vp = (const T*)A.v.p + (size_t)t * A.v.ts;
   const int64_t qs = A.q.hs, ks = A.k.hs, vs = A.v.hs;
   u32x4p x[kAppendItems], y[kAppendItems];
   auto load = [&](int it0) {
 #pragma unroll
     for (int u = 0; u < kAppendItems; ++u) {
-      const int it = it0 + 64 * u + lane;
-      if (it >= n_items) continue;
-      const Item o = item(it);
+      const Item o = item(min(it0 + 64 * u + lane, n_items - 1));
       const T* from = (o.h < A.Hq ? qp : o.h < Hr ? kp : vp) + (o.h < A.Hq ? qs : o.h < Hr ? ks : vs) * o.hs;
       x[u] = *reinterpret_cast<const u32x4p*>(from + 8 * o.c0);
       y[u] = *reinterpret_cast<const u32x4p*>(from + 8 * o.c1);
     }
   };
-  load(0);
-  const int position = A.positions[t];
-  double angle_pos = 0, angle_freq = 0;
-  if (lane < A.half) {
-    angle_pos = (double)A.positions[(size_t)A.axis[lane] * P.N + t];
-    angle_freq = A.freq[lane];
-  }
-  // the token's sequence: the first that ends behind it; the lanes look at 64 at a time
+  load(it00);
+  asm volatile("" : "+v"(sq0), "+v"(sq1), "+v"(skv));              // (requested here, not where they turn out to be needed)
+  // the token's sequence: the first that ends behind it
   int b = -1;
   Seq s = {0, 0, 0};
-  for (int i = 0; i < P.B && b < 0; i += 64) {
-    const int at = min(i + lane, P.B - 1);
-    const int q0 = P.cu_q[at], q1 = P.cu_q[at + 1], kv = P.kv_len[at];
-    const uint64_t hit = __ballot(i + lane < P.B && q1 > t);
+  for (int i = 0; i < P.B; i += 64) {
+    if (i) {
+      const int at = min(i + lane, P.B - 1);
+      sq0 = P.cu_q[at]; sq1 = P.cu_q[at + 1]; skv = P.kv_len[at];
+    }
+    const uint64_t hit = __ballot(i + lane < P.B && sq1 > t);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       b = i + l;
-      s = clamp_seq(__builtin_amdgcn_readlane(q0, l), __builtin_amdgcn_readlane(q1, l), __builtin_amdgcn_readlane(kv, l), P.N, P.max_q, P.max_kv);
+      s = clamp_seq(__builtin_amdgcn_readlane(sq0, l), __builtin_amdgcn_readlane(sq1, l), __builtin_amdgcn_readlane(skv, l), P.N, P.max_q, P.max_kv);
+      break;
     }
   }
   if (b < 0 || t < s.q0 || t >= s.q0 + s.nq) return;               // a row of no sequence
   const int slot = s.kv - s.nq + t - s.q0;
   const int row0 = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, 0, P.lg_page, s.kv, slot);
   if (lane < A.half) {
-    const double turns = angle_pos * (angle_freq * 0.15915494309189533577);
+    const int p = axis == 0 ? pos[0] : axis == 1 ? pos[1] : axis == 2 ? pos[2] : pos[3];
+    const double turns = (double)p * (freq * 0.15915494309189533577);
     float sn, cs;
     sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
     turn[wave][lane] = make_float2(cs, sn);                        // (read by this wave alone)
   }
-  if (row0 >= 0)
+  if (row0 >= 0 && it00 == 0)
     for (int h = lane; h < P.H; h += 64) {
-      P.pos[(size_t)row0 + ((size_t)h << P.lg_page)] = position;
+      P.pos[(size_t)row0 + ((size_t)h << P.lg_page)] = pos[0];
       if (P.weight) P.weight[(size_t)row0 + ((size_t)h << P.lg_page)] = 0.f;
     }
-  for (int it0 = 0; it0 < n_items; it0 += 64 * kAppendItems) {
-    if (it0) load(it0);
+  for (int it0 = it00; it0 < n_items; it0 += 64 * kAppendItems) {
+    if (it0 != it00) load(it0);
 #pragma unroll
     for (int u = 0; u < kAppendItems; ++u) {
       const int it = it0 + 64 * u + lane;
@@ -133,13 +140,17 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_paged_append(AppendArgs A
 }
 
 hipError_t launch_paged_append(int dtype, int D, const AppendArgs& A, hipStream_t st) {
-  const dim3 grid((A.P.N + kAppendWaves - 1) / kAppendWaves), block(64 * kAppendWaves);
+  // A token is one wave's work where there are tokens for the whole chip; fewer are dealt out, one load of each lane's at a
+  // time (16 tokens of 32 + 2 x 8 heads: 6.9 us as one wave each, 5.3 as two).
+  const int n_all = (A.Hq + 2 * A.P.H) * (D / 16), once = 64 * kAppendItems;
+  const int per_wave = A.P.N >= 2048 ? n_all : once;
+  const dim3 grid((A.P.N + kAppendWaves - 1) / kAppendWaves, (n_all + per_wave - 1) / per_wave), block(64 * kAppendWaves);
   if (dtype == ARKV_DTYPE_BF16) {
-    if (D == 64) k_paged_append<__bf16, 64><<<grid, block, 0, st>>>(A);
-    else k_paged_append<__bf16, 128><<<grid, block, 0, st>>>(A);
+    if (D == 64) k_paged_append<__bf16, 64><<<grid, block, 0, st>>>(A, per_wave);
+    else k_paged_append<__bf16, 128><<<grid, block, 0, st>>>(A, per_wave);
   } else {
-    if (D == 64) k_paged_append<_Float16, 64><<<grid, block, 0, st>>>(A);
-    else k_paged_append<_Float16, 128><<<grid, block, 0, st>>>(A);
+    if (D == 64) k_paged_append<_Float16, 64><<<grid, block, 0, st>>>(A, per_wave);
+    else k_paged_append<_Float16, 128><<<grid, block, 0, st>>>(A, per_wave);
   }
   return hipGetLastError();
 }
@@ -166,15 +177,20 @@ __device__ __forceinline__ Kept kept_of(const EvictArgs& A, int b) {
   return k;
 }
 
-// Adds one to hist[bin] for every lane with `on`; the lanes that share the first one's bin (equal weights, such as those of
-// rows that nobody looked at) add once: 64 additions to one word would queue.
-__device__ __forceinline__ void count_bin(int* hist, bool on, int bin, int lane) {
-  const uint64_t live = __ballot(on);
+// Adds one to hist[bin] for each of a lane's four bins with `on` set.  The lanes that share the bin of the first one (equal
+// weights, such as those of rows that nobody looked at) add once for all: additions to one word queue.
+__device__ __forceinline__ void count_bins(int* hist, const bool (&on)[4], const int (&bin)[4], int lane) {
+  const uint64_t live = __ballot(on[0] || on[1] || on[2] || on[3]);
   if (!live) return;
-  const int first = __builtin_ctzll(live), shared = __builtin_amdgcn_readlane(bin, first);
-  const uint64_t same = __ballot(on && bin == shared);
-  if (lane == first) atomicAdd(&hist[shared], __popcll(same));
-  else if (on && bin != shared) atomicAdd(&hist[bin], 1);
+  const int first = __builtin_ctzll(live);
+  const int shared = __builtin_amdgcn_readlane(on[0] ? bin[0] : on[1] ? bin[1] : on[2] ? bin[2] : bin[3], first);
+  int n = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    n += __popcll(__ballot(on[e] && bin[e] == shared));
+    if (on[e] && bin[e] != shared) atomicAdd(&hist[bin[e]], 1);
+  }
+  if (lane == first) atomicAdd(&hist[shared], n);
 }
 
 constexpr int kEvictBins = 2048;        // eleven bits of a key
@@ -230,11 +246,14 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
       auto count = [&](int q) {
         const u32x4p x = key(q);
         const int j = w0 + 256 * q + 4 * lane;
+        bool on[4];
+        int bin[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const bool on = j + e >= lo && j + e < hi && (shift == 21 || x[e] >> (shift + bits) == prefix >> (shift + bits));
-          count_bin(hist, on, x[e] >> shift & ((1 << bits) - 1), lane);
+          on[e] = j + e >= lo && j + e < hi && (shift == 21 || x[e] >> (shift + bits) == prefix >> (shift + bits));
+          bin[e] = x[e] >> shift & ((1 << bits) - 1);
         }
+        count_bins(hist, on, bin, lane);
       };
       for (int q = 0; q < nq; ++q) count(q);
       __syncthreads();

@@ -83,7 +83,8 @@ int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, con
     if (n_q_heads > 65535) return ARKV_EUNSUPPORTED;
     A.Hq = n_q_heads;
   }
-  A.q_out = q_out; A.positions = positions; A.freq = rotary->freq;
+  A.q_out = q_out; A.positions = positions;
+  A.freq = rotary->rot_dim ? rotary->freq : (const double*)pages->k;   // (read in any case, a branch would cost a round trip)
   A.half = rotary->rot_dim / 2; A.adjacent = rotary->adjacent; A.n_axes = rotary->n_axes;
   if (!A.P.N) return ARKV_OK;
   LAUNCH(launch_paged_append(pages->dtype, pages->head_dim, A, (hipStream_t)hip_stream));
