@@ -218,15 +218,11 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
   const bool all = ranked >= hi - lo, none = ranked <= 0;
   const int nq = (K.n + 256 * NW - 1) / (256 * NW);                // blocks of 256 slots per wave
   const int w0 = wave * nq * 256;
+  auto first_row = [&](int q) { return slot_row(table, A.P.n_pages, A.P.H, h, A.P.lg_page, K.n, w0 + 256 * q + 4 * lane); };
+  auto keys_of = [](const float4& w) { return u32x4p{weight_key(w.x), weight_key(w.y), weight_key(w.z), weight_key(w.w)}; };
   auto fetch = [&](int q) {                                        // keys of the lane's four slots of block q
-    const int j = w0 + 256 * q + 4 * lane;
-    u32x4p k = {0, 0, 0, 0};
-    const int r = slot_row(table, A.P.n_pages, A.P.H, h, A.P.lg_page, K.n, j);
-    if (r >= 0) {
-      const float4 w = *reinterpret_cast<const float4*>(A.P.weight + r);
-      k = u32x4p{weight_key(w.x), weight_key(w.y), weight_key(w.z), weight_key(w.w)};
-    }
-    return k;
+    const int r = first_row(q);
+    return r < 0 ? u32x4p{0, 0, 0, 0} : keys_of(*reinterpret_cast<const float4*>(A.P.weight + r));
   };
   auto key = [&](int q) { return IN_LDS ? held[q * kEvictThreads + tid] : fetch(q); };
   // survivors: keys above `last`, and of those equal to it the first `need`
@@ -235,8 +231,17 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
   if (!all && !none) {
     for (int i = tid; i < kEvictBins; i += kEvictThreads) hist[i] = 0;
     if (IN_LDS) {                                                  // (a thread's own keys: nobody else reads them)
-#pragma unroll 4
-      for (int q = 0; q < nq; ++q) held[q * kEvictThreads + tid] = fetch(q);
+      // all blocks' pages, then all their weights: two round trips to memory
+      int r[kEvictLdsBlocks];
+      float4 w[kEvictLdsBlocks];
+#pragma unroll
+      for (int q = 0; q < kEvictLdsBlocks; ++q) r[q] = q < nq ? first_row(q) : -1;
+#pragma unroll
+      for (int q = 0; q < kEvictLdsBlocks; ++q)
+        if (r[q] >= 0) w[q] = *reinterpret_cast<const float4*>(A.P.weight + r[q]);
+#pragma unroll
+      for (int q = 0; q < kEvictLdsBlocks; ++q)
+        if (q < nq) held[q * kEvictThreads + tid] = r[q] < 0 ? u32x4p{0, 0, 0, 0} : keys_of(w[q]);
     }
     __syncthreads();
     need = ranked;
@@ -343,19 +348,26 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
         ++rank;
       }
     tied += ties;
-    int to = at;
+    int to = 0, n = 0;                                             // of this block's survivors: in lanes below, in all
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint64_t kb = __ballot(take >> e & 1);
       to += __popcll(kb & below);
-      at += __popcll(kb);
+      n += __popcll(kb);
     }
+    // through LDS, in place of the block's keys, which are done with: adjacent lanes then store adjacent words
+    int* list = reinterpret_cast<int*>(&held[q * kEvictThreads + 64 * wave]);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (take >> e & 1) {
-        if (to < A.max_keep) kept[to] = w0 + 256 * q + 4 * lane + e;
+        if (IN_LDS) list[to] = w0 + 256 * q + 4 * lane + e;
+        else if (at + to < A.max_keep) kept[at + to] = w0 + 256 * q + 4 * lane + e;
         ++to;
       }
+    if (IN_LDS)
+      for (int i = lane; i < n; i += 64)
+        if (at + i < A.max_keep) kept[at + i] = list[i];
+    at += n;
   };
   for (int q = 0; q < nq; ++q) write(q);
   for (int i = K.m + tid; i < A.max_keep; i += kEvictThreads) kept[i] = -1;
