@@ -20,7 +20,7 @@
 namespace arkv {
 
 constexpr int kStepWaves = 4;
-constexpr int kStepMaxPiece = 1024;     // (at most 4096: a lane holds the page of one granule)
+constexpr int kStepMaxPiece = 2048;     // (at most 4096: a lane holds the page of one granule)
 constexpr int kChunkRows = 128, kChunkKeys = 64;
 
 // How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
@@ -30,15 +30,18 @@ static Cut cut_of(const Paged& P, int Hq) {
   Cut c = {};
   const int G = Hq / P.H;
   c.w = which_kernels(P, Hq);
+  // have: workgroups without a cut; want: how many there should be; least, most: keys per piece
   auto pieces = [&](long long have, long long want, int least, int most, int unit, int& piece, int& n) {
     const long long p = (P.max_kv * std::max(1ll, have) + want - 1) / want;
     piece = (int)std::min<long long>(most, std::max<long long>(least, (p + unit - 1) / unit * unit));
     n = std::max(1, (P.max_kv + piece - 1) / piece);
   };
-  // Sequences differ in length, so a few rounds of small pieces: the last one ends with the others.
-  pieces((long long)P.B * P.H, 2048, 256, kStepMaxPiece, 128, c.step_piece, c.n_step);
+  // Sequences differ in length, so no large pieces: the last round of workgroups ends with the others (32 requests of 800 to
+  // 16384 rows x 8 heads: 173 us in pieces of 1024, 177 of 2048, 182 of 4096; four of 131071: 373, 362, 354).  Up to 1024
+  // keys one piece: joining costs more than it saves (513 keys, 2 heads: 6.0 us, against 4.4 + 3.2 in pieces of 128 or 256).
+  pieces((long long)P.B * P.H, 1024, P.max_kv <= 1024 ? 1024 : 256, kStepMaxPiece, 128, c.step_piece, c.n_step);
   const long long blocks = ((long long)P.N * G + kChunkRows - 1) / kChunkRows * P.H;
-  pieces(blocks, 512, 512, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
+  pieces(blocks, 512, 1024, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
   return c;
 }
 
@@ -335,6 +338,7 @@ __device__ __forceinline__ bool find_block(const Paged& P, int G, int few, int r
 template <int D> struct ChunkLds {
   uint16_t k[2][kChunkKeys * D];
   uint16_t v[2][kChunkKeys * D];
+  int pos[2][kChunkKeys];
   uint32_t odd[2];
 };
 template <int D> __device__ __forceinline__ int v_chunk(int row, int c) { return D == 128 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; }
@@ -385,6 +389,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
   }
   const uint32_t lds_k = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.k;
   const uint32_t lds_v = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.v;
+  const uint32_t lds_pos = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.pos;
   // Lane i holds the page of granule i of a group of sixteen tiles, this one and the next one; one that is not there becomes
   // page 0, whose rows nobody sees.
   int pages[2];
@@ -409,6 +414,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
     for (int i = 0; i < LPG; ++i) load_lds(kp, koff[i], lds_k + at + 1024 * i);
 #pragma unroll
     for (int i = 0; i < LPG; ++i) load_lds(vp, voff[i], lds_v + at + 1024 * i);
+    if (DIST && lane < 16) load_lds4(P.pos + row + lane, lds_pos + 4 * (buf * kChunkKeys + 16 * wave));
   };
 
   f32x16g acc[CB];
@@ -478,7 +484,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
         if (DIST) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int4 kp = *reinterpret_cast<const int4*>(P.pos + granule_row(0, t, 2 * g + (e >> 1)) + 8 * (e & 1) + 4 * hh);
+            const int4 kp = *reinterpret_cast<const int4*>(&sm.pos[buf][32 * g + 8 * e + 4 * hh]);
             x[g][4 * e] -= slope * fabsf((float)(qp - kp.x));
             x[g][4 * e + 1] -= slope * fabsf((float)(qp - kp.y));
             x[g][4 * e + 2] -= slope * fabsf((float)(qp - kp.z));

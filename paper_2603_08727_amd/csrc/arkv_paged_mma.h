@@ -97,6 +97,13 @@ inline Which which_kernels(const Paged& P, int Hq) {
 __device__ __forceinline__ void load_lds(const void* base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(base), "v"(off), "s"(lds) : "memory");
 }
+// the same from an address per lane, 4 and 16 bytes
+__device__ __forceinline__ void load_lds4(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(p), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void load_lds16(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
+}
 __device__ __forceinline__ void vm_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Where the 16-byte chunk c of a row lies in LDS, so that operand reads (one chunk of 32 rows) meet in a bank no more often

@@ -112,14 +112,6 @@ template <int D> struct WeighLds {
   int qp[2][kWeighRows];
 };
 
-// 4 bytes per lane from memory to LDS, in lane order; as load_lds
-__device__ __forceinline__ void load_lds4(const void* p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(p), "s"(lds) : "memory");
-}
-__device__ __forceinline__ void load_lds16(const void* p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
-}
-
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few, int n_shares) {
   constexpr bool CAP = Mode<MODE>::cap, DIST = Mode<MODE>::dist;
