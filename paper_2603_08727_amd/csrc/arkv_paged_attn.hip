@@ -170,10 +170,10 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
         for (int i = 0; i < 4; ++i) x[g][i] = lg.logit<CAP>(x[g][i]);
         if (DIST) {
           const int4 kp = *reinterpret_cast<const int4*>(P.pos + granule_row(2 * t + g) + 4 * gq);
-          x[g][0] -= slope * fabsf((float)(qp - kp.x));
-          x[g][1] -= slope * fabsf((float)(qp - kp.y));
-          x[g][2] -= slope * fabsf((float)(qp - kp.z));
-          x[g][3] -= slope * fabsf((float)(qp - kp.w));
+          x[g][0] = fmaf(-slope, fabsf((float)(qp - kp.x)), x[g][0]);
+          x[g][1] = fmaf(-slope, fabsf((float)(qp - kp.y)), x[g][1]);
+          x[g][2] = fmaf(-slope, fabsf((float)(qp - kp.z)), x[g][2]);
+          x[g][3] = fmaf(-slope, fabsf((float)(qp - kp.w)), x[g][3]);
         }
       }
     }
@@ -245,7 +245,7 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
       float pj = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (e == 4 * g + i) pj = Mfma<T>::get(pb[e / 2], e & 1);
+        if (e == 4 * g + i) pj = Mfma<T>::get(opaque(pb[e / 2]), e & 1);
       pj = __shfl(pj, n + 16 * from);
       const bool seen = j0 + j < my_end && (ok_mask >> (2 * t + g) & 1);
       const T* v = (const T*)P.v + (granule_row(2 * t + g) + (j & 15)) * D + 4 * gq;
@@ -422,11 +422,13 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
   for (int c = 0; c < CB; ++c)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
-  float m = kUnset, l = 0.f;
+  // The row's softmax reference; rows that see none of this piece need none.
+  float m = my_end > p0 ? kUnset : 0.f, l = 0.f;
   load_pages(0, 0);
   if (nt > 0) fetch(0, 0, 0);
-  for (int t = 0; t < nt; ++t) {
-    const int buf = t & 1, j0 = p0 + kChunkKeys * t;
+  auto tile = [&](int t, auto which_buf) {
+    constexpr int buf = decltype(which_buf)::value;
+    const int j0 = p0 + kChunkKeys * t;
     if ((t & 15) == 0) {
       if (t) { pages[0] = pages[1]; there[0] = there[1]; }
       load_pages((t >> 4) + 1, 1);
@@ -474,60 +476,66 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
         const u32x4g a = *reinterpret_cast<const u32x4g*>(&sm.k[buf][(32 * g + n) * D + 8 * k_chunk<D>(n, 2 * kk + hh)]);
         x[g] = Mfma<T>::m32(a, q[kk], x[g]);
       }
-    float mul = lg.mul;
-    if (CAP || DIST) {
-      mul = 1.f;
+    // logits above the reference (above 0 where that is unset)
+    const bool unset = m == kUnset;
+    const float ref = unset ? 0.f : m;
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
+    for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[g][i] = lg.logit<CAP>(x[g][i]);
+      for (int e = 0; e < 4; ++e) {
+        int kp[4] = {0, 0, 0, 0};
         if (DIST) {
+          const int4 k4 = *reinterpret_cast<const int4*>(&sm.pos[buf][32 * g + 8 * e + 4 * hh]);
+          kp[0] = k4.x; kp[1] = k4.y; kp[2] = k4.z; kp[3] = k4.w;
+        }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int4 kp = *reinterpret_cast<const int4*>(&sm.pos[buf][32 * g + 8 * e + 4 * hh]);
-            x[g][4 * e] -= slope * fabsf((float)(qp - kp.x));
-            x[g][4 * e + 1] -= slope * fabsf((float)(qp - kp.y));
-            x[g][4 * e + 2] -= slope * fabsf((float)(qp - kp.z));
-            x[g][4 * e + 3] -= slope * fabsf((float)(qp - kp.w));
-          }
+        for (int i = 0; i < 4; ++i) {
+          float y = lg.above<CAP>(x[g][4 * e + i], ref);
+          if (DIST) y = fmaf(-slope, fabsf((float)(qp - kp[i])), y);
+          x[g][4 * e + i] = y;
         }
       }
-    }
     if (masked) {
+      stay_here();
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = 32 * g + 8 * (i >> 2) + 4 * hh + (i & 3);
-          x[g][i] = j0 + j < my_end && (ok >> (j >> 4) & 1) ? x[g][i] * mul : -INFINITY;
+          if (!(j0 + j < my_end && (ok >> (j >> 4) & 1))) x[g][i] = -INFINITY;
         }
-      mul = 1.f;
     }
     u32x4g pb[4];                                                  // probabilities of keys 16 i .. 16 i + 15, eight per lane
     auto probs = [&]() {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 32; i += 2) {
-        const float a = exp2_hw(fmaf(x[i >> 4][i & 15], mul, -m)), e = exp2_hw(fmaf(x[i >> 4][(i & 15) + 1], mul, -m));
-        sum += a + e;
+        const float a = exp2_hw(x[i >> 4][i & 15]), e = exp2_hw(x[i >> 4][(i & 15) + 1]);
+        sum += a;
+        sum += e;
         pb[i >> 3][(i & 7) >> 1] = Mfma<T>::pack(a, e);
       }
       return sum;
     };
     float sum = probs();
-    if (__any(!(sum <= kSumLimit))) {                              // rare after the first tile
-      const bool move = !(fmaxf(sum, __shfl_xor(sum, 32)) <= kSumLimit);   // (a NaN beside a small sum: stays, and so does the NaN)
+    if (__any(unset || !(sum <= kSumLimit))) {                     // rare after the first tile
       float top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i >> 4][i & 15] * mul);
+      for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i >> 4][i & 15]);
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float mn = move ? fmaxf(m, top) : m, f = exp2_hw(m - mn);
+      // (both lanes of a row alike; a NaN beside a small sum: stays, and so does the NaN)
+      const bool move = unset ? top > -INFINITY : !(fmaxf(sum, __shfl_xor(sum, 32)) <= kSumLimit);
+      const float mn = !move ? m : unset ? top : fmaxf(m, top + m);
+      const float f = !move || unset ? 1.f : exp2_hw(m - mn);      // (an unset row has nothing yet)
+      const float shift = move ? ref - mn : 0.f;
       m = mn;
       l *= f;
 #pragma unroll
       for (int c = 0; c < CB; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[c][i] *= f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i >> 4][i & 15] += shift;
       sum = probs();
     }
     l += sum;
@@ -547,7 +555,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
       float pj = 0.f;
 #pragma unroll
       for (int e = 0; e < 32; ++e)
-        if (e == 16 * (j >> 5) + 4 * (j >> 3 & 3) + (j & 3)) pj = Mfma<T>::get(pb[e >> 3][(e & 7) >> 1], e & 1);
+        if (e == 16 * (j >> 5) + 4 * (j >> 3 & 3) + (j & 3)) pj = Mfma<T>::get(opaque(pb[e >> 3][(e & 7) >> 1]), e & 1);
       pj = __shfl(pj, n + 32 * (j >> 2 & 1));
       const bool seen = j0 + j < my_end;
       const T* v = (const T*)P.v + (granule_row(0, t, j >> 4) + (j & 15)) * D + 4 * hh;
@@ -559,8 +567,13 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
           if (seen && !(fabsf(w) < INFINITY)) acc[c][i] += pj * w;
         }
     }
+  };
+  for (int t = 0; t < nt; t += 2) {
+    tile(t, Int<0>());
+    if (t + 1 < nt) tile(t + 1, Int<1>());
   }
   l += __shfl_xor(l, 32);
+  if (l == 0.f) m = kUnset;
   if (r >= R) return;
   const size_t orow = (size_t)tok * A.Hq + hq;
   if (np > 1) {

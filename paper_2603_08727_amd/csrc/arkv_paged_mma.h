@@ -7,6 +7,8 @@
 
 namespace arkv {
 
+template <int N> using Int = std::integral_constant<int, N>;
+
 typedef uint32_t u32x4g __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2g __attribute__((ext_vector_type(2)));
 typedef float f32x4g __attribute__((ext_vector_type(4)));
@@ -70,7 +72,16 @@ struct Logit {
     if (CAP) return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + exp2_hw(dot * inv_cap2)), cap2);
     return dot * mul;
   }
+  // the same less ref
+  template <bool CAP> __device__ __forceinline__ float above(float dot, float ref) const {
+    if (CAP) return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + exp2_hw(dot * inv_cap2)), cap2 - ref);
+    return fmaf(dot, mul, -ref);
+  }
 };
+
+// Keeps a rare branch a branch: without it the compiler computes what is inside for every tile and selects.
+__device__ __forceinline__ void stay_here() { asm volatile(""); }
+__device__ __forceinline__ uint32_t opaque(uint32_t x) { asm volatile("" : "+v"(x)); return x; }
 
 __device__ __forceinline__ Seq seq_of(const Paged& P, int b) {
   return clamp_seq(P.cu_q[b], P.cu_q[b + 1], P.kv_len[b], P.N, P.max_q, P.max_kv);
@@ -112,7 +123,6 @@ template <int D> __device__ __forceinline__ int k_chunk(int row, int c) { return
 
 // f(type, head dimension, mode) as compile-time values
 template <typename T> struct TypeOf { typedef T type; };
-template <int N> using Int = std::integral_constant<int, N>;
 template <typename T, int D, typename F> hipError_t dispatch_mode(int mode, F f) {
   switch (mode) {
     case 0: return f(TypeOf<T>(), Int<D>(), Int<0>());

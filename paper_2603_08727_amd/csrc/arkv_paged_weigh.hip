@@ -83,7 +83,7 @@ __global__ __launch_bounds__(256) void k_weigh_step(PagedAttnArgs A, int wave_ke
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float y = lg.logit<CAP>(x[i]);
-        if (DIST) y -= slope[i] * fabsf((float)(qp[i] - kp));
+        if (DIST) y = fmaf(-slope[i], fabsf((float)(qp[i] - kp)), y);
         sum += j < end[i] ? exp2_hw(y - lse[i]) : 0.f;
       }
       sum += __shfl_xor(sum, 16);
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few
             float y;
             if (CAP || DIST) {
               y = lg.logit<CAP>(x[g][4 * e + i]) - z[i];
-              if (DIST) y -= sl[i] * fabsf((float)(qpv[i] - kp[g]));
+              if (DIST) y = fmaf(-sl[i], fabsf((float)(qpv[i] - kp[g])), y);
             } else {
               y = fmaf(x[g][4 * e + i], lg.mul, -z[i]);
             }
