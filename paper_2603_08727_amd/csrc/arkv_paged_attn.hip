@@ -26,7 +26,7 @@ constexpr int kChunkRows = 128, kChunkKeys = 64;
 // How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
 struct Cut { int step_piece, n_step, chunk_piece, n_chunk; Which w; };
 
-static Cut cut_of(const Paged& P, int Hq) {
+static Cut cut_of(const Paged& P, int D, int Hq) {
   Cut c = {};
   const int G = Hq / P.H;
   c.w = which_kernels(P, Hq);
@@ -40,8 +40,10 @@ static Cut cut_of(const Paged& P, int Hq) {
   // 16384 rows x 8 heads: 173 us in pieces of 1024, 177 of 2048, 182 of 4096; four of 131071: 373, 362, 354).  Up to 1024
   // keys one piece: joining costs more than it saves (513 keys, 2 heads: 6.0 us, against 4.4 + 3.2 in pieces of 128 or 256).
   pieces((long long)P.B * P.H, 1024, P.max_kv <= 1024 ? 1024 : 256, kStepMaxPiece, 128, c.step_piece, c.n_step);
+  // One workgroup for every place on the chip, at d = 64 three to a CU (1686 tokens on up to 3001 rows, 12 heads: 46 us in pieces of
+  // 1024 keys, 42 of 512; d = 128, 512 tokens on 4100 rows, 16 heads: 55 us in pieces of 1024, 58 of 512).
   const long long blocks = ((long long)P.N * G + kChunkRows - 1) / kChunkRows * P.H;
-  pieces(blocks, 512, 1024, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
+  pieces(blocks, D == 64 ? 768 : 512, D == 64 ? 512 : 1024, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
   return c;
 }
 
@@ -56,7 +58,7 @@ static size_t part_rows(const Paged& P, int Hq, const Cut& c, size_t& chunk0) {
 
 size_t paged_attention_floats(const Paged& P, int D, int Hq) {
   size_t chunk0;
-  return part_rows(P, Hq, cut_of(P, Hq), chunk0) * (D + 2);
+  return part_rows(P, Hq, cut_of(P, D, Hq), chunk0) * (D + 2);
 }
 
 // four adjacent channels of a finished row
@@ -427,7 +429,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
   load_pages(0, 0);
   if (nt > 0) fetch(0, 0, 0);
   auto tile = [&](int t, auto which_buf) {
-    constexpr int buf = decltype(which_buf)::value;
+    const int buf = which_buf;
     const int j0 = p0 + kChunkKeys * t;
     if ((t & 15) == 0) {
       if (t) { pages[0] = pages[1]; there[0] = there[1]; }
@@ -568,9 +570,13 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
         }
     }
   };
-  for (int t = 0; t < nt; t += 2) {
-    tile(t, Int<0>());
-    if (t + 1 < nt) tile(t + 1, Int<1>());
+  if constexpr (DIST || D == 64) {                                 // (two copies of the tile do not fit the registers of two and three waves per SIMD)
+    for (int t = 0; t < nt; ++t) tile(t, t & 1);
+  } else {
+    for (int t = 0; t < nt; t += 2) {
+      tile(t, Int<0>());
+      if (t + 1 < nt) tile(t + 1, Int<1>());
+    }
   }
   l += __shfl_xor(l, 32);
   if (l == 0.f) m = kUnset;
@@ -601,7 +607,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
 // few (unit by unit, piece by piece).  One launch for both: a prompt's chunk and the other requests' tokens share the chip.
 // KIND: bit 0: there are the former, bit 1: the latter.
 template <typename T, int D, int MODE, int KIND>
-__global__ __launch_bounds__(256, 2) void k_paged_attn(PagedAttnArgs A, Cut cut, Parts parts, int chunk_wgs, int n_blocks) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_paged_attn(PagedAttnArgs A, Cut cut, Parts parts, int chunk_wgs, int n_blocks) {
   constexpr size_t kMost = sizeof(ChunkLds<D>) > sizeof(StepLds<D>) ? sizeof(ChunkLds<D>) : sizeof(StepLds<D>);
   __shared__ __align__(16) char lds[KIND == 1 ? sizeof(ChunkLds<D>) : KIND == 2 ? sizeof(StepLds<D>) : kMost];
   const int id = (int)blockIdx.x;
@@ -690,7 +696,7 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs A, Cut cut, P
 template <typename T, int D, int MODE>
 static hipError_t launch_attention(const PagedAttnArgs& A, hipStream_t st) {
   const Paged& P = A.P;
-  const Cut c = cut_of(P, A.Hq);
+  const Cut c = cut_of(P, D, A.Hq);
   Parts parts = {};
   const size_t n = part_rows(P, A.Hq, c, parts.chunk0);
   parts.acc = A.ws;

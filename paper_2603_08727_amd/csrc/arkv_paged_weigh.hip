@@ -105,11 +105,13 @@ __global__ __launch_bounds__(256) void k_weigh_step(PagedAttnArgs A, int wave_ke
 
 // Many rows: bound by the matrix cores and the exponentials.  One workgroup = 256 keys of a (sequence, kv-head), 64 per wave,
 // held in registers as B operands, and a share of the rows that see them; rows come through LDS, 64 at a time, the next 64
-// on their way.
+// on their way.  The logits' MFMAs of the next 32 rows stand between the exponentials of these: with the two one behind
+// the other, 2 x 1024 tokens over 8191 rows took 188 us, so PIPED.
+constexpr int kWeighBufs = 3;           // rows in use, the next ones (their first half is ahead), the ones on their way
 template <int D> struct WeighLds {
-  uint16_t q[2][kWeighRows * D];
-  float lse[2][kWeighRows], slope[2][kWeighRows];
-  int qp[2][kWeighRows];
+  uint16_t q[kWeighBufs][kWeighRows * D];
+  float lse[kWeighBufs][kWeighRows], slope[kWeighBufs][kWeighRows];
+  int qp[kWeighBufs][kWeighRows];
 };
 
 template <typename T, int D, int MODE>
@@ -150,77 +152,142 @@ __global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few
   const uint32_t lds_lse = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.lse;
   const uint32_t lds_slope = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.slope;
   const uint32_t lds_qp = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.qp;
+  // Rows of this lane's loads: their addresses move on by a tile's rows, tokens `more` and heads `rest`, without a division;
+  // in a tile that ends behind the last row they are formed anew, and stop there.
+  const int more = kWeighRows / A.G, rest = kWeighRows % A.G;
+  struct Walk {
+    int tok, head;
+    __device__ __forceinline__ void at(int r, int G) { tok = r / G; head = r % G; }
+    __device__ __forceinline__ void on(int more, int rest, int G) {
+      tok += more;
+      head += rest;
+      if (head >= G) { head -= G; ++tok; }
+    }
+  };
+  Walk row[LPW], one;
+  const int lr0 = 16 * wave + lane / CPR;
+#pragma unroll
+  for (int i = 0; i < LPW; ++i) row[i].at(kWeighRows * t0 + lr0 + RPI * i, A.G);
+  one.at(kWeighRows * t0 + lane, A.G);
+  const T* q_base = (const T*)A.q.p + (size_t)s.q0 * A.q.ts + (size_t)(h * A.G) * A.q.hs;
+  const float* lse_base = A.lse + (size_t)s.q0 * A.Hq + h * A.G;
   auto fetch = [&](int t, int buf) {
+    if (kWeighRows * (t + 1) > R) {
+#pragma unroll
+      for (int i = 0; i < LPW; ++i) row[i].at(min(kWeighRows * t + lr0 + RPI * i, R - 1), A.G);
+      one.at(min(kWeighRows * t + lane, R - 1), A.G);
+    }
 #pragma unroll
     for (int i = 0; i < LPW; ++i) {
-      const int lr = 16 * wave + RPI * i + lane / CPR, r = min(kWeighRows * t + lr, R - 1);   // (rows from R on: masked)
-      const T* p = (const T*)A.q.p + (size_t)(s.q0 + r / A.G) * A.q.ts + (size_t)(h * A.G + r % A.G) * A.q.hs + 8 * k_chunk<D>(lr, lane % CPR);
+      const T* p = q_base + (size_t)row[i].tok * A.q.ts + (size_t)row[i].head * A.q.hs + 8 * k_chunk<D>(lr0 + RPI * i, lane % CPR);
       load_lds16(p, lds_q + 2 * (buf * kWeighRows * D + (16 * wave + RPI * i) * D));
+      row[i].on(more, rest, A.G);
     }
-    const int r = min(kWeighRows * t + lane, R - 1), tok = s.q0 + r / A.G, hq = h * A.G + r % A.G;
-    if (wave == 0) load_lds4(A.lse + (size_t)tok * A.Hq + hq, lds_lse + 4 * buf * kWeighRows);
+    if (wave == 0) load_lds4(lse_base + (size_t)one.tok * A.Hq + one.head, lds_lse + 4 * buf * kWeighRows);
     if (DIST) {
-      if (wave == 1) load_lds4(A.S.slopes + hq, lds_slope + 4 * buf * kWeighRows);
-      if (wave == 2) load_lds4(A.S.q_pos + tok, lds_qp + 4 * buf * kWeighRows);
+      if (wave == 1) load_lds4(A.S.slopes + h * A.G + one.head, lds_slope + 4 * buf * kWeighRows);
+      if (wave == 2) load_lds4(A.S.q_pos + s.q0 + one.tok, lds_qp + 4 * buf * kWeighRows);
     }
+    one.on(more, rest, A.G);
   };
   const Logit lg(A.S);
   float sum[2] = {0.f, 0.f};
-  if (t0 < t1) fetch(t0, 0);
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
-    vm_wait();
-    __syncthreads();
-    if (t + 1 < t1) fetch(t + 1, buf ^ 1);
-    auto tile = [&](auto seen) {                                   // seen: every row sees every key (two copies of it pay for themselves in the plain mode alone)
-      constexpr bool full = decltype(seen)::value;
+  auto q_operand = [&](int buf, int rb, int kk) {
+    return *reinterpret_cast<const u32x4g*>(&sm.q[buf][(32 * rb + n) * D + 8 * k_chunk<D>(n, 2 * kk + hh)]);
+  };
+  auto clear = [](f32x16g (&x)[2]) {
 #pragma unroll
-    for (int rb = 0; rb < kWeighRows / 32; ++rb) {
-      f32x16g x[2];
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[g][i] = 0.f;
+  };
+  // probabilities of 32 rows from their dot products x, where some row may not see some key
+  auto add = [&](const f32x16g (&x)[2], int t, int buf, int rb) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int lr = 32 * rb + 8 * e + 4 * hh;
+      const f32x4g z = *reinterpret_cast<const f32x4g*>(&sm.lse[buf][lr]) * kLog2e;
+      f32x4g sl = {0.f, 0.f, 0.f, 0.f};
+      int4 qp = make_int4(0, 0, 0, 0);
+      if (DIST) {
+        sl = *reinterpret_cast<const f32x4g*>(&sm.slope[buf][lr]) * kLog2e;
+        qp = *reinterpret_cast<const int4*>(&sm.qp[buf][lr]);
+      }
+      const int qpv[4] = {qp.x, qp.y, qp.z, qp.w};
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[g][i] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        const u32x4g a = *reinterpret_cast<const u32x4g*>(&sm.q[buf][(32 * rb + n) * D + 8 * k_chunk<D>(n, 2 * kk + hh)]);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) x[g] = Mfma<T>::m32(a, k[g][kk], x[g]);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int lr = 32 * rb + 8 * e + 4 * hh;
-        const f32x4g z = *reinterpret_cast<const f32x4g*>(&sm.lse[buf][lr]) * kLog2e;
-        f32x4g sl = {0.f, 0.f, 0.f, 0.f};
-        int4 qp = make_int4(0, 0, 0, 0);
-        if (DIST) {
-          sl = *reinterpret_cast<const f32x4g*>(&sm.slope[buf][lr]) * kLog2e;
-          qp = *reinterpret_cast<const int4*>(&sm.qp[buf][lr]);
+        for (int i = 0; i < 4; ++i) {
+          float y = lg.above<CAP>(x[g][4 * e + i], z[i]);
+          if (DIST) y = fmaf(-sl[i], fabsf((float)(qpv[i] - kp[g])), y);
+          const int r = kWeighRows * t + lr + i;
+          sum[g] += r >= lo[g] && r < R ? exp2_hw(y) : 0.f;
         }
-        const int qpv[4] = {qp.x, qp.y, qp.z, qp.w};
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float y;
-            if (CAP || DIST) {
-              y = lg.logit<CAP>(x[g][4 * e + i]) - z[i];
-              if (DIST) y = fmaf(-sl[i], fabsf((float)(qpv[i] - kp[g])), y);
-            } else {
-              y = fmaf(x[g][4 * e + i], lg.mul, -z[i]);
-            }
-            const float p = exp2_hw(y);
-            if (full) sum[g] += p;
-            else {
-              const int r = kWeighRows * t + lr + i;
-              sum[g] += r >= lo[g] && r < R ? p : 0.f;
-            }
-          }
-      }
     }
-    };
-    if (MODE == 0 && all_there && kWeighRows * t >= wave_lo && kWeighRows * (t + 1) <= R) tile(std::true_type());
-    else tile(std::false_type());
+  };
+  // dot products of 32 rows into xn, and the probabilities of the 32 rows before, which see every key, from x
+  auto unit = [&](f32x16g (&x)[2], f32x16g (&xn)[2], int buf, int rb, int buf_n, int rb_n) {
+    f32x4g z[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = *reinterpret_cast<const f32x4g*>(&sm.lse[buf][32 * rb + 8 * e + 4 * hh]) * kLog2e;
+    clear(xn);
+    u32x4g a[KK];
+    a[0] = q_operand(buf_n, rb_n, 0);
+    a[1] = q_operand(buf_n, rb_n, 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      if (kk + 2 < KK) a[kk + 2] = q_operand(buf_n, rb_n, kk + 2);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        xn[g] = Mfma<T>::m32(a[kk], k[g][kk], xn[g]);
+        constexpr int EPK = 16 / KK;                               // elements per MFMA
+#pragma unroll
+        for (int i = EPK * kk; i < EPK * kk + EPK; ++i) sum[g] += exp2_hw(fmaf(x[g][i], lg.mul, -z[i >> 2][i & 3]));
+      }
+      // the order is pinned by what the next MFMA and these sums need
+      asm volatile("" : "+v"(sum[0]), "+v"(sum[1]) : : "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  f32x16g xa[2], xb[2];
+  int cur = 0, nxt = 1, old = 2;                                   // buffers of tiles t, t + 1, t + 2
+  if (t0 < t1) {
+    fetch(t0, 0);
+    if (t0 + 1 < t1) fetch(t0 + 1, 1);
+    vm_wait();
+    __syncthreads();
+    clear(xa);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int g = 0; g < 2; ++g) xa[g] = Mfma<T>::m32(q_operand(0, 0, kk), k[g][kk], xa[g]);
+  }
+  for (int t = t0; t < t1; ++t) {
+    if (t != t0) {
+      vm_wait();                                                   // tile t + 1 is in LDS, and tile t - 1 is done with
+      __syncthreads();
+    }
+    if (t + 2 < t1) fetch(t + 2, old);
+    if (MODE == 0 && all_there && kWeighRows * t >= wave_lo && kWeighRows * (t + 1) <= R) {
+      unit(xa, xb, cur, 0, cur, 1);
+      unit(xb, xa, cur, 1, nxt, 0);                                // (behind the last tile: of what the buffer holds, unused)
+    } else {
+      clear(xb);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) xb[g] = Mfma<T>::m32(q_operand(cur, 1, kk), k[g][kk], xb[g]);
+      add(xa, t, cur, 0);
+      clear(xa);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) xa[g] = Mfma<T>::m32(q_operand(nxt, 0, kk), k[g][kk], xa[g]);
+      add(xb, t, cur, 1);
+    }
+    const int c = cur;
+    cur = nxt; nxt = old; old = c;
   }
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
