@@ -152,43 +152,50 @@ __global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few
   const uint32_t lds_lse = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.lse;
   const uint32_t lds_slope = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.slope;
   const uint32_t lds_qp = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)sm.qp;
-  // Rows of this lane's loads: their addresses move on by a tile's rows, tokens `more` and heads `rest`, without a division;
-  // in a tile that ends behind the last row they are formed anew, and stop there.
+  // Where this lane's loads of the next tile lie: addresses move on by a tile's rows, `more` tokens and `rest` heads, without a
+  // division; in a tile that ends behind the last row they are formed anew, and stop there.
   const int more = kWeighRows / A.G, rest = kWeighRows % A.G;
-  struct Walk {
-    int tok, head;
-    __device__ __forceinline__ void at(int r, int G) { tok = r / G; head = r % G; }
-    __device__ __forceinline__ void on(int more, int rest, int G) {
-      tok += more;
-      head += rest;
-      if (head >= G) { head -= G; ++tok; }
-    }
-  };
-  Walk row[LPW], one;
   const int lr0 = 16 * wave + lane / CPR;
-#pragma unroll
-  for (int i = 0; i < LPW; ++i) row[i].at(kWeighRows * t0 + lr0 + RPI * i, A.G);
-  one.at(kWeighRows * t0 + lane, A.G);
-  const T* q_base = (const T*)A.q.p + (size_t)s.q0 * A.q.ts + (size_t)(h * A.G) * A.q.hs;
-  const float* lse_base = A.lse + (size_t)s.q0 * A.Hq + h * A.G;
-  auto fetch = [&](int t, int buf) {
-    if (kWeighRows * (t + 1) > R) {
-#pragma unroll
-      for (int i = 0; i < LPW; ++i) row[i].at(min(kWeighRows * t + lr0 + RPI * i, R - 1), A.G);
-      one.at(min(kWeighRows * t + lane, R - 1), A.G);
-    }
+  const T* qa[LPW];
+  int head[LPW], one_head, one_tok;
+  auto locate = [&](int t) {
 #pragma unroll
     for (int i = 0; i < LPW; ++i) {
-      const T* p = q_base + (size_t)row[i].tok * A.q.ts + (size_t)row[i].head * A.q.hs + 8 * k_chunk<D>(lr0 + RPI * i, lane % CPR);
-      load_lds16(p, lds_q + 2 * (buf * kWeighRows * D + (16 * wave + RPI * i) * D));
-      row[i].on(more, rest, A.G);
+      const int r = min(kWeighRows * t + lr0 + RPI * i, R - 1);
+      head[i] = r % A.G;
+      qa[i] = (const T*)A.q.p + (size_t)(s.q0 + r / A.G) * A.q.ts + (size_t)(h * A.G + head[i]) * A.q.hs + 8 * k_chunk<D>(lr0 + RPI * i, lane % CPR);
     }
-    if (wave == 0) load_lds4(lse_base + (size_t)one.tok * A.Hq + one.head, lds_lse + 4 * buf * kWeighRows);
+    const int r = min(kWeighRows * t + lane, R - 1);
+    one_head = r % A.G;
+    one_tok = s.q0 + r / A.G;
+  };
+  const int64_t inc = (int64_t)more * A.q.ts + (int64_t)rest * A.q.hs, wrap = A.q.ts - (int64_t)A.G * A.q.hs;
+  auto fetch = [&](int t, int buf) {
+    if (t == t0 || kWeighRows * (t + 1) > R) locate(t);
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) load_lds16(qa[i], lds_q + 2 * (buf * kWeighRows * D + (16 * wave + RPI * i) * D));
+    if (wave == 0) load_lds4(A.lse + (size_t)one_tok * A.Hq + h * A.G + one_head, lds_lse + 4 * buf * kWeighRows);
     if (DIST) {
-      if (wave == 1) load_lds4(A.S.slopes + h * A.G + one.head, lds_slope + 4 * buf * kWeighRows);
-      if (wave == 2) load_lds4(A.S.q_pos + s.q0 + one.tok, lds_qp + 4 * buf * kWeighRows);
+      if (wave == 1) load_lds4(A.S.slopes + h * A.G + one_head, lds_slope + 4 * buf * kWeighRows);
+      if (wave == 2) load_lds4(A.S.q_pos + one_tok, lds_qp + 4 * buf * kWeighRows);
     }
-    one.on(more, rest, A.G);
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) qa[i] += inc;
+    one_tok += more;
+    if (rest) {                                                    // (uniform; a group size that does not divide a tile)
+#pragma unroll
+      for (int i = 0; i < LPW; ++i) {
+        head[i] += rest;
+        if (head[i] >= A.G) { head[i] -= A.G; qa[i] += wrap; }
+      }
+      one_head += rest;
+      if (one_head >= A.G) { one_head -= A.G; ++one_tok; }
+    }
+  };
+  // (lse and slopes of a tile that has arrived, times log2(e), by one wave for all)
+  auto to_log2 = [&](int buf) {
+    if (wave == 0) sm.lse[buf][lane] *= kLog2e;
+    if (DIST && wave == 1) sm.slope[buf][lane] *= kLog2e;
   };
   const Logit lg(A.S);
   float sum[2] = {0.f, 0.f};
@@ -206,11 +213,11 @@ __global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int lr = 32 * rb + 8 * e + 4 * hh;
-      const f32x4g z = *reinterpret_cast<const f32x4g*>(&sm.lse[buf][lr]) * kLog2e;
+      const f32x4g z = *reinterpret_cast<const f32x4g*>(&sm.lse[buf][lr]);
       f32x4g sl = {0.f, 0.f, 0.f, 0.f};
       int4 qp = make_int4(0, 0, 0, 0);
       if (DIST) {
-        sl = *reinterpret_cast<const f32x4g*>(&sm.slope[buf][lr]) * kLog2e;
+        sl = *reinterpret_cast<const f32x4g*>(&sm.slope[buf][lr]);
         qp = *reinterpret_cast<const int4*>(&sm.qp[buf][lr]);
       }
       const int qpv[4] = {qp.x, qp.y, qp.z, qp.w};
@@ -229,7 +236,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few
   auto unit = [&](f32x16g (&x)[2], f32x16g (&xn)[2], int buf, int rb, int buf_n, int rb_n) {
     f32x4g z[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = *reinterpret_cast<const f32x4g*>(&sm.lse[buf][32 * rb + 8 * e + 4 * hh]) * kLog2e;
+    for (int e = 0; e < 4; ++e) z[e] = *reinterpret_cast<const f32x4g*>(&sm.lse[buf][32 * rb + 8 * e + 4 * hh]);
     clear(xn);
     u32x4g a[KK];
     a[0] = q_operand(buf_n, rb_n, 0);
@@ -257,6 +264,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few
     if (t0 + 1 < t1) fetch(t0 + 1, 1);
     vm_wait();
     __syncthreads();
+    to_log2(0);
     clear(xa);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
@@ -264,11 +272,10 @@ __global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few
       for (int g = 0; g < 2; ++g) xa[g] = Mfma<T>::m32(q_operand(0, 0, kk), k[g][kk], xa[g]);
   }
   for (int t = t0; t < t1; ++t) {
-    if (t != t0) {
-      vm_wait();                                                   // tile t + 1 is in LDS, and tile t - 1 is done with
-      __syncthreads();
-    }
+    vm_wait();                                                     // tile t + 1 is in LDS, and tile t - 1 is done with
+    __syncthreads();
     if (t + 2 < t1) fetch(t + 2, old);
+    if (t + 1 < t1) to_log2(nxt);
     if (MODE == 0 && all_there && kWeighRows * t >= wave_lo && kWeighRows * (t + 1) <= R) {
       unit(xa, xb, cur, 0, cur, 1);
       unit(xb, xa, cur, 1, nxt, 0);                                // (behind the last tile: of what the buffer holds, unused)
