@@ -89,7 +89,9 @@ int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, con
                       const arkv_rows* q, const arkv_rows* k, const arkv_rows* v, const int32_t* positions, void* q_out,
                       void* hip_stream);
 
-/* Bytes of DEVICE workspace that the calls below need for this batch and any of their options.  HOST, pure. */
+/* Bytes of DEVICE workspace that the calls below need for this batch and any of their options (64 KiB or more).  HOST, pure.
+ * The first 64 KiB must be zero before the workspace's first use; every call leaves them zero, so one workspace serves calls on
+ * batches of any shape, one after the other.  Calls that may overlap in time need workspaces of their own. */
 int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, int32_t n_q_heads, size_t* bytes);
 
 /* out [n_tokens][H_q][d] (dense, DEVICE, of the pages' dtype) = softmax over the visible slots of x, times v.  lse DEVICE float
@@ -97,7 +99,7 @@ int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, 
  * -infinity.  What lies in slots that a token does not see has no influence on its row, whatever bits it holds.
  * The new tokens' own rows must be in the pages already (arkv_paged_append).  G <= 16.
  * Probabilities are rounded to the pages' dtype in front of the product with v; sums, maxima and the denominator are fp32.  workspace 16-byte
- * aligned; its contents need no preparation. */
+ * aligned, as arkv_paged_workspace says. */
 int arkv_paged_attention(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,
                          int32_t n_q_heads, const arkv_rows* q, void* out, float* lse, void* workspace, size_t bytes,
                          void* hip_stream);

@@ -24,7 +24,9 @@ constexpr int kStepMaxPiece = 2048;     // (at most 4096: a lane holds the page 
 constexpr int kChunkRows = 128, kChunkKeys = 64;
 
 // How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
-struct Cut { int step_piece, n_step, chunk_piece, n_chunk; Which w; };
+// joined: the step kernel's last workgroup of a (sequence, kv-head) joins its pieces, no launch is needed for that.
+struct Cut { int step_piece, n_step, chunk_piece, n_chunk; bool joined; Which w; };
+constexpr int kJoinPieces = 16;         // at most: a lane has all pieces' loads under way at once
 
 static Cut cut_of(const Paged& P, int D, int Hq) {
   Cut c = {};
@@ -44,12 +46,13 @@ static Cut cut_of(const Paged& P, int D, int Hq) {
   // 1024 keys, 42 of 512; d = 128, 512 tokens on 4100 rows, 16 heads: 55 us in pieces of 1024, 58 of 512).
   const long long blocks = ((long long)P.N * G + kChunkRows - 1) / kChunkRows * P.H;
   pieces(blocks, D == 64 ? 768 : 512, D == 64 ? 512 : 1024, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
+  c.joined = c.n_step <= kJoinPieces && (long long)P.B * P.H <= kJoinUnits;
   return c;
 }
 
 // Pieces' results: sums [row][D] and (reference, denominator) [row].  Rows of k_paged_step: ((unit * n_step + piece) * 16 +
 // row), behind them rows of k_paged_chunk: (piece * N + token) * Hq + head.
-struct Parts { float* acc; float2* ml; size_t chunk0; };
+struct Parts { float* acc; float2* ml; int* tickets; size_t chunk0; };
 
 static size_t part_rows(const Paged& P, int Hq, const Cut& c, size_t& chunk0) {
   chunk0 = c.w.step && c.n_step > 1 ? (size_t)P.B * P.H * c.n_step * kStepRows : 0;
@@ -58,7 +61,30 @@ static size_t part_rows(const Paged& P, int Hq, const Cut& c, size_t& chunk0) {
 
 size_t paged_attention_floats(const Paged& P, int D, int Hq) {
   size_t chunk0;
-  return part_rows(P, Hq, cut_of(P, D, Hq), chunk0) * (D + 2);
+  return kTicketFloats + part_rows(P, Hq, cut_of(P, D, Hq), chunk0) * (D + 2);
+}
+
+// Partial results and tickets go past the L2 of one XCD: device-scope relaxed atomics.  A workgroup waits until its stores are
+// acknowledged before it draws its ticket, and the last one reads nothing that an L2 may hold from before.
+__device__ __forceinline__ void put4(float* p, f32x4g x) {
+  union { float f[4]; unsigned long long u[2]; } w = {{x[0], x[1], x[2], x[3]}};
+  __hip_atomic_store((unsigned long long*)p, w.u[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store((unsigned long long*)p + 1, w.u[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void put2(float2* p, float a, float b) {
+  union { float f[2]; unsigned long long u; } w = {{a, b}};
+  __hip_atomic_store((unsigned long long*)p, w.u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x4g take4(const float* p) {
+  union { float f[4]; unsigned long long u[2]; } w;
+  w.u[0] = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  w.u[1] = __hip_atomic_load((const unsigned long long*)p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return f32x4g{w.f[0], w.f[1], w.f[2], w.f[3]};
+}
+__device__ __forceinline__ float2 take2(const float2* p) {
+  union { float f[2]; unsigned long long u; } w;
+  w.u = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(w.f[0], w.f[1]);
 }
 
 // four adjacent channels of a finished row
@@ -76,6 +102,7 @@ template <int D> struct StepLds {
   uint16_t v[kStepWaves][32][D + 16];     // (the pitch: transposing reads of 16 rows meet each bank twice, as they must)
   float acc[kStepWaves][kStepRows][D + 4];
   float2 ml[kStepWaves][kStepRows];
+  int last;                               // whether this workgroup's piece was the last one to be finished
 };
 
 template <typename T, int D, int MODE>
@@ -278,6 +305,12 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
   for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4g*>(&sm.acc[wave][n][16 * c + 4 * gq]) = acc[c];
   if (gq == 0) sm.ml[wave][n] = make_float2(m, l);
   __syncthreads();
+  auto finish = [&](int r, int c, f32x4g o, float mm, float ll) {  // four channels of a row's result
+    const size_t orow = (size_t)(s.q0 + r / A.G) * A.Hq + h * A.G + r % A.G;
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;                  // (NaN stays)
+    store4((T*)A.out + orow * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    if (c == 0 && A.lse) A.lse[orow] = ll == 0.f ? -INFINITY : kLn2 * (mm + log2f(ll));
+  };
   // the waves' parts: thread = four channels of a row
   for (int it = threadIdx.x; it < R * (D / 4); it += 64 * kStepWaves) {
     const int r = it / (D / 4), c = 4 * (it % (D / 4));
@@ -293,14 +326,48 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
     }
     if (np > 1) {
       const size_t pr = ((size_t)unit * n_pieces + piece) * kStepRows + r;
-      *reinterpret_cast<f32x4g*>(parts.acc + pr * D + c) = o;
-      if (c == 0) parts.ml[pr] = make_float2(mm, ll);
+      put4(parts.acc + pr * D + c, o);
+      if (c == 0) put2(parts.ml + pr, mm, ll);
     } else {
-      const size_t orow = (size_t)(s.q0 + r / A.G) * A.Hq + h * A.G + r % A.G;
-      const float inv = ll == 0.f ? 0.f : 1.f / ll;                // (NaN stays)
-      store4((T*)A.out + orow * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-      if (c == 0 && A.lse) A.lse[orow] = ll == 0.f ? -INFINITY : kLn2 * (mm + log2f(ll));
+      finish(r, c, o, mm, ll);
     }
+  }
+  if (np == 1 || !cut.joined) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                 // this wave's stores are where everyone sees them
+  __syncthreads();
+  int* ticket = parts.tickets + unit * kTicketWords;
+  if (threadIdx.x == 0) {
+    const int drawn = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    sm.last = drawn == np - 1;
+    if (sm.last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call wants it
+  }
+  __syncthreads();
+  if (!sm.last) return;
+  for (int it = threadIdx.x; it < R * (D / 4); it += 64 * kStepWaves) {
+    const int r = it / (D / 4), c = 4 * (it % (D / 4));
+    const size_t first = (size_t)unit * n_pieces * kStepRows + r;
+    float2 ml[kJoinPieces];
+    f32x4g x[kJoinPieces];
+#pragma unroll
+    for (int p = 0; p < kJoinPieces; ++p) {
+      if (p < np) {
+        ml[p] = take2(parts.ml + first + p * kStepRows);
+        x[p] = take4(parts.acc + (first + p * kStepRows) * D + c);
+      }
+    }
+    float mm = kUnset, ll = 0.f;
+#pragma unroll
+    for (int p = 0; p < kJoinPieces; ++p)
+      if (p < np) mm = fmaxf(mm, ml[p].x);
+    f32x4g o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < kJoinPieces; ++p)
+      if (p < np) {
+        const float f = exp2_hw(ml[p].x - mm);
+        ll += f * ml[p].y;
+        o += f * x[p];
+      }
+    finish(r, c, o, mm, ll);
   }
 }
 
@@ -652,7 +719,7 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs A, Cut cut, P
   const int last = step ? s.nq - 1 : min(R - 1, r / kChunkRows * kChunkRows + kChunkRows - 1) / A.G;
   const int piece = step ? cut.step_piece : cut.chunk_piece;
   int np = (row_end(s, last, prefix) + piece - 1) / piece;
-  if (want >= rows || b >= P.B || i < 0 || i >= s.nq || np <= 1) np = 0;
+  if (want >= rows || b >= P.B || i < 0 || i >= s.nq || np <= 1 || (step && cut.joined)) np = 0;
   if (MANY && np == 0) return;
   const size_t first = step ? (size_t)(b * P.H + hq / A.G) * cut.n_step * kStepRows + r : parts.chunk0 + (size_t)t * A.Hq + hq;
   const size_t stride = step ? kStepRows : (size_t)P.N * A.Hq;
@@ -699,14 +766,15 @@ static hipError_t launch_attention(const PagedAttnArgs& A, hipStream_t st) {
   const Cut c = cut_of(P, D, A.Hq);
   Parts parts = {};
   const size_t n = part_rows(P, A.Hq, c, parts.chunk0);
-  parts.acc = A.ws;
-  parts.ml = (float2*)(A.ws + n * D);
+  parts.tickets = (int*)A.ws;
+  parts.acc = A.ws + kTicketFloats;
+  parts.ml = (float2*)(parts.acc + n * D);
   const int blocks = (int)((long long)P.N * A.G / kChunkRows + P.B);       // blocks of all sequences, at most
   const int chunk = c.w.chunk ? blocks * P.H * c.n_chunk : 0, step = c.w.step ? P.B * P.H * c.n_step : 0;
   if (chunk && step) k_paged_attn<T, D, MODE, 3><<<chunk + step, 256, 0, st>>>(A, c, parts, chunk, blocks);
   else if (chunk) k_paged_attn<T, D, MODE, 1><<<chunk, 256, 0, st>>>(A, c, parts, chunk, blocks);
   else k_paged_attn<T, D, MODE, 2><<<step, 256, 0, st>>>(A, c, parts, 0, blocks);
-  if (n) {
+  if ((chunk && c.n_chunk > 1) || (step && c.n_step > 1 && !c.joined)) {
     const int rows = P.N * A.Hq;
     // with few pieces a row is little work, and eight fit a workgroup
     if ((c.w.chunk ? c.n_chunk : c.n_step) >= 8) k_paged_merge<T, D, true><<<rows, 256, 0, st>>>(A, c, parts);

@@ -61,16 +61,21 @@ __global__ __launch_bounds__(256) void k_weigh_step(PagedAttnArgs A, int wave_ke
     qp[i] = DIST && R ? A.S.q_pos[tok] : 0;
   }
   const Logit lg(A.S);
+  // (the carried weights come with the keys: requested at the store they cost a round trip to memory every 16 keys)
   u32x4g kb[2][2][KK];
-  auto load_k = [&](int t, u32x4g (&to)[2][KK]) {
+  float wb[2][2] = {};
+  const bool carry = A.decay != 0.f;
+  auto load_k = [&](int t, u32x4g (&to)[2][KK], float (&w)[2]) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      const T* p = (const T*)P.k + (size_t)(unsigned)granule_row(2 * t + g) * D + n * D + 8 * gq;
+      const int row = granule_row(2 * t + g) + n;
+      if (carry) w[g] = A.carried[row];
+      const T* p = (const T*)P.k + (size_t)(unsigned)row * D + 8 * gq;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) to[g][kk] = *reinterpret_cast<const u32x4g*>(p + 32 * kk);
     }
   };
-  auto tile = [&](int t, const u32x4g (&kc)[2][KK]) {
+  auto tile = [&](int t, const u32x4g (&kc)[2][KK], const float (&w)[2]) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       f32x4g x = {0.f, 0.f, 0.f, 0.f};
@@ -88,17 +93,17 @@ __global__ __launch_bounds__(256) void k_weigh_step(PagedAttnArgs A, int wave_ke
       }
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
-      if (there && gq == 0) store_weight(A, row, sum);
+      if (there && gq == 0) P.weight[row] = (carry ? A.decay * w[g] : 0.f) + sum;
     }
   };
   const int nt = (w1 - w0 + 31) / 32;
-  load_k(0, kb[0]);
+  load_k(0, kb[0], wb[0]);
   for (int t = 0; t < nt; t += 2) {
-    if (t + 1 < nt) load_k(t + 1, kb[1]);
-    tile(t, kb[0]);
+    if (t + 1 < nt) load_k(t + 1, kb[1], wb[1]);
+    tile(t, kb[0], wb[0]);
     if (t + 1 < nt) {
-      if (t + 2 < nt) load_k(t + 2, kb[0]);
-      tile(t + 1, kb[1]);
+      if (t + 2 < nt) load_k(t + 2, kb[0], wb[0]);
+      tile(t + 1, kb[1], wb[1]);
     }
   }
 }
@@ -301,7 +306,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few
     sum[g] += __shfl_xor(sum[g], 32);
     if (hh == 0 && krow[g] >= 0) {
       if (n_shares == 1) store_weight(A, krow[g], sum[g]);
-      else A.ws[((size_t)share * P.B * P.H + (size_t)b * P.H + h) * P.max_kv + w0 + 32 * g + n] = sum[g];
+      else A.ws[kTicketFloats + ((size_t)share * P.B * P.H + (size_t)b * P.H + h) * P.max_kv + w0 + 32 * g + n] = sum[g];
     }
   }
 }
@@ -315,7 +320,7 @@ __global__ __launch_bounds__(256) void k_weigh_join(PagedAttnArgs A, int few, in
   const int row = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, s.kv, j);
   if (row < 0) return;
   float sum = 0.f;
-  for (int i = 0; i < n_shares; ++i) sum += A.ws[((size_t)i * P.B * P.H + (size_t)b * P.H + h) * P.max_kv + j];
+  for (int i = 0; i < n_shares; ++i) sum += A.ws[kTicketFloats + ((size_t)i * P.B * P.H + (size_t)b * P.H + h) * P.max_kv + j];
   store_weight(A, row, sum);
 }
 
@@ -329,7 +334,7 @@ static int weigh_shares(const Paged& P, int Hq) {
 
 size_t paged_weights_floats(const Paged& P, int Hq) {
   const int n = weigh_shares(P, Hq);
-  return n == 1 ? 0 : (size_t)n * P.B * P.H * P.max_kv;
+  return n == 1 ? 0 : kTicketFloats + (size_t)n * P.B * P.H * P.max_kv;
 }
 
 template <typename T, int D, int MODE>

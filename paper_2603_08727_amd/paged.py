@@ -80,15 +80,12 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _dense(t, shape, dtype, what, device=None):
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous GPU tensor is needed")
-    if t.dtype != dtype:
-        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{what}: on {t.device}, the pages are on {device}")
+def _dense(t, shape, dtype, what, index=None):
+    """Address of a contiguous GPU tensor (on GPU `index`) of that shape and type."""
+    at = t.get_device()
+    if t.dtype is not dtype or t.shape != shape or at < 0 or (index is not None and at != index) or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on the pages' GPU, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
@@ -101,9 +98,9 @@ class arkv_pages:
         _need(k.dim() == 4, "k: [n_pages][H_kv][page_size][d]")
         _need(k.dtype in (torch.bfloat16, torch.float16), f"k: bf16 or fp16, got {k.dtype}")
         self.k, self.v, self.pos, self.weight = k, v, pos, weight
-        self.device, self.dtype, self.index = k.device, k.dtype, k.device.index
+        self.device, self.dtype, self.index = k.device, k.dtype, k.get_device()
         self.n_pages, self.H, self.page_size, self.d = k.shape
-        dev = k.device
+        dev = self.index
         self.c = _Pages(0 if k.dtype == torch.bfloat16 else 1, self.n_pages, self.page_size, self.H, self.d,
                         _dense(k, k.shape, k.dtype, "k"), _dense(v, k.shape, k.dtype, "v", dev),
                         _dense(pos, k.shape[:3], torch.int32, "pos", dev),
@@ -120,10 +117,10 @@ class arkv_page_batch:
         _need(table.dim() == 2 and table.shape[0] >= 1, "table: [B][pages]")
         B, width = table.shape
         self.cu_q, self.kv_len, self.table = cu_q, kv_len, table
-        self.device, self.B, self.n_tokens = table.device, B, n_tokens
+        self.device, self.index, self.B, self.n_tokens = table.device, table.get_device(), B, n_tokens
         _need(max_kv is not None or page_size is not None, "max_kv or page_size is needed")
         self.c = _Batch(B, n_tokens, n_tokens if max_q is None else max_q, width * page_size if max_kv is None else max_kv, width,
-                        _dense(cu_q, (B + 1,), torch.int32, "cu_q", table.device), _dense(kv_len, (B,), torch.int32, "kv_len", table.device),
+                        _dense(cu_q, (B + 1,), torch.int32, "cu_q", self.index), _dense(kv_len, (B,), torch.int32, "kv_len", self.index),
                         _dense(table, (B, width), torch.int32, "table"))
         self.ref = C.byref(self.c)
 
@@ -138,7 +135,7 @@ class arkv_rotary:
         _need(half <= 64, "at most 64 pairs")
         axis = [0] * half if axis is None else [int(a) for a in axis]
         _need(len(axis) == half and all(0 <= a < 256 for a in axis), "axis: one entry per pair")
-        self.freq, self.n_axes = freq, n_axes
+        self.freq, self.n_axes, self.index = freq, n_axes, None if freq is None else freq.get_device()
         self.c = _Rotary(2 * half, n_axes, 1 if adjacent else 0, (C.c_uint8 * 64)(*axis),
                          None if freq is None else _dense(freq, (half,), torch.float64, "freq"))
         self.ref = C.byref(self.c)
@@ -156,28 +153,28 @@ _own = _Own()
 
 
 def _rows(to, t, n, pages, what):
-    """[n][heads][d] with any token and head stride; the channels are adjacent."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != n or shape[2] != pages.d or not t.is_cuda:
-        raise ValueError(f"{what}: expected [{n}][heads][{pages.d}] on the GPU, got {tuple(shape)}")
-    if t.dtype != pages.dtype or t.device != pages.device:
-        raise ValueError(f"{what}: expected {pages.dtype} on {pages.device}")
-    if stride[2] != 1:
+    """[n][heads][d] with any token and head stride; the channels are adjacent.  Returns the number of heads."""
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != n or shape[2] != pages.d or t.dtype is not pages.dtype or t.get_device() != pages.index:
+        raise ValueError(f"{what}: expected {pages.dtype} [{n}][heads][{pages.d}] on {pages.device}, got {t.dtype} {tuple(shape)} on {t.device}")
+    token, head, channel = t.stride()
+    if channel != 1:
         raise ValueError(f"{what}: channels must be adjacent")
-    to.p, to.token_stride, to.head_stride = t.data_ptr(), stride[0], stride[1]
+    to.p = t.data_ptr()
+    to.token_stride = token
+    to.head_stride = head
+    return shape[1]
 
 
 def _current(pages, batch):
-    if batch.device != pages.device:
-        raise ValueError("pages and batch are on different devices")
-    if pages.index != _b._device():
-        raise ValueError(f"the pages are on {pages.device}, which is not the current device")
+    if batch.index != pages.index or pages.index != _b._device():
+        raise ValueError(f"pages on {pages.device}, batch on {batch.device}: both must be on the current device")
 
 
 def _workspace(ws, pages):
     if ws is None:
         return None, 0
-    if not ws.is_contiguous() or ws.device != pages.device:
+    if ws.get_device() != pages.index or not ws.is_contiguous():
         raise ValueError("workspace: a contiguous tensor on the pages' device")
     return ws.data_ptr(), ws.nbytes
 
@@ -191,11 +188,11 @@ def _call(name, *args):
 # ---- entry points, same names as the C ABI -----------------------------------------------------
 
 def arkv_paged_workspace(pages, batch, n_q_heads):
-    """A workspace tensor for the calls below (uint8; allocate once for the largest batch)."""
+    """A workspace tensor for the calls below (zeros, as its first use wants it; one for the largest batch serves all)."""
     torch = _TORCH or _torch()
     n = C.c_size_t()
     _call("arkv_paged_workspace", pages.ref, batch.ref, n_q_heads, C.byref(n))
-    return torch.empty(max(n.value, 16), dtype=torch.uint8, device=pages.device)
+    return torch.zeros(n.value, dtype=torch.uint8, device=pages.device)
 
 
 def arkv_paged_append(pages, batch, rotary, q, k, v, positions, q_out):
@@ -203,21 +200,16 @@ def arkv_paged_append(pages, batch, rotary, q, k, v, positions, q_out):
     torch = _TORCH or _torch()
     _current(pages, batch)
     n, H, o = batch.n_tokens, pages.H, _own
-    if k.dim() != 3 or v.dim() != 3 or k.shape[1] != H or v.shape[1] != H:
-        raise ValueError(f"k, v: expected [{n}][{H}][{pages.d}]")
-    if rotary.freq is not None and rotary.freq.device != pages.device:
+    if rotary.index != pages.index and rotary.index is not None:
         raise ValueError("freq: on another device than the pages")
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
-    _rows(o.k, k, n, pages, "k")
-    _rows(o.v, v, n, pages, "v")
-    hq = 0
-    if q is not None:
-        _rows(o.q, q, n, pages, "q")
-        hq = q.shape[1]
+    if _rows(o.k, k, n, pages, "k") != H or _rows(o.v, v, n, pages, "v") != H:
+        raise ValueError(f"k, v: expected {H} heads")
+    hq = 0 if q is None else _rows(o.q, q, n, pages, "q")
     _call("arkv_paged_append", pages.ref, batch.ref, rotary.ref, hq, None if q is None else o.rq, o.rk, o.rv,
-          _dense(positions, (rotary.n_axes, n), torch.int32, "positions", pages.device),
-          None if q is None else _dense(q_out, (n, hq, pages.d), pages.dtype, "q_out", pages.device), _b._stream())
+          _dense(positions, (rotary.n_axes, n), torch.int32, "positions", pages.index),
+          None if q is None else _dense(q_out, (n, hq, pages.d), pages.dtype, "q_out", pages.index), _b._stream())
 
 
 def _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix):
@@ -226,10 +218,10 @@ def _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix):
     if slopes is not None:
         if q_pos is None:
             raise ValueError("slopes need q_pos")
-        s.slopes = _dense(slopes, (hq,), torch.float32, "slopes", pages.device)
-        s.q_pos = _dense(q_pos, (batch.n_tokens,), torch.int32, "q_pos", pages.device)
+        s.slopes = _dense(slopes, (hq,), torch.float32, "slopes", pages.index)
+        s.q_pos = _dense(q_pos, (batch.n_tokens,), torch.int32, "q_pos", pages.index)
     if prefix is not None:
-        s.prefix = _dense(prefix, (batch.B,), torch.int32, "prefix", pages.device)
+        s.prefix = _dense(prefix, (batch.B,), torch.int32, "prefix", pages.index)
     return _own.rs
 
 
@@ -238,12 +230,11 @@ def arkv_paged_attention(pages, batch, q, scale, out, lse=None, cap=0.0, slopes=
     torch = _TORCH or _torch()
     _current(pages, batch)
     n, o = batch.n_tokens, _own
-    _rows(o.q, q, n, pages, "q")
-    hq = q.shape[1]
+    hq = _rows(o.q, q, n, pages, "q")
     ws, size = _workspace(workspace, pages)
     _call("arkv_paged_attention", pages.ref, batch.ref, _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix), hq, o.rq,
-          _dense(out, (n, hq, pages.d), pages.dtype, "out", pages.device),
-          None if lse is None else _dense(lse, (n, hq), torch.float32, "lse", pages.device), ws, size, _b._stream())
+          _dense(out, (n, hq, pages.d), pages.dtype, "out", pages.index),
+          None if lse is None else _dense(lse, (n, hq), torch.float32, "lse", pages.index), ws, size, _b._stream())
 
 
 def arkv_paged_weights(pages, batch, q, scale, lse, decay=1.0, carried=None, cap=0.0, slopes=None, q_pos=None, prefix=None,
@@ -252,12 +243,11 @@ def arkv_paged_weights(pages, batch, q, scale, lse, decay=1.0, carried=None, cap
     torch = _TORCH or _torch()
     _current(pages, batch)
     n, o = batch.n_tokens, _own
-    _rows(o.q, q, n, pages, "q")
-    hq = q.shape[1]
+    hq = _rows(o.q, q, n, pages, "q")
     ws, size = _workspace(workspace, pages)
     _call("arkv_paged_weights", pages.ref, batch.ref, _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix), hq, o.rq,
-          _dense(lse, (n, hq), torch.float32, "lse", pages.device), decay,
-          None if carried is None else _dense(carried, pages.k.shape[:3], torch.float32, "carried", pages.device),
+          _dense(lse, (n, hq), torch.float32, "lse", pages.index), decay,
+          None if carried is None else _dense(carried, pages.k.shape[:3], torch.float32, "carried", pages.index),
           ws, size, _b._stream())
 
 
@@ -269,10 +259,10 @@ def arkv_paged_evict(pages, batch, keep, dst_table, kept, new_len, sink=4, recen
     _need(dst_table.dim() == 2 and kept.dim() == 3, "dst_table: [B][pages]; kept: [B][H_kv][max_keep]")
     width, max_keep = dst_table.shape[1], kept.shape[2]
     ws, size = _workspace(workspace, pages)
-    _call("arkv_paged_evict", pages.ref, batch.ref, _dense(keep, (B,), torch.int32, "keep", pages.device), max_keep, sink, recent,
-          _dense(dst_table, (B, width), torch.int32, "dst_table", pages.device), width,
-          _dense(kept, (B, pages.H, max_keep), torch.int32, "kept", pages.device),
-          _dense(new_len, (B,), torch.int32, "new_len", pages.device), ws, size, _b._stream())
+    _call("arkv_paged_evict", pages.ref, batch.ref, _dense(keep, (B,), torch.int32, "keep", pages.index), max_keep, sink, recent,
+          _dense(dst_table, (B, width), torch.int32, "dst_table", pages.index), width,
+          _dense(kept, (B, pages.H, max_keep), torch.int32, "kept", pages.index),
+          _dense(new_len, (B,), torch.int32, "new_len", pages.index), ws, size, _b._stream())
 
 
 def arkv_debug_paged_row(table_row, n_pages, page_size, n_kv_heads, kv_head, length, slot):

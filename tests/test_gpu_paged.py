@@ -9,6 +9,7 @@ import paged_ref as R
 
 pytestmark = pytest.mark.gpu
 BF, FP = torch.bfloat16, torch.float16
+TICKETS = 1 << 16                                      # bytes of a workspace that are zero between calls
 
 
 def handles(s, max_q=None, max_kv=None):
@@ -19,11 +20,12 @@ def handles(s, max_q=None, max_kv=None):
 
 def attend(s, **kw):
     pages, batch, ws = handles(s)
-    ws.fill_(0xFF)                                     # what a workspace holds does not matter
+    ws[TICKETS:].fill_(0xFF)                           # what a workspace holds behind its tickets does not matter
     out = torch.full((s.n, s.hq, s.d), 7.0, dtype=s.dtype, device="cuda")
     lse = torch.full((s.n, s.hq), 7.0, device="cuda")
     P.arkv_paged_attention(pages, batch, s.q, s.scale, out, lse=lse, workspace=ws, **kw)
     torch.cuda.synchronize()
+    assert not ws[:TICKETS].any()
     return out, lse
 
 
@@ -160,6 +162,33 @@ def test_long_caches(q, kv, hq, hkv):
     check_attention(s, slopes=sl, q_pos=qp)
 
 
+@pytest.mark.parametrize("lens", [(1025,), (2048,), (4100,), (2049, 1, 5000, 0, 1024), (1500,) * 40, (30000,), (33000, 70)])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(BF, 8, 2, 128), (FP, 16, 1, 64)])
+def test_pieces_are_joined(lens, dtype, hq, hkv, d):
+    """Sequences of one piece, of a few (joined by the last workgroup) and of many (by a launch), the same workspace again and again."""
+    s = R.problem("cuda", dtype, hq, hkv, d, 16, tuple(min(1, t) for t in lens), lens, seed=13)
+    out, lse = check_attention(s)
+    pages, batch, ws = handles(s)
+    for _ in range(5):
+        o2, l2 = torch.empty_like(out), torch.empty_like(lse)
+        P.arkv_paged_attention(pages, batch, s.q, s.scale, o2, lse=l2, workspace=ws)
+        assert torch.equal(out, o2) and torch.equal(lse, l2)
+
+
+def test_one_workspace_for_batches_of_any_shape():
+    big = R.problem("cuda", BF, 8, 8, 128, 16, (1,) * 20, (3000,) * 20, seed=14)
+    small = R.problem("cuda", BF, 8, 2, 128, 16, (100, 1), (5000, 2100), seed=15)
+    want = [attend(big), attend(small)]
+    ws = torch.zeros(max(handles(s)[2].numel() for s in (big, small)), dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        for s, (out, lse) in zip((big, small), want):
+            pages, batch, _ = handles(s)
+            o2, l2 = torch.empty_like(out), torch.empty_like(lse)
+            P.arkv_paged_attention(pages, batch, s.q, s.scale, o2, lse=l2, workspace=ws)
+            assert torch.equal(out, o2) and torch.equal(lse, l2)
+            P.arkv_paged_weights(pages, batch, s.q, s.scale, l2, workspace=ws)
+
+
 def test_offsets_beyond_32_bits():
     """A pool of more than 4 GiB, its last pages in use."""
     n_pages, hkv, page, d = 40000, 8, 64, 128
@@ -202,7 +231,7 @@ def test_weights(i, hq, hkv, d, page, dtype):
     s = R.problem("cuda", dtype, hq, hkv, d, page, q, kv, seed=20 + i, fused=bool(i & 1), extra_tokens=i % 2)
     _, lse = attend(s)
     pages, batch, ws = handles(s)
-    ws.fill_(0xFF)
+    ws[TICKETS:].fill_(0xFF)
     for decay, other in [(1.0, False), (0.0, False), (0.75, True)]:
         carried = torch.rand_like(s.weight) if other else s.weight.clone()
         ref, tol = R.weights(s, lse, decay, carried)
@@ -345,7 +374,7 @@ def test_evict(kv, keep, sink, recent, seed):
     ref, lens = R.evict(s, keep, sink, recent, max_keep)
     before = {n: getattr(s, n).clone() for n in ("k", "v", "pos", "weight")}
     pages, batch, ws = handles(s)
-    ws.fill_(0xFF)
+    ws[TICKETS:].fill_(0xFF)
     kept = torch.full((len(kv), 2, max_keep), 99, dtype=torch.int32, device="cuda")
     new_len = torch.full((len(kv),), 99, dtype=torch.int32, device="cuda")
     P.arkv_paged_evict(pages, batch, torch.tensor(keep, dtype=torch.int32, device="cuda"), dst, kept, new_len, sink=sink, recent=recent, workspace=ws)
