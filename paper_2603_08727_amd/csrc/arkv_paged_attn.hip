@@ -38,10 +38,13 @@ static Cut cut_of(const Paged& P, int D, int Hq) {
     piece = (int)std::min<long long>(most, std::max<long long>(least, (p + unit - 1) / unit * unit));
     n = std::max(1, (P.max_kv + piece - 1) / piece);
   };
-  // Sequences differ in length, so no large pieces: the last round of workgroups ends with the others (32 requests of 800 to
-  // 16384 rows x 8 heads: 173 us in pieces of 1024, 177 of 2048, 182 of 4096; four of 131071: 373, 362, 354).  Up to 1024
-  // keys one piece: joining costs more than it saves (513 keys, 2 heads: 6.0 us, against 4.4 + 3.2 in pieces of 128 or 256).
-  pieces((long long)P.B * P.H, 1024, P.max_kv <= 1024 ? 1024 : 256, kStepMaxPiece, 128, c.step_piece, c.n_step);
+  // A workgroup for each CU, and no more pieces than the last workgroup joins (8 heads x 1024 rows: 6.6 us in pieces of 128
+  // keys, 9.6 of 512, 12.4 in one; x 8192: 13.7 us in pieces of 128 and a launch that joins them, 11.9 of 512; 32 heads x
+  // 8192: 29.6 us in pieces of 512, 28.7 of 1024), but no large ones: sequences differ in length, and the last round of
+  // workgroups should end with the others (32 requests of 800 to 16384 rows x 8 heads: 177 us in pieces of 2048, 182 of
+  // 4096; four of 131071 rows: 362 and 354).  Fewer than 16 heads do not fill the chip in 16 pieces.
+  const long long units = (long long)P.B * P.H;
+  pieces(units, std::min(256ll, kJoinPieces * units), 128, units < 16 ? kStepMaxPiece / 2 : kStepMaxPiece, 128, c.step_piece, c.n_step);
   // One workgroup for every place on the chip, at d = 64 three to a CU (1686 tokens on up to 3001 rows, 12 heads: 46 us in pieces of
   // 1024 keys, 42 of 512; d = 128, 512 tokens on 4100 rows, 16 heads: 55 us in pieces of 1024, 58 of 512).
   const long long blocks = ((long long)P.N * G + kChunkRows - 1) / kChunkRows * P.H;
