@@ -193,15 +193,62 @@ __device__ __forceinline__ void count_bins(int* hist, const bool (&on)[4], const
   if (lane == first) atomicAdd(&hist[shared], n);
 }
 
+// Survivors times channels up to which the choosing workgroup copies them, which saves a launch (8 x 2 heads, 250 of 1000 rows of 64
+// channels: 11.5 us against 12.6; 8 heads, 250 of 128 channels: 12.5 and 12.4; 500: 16.6 and 12.6).
+constexpr int kSelectMoves = 32768;
 constexpr int kEvictBins = 2048;        // eleven bits of a key
 constexpr int kEvictLdsBlocks = 9;      // blocks of 4 x kEvictThreads keys that fit LDS beside the bins
+
+// Copies survivors first, first + step, .. to their new slots: D / 8 lanes a row, kMoveRows rows per lane whose loads are all
+// under way together.
+constexpr int kMoveRows = 4;
+template <int D>
+__device__ __forceinline__ void move_rows(const EvictArgs& A, const Kept& K, int h, int b, int first, int step) {
+  constexpr int LPR = D / 8;
+  const int c = threadIdx.x % LPR;
+  const Paged& P = A.P;
+  const int32_t* kept = A.kept + ((size_t)b * P.H + h) * A.max_keep;
+  int from[kMoveRows], to[kMoveRows];
+#pragma unroll
+  for (int r = 0; r < kMoveRows; ++r) {
+    const int i = first + r * step;
+    from[r] = i < K.m ? kept[i] : -1;
+  }
+#pragma unroll
+  for (int r = 0; r < kMoveRows; ++r) {
+    from[r] = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, K.n, from[r]);
+    to[r] = slot_row(A.dst_table + (size_t)b * A.dst_width, P.n_pages, P.H, h, P.lg_page, K.m, first + r * step);
+  }
+  u32x4p x[kMoveRows], y[kMoveRows];
+#pragma unroll
+  for (int r = 0; r < kMoveRows; ++r) {
+    x[r] = ((const u32x4p*)P.k)[(size_t)max(from[r], 0) * LPR + c];
+    y[r] = ((const u32x4p*)P.v)[(size_t)max(from[r], 0) * LPR + c];
+  }
+#pragma unroll
+  for (int r = 0; r < kMoveRows; ++r) {
+    if (from[r] < 0 || to[r] < 0) continue;
+    ((u32x4p*)P.k)[(size_t)to[r] * LPR + c] = x[r];
+    ((u32x4p*)P.v)[(size_t)to[r] * LPR + c] = y[r];
+    if (c == 0) P.pos[to[r]] = P.pos[from[r]];
+    if (c == 1) P.weight[to[r]] = P.weight[from[r]];
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void k_evict_move(EvictArgs A) {
+  constexpr int RPW = 256 / (D / 8);
+  const int h = blockIdx.y, b = blockIdx.z;
+  move_rows<D>(A, kept_of(A, b), h, b, blockIdx.x * RPW * kMoveRows + threadIdx.x / (D / 8), RPW);
+}
 
 // Which rows of a (sequence, kv-head) stay.  One workgroup finds the key of the last one digit by digit, from the top: how
 // many rows have which digit, and the digit at which the rows to keep run out; a digit whose rows all stay ends the search.
 // Then every wave writes the survivors among its slots, behind those of the waves before.  A wave's slots are adjacent,
 // four per lane and block (in one page: one look at the table and one 16-byte load).  IN_LDS: the keys are read from memory
-// once and stay in LDS; else (more rows than it holds) they are read in every pass.
-template <bool IN_LDS>
+// once and stay in LDS; else (more rows than it holds) they are read in every pass.  MOVE > 0: the workgroup then copies the
+// survivors of MOVE channels itself.
+template <bool IN_LDS, int MOVE>
 __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
   constexpr int NW = kEvictThreads / 64, BPT = kEvictBins / kEvictThreads;
   extern __shared__ u32x4p held[];                                 // [block][thread]
@@ -371,58 +418,32 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
   };
   for (int q = 0; q < nq; ++q) write(q);
   for (int i = K.m + tid; i < A.max_keep; i += kEvictThreads) kept[i] = -1;
-}
-
-// Copies the survivors to their new slots: D / 8 lanes a row, kMoveRows rows per lane whose loads are all under way together.
-constexpr int kMoveRows = 4;
-template <int D>
-__global__ __launch_bounds__(256) void k_evict_move(EvictArgs A) {
-  constexpr int LPR = D / 8, RPW = 256 / LPR;
-  const int h = blockIdx.y, b = blockIdx.z, c = threadIdx.x % LPR;
-  const int i0 = blockIdx.x * RPW * kMoveRows + threadIdx.x / LPR;
-  const Paged& P = A.P;
-  const Kept K = kept_of(A, b);
-  const int32_t* kept = A.kept + ((size_t)b * P.H + h) * A.max_keep;
-  int from[kMoveRows], to[kMoveRows];
-#pragma unroll
-  for (int r = 0; r < kMoveRows; ++r) {
-    const int i = i0 + r * RPW;
-    from[r] = i < K.m ? kept[i] : -1;
-  }
-#pragma unroll
-  for (int r = 0; r < kMoveRows; ++r) {
-    from[r] = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, K.n, from[r]);
-    to[r] = slot_row(A.dst_table + (size_t)b * A.dst_width, P.n_pages, P.H, h, P.lg_page, K.m, i0 + r * RPW);
-  }
-  u32x4p x[kMoveRows], y[kMoveRows];
-#pragma unroll
-  for (int r = 0; r < kMoveRows; ++r) {
-    x[r] = ((const u32x4p*)P.k)[(size_t)max(from[r], 0) * LPR + c];
-    y[r] = ((const u32x4p*)P.v)[(size_t)max(from[r], 0) * LPR + c];
-  }
-#pragma unroll
-  for (int r = 0; r < kMoveRows; ++r) {
-    if (from[r] < 0 || to[r] < 0) continue;
-    ((u32x4p*)P.k)[(size_t)to[r] * LPR + c] = x[r];
-    ((u32x4p*)P.v)[(size_t)to[r] * LPR + c] = y[r];
-    if (c == 0) P.pos[to[r]] = P.pos[from[r]];
-    if (c == 1) P.weight[to[r]] = P.weight[from[r]];
+  if constexpr (MOVE > 0) {
+    constexpr int RPW = kEvictThreads / (MOVE / 8);
+    __syncthreads();                                               // the list is written
+    for (int i = 0; i < K.m; i += RPW * kMoveRows) move_rows<MOVE>(A, K, h, b, i + tid / (MOVE / 8), RPW);
   }
 }
 
 hipError_t launch_paged_evict(int D, const EvictArgs& A, hipStream_t st) {
   const dim3 units(A.P.H, A.P.B);
+  const int rows = std::min(A.max_keep, A.P.max_kv), rpw = 256 / (D / 8) * kMoveRows;
+  const bool moves = rows * D <= kSelectMoves;
   const int blocks = (A.P.max_kv + 4 * kEvictThreads - 1) / (4 * kEvictThreads);
   if (blocks <= kEvictLdsBlocks) {
-    const int bytes = 16 * kEvictThreads * blocks, most = 16 * kEvictThreads * kEvictLdsBlocks;
-    const hipError_t e = hipFuncSetAttribute((const void*)k_evict_select<true>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+    const void* kernel = !moves ? (const void*)k_evict_select<true, 0> : D == 64 ? (const void*)k_evict_select<true, 64> : (const void*)k_evict_select<true, 128>;
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 16 * kEvictThreads * kEvictLdsBlocks);
     if (e != hipSuccess) return e;
-    k_evict_select<true><<<units, kEvictThreads, bytes, st>>>(A);
+    const int bytes = 16 * kEvictThreads * blocks;
+    if (!moves) k_evict_select<true, 0><<<units, kEvictThreads, bytes, st>>>(A);
+    else if (D == 64) k_evict_select<true, 64><<<units, kEvictThreads, bytes, st>>>(A);
+    else k_evict_select<true, 128><<<units, kEvictThreads, bytes, st>>>(A);
   } else {
-    k_evict_select<false><<<units, kEvictThreads, 0, st>>>(A);
+    if (!moves) k_evict_select<false, 0><<<units, kEvictThreads, 0, st>>>(A);
+    else if (D == 64) k_evict_select<false, 64><<<units, kEvictThreads, 0, st>>>(A);
+    else k_evict_select<false, 128><<<units, kEvictThreads, 0, st>>>(A);
   }
-  const int rows = std::min(A.max_keep, A.P.max_kv), rpw = 256 / (D / 8) * kMoveRows;
-  if (rows > 0) {
+  if (!moves && rows > 0) {
     const dim3 grid((rows + rpw - 1) / rpw, A.P.H, A.P.B);
     if (D == 64) k_evict_move<64><<<grid, 256, 0, st>>>(A);
     else k_evict_move<128><<<grid, 256, 0, st>>>(A);

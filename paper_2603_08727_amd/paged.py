@@ -187,12 +187,17 @@ def _call(name, *args):
 
 # ---- entry points, same names as the C ABI -----------------------------------------------------
 
+def arkv_paged_workspace_bytes(pages, batch, n_q_heads):
+    """Bytes of workspace that the calls below need for this batch."""
+    n = C.c_size_t()
+    _call("arkv_paged_workspace", pages.ref, batch.ref, n_q_heads, C.byref(n))
+    return n.value
+
+
 def arkv_paged_workspace(pages, batch, n_q_heads):
     """A workspace tensor for the calls below (zeros, as its first use wants it; one for the largest batch serves all)."""
     torch = _TORCH or _torch()
-    n = C.c_size_t()
-    _call("arkv_paged_workspace", pages.ref, batch.ref, n_q_heads, C.byref(n))
-    return torch.zeros(n.value, dtype=torch.uint8, device=pages.device)
+    return torch.zeros(arkv_paged_workspace_bytes(pages, batch, n_q_heads), dtype=torch.uint8, device=pages.device)
 
 
 def arkv_paged_append(pages, batch, rotary, q, k, v, positions, q_out):

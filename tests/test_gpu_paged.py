@@ -461,3 +461,55 @@ def test_a_captured_step_follows_lengths_and_tables():
             got.append([x.clone() for x in (out, lse, kept, lens, s.k, s.weight, s.pos)])
         for a, b in zip(*got):
             assert torch.equal(a.float().nan_to_num(3.0), b.float().nan_to_num(3.0)), i
+
+
+def test_the_example_equals_dense_attention_until_it_evicts():
+    """Chunked prompts and single tokens through the example's layer against one dense causal attention per request."""
+    from paper_2603_08727_amd.paged_example import PagedLayer
+    torch.manual_seed(3)
+    layer = PagedLayer(3, n_pages=128, limit=4000, budget=100, max_tokens=64)
+    plan = [(64, 0, 5), (64, 40, 0), (1, 60, 1), (30, 1, 1), (1, 1, 1)]
+    xs, ys = [[], [], []], [[], [], []]
+    for q_len in plan:
+        x = torch.randn(sum(q_len), 512, device="cuda").to(BF)
+        y = layer.step(x, list(q_len))
+        at = 0
+        for r, a in enumerate(q_len):
+            xs[r].append(x[at:at + a]); ys[r].append(y[at:at + a])
+            at += a
+    for r in range(3):
+        x, y = torch.cat(xs[r]), torch.cat(ys[r])
+        n = x.shape[0]
+        assert layer.rows[r] == layer.seen[r] == n
+        qkv = (x @ layer.w_qkv).view(n, 12, 64)
+        positions = torch.arange(n, device="cuda")[None]
+        q, k = (R.rotate(part, positions, layer.rotary.freq, [0] * 32, False)[0].to(BF).double() for part in (qkv[:, :8], qkv[:, 8:10]))
+        v = qkv[:, 10:].double()
+        out = torch.empty(n, 8, 64, dtype=torch.float64, device="cuda")
+        for h in range(8):
+            s = (q[:, h] @ k[:, h // 4].t()) / 8.0
+            s = s.masked_fill(torch.ones_like(s).triu(1).bool(), -math.inf)
+            out[:, h] = torch.softmax(s, -1) @ v[:, h // 4]
+        ref = out.reshape(n, 512) @ layer.w_out.double()
+        # stored roundings: rotated q and k (2^-9 of a logit each, at one rounding that falls the other way), probabilities, the
+        # output, its projection: a few 2^-8 of the row's size
+        assert float((y.double() - ref).norm() / ref.norm()) < 4 * 2.0 ** -8
+
+
+def test_the_example_keeps_its_requests_within_their_budget():
+    from paper_2603_08727_amd.paged_example import PagedLayer
+    torch.manual_seed(4)
+    layer = PagedLayer(2, n_pages=64, limit=96, budget=64, max_tokens=64)
+    for step in range(30):
+        q_len = [64, 0] if step < 3 else [1, 64] if step < 6 else [1, 1]
+        y = layer.step(torch.randn(sum(q_len), 512, device="cuda").to(BF), q_len)
+        assert torch.isfinite(y).all()
+        assert all(n <= 96 for n in layer.rows)
+        pages = layer.held[0] + layer.held[1] + layer.free
+        assert sorted(pages) == list(range(64))        # no page is lost or held twice
+    for r in range(2):
+        for h in range(2):
+            held = torch.tensor(layer.held[r], device="cuda").long()
+            pos = layer.pages.pos[held, h].reshape(-1)[:layer.rows[r]]
+            assert (pos[1:] > pos[:-1]).all() and int(pos[-1]) == layer.seen[r] - 1   # in order, the latest there
+            assert pos[:4].tolist() == [0, 1, 2, 3]                                    # and the first four
