@@ -1,6 +1,7 @@
 // Rows of a paged cache: rotary positions on the way in (k_paged_append), and eviction by collected weight
 // (k_evict_select, k_evict_move).
 #include <algorithm>
+#include <type_traits>
 
 #include "arkv_dev.h"
 #include "arkv_paged_dev.h"
@@ -157,24 +158,66 @@ hipError_t launch_paged_append(int dtype, int D, const AppendArgs& A, hipStream_
 
 // ---- eviction -------------------------------------------------------------------------------------
 
-constexpr int kEvictThreads = 1024;
+constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
+constexpr int kEvictBins = 2048;        // eleven bits of a key
+constexpr int kEvictRows = 4 * kEvictThreads;   // slots that a workgroup looks at at a time: four adjacent ones per lane
+constexpr int kEvictRegs = 9;           // times that many slots whose keys a lane keeps in registers
+constexpr int kEvictSlots = 256;        // slots per workgroup of k_evict_move: those of one wave, kEvictRows at a time
+// Survivors times channels up to which the choosing workgroup copies them, which saves a launch and the workspace (8 x 2 heads,
+// 250 of 1000 rows of 64 channels: 9.6 us against 9.9; 512: 10.8 and 11.1; 8 x 8 heads, 250 of 2000 rows of 128: 12.5 and 13.4).
+constexpr int kSelectMoves = 32768;
 
-// Order of weights as an order of words: NaN (and a row that is not there) lowest, -0 with +0.
+// Order of weights as an order of words: NaN (and a row that is not there) lowest, -0 with +0; 0 is no weight's.
 __device__ __forceinline__ uint32_t weight_key(float w) {
-  if (!(w == w)) return 0;
+  if (!(w == w)) return 1;
   const uint32_t u = __float_as_uint(w + 0.f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// What a unit keeps: m rows, the first `front` and the last `back` of n among them.
-struct Kept { int n, m, front, back; };
+// What a unit keeps: m of its n rows, the first `lo` and those from `hi` on among them, and `ranked` of the others.
+struct Kept {
+  int n, m, lo, hi, ranked;
+  __device__ __forceinline__ bool all() const { return ranked >= hi - lo; }
+  __device__ __forceinline__ bool by_weight() const { return !all() && ranked > 0; }
+};
 __device__ __forceinline__ Kept kept_of(const EvictArgs& A, int b) {
   Kept k;
   k.n = min(max(A.P.kv_len[b], 0), A.P.max_kv);
   k.m = min(k.n, min(max(A.keep[b], 0), A.max_keep));
-  k.front = min(A.sink, k.m);
-  k.back = min(A.recent, k.m - k.front);
+  k.lo = min(A.sink, k.m);
+  const int back = min(A.recent, k.m - k.lo);
+  k.hi = k.n - back;
+  k.ranked = k.m - k.lo - back;
   return k;
+}
+
+// How a launch is cut: workgroups per unit that count, slots of each; where the workspace holds what they pass on: [unit][chunk]
+// histograms, per unit the key of the last survivor and how many rows of that key stay, per unit and kEvictSlots slots the
+// rows in front that stay for certain and those of the last survivor's key.
+struct EvictCut { int chunks, per, blocks; };
+struct EvictParts { int* tickets; unsigned long long* hist; uint2* last; int2* before; };
+
+static EvictCut evict_cut(const Paged& P) {
+  // Where there are fewer units than half the CUs, several workgroups count the first digit (32 units of 32768 rows:
+  // 6 us; by one workgroup each, 14).
+  const long long units = (long long)P.B * P.H;
+  const int steps = std::max(1, (P.max_kv + kEvictRows - 1) / kEvictRows);
+  EvictCut c;
+  c.chunks = (int)std::max(1ll, std::min<long long>(steps, 256 / units));
+  c.per = (steps + c.chunks - 1) / c.chunks * kEvictRows;
+  c.chunks = std::max(1, (P.max_kv + c.per - 1) / c.per);
+  c.blocks = steps * (kEvictRows / kEvictSlots);
+  return c;
+}
+static_assert(kJoinUnits >= 128, "a ticket for every unit that is cut");
+
+size_t paged_evict_floats(const Paged& P) {
+  const EvictCut c = evict_cut(P);
+  const size_t units = (size_t)P.B * P.H;
+  return kTicketFloats + units * (c.chunks > 1 ? (size_t)c.chunks * kEvictBins : 0) + 2 * units + 2 * units * c.blocks;
+}
+bool paged_evict_needs_workspace(const Paged& P, int D, int max_keep) {
+  return (int64_t)max_keep * D > kSelectMoves || P.max_kv > kEvictRegs * kEvictRows;
 }
 
 // Adds one to hist[bin] for each of a lane's four bins with `on` set.  The lanes that share the bin of the first one (equal
@@ -182,6 +225,12 @@ __device__ __forceinline__ Kept kept_of(const EvictArgs& A, int b) {
 __device__ __forceinline__ void count_bins(int* hist, const bool (&on)[4], const int (&bin)[4], int lane) {
   const uint64_t live = __ballot(on[0] || on[1] || on[2] || on[3]);
   if (!live) return;
+  if (__popcll(live) <= 8) {                                       // (few: the queue is short)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (on[e]) atomicAdd(&hist[bin[e]], 1);
+    return;
+  }
   const int first = __builtin_ctzll(live);
   const int shared = __builtin_amdgcn_readlane(on[0] ? bin[0] : on[1] ? bin[1] : on[2] ? bin[2] : bin[3], first);
   int n = 0;
@@ -193,35 +242,28 @@ __device__ __forceinline__ void count_bins(int* hist, const bool (&on)[4], const
   if (lane == first) atomicAdd(&hist[shared], n);
 }
 
-// Survivors times channels up to which the choosing workgroup copies them, which saves a launch (8 x 2 heads, 250 of 1000 rows of 64
-// channels: 11.5 us against 12.6; 8 heads, 250 of 128 channels: 12.5 and 12.4; 500: 16.6 and 12.6).
-constexpr int kSelectMoves = 32768;
-constexpr int kEvictBins = 2048;        // eleven bits of a key
-constexpr int kEvictLdsBlocks = 9;      // blocks of 4 x kEvictThreads keys that fit LDS beside the bins
-
-// Copies survivors first, first + step, .. to their new slots: D / 8 lanes a row, kMoveRows rows per lane whose loads are all
-// under way together.
+// Copies survivors i = first, first + step, .. < n, which are at slots list[i], to slots to0 + i: D / 8 lanes a row, kMoveRows
+// rows per lane whose loads are all under way together.
 constexpr int kMoveRows = 4;
 template <int D>
-__device__ __forceinline__ void move_rows(const EvictArgs& A, const Kept& K, int h, int b, int first, int step) {
+__device__ __forceinline__ void move_rows(const EvictArgs& A, const Kept& K, int h, int b, const int* list, int n, int to0, int first, int step) {
   constexpr int LPR = D / 8;
   const int c = threadIdx.x % LPR;
   const Paged& P = A.P;
-  const int32_t* kept = A.kept + ((size_t)b * P.H + h) * A.max_keep;
   int from[kMoveRows], to[kMoveRows];
 #pragma unroll
   for (int r = 0; r < kMoveRows; ++r) {
     const int i = first + r * step;
-    from[r] = i < K.m ? kept[i] : -1;
+    from[r] = i < n ? slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, K.n, list[i]) : -1;
+    to[r] = i < n ? slot_row(A.dst_table + (size_t)b * A.dst_width, P.n_pages, P.H, h, P.lg_page, K.m, to0 + i) : -1;
   }
-#pragma unroll
-  for (int r = 0; r < kMoveRows; ++r) {
-    from[r] = slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, K.n, from[r]);
-    to[r] = slot_row(A.dst_table + (size_t)b * A.dst_width, P.n_pages, P.H, h, P.lg_page, K.m, first + r * step);
-  }
+  // (lanes 0 and 1 of a row take its position and weight)
+  uint32_t* meta = c == 0 ? (uint32_t*)P.pos : (uint32_t*)P.weight;
   u32x4p x[kMoveRows], y[kMoveRows];
+  uint32_t z[kMoveRows];
 #pragma unroll
   for (int r = 0; r < kMoveRows; ++r) {
+    z[r] = c < 2 ? meta[max(from[r], 0)] : 0;
     x[r] = ((const u32x4p*)P.k)[(size_t)max(from[r], 0) * LPR + c];
     y[r] = ((const u32x4p*)P.v)[(size_t)max(from[r], 0) * LPR + c];
   }
@@ -230,84 +272,117 @@ __device__ __forceinline__ void move_rows(const EvictArgs& A, const Kept& K, int
     if (from[r] < 0 || to[r] < 0) continue;
     ((u32x4p*)P.k)[(size_t)to[r] * LPR + c] = x[r];
     ((u32x4p*)P.v)[(size_t)to[r] * LPR + c] = y[r];
-    if (c == 0) P.pos[to[r]] = P.pos[from[r]];
-    if (c == 1) P.weight[to[r]] = P.weight[from[r]];
+    if (c < 2) meta[to[r]] = z[r];
   }
 }
 
-template <int D>
-__global__ __launch_bounds__(256) void k_evict_move(EvictArgs A) {
-  constexpr int RPW = 256 / (D / 8);
-  const int h = blockIdx.y, b = blockIdx.z;
-  move_rows<D>(A, kept_of(A, b), h, b, blockIdx.x * RPW * kMoveRows + threadIdx.x / (D / 8), RPW);
-}
-
-// Which rows of a (sequence, kv-head) stay.  One workgroup finds the key of the last one digit by digit, from the top: how
-// many rows have which digit, and the digit at which the rows to keep run out; a digit whose rows all stay ends the search.
-// Then every wave writes the survivors among its slots, behind those of the waves before.  A wave's slots are adjacent,
-// four per lane and block (in one page: one look at the table and one 16-byte load).  IN_LDS: the keys are read from memory
-// once and stay in LDS; else (more rows than it holds) they are read in every pass.  MOVE > 0: the workgroup then copies the
-// survivors of MOVE channels itself.
-template <bool IN_LDS, int MOVE>
-__global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
-  constexpr int NW = kEvictThreads / 64, BPT = kEvictBins / kEvictThreads;
-  extern __shared__ u32x4p held[];                                 // [block][thread]
-  __shared__ int hist[kEvictBins];
-  __shared__ int sums[NW], gts[NW], ties_in[NW];
-  __shared__ int s_bin, s_left, s_count;
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+// Which rows of a (sequence, kv-head) stay.  The key of the last one is found digit by digit, from the top: how many rows have
+// which digit, and the digit at which the rows to keep run out; a digit whose rows all stay ends the search.  The first digit,
+// which every row takes part in, is counted by cut.chunks workgroups; the last one to finish goes on alone with the keys in its
+// lanes' registers (REGS times 4096 of them; 0: there are more rows than fit, which are read in every pass).  MOVE > 0: it then lists the survivors
+// and copies their MOVE channels itself; else it leaves to k_evict_move the last survivor's key and the counts in front of every 256 slots.
+template <int REGS, int MOVE>
+__global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A, EvictCut cut, EvictParts parts) {
+  constexpr int NW = kEvictWaves, BPT = kEvictBins / kEvictThreads;
+  __shared__ __align__(8) int hist[kEvictBins];
+  __shared__ int sums[NW];
+  __shared__ int s_bin, s_left, s_count, s_last;
+  constexpr int GROUP = REGS ? REGS : kEvictRegs;                  // steps whose counts are added up together
+  __shared__ int2 counts[GROUP * NW];                        // of every wave's slots: rows that stay for certain, equal ones
+  __shared__ int list[MOVE ? kSelectMoves / (MOVE ? MOVE : 1) : 1];
+  const int chunk = blockIdx.x, h = blockIdx.y, b = blockIdx.z, unit = b * A.P.H + h;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Kept K = kept_of(A, b);
+  const bool ranks = K.by_weight();
+  // a unit that does not rank, or is short, is the first workgroup's alone
+  const int chunks = ranks ? (K.n + cut.per - 1) / cut.per : 1;
+  if (chunk >= chunks) return;
   const int32_t* table = A.P.table + (size_t)b * A.P.width;
-  int32_t* kept = A.kept + ((size_t)b * A.P.H + h) * A.max_keep;
-  if (h == 0 && tid == 0) A.new_len[b] = K.m;
-  const int lo = K.front, hi = K.n - K.back;                       // ranked slots
-  const int ranked = K.m - K.front - K.back;
-  const bool all = ranked >= hi - lo, none = ranked <= 0;
-  const int nq = (K.n + 256 * NW - 1) / (256 * NW);                // blocks of 256 slots per wave
-  const int w0 = wave * nq * 256;
-  auto first_row = [&](int q) { return slot_row(table, A.P.n_pages, A.P.H, h, A.P.lg_page, K.n, w0 + 256 * q + 4 * lane); };
-  auto keys_of = [](const float4& w) { return u32x4p{weight_key(w.x), weight_key(w.y), weight_key(w.z), weight_key(w.w)}; };
-  auto fetch = [&](int q) {                                        // keys of the lane's four slots of block q
-    const int r = first_row(q);
-    return r < 0 ? u32x4p{0, 0, 0, 0} : keys_of(*reinterpret_cast<const float4*>(A.P.weight + r));
-  };
-  auto key = [&](int q) { return IN_LDS ? held[q * kEvictThreads + tid] : fetch(q); };
-  // survivors: keys above `last`, and of those equal to it the first `need`
-  uint32_t last = 0;
-  int need = 0;
-  if (!all && !none) {
-    for (int i = tid; i < kEvictBins; i += kEvictThreads) hist[i] = 0;
-    if (IN_LDS) {                                                  // (a thread's own keys: nobody else reads them)
-      // all blocks' pages, then all their weights: two round trips to memory
-      int r[kEvictLdsBlocks];
-      float4 w[kEvictLdsBlocks];
-#pragma unroll
-      for (int q = 0; q < kEvictLdsBlocks; ++q) r[q] = q < nq ? first_row(q) : -1;
-#pragma unroll
-      for (int q = 0; q < kEvictLdsBlocks; ++q)
-        if (r[q] >= 0) w[q] = *reinterpret_cast<const float4*>(A.P.weight + r[q]);
-#pragma unroll
-      for (int q = 0; q < kEvictLdsBlocks; ++q)
-        if (q < nq) held[q * kEvictThreads + tid] = r[q] < 0 ? u32x4p{0, 0, 0, 0} : keys_of(w[q]);
+  int32_t* kept = A.kept + (size_t)unit * A.max_keep;
+  // keys of slots j .. j + 3, which lie in one page; 0 where a slot is not ranked
+  auto first_row = [&](int j) { return slot_row(table, A.P.n_pages, A.P.H, h, A.P.lg_page, K.n, j); };
+  auto keys_at = [&](int j, int row) {
+    u32x4p x = {1, 1, 1, 1};
+    if (ranks && row >= 0) {
+      const float4 w = *reinterpret_cast<const float4*>(A.P.weight + row);
+      x = u32x4p{weight_key(w.x), weight_key(w.y), weight_key(w.z), weight_key(w.w)};
     }
-    __syncthreads();
-    need = ranked;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < K.lo || j + e >= K.hi) x[e] = 0;
+    return x;
+  };
+  // counts the digit at `shift` of the keys from max(prefix, 1) up to prefix + width - 1
+  auto count = [&](const u32x4p& x, int shift, uint32_t prefix, uint32_t width) {
+    const uint32_t low = max(prefix, 1u), some = width - (low - prefix);
+    bool on[4];
+    int bin[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      on[e] = x[e] - low < some;
+      bin[e] = (int)((x[e] - prefix) >> shift);
+    }
+    count_bins(hist, on, bin, lane);
+  };
+  const int steps = (K.n + kEvictRows - 1) / kEvictRows;           // of 4096 slots each
+  u32x4p keys[GROUP];
+  // all steps' pages, then all their weights: two round trips to memory
+  int row[GROUP];
+#pragma unroll
+  for (int q = 0; q < REGS; ++q) row[q] = q < steps ? first_row(kEvictRows * q + 4 * tid) : -1;
+  auto load_all = [&]() {
+#pragma unroll
+    for (int q = 0; q < REGS; ++q) keys[q] = q < steps ? keys_at(kEvictRows * q + 4 * tid, row[q]) : u32x4p{0, 0, 0, 0};
+  };
+  // f(keys, q) for all steps
+  auto each = [&](auto f) {
+    if constexpr (REGS > 0) {
+#pragma unroll
+      for (int q = 0; q < REGS; ++q)
+        if (q < steps) f(keys[q], q);
+    } else {
+      for (int q = 0; q < steps; ++q) f(keys_at(kEvictRows * q + 4 * tid, first_row(kEvictRows * q + 4 * tid)), q);
+    }
+  };
+  for (int i = tid; i < kEvictBins; i += kEvictThreads) hist[i] = 0;
+  if (REGS && chunks == 1) load_all();
+  __syncthreads();
+  // survivors: keys above `last`, and of those equal to it the first `need`
+  uint32_t last = K.all() ? 0u : ~0u;
+  int need = 0;
+  if (ranks) {
+    if (chunks == 1) {
+      each([&](const u32x4p& x, int) { count(x, 21, 0, ~0u); });   // (no weight's key is ~0)
+    } else {
+      for (int j = cut.per * chunk + 4 * tid; j < min(cut.per * (chunk + 1), K.n); j += kEvictRows) count(keys_at(j, first_row(j)), 21, 0, ~0u);
+      __syncthreads();
+      // (past the L2 of one XCD; the stores are acknowledged before the ticket is drawn)
+      unsigned long long* mine = parts.hist + ((size_t)unit * cut.chunks + chunk) * (kEvictBins / 2);
+      __hip_atomic_store(mine + tid, reinterpret_cast<const unsigned long long*>(hist)[tid], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      int* ticket = parts.tickets + unit * kTicketWords;
+      if (tid == 0) {
+        s_last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == chunks - 1;
+        if (s_last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call wants it
+      }
+      __syncthreads();
+      if (!s_last) return;
+      if (REGS) load_all();
+      int c0 = 0, c1 = 0;
+#pragma unroll 8
+      for (int c = 0; c < chunks; ++c) {
+        const unsigned long long u = __hip_atomic_load(parts.hist + ((size_t)unit * cut.chunks + c) * (kEvictBins / 2) + tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        c0 += (int)(uint32_t)u;
+        c1 += (int)(u >> 32);
+      }
+      hist[2 * tid] = c0;
+      hist[2 * tid + 1] = c1;
+    }
+    need = K.ranked;
     uint32_t prefix = 0;
     for (int shift = 21; ; shift = shift == 21 ? 10 : 0) {
-      const int bits = shift ? 11 : 10;
-      auto count = [&](int q) {
-        const u32x4p x = key(q);
-        const int j = w0 + 256 * q + 4 * lane;
-        bool on[4];
-        int bin[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          on[e] = j + e >= lo && j + e < hi && (shift == 21 || x[e] >> (shift + bits) == prefix >> (shift + bits));
-          bin[e] = x[e] >> shift & ((1 << bits) - 1);
-        }
-        count_bins(hist, on, bin, lane);
-      };
-      for (int q = 0; q < nq; ++q) count(q);
+      if (shift != 21) each([&](const u32x4p& x, int) { count(x, shift, prefix, shift ? 1u << 21 : 1u << 10); });
       __syncthreads();
       // thread t: the bins at BPT t from the top
       int c[BPT], mine = 0;
@@ -326,7 +401,8 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
       if (lane == 63) sums[wave] = upto;
       __syncthreads();
       int before = upto - mine;
-      for (int w = 0; w < wave; ++w) before += sums[w];
+#pragma unroll
+      for (int w = 0; w < NW; ++w) before += w < wave ? sums[w] : 0;
 #pragma unroll
       for (int i = 0; i < BPT; ++i) {
         if (before < need && need <= before + c[i]) {
@@ -339,8 +415,8 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
       __syncthreads();
       prefix |= (uint32_t)s_bin << shift;
       need = s_left;
-      if (s_count == need && prefix) {                             // the whole digit stays: everything from its lowest key on
-        last = prefix - 1;
+      if (s_count == need) {                                       // the whole digit stays: everything from its lowest key on
+        last = prefix ? prefix - 1 : 0;
         need = 0;
         break;
       }
@@ -348,107 +424,175 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A) {
       if (!shift) break;
     }
   }
-  // bit e: slot e of the lane's four stays for certain, bit 4 + e: it is one of the equal ones
-  auto fate = [&](int q) {
-    const u32x4p x = all || none ? u32x4p{0, 0, 0, 0} : key(q);
-    const int j = w0 + 256 * q + 4 * lane;
-    uint32_t f = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool held_ = j + e < lo || j + e >= hi || all;
-      if (j + e < K.n && (held_ || (!none && x[e] > last))) f |= 1u << e;
-      if (j + e < K.n && !held_ && !none && x[e] == last && need > 0) f |= 16u << e;
-    }
-    return f;
-  };
-  int n_gt = 0, n_tie = 0;
-  auto tally = [&](int q) {
-    const uint32_t f = fate(q);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      n_gt += __popcll(__ballot(f >> e & 1));
-      n_tie += __popcll(__ballot(f >> (4 + e) & 1));
-    }
-  };
-  for (int q = 0; q < nq; ++q) tally(q);
-  if (lane == 0) { gts[wave] = n_gt; ties_in[wave] = n_tie; }
-  __syncthreads();
-  int at = 0, tied = 0;                                            // survivors and equal keys in front of this wave's slots
-  for (int w = 0; w < wave; ++w) { at += gts[w]; tied += ties_in[w]; }
-  at += min(tied, need);
-  const uint64_t below = (1ull << lane) - 1;
-  auto write = [&](int q) {
-    const uint32_t f = fate(q);
-    int mine = 0, ties = 0;                                        // equal ones in lanes below, and in all
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint64_t tb = __ballot(f >> (4 + e) & 1);
-      mine += __popcll(tb & below);
-      ties += __popcll(tb);
-    }
-    uint32_t take = f & 15;
-    int rank = tied + mine;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (f >> (4 + e) & 1) {
-        if (rank < need) take |= 1u << e;
-        ++rank;
-      }
-    tied += ties;
-    int to = 0, n = 0;                                             // of this block's survivors: in lanes below, in all
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint64_t kb = __ballot(take >> e & 1);
-      to += __popcll(kb & below);
-      n += __popcll(kb);
-    }
-    // through LDS, in place of the block's keys, which are done with: adjacent lanes then store adjacent words
-    int* list = reinterpret_cast<int*>(&held[q * kEvictThreads + 64 * wave]);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (take >> e & 1) {
-        if (IN_LDS) list[to] = w0 + 256 * q + 4 * lane + e;
-        else if (at + to < A.max_keep) kept[at + to] = w0 + 256 * q + 4 * lane + e;
-        ++to;
-      }
-    if (IN_LDS)
-      for (int i = lane; i < n; i += 64)
-        if (at + i < A.max_keep) kept[at + i] = list[i];
-    at += n;
-  };
-  for (int q = 0; q < nq; ++q) write(q);
+  if (h == 0 && tid == 0) A.new_len[b] = K.m;
   for (int i = K.m + tid; i < A.max_keep; i += kEvictThreads) kept[i] = -1;
+  int carry_sure = 0, carry_ties = 0;                              // in front of the group of steps at hand
+  for (int q0 = 0; q0 < max(1, REGS ? 1 : steps); q0 += GROUP) {
+    auto tally = [&](const u32x4p& x, int q) {
+      const int j = kEvictRows * q + 256 * wave;                   // the wave's slots; of those that are not ranked, which stay
+      int sure = max(0, min(K.lo, j + 256) - j) + max(0, min(K.n, j + 256) - max(K.hi, j)), ties = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sure += __popcll(__ballot(x[e] > last));
+        if (need > 0) ties += __popcll(__ballot(x[e] == last));
+      }
+      if (lane == 0) counts[(q - q0) * NW + wave] = make_int2(sure, ties);
+    };
+    if constexpr (REGS > 0) each(tally);
+    else for (int q = q0; q < min(steps, q0 + GROUP); ++q) tally(keys_at(kEvictRows * q + 4 * tid, first_row(kEvictRows * q + 4 * tid)), q);
+    __syncthreads();
+    // counts become what is in front; a lane adds up three of them
+    const int n = min(GROUP, steps - q0) * NW;
+    if (wave == 0) {
+      constexpr int PL = (GROUP * NW + 63) / 64;
+      int2 c[PL];
+      int sure = 0, ties = 0;
+#pragma unroll
+      for (int i = 0; i < PL; ++i) {
+        c[i] = PL * lane + i < n ? counts[PL * lane + i] : make_int2(0, 0);
+        sure += c[i].x;
+        ties += c[i].y;
+      }
+      int us = sure, ut = ties;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int vs = __shfl_up(us, o), vt = __shfl_up(ut, o);
+        if (lane >= o) { us += vs; ut += vt; }
+      }
+      sure = carry_sure + us - sure;
+      ties = carry_ties + ut - ties;
+#pragma unroll
+      for (int i = 0; i < PL; ++i) {
+        if (PL * lane + i < n) {
+          if (MOVE) counts[PL * lane + i] = make_int2(sure, ties);
+          else parts.before[(size_t)unit * cut.blocks + q0 * NW + PL * lane + i] = make_int2(sure, ties);
+        }
+        sure += c[i].x;
+        ties += c[i].y;
+      }
+      carry_sure = __builtin_amdgcn_readlane(sure, 63);
+      carry_ties = __builtin_amdgcn_readlane(ties, 63);
+    }
+    if (MOVE || !REGS) __syncthreads();
+  }
+  if (MOVE == 0 && tid == 0) parts.last[unit] = make_uint2(last, (uint32_t)need);
   if constexpr (MOVE > 0) {
+    static_assert(REGS > 0, "");
+    const uint64_t below = (1ull << lane) - 1;
+    // bit e: slot e of the lane's four stays for certain, bit 4 + e: it is one of the equal ones
+    auto fate = [&](const u32x4p& x, int q) {
+      const int j = kEvictRows * q + 4 * tid;
+      uint32_t f = 0;
+  #pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (x[e] ? x[e] > last : j + e < K.n) f |= 1u << e;
+        if (need > 0 && x[e] == last) f |= 16u << e;
+      }
+      return f;
+    };
+    each([&](const u32x4p& x, int q) {
+      const uint32_t f = fate(x, q);
+      const int2 front = counts[q * NW + wave];
+      int rank = front.y;                                          // of a lane's equal slots
+#pragma unroll
+      for (int e = 0; e < 4; ++e) rank += __popcll(__ballot(f >> (4 + e) & 1) & below);
+      uint32_t take = f & 15;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (f >> (4 + e) & 1) {
+          if (rank < need) take |= 1u << e;
+          ++rank;
+        }
+      int to = front.x + min(front.y, need);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to += __popcll(__ballot(take >> e & 1) & below);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (take >> e & 1) {
+          if (to < K.m) list[to] = kEvictRows * q + 4 * tid + e;
+          ++to;
+        }
+    });
+    __syncthreads();
     constexpr int RPW = kEvictThreads / (MOVE / 8);
-    __syncthreads();                                               // the list is written
-    for (int i = 0; i < K.m; i += RPW * kMoveRows) move_rows<MOVE>(A, K, h, b, i + tid / (MOVE / 8), RPW);
+    for (int i = tid; i < K.m; i += kEvictThreads) kept[i] = list[i];
+    for (int i = 0; i < K.m; i += RPW * kMoveRows) move_rows<MOVE>(A, K, h, b, list, K.m, 0, i + tid / (MOVE / 8), RPW);
   }
 }
 
-hipError_t launch_paged_evict(int D, const EvictArgs& A, hipStream_t st) {
-  const dim3 units(A.P.H, A.P.B);
-  const int rows = std::min(A.max_keep, A.P.max_kv), rpw = 256 / (D / 8) * kMoveRows;
-  const bool moves = rows * D <= kSelectMoves;
-  const int blocks = (A.P.max_kv + 4 * kEvictThreads - 1) / (4 * kEvictThreads);
-  if (blocks <= kEvictLdsBlocks) {
-    const void* kernel = !moves ? (const void*)k_evict_select<true, 0> : D == 64 ? (const void*)k_evict_select<true, 64> : (const void*)k_evict_select<true, 128>;
-    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 16 * kEvictThreads * kEvictLdsBlocks);
-    if (e != hipSuccess) return e;
-    const int bytes = 16 * kEvictThreads * blocks;
-    if (!moves) k_evict_select<true, 0><<<units, kEvictThreads, bytes, st>>>(A);
-    else if (D == 64) k_evict_select<true, 64><<<units, kEvictThreads, bytes, st>>>(A);
-    else k_evict_select<true, 128><<<units, kEvictThreads, bytes, st>>>(A);
-  } else {
-    if (!moves) k_evict_select<false, 0><<<units, kEvictThreads, 0, st>>>(A);
-    else if (D == 64) k_evict_select<false, 64><<<units, kEvictThreads, 0, st>>>(A);
-    else k_evict_select<false, 128><<<units, kEvictThreads, 0, st>>>(A);
+// Lists the survivors among 256 slots, a slot per lane, and copies them: the units' slots are spread over the whole chip.
+template <int D>
+__global__ __launch_bounds__(kEvictSlots) void k_evict_move(EvictArgs A, EvictCut cut, EvictParts parts) {
+  constexpr int NW = kEvictSlots / 64, RPW = kEvictSlots / (D / 8);
+  __shared__ int list[kEvictSlots];
+  __shared__ int2 counts[NW];
+  const int blk = blockIdx.x, h = blockIdx.y, b = blockIdx.z, unit = b * A.P.H + h;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Kept K = kept_of(A, b);
+  const int j = kEvictSlots * blk + tid;
+  if (kEvictSlots * blk >= K.n) return;
+  const int2 front = parts.before[(size_t)unit * cut.blocks + blk];
+  const uint2 pivot = parts.last[unit];
+  const int need = (int)pivot.y;
+  uint32_t x = 0;
+  if (j >= K.lo && j < K.hi) {
+    const int row = slot_row(A.P.table + (size_t)b * A.P.width, A.P.n_pages, A.P.H, h, A.P.lg_page, K.n, j);
+    x = K.by_weight() && row >= 0 ? weight_key(A.P.weight[row]) : 1;
   }
-  if (!moves && rows > 0) {
-    const dim3 grid((rows + rpw - 1) / rpw, A.P.H, A.P.B);
-    if (D == 64) k_evict_move<64><<<grid, 256, 0, st>>>(A);
-    else k_evict_move<128><<<grid, 256, 0, st>>>(A);
+  const bool sure = x ? x > pivot.x : j < K.n, tie = need > 0 && x == pivot.x;
+  const uint64_t sb = __ballot(sure), tb = __ballot(tie), below = (1ull << lane) - 1;
+  if (lane == 0) counts[wave] = make_int2(__popcll(sb), __popcll(tb));
+  __syncthreads();
+  int certain = 0, ties = front.y, n_sure = 0, n_ties = front.y;   // in front of this lane; in the whole block
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    const int2 c = counts[w];
+    if (w < wave) { certain += c.x; ties += c.y; }
+    n_sure += c.x;
+    n_ties += c.y;
   }
+  certain += __popcll(sb & below);
+  ties += __popcll(tb & below);
+  const int taken = min(front.y, need), to0 = front.x + taken;     // equal rows of earlier blocks that stay; this block's first new slot
+  if (sure || (tie && ties < need)) list[certain + min(ties, need) - taken] = j;
+  __syncthreads();
+  const int n = min(n_sure + min(n_ties, need) - taken, K.m - to0);
+  int32_t* kept = A.kept + (size_t)unit * A.max_keep + to0;
+  for (int i = tid; i < n; i += kEvictSlots) kept[i] = list[i];
+  for (int i = 0; i < n; i += RPW * kMoveRows) move_rows<D>(A, K, h, b, list, n, to0, i + tid / (D / 8), RPW);
+}
+
+template <int D>
+static hipError_t launch_evict(const EvictArgs& A, hipStream_t st) {
+  const Paged& P = A.P;
+  const EvictCut c = evict_cut(P);
+  const bool moves = !paged_evict_needs_workspace(P, D, A.max_keep);
+  const size_t units = (size_t)P.B * P.H;
+  EvictParts parts = {};
+  EvictCut cut = c;
+  if (A.ws) {
+    parts.tickets = (int*)A.ws;
+    parts.hist = (unsigned long long*)(A.ws + kTicketFloats);
+    parts.last = (uint2*)(A.ws + kTicketFloats + (c.chunks > 1 ? units * c.chunks * kEvictBins : 0));
+    parts.before = (int2*)(parts.last + units);
+  }
+  else { cut.chunks = 1; cut.per = kEvictRegs * kEvictRows; }      // (one workgroup a unit needs none)
+  const dim3 grid(cut.chunks, P.H, P.B);
+  auto select = [&](auto regs) {
+    constexpr int N = decltype(regs)::value;
+    if constexpr (N > 0) {
+      if (moves) { k_evict_select<N, D><<<grid, kEvictThreads, 0, st>>>(A, cut, parts); return; }
+    }
+    k_evict_select<N, 0><<<grid, kEvictThreads, 0, st>>>(A, cut, parts);
+  };
+  // (8 x 2 units of 1000 rows: 9.5 us; with the code of nine steps, which has to come from memory, 14.0)
+  if (P.max_kv <= kEvictRows) select(std::integral_constant<int, 1>());
+  else if (P.max_kv <= kEvictRegs * kEvictRows) select(std::integral_constant<int, kEvictRegs>());
+  else select(std::integral_constant<int, 0>());
+  if (!moves && P.max_kv) k_evict_move<D><<<dim3((P.max_kv + kEvictSlots - 1) / kEvictSlots, P.H, P.B), kEvictSlots, 0, st>>>(A, c, parts);
   return hipGetLastError();
 }
+
+hipError_t launch_paged_evict(int D, const EvictArgs& A, hipStream_t st) { return D == 64 ? launch_evict<64>(A, st) : launch_evict<128>(A, st); }
 
 }  // namespace arkv

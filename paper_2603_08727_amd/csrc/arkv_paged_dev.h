@@ -42,6 +42,10 @@ __host__ __device__ inline int slot_row(const int32_t* table_row, int n_pages, i
   return page_row(table_row[slot >> lg_page], n_pages, H, h, lg_page, slot & ((1 << lg_page) - 1));
 }
 
+// The front of a workspace holds the tickets of k_paged_attn and k_evict_select, zero between calls; nothing else is kept there.
+constexpr int kJoinUnits = 1024, kTicketWords = 16;                // (a ticket has a cache line of its own)
+constexpr size_t kTicketFloats = (size_t)kJoinUnits * kTicketWords;
+
 struct AppendArgs {
   Paged P;
   Rows q, k, v;
@@ -74,7 +78,10 @@ struct EvictArgs {
   const int32_t *keep, *dst_table;
   int32_t *kept, *new_len;
   int max_keep, sink, recent, dst_width;
+  float* ws;           // null: none given
 };
+size_t paged_evict_floats(const Paged& P);
+bool paged_evict_needs_workspace(const Paged& P, int D, int max_keep);
 hipError_t launch_paged_evict(int D, const EvictArgs& A, hipStream_t st);
 
 }  // namespace arkv

@@ -48,7 +48,7 @@ static int check_heads(int n_q_heads, int H, int n_tokens, int& G) {
 
 // One size for all calls, so that a workspace serves every one of them.
 static size_t workspace_bytes(const Paged& P, int D, int Hq) {
-  return 4 * std::max(paged_attention_floats(P, D, Hq), paged_weights_floats(P, Hq));
+  return 4 * std::max({paged_attention_floats(P, D, Hq), paged_weights_floats(P, Hq), paged_evict_floats(P)});
 }
 
 static int check_scores(const arkv_scores* s, Scores& out) {
@@ -138,12 +138,15 @@ int arkv_paged_weights(const arkv_pages* pages, const arkv_page_batch* batch, co
 int arkv_paged_evict(const arkv_pages* pages, const arkv_page_batch* batch, const int32_t* keep, int32_t max_keep,
                      int32_t sink, int32_t recent, const int32_t* dst_table, int32_t dst_width, int32_t* kept,
                      int32_t* new_len, void* workspace, size_t bytes, void* hip_stream) {
-  (void)workspace; (void)bytes;
   EvictArgs A = {};
   TRY(check(pages, batch, A.P));
   if (!keep || !dst_table || !kept || !new_len || !pages->weight || sink < 0 || recent < 0 || dst_width < 1 || max_keep < 1 ||
       (int64_t)max_keep > (int64_t)dst_width * pages->page_size)
     return ARKV_EINVAL;
+  if (workspace || paged_evict_needs_workspace(A.P, pages->head_dim, max_keep)) {
+    if (!workspace || !aligned16(workspace) || bytes < 4 * paged_evict_floats(A.P)) return ARKV_EINVAL;
+  }
+  A.ws = (float*)workspace;
   A.keep = keep; A.dst_table = dst_table; A.kept = kept; A.new_len = new_len;
   A.max_keep = max_keep; A.sink = sink; A.recent = recent; A.dst_width = dst_width;
   LAUNCH(launch_paged_evict(pages->head_dim, A, (hipStream_t)hip_stream));

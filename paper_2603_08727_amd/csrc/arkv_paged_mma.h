@@ -91,10 +91,6 @@ __device__ __forceinline__ int row_end(const Seq& s, int i, int prefix) { return
 
 constexpr int kStepRows = 16;           // rows of a sequence that the step kernels take
 
-// The front of a workspace holds the tickets of k_paged_attn, zero between calls; nothing else is kept there.
-constexpr int kJoinUnits = 1024, kTicketWords = 16;                // (a ticket has a cache line of its own)
-constexpr size_t kTicketFloats = (size_t)kJoinUnits * kTicketWords;
-
 // Which kernels a launch needs.  few: sequences of up to so many rows are the step kernel's; -1 where only the other one is
 // launched, which then takes all of them.
 struct Which { bool step, chunk; int few; };

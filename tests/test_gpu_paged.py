@@ -390,6 +390,45 @@ def test_evict(kv, keep, sink, recent, seed):
         assert torch.equal(getattr(s, name).view(torch.uint8), want.view(torch.uint8)), name
 
 
+@pytest.mark.parametrize("what", ["drawn", "few", "equal", "nan", "one digit"])
+@pytest.mark.parametrize("kv,keep,announced", [
+    ((9000, 4097, 300), (2000, 4096, 299), None), ((20000,), (5001,), 36864), ((40001, 5), (10000, 5), None), ((4096, 0), (1000, 50), 70000),
+    ((36864,), (36000,), None)])
+def test_evict_of_many_rows(kv, keep, announced, what):
+    """Units whose rows several workgroups count, or that do not fit a workgroup's registers; the same workspace again and again."""
+    s = R.problem("cuda", BF, 2, 2, 64, 64, (0,) * len(kv), kv, seed=61, spare_pages=len(kv) * (-(-max(keep) // 64)), width=1100)
+    g = torch.Generator().manual_seed(5)
+    if what == "few":
+        s.weight = torch.tensor([0.0, 1.0, 2.0, math.inf]).cuda()[torch.randint(0, 4, s.weight.shape, generator=g).cuda()].contiguous()
+    elif what == "one digit":                          # keys that differ in their lowest bits alone
+        s.weight = 1.0 + torch.randint(0, 300, s.weight.shape, generator=g).float().cuda() * 2.0 ** -23
+    elif what != "drawn":
+        s.weight.fill_(0.0 if what == "equal" else math.nan)
+    s.table[0, 3] = -1
+    max_keep, need = max(keep), -(-max(keep) // 64)
+    dst = torch.tensor(s.spare[:need * len(kv)], dtype=torch.int32, device="cuda").reshape(len(kv), need)
+    ref, lens = R.evict(s, keep, 4, 32, max_keep)
+    before = {n: getattr(s, n).clone() for n in ("k", "v", "pos", "weight")}
+    pages, batch, ws = handles(s, max_kv=announced)
+    ws[TICKETS:].fill_(0xFF)
+    keep_dev = torch.tensor(keep, dtype=torch.int32, device="cuda")
+    for _ in range(3):
+        kept = torch.full((len(kv), 2, max_keep), 99, dtype=torch.int32, device="cuda")
+        new_len = torch.full((len(kv),), 99, dtype=torch.int32, device="cuda")
+        P.arkv_paged_evict(pages, batch, keep_dev, dst, kept, new_len, workspace=ws)
+        assert new_len.tolist() == lens and torch.equal(kept.cpu(), ref)
+        assert not ws[:TICKETS].any()
+    for name, old in before.items():
+        want = old.clone()
+        for b, m in enumerate(lens):
+            for h in range(2):
+                j, to = ref[b, h, :m].long().cuda(), torch.arange(m, device="cuda")
+                page = s.table[b].long()[j // 64]
+                real = (page >= 0) & (page < s.n_pages)
+                want[dst[b].long()[to // 64][real], h, (to % 64)[real]] = old[page[real], h, (j % 64)[real]]
+        assert torch.equal(getattr(s, name).view(torch.uint8), want.view(torch.uint8)), name
+
+
 def test_evict_around_absent_pages():
     s = R.problem("cuda", BF, 4, 2, 64, 16, (0,), (200,), seed=60, spare_pages=9)
     s.table[0, 2] = -1

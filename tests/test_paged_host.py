@@ -180,6 +180,18 @@ def test_workspaces_that_are_too_small_are_refused():
             assert _call(name, pages, batch, rows, rot, sc, ws=ADDR + 4) == A.EINVAL
 
 
+def test_evictions_that_need_a_workspace():
+    a = _args()
+    a[1].table_width, a[1].max_kv = 4096, 36864
+    for kw in [dict(max_keep=513, dst_width=33), dict(max_keep=32)]:   # more survivors, or more rows, than one workgroup takes
+        assert _call("evict", *a, ws=None, **kw) == A.EINVAL
+        assert _call("evict", *a, size=1 << 16, **kw) == A.EINVAL
+        assert _call("evict", *a, ws=ADDR + 4, **kw) == A.EINVAL
+        a[1].max_kv = 36865
+    n = C.c_size_t()
+    assert P.load().arkv_paged_workspace(C.byref(a[0]), C.byref(a[1]), 8, C.byref(n)) == A.OK and n.value > 1 << 16
+
+
 def test_evict_refusals():
     a = _args()
     for kw in [dict(keep=None), dict(dst=None), dict(kept=None), dict(new_len=None), dict(max_keep=0), dict(max_keep=33), dict(sink=-1),
