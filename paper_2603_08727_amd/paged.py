@@ -47,15 +47,15 @@ def load():
     global _lib
     if _lib is None:
         lib = _b.load()
-        vp, i32, P = C.c_void_p, C.c_int32, C.POINTER
-        pg, bt, sc, rw = P(_Pages), P(_Batch), P(_Scores), P(_Rows)
+        vp, i32 = C.c_void_p, C.c_int32
+        pg = bt = sc = rw = rt = vp            # (structs go as plain addresses: ctypes checks a pointer type in 0.1 us each)
         sig = {
-            "arkv_paged_append": [pg, bt, P(_Rotary), i32, rw, rw, rw, vp, vp, vp],
-            "arkv_paged_workspace": [pg, bt, i32, P(C.c_size_t)],
+            "arkv_paged_append": [pg, bt, rt, i32, rw, rw, rw, vp, vp, vp],
+            "arkv_paged_workspace": [pg, bt, i32, vp],
             "arkv_paged_attention": [pg, bt, sc, i32, rw, vp, vp, vp, C.c_size_t, vp],
             "arkv_paged_weights": [pg, bt, sc, i32, rw, vp, C.c_float, vp, vp, C.c_size_t, vp],
             "arkv_paged_evict": [pg, bt, vp, i32, i32, i32, vp, i32, vp, vp, vp, C.c_size_t, vp],
-            "arkv_debug_paged_row": [vp] + [i32] * 7 + [P(C.c_int64)],
+            "arkv_debug_paged_row": [vp] + [i32] * 7 + [vp],
         }
         for name, args in sig.items():
             fn = getattr(lib, name)
@@ -83,7 +83,7 @@ def _need(ok, what):
 def _dense(t, shape, dtype, what, index=None):
     """Address of a contiguous GPU tensor (on GPU `index`) of that shape and type."""
     at = t.get_device()
-    if t.dtype is not dtype or t.shape != shape or at < 0 or (index is not None and at != index) or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or at != (at if index is None else index) or at < 0 or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on the pages' GPU, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")
     return t.data_ptr()
@@ -100,12 +100,13 @@ class arkv_pages:
         self.k, self.v, self.pos, self.weight = k, v, pos, weight
         self.device, self.dtype, self.index = k.device, k.dtype, k.get_device()
         self.n_pages, self.H, self.page_size, self.d = k.shape
+        self.rows = k.shape[:3]
         dev = self.index
         self.c = _Pages(0 if k.dtype == torch.bfloat16 else 1, self.n_pages, self.page_size, self.H, self.d,
                         _dense(k, k.shape, k.dtype, "k"), _dense(v, k.shape, k.dtype, "v", dev),
                         _dense(pos, k.shape[:3], torch.int32, "pos", dev),
                         None if weight is None else _dense(weight, k.shape[:3], torch.float32, "weight", dev))
-        self.ref = C.byref(self.c)
+        self.ref = C.addressof(self.c)
 
 
 class arkv_page_batch:
@@ -122,7 +123,7 @@ class arkv_page_batch:
         self.c = _Batch(B, n_tokens, n_tokens if max_q is None else max_q, width * page_size if max_kv is None else max_kv, width,
                         _dense(cu_q, (B + 1,), torch.int32, "cu_q", self.index), _dense(kv_len, (B,), torch.int32, "kv_len", self.index),
                         _dense(table, (B, width), torch.int32, "table"))
-        self.ref = C.byref(self.c)
+        self.ref = C.addressof(self.c)
 
 
 class arkv_rotary:
@@ -138,15 +139,20 @@ class arkv_rotary:
         self.freq, self.n_axes, self.index = freq, n_axes, None if freq is None else freq.get_device()
         self.c = _Rotary(2 * half, n_axes, 1 if adjacent else 0, (C.c_uint8 * 64)(*axis),
                          None if freq is None else _dense(freq, (half,), torch.float64, "freq"))
-        self.ref = C.byref(self.c)
+        self.ref = C.addressof(self.c)
 
 
 # A call's own structs.  Making one costs a microsecond, so every thread keeps its set and fills it anew in each call (the C
 # side reads them before it returns).
+class _Set:
+    def __init__(self):
+        self.q, self.k, self.v, self.s, self.plain = _Rows(), _Rows(), _Rows(), _Scores(), _Scores()   # (plain: no arrays)
+        self.rq, self.rk, self.rv, self.rs, self.rplain = (C.addressof(x) for x in (self.q, self.k, self.v, self.s, self.plain))
+
+
 class _Own(threading.local):
     def __init__(self):
-        self.q, self.k, self.v, self.s = _Rows(), _Rows(), _Rows(), _Scores()
-        self.rq, self.rk, self.rv, self.rs = (C.byref(x) for x in (self.q, self.k, self.v, self.s))
+        self.set = _Set()
 
 
 _own = _Own()
@@ -155,20 +161,23 @@ _own = _Own()
 def _rows(to, t, n, pages, what):
     """[n][heads][d] with any token and head stride; the channels are adjacent.  Returns the number of heads."""
     shape = t.shape
-    if len(shape) != 3 or shape[0] != n or shape[2] != pages.d or t.dtype is not pages.dtype or t.get_device() != pages.index:
-        raise ValueError(f"{what}: expected {pages.dtype} [{n}][heads][{pages.d}] on {pages.device}, got {t.dtype} {tuple(shape)} on {t.device}")
-    token, head, channel = t.stride()
-    if channel != 1:
-        raise ValueError(f"{what}: channels must be adjacent")
-    to.p = t.data_ptr()
-    to.token_stride = token
-    to.head_stride = head
-    return shape[1]
+    if len(shape) == 3:
+        tokens, heads, channels = shape
+        if tokens == n and channels == pages.d and t.dtype is pages.dtype and t.get_device() == pages.index:
+            to.token_stride, to.head_stride, channel = t.stride()
+            if channel != 1:
+                raise ValueError(f"{what}: channels must be adjacent")
+            to.p = t.data_ptr()
+            return heads
+    raise ValueError(f"{what}: expected {pages.dtype} [{n}][heads][{pages.d}] on {pages.device}, got {t.dtype} {tuple(shape)} on {t.device}")
 
 
 def _current(pages, batch):
-    if batch.index != pages.index or pages.index != _b._device():
+    """Handle of torch's current stream on the device where everything has to be."""
+    at = pages.index
+    if batch.index != at or at != _b._device():
         raise ValueError(f"pages on {pages.device}, batch on {batch.device}: both must be on the current device")
+    return _b._raw_stream(at)
 
 
 def _workspace(ws, pages):
@@ -179,8 +188,7 @@ def _workspace(ws, pages):
     return ws.data_ptr(), ws.nbytes
 
 
-def _call(name, *args):
-    rc = getattr(_lib or load(), name)(*args)
+def _check(rc, name):
     if rc != OK:
         raise ArkvError(rc, name)
 
@@ -190,7 +198,7 @@ def _call(name, *args):
 def arkv_paged_workspace_bytes(pages, batch, n_q_heads):
     """Bytes of workspace that the calls below need for this batch."""
     n = C.c_size_t()
-    _call("arkv_paged_workspace", pages.ref, batch.ref, n_q_heads, C.byref(n))
+    _check((_lib or load()).arkv_paged_workspace(pages.ref, batch.ref, n_q_heads, C.addressof(n)), "arkv_paged_workspace")
     return n.value
 
 
@@ -203,22 +211,28 @@ def arkv_paged_workspace(pages, batch, n_q_heads):
 def arkv_paged_append(pages, batch, rotary, q, k, v, positions, q_out):
     """q [n][H_q][d], k, v [n][H_kv][d] (strided), positions int32 [n_axes][n]; q and q_out may both be None."""
     torch = _TORCH or _torch()
-    _current(pages, batch)
-    n, H, o = batch.n_tokens, pages.H, _own
+    stream = _current(pages, batch)
+    n, H, o = batch.n_tokens, pages.H, _own.set
     if rotary.index != pages.index and rotary.index is not None:
         raise ValueError("freq: on another device than the pages")
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
     if _rows(o.k, k, n, pages, "k") != H or _rows(o.v, v, n, pages, "v") != H:
         raise ValueError(f"k, v: expected {H} heads")
-    hq = 0 if q is None else _rows(o.q, q, n, pages, "q")
-    _call("arkv_paged_append", pages.ref, batch.ref, rotary.ref, hq, None if q is None else o.rq, o.rk, o.rv,
-          _dense(positions, (rotary.n_axes, n), torch.int32, "positions", pages.index),
-          None if q is None else _dense(q_out, (n, hq, pages.d), pages.dtype, "q_out", pages.index), _b._stream())
+    hq, rq, to = 0, None, None
+    if q is not None:
+        hq, rq = _rows(o.q, q, n, pages, "q"), o.rq
+        to = _dense(q_out, (n, hq, pages.d), pages.dtype, "q_out", pages.index)
+    rc = (_lib or load()).arkv_paged_append(pages.ref, batch.ref, rotary.ref, hq, rq, o.rk, o.rv,
+                                            _dense(positions, (rotary.n_axes, n), torch.int32, "positions", pages.index), to, stream)
+    _check(rc, "arkv_paged_append")
 
 
-def _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix):
-    torch, s = _TORCH, _own.s
+def _scores(o, pages, batch, hq, scale, cap, slopes, q_pos, prefix):
+    if slopes is None and prefix is None:
+        o.plain.scale, o.plain.cap = scale, cap
+        return o.rplain
+    torch, s = _TORCH, o.s
     s.scale, s.cap, s.slopes, s.q_pos, s.prefix = scale, cap, None, None, None
     if slopes is not None:
         if q_pos is None:
@@ -227,47 +241,50 @@ def _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix):
         s.q_pos = _dense(q_pos, (batch.n_tokens,), torch.int32, "q_pos", pages.index)
     if prefix is not None:
         s.prefix = _dense(prefix, (batch.B,), torch.int32, "prefix", pages.index)
-    return _own.rs
+    return o.rs
 
 
 def arkv_paged_attention(pages, batch, q, scale, out, lse=None, cap=0.0, slopes=None, q_pos=None, prefix=None, workspace=None):
     """q [n][H_q][d] (strided), out [n][H_q][d], lse fp32 [n][H_q] or None; the other arguments as arkv_scores."""
     torch = _TORCH or _torch()
-    _current(pages, batch)
-    n, o = batch.n_tokens, _own
+    stream = _current(pages, batch)
+    n, o, at = batch.n_tokens, _own.set, pages.index
     hq = _rows(o.q, q, n, pages, "q")
     ws, size = _workspace(workspace, pages)
-    _call("arkv_paged_attention", pages.ref, batch.ref, _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix), hq, o.rq,
-          _dense(out, (n, hq, pages.d), pages.dtype, "out", pages.index),
-          None if lse is None else _dense(lse, (n, hq), torch.float32, "lse", pages.index), ws, size, _b._stream())
+    rc = (_lib or load()).arkv_paged_attention(
+        pages.ref, batch.ref, _scores(o, pages, batch, hq, scale, cap, slopes, q_pos, prefix), hq, o.rq,
+        _dense(out, (n, hq, pages.d), pages.dtype, "out", at), None if lse is None else _dense(lse, (n, hq), torch.float32, "lse", at),
+        ws, size, stream)
+    _check(rc, "arkv_paged_attention")
 
 
 def arkv_paged_weights(pages, batch, q, scale, lse, decay=1.0, carried=None, cap=0.0, slopes=None, q_pos=None, prefix=None,
                        workspace=None):
     """Adds the tokens' probabilities to pages.weight (decay * carried + sum); carried None: pages.weight itself."""
     torch = _TORCH or _torch()
-    _current(pages, batch)
-    n, o = batch.n_tokens, _own
+    stream = _current(pages, batch)
+    n, o, at = batch.n_tokens, _own.set, pages.index
     hq = _rows(o.q, q, n, pages, "q")
     ws, size = _workspace(workspace, pages)
-    _call("arkv_paged_weights", pages.ref, batch.ref, _scores(pages, batch, hq, scale, cap, slopes, q_pos, prefix), hq, o.rq,
-          _dense(lse, (n, hq), torch.float32, "lse", pages.index), decay,
-          None if carried is None else _dense(carried, pages.k.shape[:3], torch.float32, "carried", pages.index),
-          ws, size, _b._stream())
+    rc = (_lib or load()).arkv_paged_weights(
+        pages.ref, batch.ref, _scores(o, pages, batch, hq, scale, cap, slopes, q_pos, prefix), hq, o.rq,
+        _dense(lse, (n, hq), torch.float32, "lse", at), decay, None if carried is None else _dense(carried, pages.rows, torch.float32, "carried", at),
+        ws, size, stream)
+    _check(rc, "arkv_paged_weights")
 
 
 def arkv_paged_evict(pages, batch, keep, dst_table, kept, new_len, sink=4, recent=32, workspace=None):
     """keep int32 [B], dst_table int32 [B][pages], kept int32 [B][H_kv][max_keep] (out), new_len int32 [B] (out)."""
     torch = _TORCH or _torch()
-    _current(pages, batch)
-    B = batch.B
+    stream = _current(pages, batch)
+    B, at, i32 = batch.B, pages.index, torch.int32
     _need(dst_table.dim() == 2 and kept.dim() == 3, "dst_table: [B][pages]; kept: [B][H_kv][max_keep]")
-    width, max_keep = dst_table.shape[1], kept.shape[2]
+    width, max_keep = dst_table.size(1), kept.size(2)
     ws, size = _workspace(workspace, pages)
-    _call("arkv_paged_evict", pages.ref, batch.ref, _dense(keep, (B,), torch.int32, "keep", pages.index), max_keep, sink, recent,
-          _dense(dst_table, (B, width), torch.int32, "dst_table", pages.index), width,
-          _dense(kept, (B, pages.H, max_keep), torch.int32, "kept", pages.index),
-          _dense(new_len, (B,), torch.int32, "new_len", pages.index), ws, size, _b._stream())
+    rc = (_lib or load()).arkv_paged_evict(
+        pages.ref, batch.ref, _dense(keep, (B,), i32, "keep", at), max_keep, sink, recent, _dense(dst_table, (B, width), i32, "dst_table", at), width,
+        _dense(kept, (B, pages.H, max_keep), i32, "kept", at), _dense(new_len, (B,), i32, "new_len", at), ws, size, stream)
+    _check(rc, "arkv_paged_evict")
 
 
 def arkv_debug_paged_row(table_row, n_pages, page_size, n_kv_heads, kv_head, length, slot):
@@ -275,6 +292,6 @@ def arkv_debug_paged_row(table_row, n_pages, page_size, n_kv_heads, kv_head, len
     import numpy as np
     t = np.ascontiguousarray(table_row, dtype=np.int32)
     row = C.c_int64()
-    _call("arkv_debug_paged_row", t.ctypes.data_as(C.c_void_p), len(t), n_pages, page_size, n_kv_heads, kv_head, length, slot,
-          C.byref(row))
+    _check((_lib or load()).arkv_debug_paged_row(t.ctypes.data, len(t), n_pages, page_size, n_kv_heads, kv_head, length, slot, C.addressof(row)),
+           "arkv_debug_paged_row")
     return row.value
