@@ -16,7 +16,8 @@
  * What lies on the device cannot be checked by the host; the kernels check it.  Lengths are cut to what the caller
  * announced (n_tokens, max_q, max_kv, table_width).  A page id outside [0, n_pages) makes its slots absent: nobody sees
  * them, nothing is written there.  A new token whose slot would be negative (kv_len < q_len) has no slot and sees
- * nothing but a prefix.  Rows of the token-major arrays that belong to no sequence are left alone.
+ * nothing but a prefix.  Rows of the token-major arrays that belong to no sequence are left alone.  With n_tokens = 0 the
+ * addresses of token-major arrays may be NULL.
  */
 #ifndef ARKV_PAGED_H
 #define ARKV_PAGED_H

@@ -33,8 +33,9 @@ static int check(const arkv_pages* p, const arkv_page_batch* b, Paged& P) {
   return ARKV_OK;
 }
 
-static int check_rows(const arkv_rows* r, Rows& out) {
-  if (!r || !r->p || !aligned16(r->p) || r->token_stride < 0 || r->head_stride < 0 || r->token_stride % 8 || r->head_stride % 8)
+// (n: how many there are; arrays of none may have no address)
+static int check_rows(const arkv_rows* r, int n, Rows& out) {
+  if (!r || (!r->p && n) || !aligned16(r->p) || r->token_stride < 0 || r->head_stride < 0 || r->token_stride % 8 || r->head_stride % 8)
     return ARKV_EINVAL;
   out = {r->p, r->token_stride, r->head_stride};
   return ARKV_OK;
@@ -67,7 +68,7 @@ int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, con
                       void* hip_stream) {
   AppendArgs A = {};
   TRY(check(pages, batch, A.P));
-  if (!rotary || !positions || !q != !q_out) return ARKV_EINVAL;
+  if (!rotary || (!positions && A.P.N) || (!q != !q_out && A.P.N)) return ARKV_EINVAL;
   if (rotary->rot_dim < 0 || rotary->rot_dim % 16 || rotary->rot_dim > pages->head_dim || rotary->n_axes < 1 || rotary->n_axes > 4 ||
       (rotary->adjacent != 0 && rotary->adjacent != 1) || (rotary->rot_dim && !rotary->freq))
     return ARKV_EINVAL;
@@ -75,11 +76,11 @@ int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, con
     if (rotary->axis[i] >= rotary->n_axes) return ARKV_EINVAL;
     A.axis[i] = rotary->axis[i];
   }
-  TRY(check_rows(k, A.k));
-  TRY(check_rows(v, A.v));
+  TRY(check_rows(k, A.P.N, A.k));
+  TRY(check_rows(v, A.P.N, A.v));
   if (q) {
     if (n_q_heads < 1 || !aligned16(q_out)) return ARKV_EINVAL;
-    TRY(check_rows(q, A.q));
+    TRY(check_rows(q, A.P.N, A.q));
     if (n_q_heads > 65535) return ARKV_EUNSUPPORTED;
     A.Hq = n_q_heads;
   }
@@ -105,7 +106,7 @@ static int attn_args(const arkv_pages* pages, const arkv_page_batch* batch, cons
   TRY(check(pages, batch, A.P));
   TRY(check_heads(n_q_heads, A.P.H, A.P.N, A.G));
   TRY(check_scores(scores, A.S));
-  TRY(check_rows(q, A.q));
+  TRY(check_rows(q, A.P.N, A.q));
   A.Hq = n_q_heads;
   const size_t need = workspace_bytes(A.P, pages->head_dim, n_q_heads);
   if (need && (!workspace || !aligned16(workspace) || bytes < need)) return ARKV_EINVAL;
@@ -118,7 +119,7 @@ int arkv_paged_attention(const arkv_pages* pages, const arkv_page_batch* batch, 
                          void* hip_stream) {
   PagedAttnArgs A = {};
   TRY(attn_args(pages, batch, scores, n_q_heads, q, workspace, bytes, A));
-  if (!out || !aligned16(out)) return ARKV_EINVAL;
+  if ((!out && A.P.N) || !aligned16(out)) return ARKV_EINVAL;
   A.out = out; A.lse = lse;
   if (!A.P.N || !A.P.max_q) return ARKV_OK;
   LAUNCH(launch_paged_attention(pages->dtype, pages->head_dim, A, (hipStream_t)hip_stream));
@@ -129,7 +130,7 @@ int arkv_paged_weights(const arkv_pages* pages, const arkv_page_batch* batch, co
                        void* workspace, size_t bytes, void* hip_stream) {
   PagedAttnArgs A = {};
   TRY(attn_args(pages, batch, scores, n_q_heads, q, workspace, bytes, A));
-  if (!lse || !pages->weight || !isfinite(decay)) return ARKV_EINVAL;
+  if ((!lse && A.P.N) || !pages->weight || !isfinite(decay)) return ARKV_EINVAL;
   A.lse = const_cast<float*>(lse); A.decay = decay; A.carried = carried ? carried : pages->weight;
   if (!A.P.max_kv) return ARKV_OK;
   LAUNCH(launch_paged_weights(pages->dtype, pages->head_dim, A, (hipStream_t)hip_stream));

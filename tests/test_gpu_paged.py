@@ -270,6 +270,20 @@ def test_sequences_shorter_than_announced(lens):
     R.close(s.weight, ref, tol, "weight")
 
 
+def test_a_batch_without_new_tokens():
+    s = R.problem("cuda", BF, 8, 2, 64, 16, (0, 0), (40, 0), seed=34)
+    pages, batch, ws = handles(s)
+    before = {n: getattr(s, n).clone() for n in ("k", "v", "pos")}
+    new, lse = torch.empty(0, 2, 64, dtype=BF, device="cuda"), torch.empty(0, 8, device="cuda")
+    P.arkv_paged_append(pages, batch, P.arkv_rotary(None), s.q, new, new, torch.empty(1, 0, dtype=torch.int32, device="cuda"), torch.empty_like(s.q))
+    P.arkv_paged_attention(pages, batch, s.q, s.scale, torch.empty_like(s.q), lse=lse, workspace=ws)
+    ref, tol = R.weights(s, lse, 0.5, s.weight)
+    P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=0.5, workspace=ws)
+    R.close(s.weight, ref, tol, "weight")
+    for name, old in before.items():
+        assert torch.equal(getattr(s, name).view(torch.uint8), old.view(torch.uint8)), name
+
+
 def test_weights_of_a_step_sum_to_the_tokens_and_heads():
     s = R.problem("cuda", BF, 8, 2, 128, 16, (50, 1), (333, 1000), seed=31)
     _, lse = attend(s)

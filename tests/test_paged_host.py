@@ -180,6 +180,18 @@ def test_workspaces_that_are_too_small_are_refused():
             assert _call(name, pages, batch, rows, rot, sc, ws=ADDR + 4) == A.EINVAL
 
 
+def test_a_batch_without_new_tokens():
+    """Token-major arrays of no rows have no address: that is no error."""
+    pages, batch, rows, rot, sc = _args()
+    rows.p = None
+    assert _call("append", pages, batch, rows, rot, sc) == A.EINVAL and _call("attention", pages, batch, rows, rot, sc) == A.EINVAL
+    batch.n_tokens = batch.max_q = 0
+    assert _call("append", pages, batch, rows, rot, sc, positions=None, out=None) == A.OK
+    assert _call("attention", pages, batch, rows, rot, sc, out=None) == A.OK
+    rows.token_stride = 4
+    assert _call("append", pages, batch, rows, rot, sc) == A.EINVAL and _call("attention", pages, batch, rows, rot, sc) == A.EINVAL
+
+
 def test_evictions_that_need_a_workspace():
     a = _args()
     a[1].table_width, a[1].max_kv = 4096, 36864
