@@ -4,7 +4,8 @@
 // r % G, so the heads of a group share every key and value that is fetched.  Two kernels divide the sequences between them:
 //   k_paged_step   up to 16 rows (a generated token, a few drafted ones): bound by reading the pages
 //   k_paged_chunk  more rows: bound by the matrix cores
-// Both split a sequence's keys over workgroups where that fills the chip; k_paged_merge joins the pieces.
+// Both split a sequence's keys over workgroups where that fills the chip.  The last workgroup to finish joins up to 16 pieces, a
+// launch of k_paged_merge more than that.
 //
 // In both, keys are on the M side of the logits MFMA (S^T = K Q^T), which leaves one row per lane, and the lane's
 // probabilities are, as they lie, the B operand of O^T = V^T P^T once the contraction index is read in their order; the
@@ -24,9 +25,11 @@ constexpr int kStepMaxPiece = 2048;     // (at most 4096: a lane holds the page 
 constexpr int kChunkRows = 128, kChunkKeys = 64;
 
 // How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
-// joined: the step kernel's last workgroup of a (sequence, kv-head) joins its pieces, no launch is needed for that.
-struct Cut { int step_piece, n_step, chunk_piece, n_chunk; bool joined; Which w; };
+// blocks: of kChunkRows rows, of all sequences, at most.  joined: the last workgroup of a (sequence, kv-head), chunk_joined: of a block
+// and kv-head joins its pieces (tickets from chunk_ticket0 on), no launch is needed for that.
+struct Cut { int step_piece, n_step, chunk_piece, n_chunk, blocks, chunk_ticket0; bool joined, chunk_joined; Which w; };
 constexpr int kJoinPieces = 16;         // at most: a lane has all pieces' loads under way at once
+constexpr int kJoinBlocks = 2048;       // pieces of blocks that are joined in the launch, at most (they take 67 KB of workspace each)
 
 static Cut cut_of(const Paged& P, int D, int Hq) {
   Cut c = {};
@@ -45,21 +48,34 @@ static Cut cut_of(const Paged& P, int D, int Hq) {
   // 4096; four of 131071 rows: 362 and 354).  Fewer than 16 heads do not fill the chip in 16 pieces.
   const long long units = (long long)P.B * P.H;
   pieces(units, std::min(256ll, kJoinPieces * units), 128, units < 16 ? kStepMaxPiece / 2 : kStepMaxPiece, 128, c.step_piece, c.n_step);
-  // One workgroup for every place on the chip, at d = 64 three to a CU (1686 tokens on up to 3001 rows, 12 heads: 46 us in pieces of
-  // 1024 keys, 42 of 512; d = 128, 512 tokens on 4100 rows, 16 heads: 55 us in pieces of 1024, 58 of 512).
-  const long long blocks = ((long long)P.N * G + kChunkRows - 1) / kChunkRows * P.H;
+  // One workgroup for each CU; then for every place on the chip, at d = 64 three to a CU, in larger pieces (1686 tokens on up to 3001
+  // rows, 12 heads: 46 us in pieces of 1024 keys, 42 of 512; d = 128, 512 tokens on 4100 rows, 16 heads, 7 single tokens: 66 us in pieces of
+  // 1024, 70 of 768, 82 of 512; 128 tokens on 1024 rows: 28 us in one piece, 22 in
+  // pieces of 256).
+  const long long rows = (long long)P.N * G, blocks = (rows + kChunkRows - 1) / kChunkRows * P.H;
+  int alone, n_alone;
+  pieces(blocks, 256, 256, 1 << 28, kChunkKeys, alone, n_alone);
   pieces(blocks, D == 64 ? 768 : 512, D == 64 ? 512 : 1024, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
-  c.joined = c.n_step <= kJoinPieces && (long long)P.B * P.H <= kJoinUnits;
+  if (alone < c.chunk_piece) { c.chunk_piece = alone; c.n_chunk = n_alone; }
+  c.joined = c.n_step <= kJoinPieces && units <= kJoinUnits;
+  // (a sequence that is the chunk kernel's has more rows than the step kernel takes)
+  c.blocks = (int)(rows / kChunkRows + std::min<long long>(P.B, c.w.step ? rows / (kStepRows + 1) : P.B));
+  c.chunk_ticket0 = c.w.step && c.joined ? (int)units : 0;
+  // (512 tokens on 4100 rows, 16 heads, beside 7 single tokens: 60 us, with a launch that joins 70)
+  c.chunk_joined = c.n_chunk <= kJoinPieces && (long long)c.blocks * P.H + c.chunk_ticket0 <= kJoinUnits &&
+                   (long long)c.blocks * P.H * c.n_chunk <= kJoinBlocks;
   return c;
 }
 
 // Pieces' results: sums [row][D] and (reference, denominator) [row].  Rows of k_paged_step: ((unit * n_step + piece) * 16 +
-// row), behind them rows of k_paged_chunk: (piece * N + token) * Hq + head.
+// row), behind them rows of k_paged_chunk: (piece * N + token) * Hq + head, or, where its workgroups join them, kChunkRows rows of
+// ((block * H + head) * n_chunk + piece), each wave's as they lie in its lanes.
 struct Parts { float* acc; float2* ml; int* tickets; size_t chunk0; };
 
 static size_t part_rows(const Paged& P, int Hq, const Cut& c, size_t& chunk0) {
   chunk0 = c.w.step && c.n_step > 1 ? (size_t)P.B * P.H * c.n_step * kStepRows : 0;
-  return chunk0 + (c.w.chunk && c.n_chunk > 1 ? (size_t)c.n_chunk * P.N * Hq : 0);
+  if (!c.w.chunk || c.n_chunk == 1) return chunk0;
+  return chunk0 + (c.chunk_joined ? (size_t)c.blocks * P.H * c.n_chunk * kChunkRows : (size_t)c.n_chunk * P.N * Hq);
 }
 
 size_t paged_attention_floats(const Paged& P, int D, int Hq) {
@@ -380,9 +396,10 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
 __host__ __device__ __forceinline__ int chunk_blocks(int nq, int G, int few) { return nq * G <= few ? 0 : (nq * G + kChunkRows - 1) / kChunkRows; }
 
 // Sequence and block of the rank-th block of a launch; the lanes of a wave look at 64 sequences at a time.
-__device__ __forceinline__ bool find_block(const Paged& P, int G, int few, int rank, int lane, int& b, int& blk) {
+__device__ __forceinline__ bool find_block(const Paged& P, int G, int few, int rank, int lane, int& b, int& blk, Seq& s) {
   for (int i = 0; i < P.B; i += 64) {
-    const int mine = i + lane < P.B ? chunk_blocks(seq_of(P, i + lane).nq, G, few) : 0;
+    const Seq own = seq_of(P, min(i + lane, P.B - 1));
+    const int mine = i + lane < P.B ? chunk_blocks(own.nq, G, few) : 0;
     int sum = mine;                                                // blocks up to and with this lane's sequence
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -395,6 +412,7 @@ __device__ __forceinline__ bool find_block(const Paged& P, int G, int few, int r
       b = i + first;
       const int n = __builtin_amdgcn_readlane(mine, first);
       blk = n - 1 - (rank - (__builtin_amdgcn_readlane(sum, first) - n));   // the block that sees most comes first
+      s = {__builtin_amdgcn_readlane(own.q0, first), __builtin_amdgcn_readlane(own.nq, first), __builtin_amdgcn_readlane(own.kv, first)};
       return true;
     }
     rank -= __builtin_amdgcn_readlane(sum, 63);
@@ -412,21 +430,22 @@ template <int D> struct ChunkLds {
   uint16_t v[2][kChunkKeys * D];
   int pos[2][kChunkKeys];
   uint32_t odd[2];
+  int last;                               // whether this workgroup's piece was the last one to be finished
 };
 template <int D> __device__ __forceinline__ int v_chunk(int row, int c) { return D == 128 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; }
 
 template <typename T, int D, int MODE>
-__device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, ChunkLds<D>& sm, int id, int n_blocks) {
+__device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, ChunkLds<D>& sm, int id) {
   constexpr bool CAP = Mode<MODE>::cap, DIST = Mode<MODE>::dist;
   const int piece_keys = cut.chunk_piece;
   constexpr int KK = D / 16, CB = D / 32, CPR = D / 8, RPI = 64 / CPR, LPG = 16 / RPI;   // LPG: 1 KB loads of a granule
   const Paged& P = A.P;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, hh = lane >> 5;
-  const int h = id % P.H, piece = id / (n_blocks * P.H);
+  const int h = id % P.H, piece = id / (cut.blocks * P.H), bh = id % (cut.blocks * P.H);
   int b, blk;
-  if (!find_block(P, A.G, cut.w.few, id / P.H % n_blocks, lane, b, blk)) return;
-  const Seq s = seq_of(P, b);
+  Seq s;
+  if (!find_block(P, A.G, cut.w.few, bh / P.H, lane, b, blk, s)) return;
   const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
   const int R = s.nq * A.G, r0 = blk * kChunkRows;
   const int end = row_end(s, min(R - 1, r0 + kChunkRows - 1) / A.G, prefix);
@@ -650,9 +669,9 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
   }
   l += __shfl_xor(l, 32);
   if (l == 0.f) m = kUnset;
-  if (r >= R) return;
   const size_t orow = (size_t)tok * A.Hq + hq;
-  if (np > 1) {
+  if (np > 1 && !cut.chunk_joined) {
+    if (r >= R) return;
     const size_t pr = parts.chunk0 + (size_t)piece * P.N * A.Hq + orow;
 #pragma unroll
     for (int c = 0; c < CB; ++c)
@@ -661,28 +680,75 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
         *reinterpret_cast<f32x4g*>(parts.acc + pr * D + 32 * c + 8 * e + 4 * hh) =
             f32x4g{acc[c][4 * e], acc[c][4 * e + 1], acc[c][4 * e + 2], acc[c][4 * e + 3]};
     if (hh == 0) parts.ml[pr] = make_float2(m, l);
-  } else {
-    const float inv = l == 0.f ? 0.f : 1.f / l;                    // (NaN stays)
+    return;
+  }
+  if (np > 1) {
+    // 8 bytes per lane, adjacent lanes adjacent: where wave w's two channels i, i + 1 of block c lie in a piece's rows
+    const size_t row0 = parts.chunk0 + (size_t)bh * cut.n_chunk * kChunkRows + 32 * wave;
+    const uint32_t at = 8 * (uint32_t)lane;                        // (beside a uniform address: 64 bits a lane would not fit the registers)
+    auto sums = [&](int p, int c, int i) {
+      return reinterpret_cast<float2*>(reinterpret_cast<char*>(parts.acc + (row0 + (size_t)p * kChunkRows) * D) + (8 * c + i / 2) * 512 + at);
+    };
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        store4((T*)A.out + orow * D + 32 * c + 8 * e + 4 * hh, acc[c][4 * e] * inv, acc[c][4 * e + 1] * inv, acc[c][4 * e + 2] * inv,
-               acc[c][4 * e + 3] * inv);
-    if (hh == 0 && A.lse) A.lse[orow] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+      for (int i = 0; i < 16; i += 2) put2(sums(piece, c, i), acc[c][i], acc[c][i + 1]);
+    if (hh == 0) put2(parts.ml + row0 + (size_t)piece * kChunkRows + n, m, l);
+    vm_wait();                                                     // this wave's stores are where everyone sees them
+    __syncthreads();
+    int* ticket = parts.tickets + (cut.chunk_ticket0 + bh) * kTicketWords;
+    if (tid == 0) {
+      sm.last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == np - 1;
+      if (sm.last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call wants it
+    }
+    __syncthreads();
+    if (!sm.last) return;
+    m = kUnset;
+    l = 0.f;
+    for (int p = 0; p < np; ++p) m = fmaxf(m, take2(parts.ml + row0 + (size_t)p * kChunkRows + n).x);
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
+    for (int p = 0; p < np; ++p) {                                 // (always in this order, whoever is last)
+      const float2 z = take2(parts.ml + row0 + (size_t)p * kChunkRows + n);
+      float2 x[CB * 8];
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) x[8 * c + i / 2] = take2(sums(p, c, i));
+      const float f = exp2_hw(z.x - m);
+      l += f * z.y;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          acc[c][i] += f * x[8 * c + i / 2].x;
+          acc[c][i + 1] += f * x[8 * c + i / 2].y;
+        }
+    }
   }
+  if (r >= R) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;                      // (NaN stays)
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      store4((T*)A.out + orow * D + 32 * c + 8 * e + 4 * hh, acc[c][4 * e] * inv, acc[c][4 * e + 1] * inv, acc[c][4 * e + 2] * inv,
+             acc[c][4 * e + 3] * inv);
+  if (hh == 0 && A.lse) A.lse[orow] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
 }
 
-// A launch: chunk_wgs workgroups for sequences of many rows (n_blocks blocks of each kv-head, piece by piece), behind them those for
+// A launch: chunk_wgs workgroups for sequences of many rows (cut.blocks blocks of each kv-head, piece by piece), behind them those for
 // few (unit by unit, piece by piece).  One launch for both: a prompt's chunk and the other requests' tokens share the chip.
 // KIND: bit 0: there are the former, bit 1: the latter.
 template <typename T, int D, int MODE, int KIND>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_paged_attn(PagedAttnArgs A, Cut cut, Parts parts, int chunk_wgs, int n_blocks) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_paged_attn(PagedAttnArgs A, Cut cut, Parts parts, int chunk_wgs) {
   constexpr size_t kMost = sizeof(ChunkLds<D>) > sizeof(StepLds<D>) ? sizeof(ChunkLds<D>) : sizeof(StepLds<D>);
   __shared__ __align__(16) char lds[KIND == 1 ? sizeof(ChunkLds<D>) : KIND == 2 ? sizeof(StepLds<D>) : kMost];
   const int id = (int)blockIdx.x;
   if ((KIND & 1) && (KIND == 1 || id < chunk_wgs)) {
-    if constexpr (KIND & 1) paged_chunk<T, D, MODE>(A, cut, parts, *reinterpret_cast<ChunkLds<D>*>(lds), id, n_blocks);
+    if constexpr (KIND & 1) paged_chunk<T, D, MODE>(A, cut, parts, *reinterpret_cast<ChunkLds<D>*>(lds), id);
   } else {
     if constexpr (KIND & 2) paged_step<T, D, MODE>(A, cut, parts, *reinterpret_cast<StepLds<D>*>(lds), id - chunk_wgs);
   }
@@ -722,7 +788,7 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs A, Cut cut, P
   const int last = step ? s.nq - 1 : min(R - 1, r / kChunkRows * kChunkRows + kChunkRows - 1) / A.G;
   const int piece = step ? cut.step_piece : cut.chunk_piece;
   int np = (row_end(s, last, prefix) + piece - 1) / piece;
-  if (want >= rows || b >= P.B || i < 0 || i >= s.nq || np <= 1 || (step && cut.joined)) np = 0;
+  if (want >= rows || b >= P.B || i < 0 || i >= s.nq || np <= 1 || (step ? cut.joined : cut.chunk_joined)) np = 0;
   if (MANY && np == 0) return;
   const size_t first = step ? (size_t)(b * P.H + hq / A.G) * cut.n_step * kStepRows + r : parts.chunk0 + (size_t)t * A.Hq + hq;
   const size_t stride = step ? kStepRows : (size_t)P.N * A.Hq;
@@ -772,15 +838,14 @@ static hipError_t launch_attention(const PagedAttnArgs& A, hipStream_t st) {
   parts.tickets = (int*)A.ws;
   parts.acc = A.ws + kTicketFloats;
   parts.ml = (float2*)(parts.acc + n * D);
-  const int blocks = (int)((long long)P.N * A.G / kChunkRows + P.B);       // blocks of all sequences, at most
-  const int chunk = c.w.chunk ? blocks * P.H * c.n_chunk : 0, step = c.w.step ? P.B * P.H * c.n_step : 0;
-  if (chunk && step) k_paged_attn<T, D, MODE, 3><<<chunk + step, 256, 0, st>>>(A, c, parts, chunk, blocks);
-  else if (chunk) k_paged_attn<T, D, MODE, 1><<<chunk, 256, 0, st>>>(A, c, parts, chunk, blocks);
-  else k_paged_attn<T, D, MODE, 2><<<step, 256, 0, st>>>(A, c, parts, 0, blocks);
-  if ((chunk && c.n_chunk > 1) || (step && c.n_step > 1 && !c.joined)) {
+  const int chunk = c.w.chunk ? c.blocks * P.H * c.n_chunk : 0, step = c.w.step ? P.B * P.H * c.n_step : 0;
+  if (chunk && step) k_paged_attn<T, D, MODE, 3><<<chunk + step, 256, 0, st>>>(A, c, parts, chunk);
+  else if (chunk) k_paged_attn<T, D, MODE, 1><<<chunk, 256, 0, st>>>(A, c, parts, chunk);
+  else k_paged_attn<T, D, MODE, 2><<<step, 256, 0, st>>>(A, c, parts, 0);
+  if ((chunk && c.n_chunk > 1 && !c.chunk_joined) || (step && c.n_step > 1 && !c.joined)) {
     const int rows = P.N * A.Hq;
     // with few pieces a row is little work, and eight fit a workgroup
-    if ((c.w.chunk ? c.n_chunk : c.n_step) >= 8) k_paged_merge<T, D, true><<<rows, 256, 0, st>>>(A, c, parts);
+    if ((chunk && !c.chunk_joined ? c.n_chunk : c.n_step) >= 8) k_paged_merge<T, D, true><<<rows, 256, 0, st>>>(A, c, parts);
     else k_paged_merge<T, D, false><<<(rows + 7) / 8, 256, 0, st>>>(A, c, parts);
   }
   return hipGetLastError();

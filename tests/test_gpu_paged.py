@@ -175,6 +175,22 @@ def test_pieces_are_joined(lens, dtype, hq, hkv, d):
         assert torch.equal(out, o2) and torch.equal(lse, l2)
 
 
+@pytest.mark.parametrize("q,kv", [((17,), (600,)), ((128,), (1025,)), ((200, 1, 0, 130), (2000, 3000, 0, 257)), ((300,) * 3, (300, 2600, 900)),
+                                  ((20,), (9001,)), ((33, 1), (70001, 40000)), ((1, 1, 19), (5000, 16, 4500))])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(BF, 8, 2, 128), (FP, 12, 4, 64), (BF, 1, 1, 128)])
+def test_pieces_of_chunks_are_joined(q, kv, dtype, hq, hkv, d):
+    """Blocks of rows whose keys are a few workgroups' (the last one joins them) or many; the same workspace again and again."""
+    s = R.problem("cuda", dtype, hq, hkv, d, 16, q, kv, seed=16)
+    out, lse = check_attention(s)
+    pages, batch, ws = handles(s)
+    for i in range(4):
+        ws[TICKETS:].fill_(0xFF)
+        o2, l2 = torch.empty_like(out), torch.empty_like(lse)
+        P.arkv_paged_attention(pages, batch, s.q, s.scale, o2, lse=l2, workspace=ws)
+        assert torch.equal(out, o2) and torch.equal(lse, l2)
+        assert not ws[:TICKETS].any()
+
+
 def test_one_workspace_for_batches_of_any_shape():
     big = R.problem("cuda", BF, 8, 8, 128, 16, (1,) * 20, (3000,) * 20, seed=14)
     small = R.problem("cuda", BF, 8, 2, 128, 16, (100, 1), (5000, 2100), seed=15)
