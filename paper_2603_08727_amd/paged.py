@@ -12,6 +12,8 @@ import threading
 from . import binding as _b
 from .binding import ArkvError, EINVAL, EUNSUPPORTED, EHIP, OK  # noqa: F401
 
+TICKET_BYTES = 1 << 16                             # of a workspace's front, zero between calls
+
 EXPORTED = ["arkv_paged_append", "arkv_paged_workspace", "arkv_paged_attention", "arkv_paged_weights", "arkv_paged_evict",
             "arkv_debug_paged_row"]
 
@@ -203,9 +205,11 @@ def arkv_paged_workspace_bytes(pages, batch, n_q_heads):
 
 
 def arkv_paged_workspace(pages, batch, n_q_heads):
-    """A workspace tensor for the calls below (zeros, as its first use wants it; one for the largest batch serves all)."""
+    """A workspace tensor for the calls below, its front zeroed as its first use wants it; one for the largest batch serves all."""
     torch = _TORCH or _torch()
-    return torch.zeros(arkv_paged_workspace_bytes(pages, batch, n_q_heads), dtype=torch.uint8, device=pages.device)
+    ws = torch.empty(arkv_paged_workspace_bytes(pages, batch, n_q_heads), dtype=torch.uint8, device=pages.device)
+    ws[:TICKET_BYTES].zero_()
+    return ws
 
 
 def arkv_paged_append(pages, batch, rotary, q, k, v, positions, q_out):
