@@ -165,7 +165,7 @@ constexpr int kEvictRows = 4 * kEvictThreads;   // slots that a workgroup looks 
 constexpr int kEvictRegs = 9;           // times that many slots whose keys a lane keeps in registers
 constexpr int kEvictSlots = 256;        // slots per workgroup of k_evict_move: those of one wave, kEvictRows at a time
 // Survivors times channels up to which the choosing workgroup copies them, which saves a launch and the workspace (8 x 2 heads,
-// 250 of 1000 rows of 64 channels: 9.6 us against 9.9; 512: 10.8 and 11.1; 8 x 8 heads, 250 of 2000 rows of 128: 12.5 and 13.4).
+// 250 of 1000 rows of 64 channels: 9.0 us against 9.9; 512: 10.8 and 11.1; 8 x 8 heads, 250 of 2000 rows of 128: 12.5 and 13.4).
 constexpr int kSelectMoves = 32768;
 
 // Order of weights as an order of words: NaN (and a row that is not there) lowest, -0 with +0; 0 is no weight's.
@@ -243,36 +243,37 @@ __device__ __forceinline__ void count_bins(int* hist, const bool (&on)[4], const
   if (lane == first) atomicAdd(&hist[shared], n);
 }
 
-// Copies survivors i = first, first + step, .. < n, which are at slots list[i], to slots to0 + i: D / 8 lanes a row, kMoveRows
-// rows per lane whose loads are all under way together.
-constexpr int kMoveRows = 4;
-template <int D>
+// Copies survivors i = first, first + step, .. < n, which are at slots list[i], to slots to0 + i: D / 8 lanes a row, N rows
+// per lane whose loads are all under way together (k_evict_move: 4; of the few rows that k_evict_select copies 2: 8 x 2 heads x 250 rows
+// 9.0 us, with 4 9.7).  The stores pass the caches by: with ordinary ones, 32 units x 8192 rows took 90 instead of 86 us.
+constexpr int kMoveRows = 4, kSelectRows = 2;
+template <int D, int N>
 __device__ __forceinline__ void move_rows(const EvictArgs& A, const Kept& K, int h, int b, const int* list, int n, int to0, int first, int step) {
   constexpr int LPR = D / 8;
   const int c = threadIdx.x % LPR;
   const Paged& P = A.P;
-  int from[kMoveRows], to[kMoveRows];
+  int from[N], to[N];
 #pragma unroll
-  for (int r = 0; r < kMoveRows; ++r) {
+  for (int r = 0; r < N; ++r) {
     const int i = first + r * step;
     from[r] = i < n ? slot_row(P.table + (size_t)b * P.width, P.n_pages, P.H, h, P.lg_page, K.n, list[i]) : -1;
     to[r] = i < n ? slot_row(A.dst_table + (size_t)b * A.dst_width, P.n_pages, P.H, h, P.lg_page, K.m, to0 + i) : -1;
   }
   // (lanes 0 and 1 of a row take its position and weight)
   uint32_t* meta = c == 0 ? (uint32_t*)P.pos : (uint32_t*)P.weight;
-  u32x4p x[kMoveRows], y[kMoveRows];
-  uint32_t z[kMoveRows];
+  u32x4p x[N], y[N];
+  uint32_t z[N];
 #pragma unroll
-  for (int r = 0; r < kMoveRows; ++r) {
+  for (int r = 0; r < N; ++r) {
     z[r] = c < 2 ? meta[max(from[r], 0)] : 0;
     x[r] = ((const u32x4p*)P.k)[(size_t)max(from[r], 0) * LPR + c];
     y[r] = ((const u32x4p*)P.v)[(size_t)max(from[r], 0) * LPR + c];
   }
 #pragma unroll
-  for (int r = 0; r < kMoveRows; ++r) {
+  for (int r = 0; r < N; ++r) {
     if (from[r] < 0 || to[r] < 0) continue;
-    ((u32x4p*)P.k)[(size_t)to[r] * LPR + c] = x[r];
-    ((u32x4p*)P.v)[(size_t)to[r] * LPR + c] = y[r];
+    __builtin_nontemporal_store(x[r], (u32x4p*)P.k + (size_t)to[r] * LPR + c);
+    __builtin_nontemporal_store(y[r], (u32x4p*)P.v + (size_t)to[r] * LPR + c);
     if (c < 2) meta[to[r]] = z[r];
   }
 }
@@ -517,12 +518,12 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A, Evi
     __syncthreads();
     constexpr int RPW = kEvictThreads / (MOVE / 8);
     for (int i = tid; i < K.m; i += kEvictThreads) kept[i] = list[i];
-    for (int i = 0; i < K.m; i += RPW * kMoveRows) move_rows<MOVE>(A, K, h, b, list, K.m, 0, i + tid / (MOVE / 8), RPW);
+    for (int i = 0; i < K.m; i += RPW * kSelectRows) move_rows<MOVE, kSelectRows>(A, K, h, b, list, K.m, 0, i + tid / (MOVE / 8), RPW);
   }
 }
 
 // Lists the survivors among 256 slots, a slot per lane, and copies them: the units' slots are spread over the whole chip (8192 of 32768
-// rows of 32 units, 272 MB: 55 us where the rows are in the last cache, 59-66 from memory).
+// rows of 32 units, 272 MB: 62 us, 4.4 TB/s).
 template <int D>
 __global__ __launch_bounds__(kEvictSlots) void k_evict_move(EvictArgs A, EvictCut cut, EvictParts parts) {
   constexpr int NW = kEvictSlots / 64, RPW = kEvictSlots / (D / 8);
@@ -561,7 +562,7 @@ __global__ __launch_bounds__(kEvictSlots) void k_evict_move(EvictArgs A, EvictCu
   const int n = min(n_sure + min(n_ties, need) - taken, K.m - to0);
   int32_t* kept = A.kept + (size_t)unit * A.max_keep + to0;
   for (int i = tid; i < n; i += kEvictSlots) kept[i] = list[i];
-  for (int i = 0; i < n; i += RPW * kMoveRows) move_rows<D>(A, K, h, b, list, n, to0, i + tid / (D / 8), RPW);
+  for (int i = 0; i < n; i += RPW * kMoveRows) move_rows<D, kMoveRows>(A, K, h, b, list, n, to0, i + tid / (D / 8), RPW);
 }
 
 template <int D>
