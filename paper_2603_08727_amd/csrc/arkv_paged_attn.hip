@@ -589,14 +589,13 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
         }
       }
     if (masked) {
-      stay_here();
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
+      for (int g = 0; g < 4; ++g) {                                // granules
+        const int left = opaque(ok >> g & 1 ? my_end - j0 - 16 * g - 4 * hh : 0);   // (what depends on it stays in this branch)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = 32 * g + 8 * (i >> 2) + 4 * hh + (i & 3);
-          if (!(j0 + j < my_end && (ok >> (j >> 4) & 1))) x[g][i] = -INFINITY;
-        }
+        for (int i = 0; i < 8; ++i)
+          if (8 * (i >> 2) + (i & 3) >= left) x[g >> 1][8 * (g & 1) + i] = -INFINITY;
+      }
     }
     u32x4g pb[4];                                                  // probabilities of keys 16 i .. 16 i + 15, eight per lane
     auto probs = [&]() {

@@ -79,8 +79,8 @@ struct Logit {
   }
 };
 
-// Keeps a rare branch a branch: without it the compiler computes what is inside for every tile and selects.
-__device__ __forceinline__ void stay_here() { asm volatile(""); }
+// Keeps a rare branch a branch: what depends on the result is not computed in front of it (the compiler would compute a tile's masks
+// for every tile, and select).
 __device__ __forceinline__ uint32_t opaque(uint32_t x) { asm volatile("" : "+v"(x)); return x; }
 
 __device__ __forceinline__ Seq seq_of(const Paged& P, int b) {
