@@ -200,7 +200,7 @@ struct EvictParts { int* tickets; unsigned long long* hist; uint2* last; int2* b
 
 static EvictCut evict_cut(const Paged& P) {
   // Where there are fewer units than half the CUs, several workgroups count the first digit (32 units of 32768 rows:
-  // 6 us; by one workgroup each, 14).
+  // 3 us with reading the weights; by one workgroup each 12).
   const long long units = (long long)P.B * P.H;
   const int steps = std::max(1, (P.max_kv + kEvictRows - 1) / kEvictRows);
   EvictCut c;
