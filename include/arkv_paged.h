@@ -120,9 +120,10 @@ int arkv_paged_weights(const arkv_pages* pages, const arkv_page_batch* batch, co
  * ([B][dst_width] DEVICE int32), which must be pages that no table of the batch names: the sources stay as they are, so
  * pages that other sequences share can be evicted from.  kept DEVICE int32 [B][H_kv][max_keep]: the survivors' former
  * slots, -1 behind them.  new_len DEVICE int32 [B] = m.  keep DEVICE int32 [B], cut to [0, max_keep].  cu_q and the new tokens play no
- * part.  A row in an absent page ranks below every other and is not copied.  workspace as arkv_paged_workspace says; NULL will do
+ * part.  kept and new_len must not overlap kv_len, keep, the tables or each other (lengths are read until the end of the call: copy new_len
+ * over kv_len behind it).  A row in an absent page ranks below every other and is not copied.  workspace as arkv_paged_workspace says; NULL will do
  * where max_keep head_dim <= 32768 and max_kv <= 36864 (with one, few units of many rows are counted faster).
- * ARKV_EINVAL: as above, weight NULL, max_keep outside [1, dst_width * page_size], sink or recent negative, a workspace
+ * ARKV_EINVAL: as above, weight NULL, arrays that overlap, max_keep outside [1, dst_width * page_size], sink or recent negative, a workspace
  * that is too small, not aligned to 16 bytes, or missing. */
 int arkv_paged_evict(const arkv_pages* pages, const arkv_page_batch* batch, const int32_t* keep, int32_t max_keep,
                      int32_t sink, int32_t recent, const int32_t* dst_table, int32_t dst_width, int32_t* kept,

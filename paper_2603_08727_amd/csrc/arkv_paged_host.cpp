@@ -10,6 +10,11 @@ using namespace arkv;
 
 
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// whether n words from p and m words from q share one
+static bool overlap(const int32_t* p, size_t n, const int32_t* q, size_t m) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return a < b ? b - a < 4 * n : a - b < 4 * m;
+}
 
 static int check(const arkv_pages* p, const arkv_page_batch* b, Paged& P) {
   if (!p || !b || !p->k || !p->v || !p->pos || !b->cu_q || !b->kv_len || !b->table) return ARKV_EINVAL;
@@ -147,6 +152,12 @@ int arkv_paged_evict(const arkv_pages* pages, const arkv_page_batch* batch, cons
   if (workspace || paged_evict_needs_workspace(A.P, pages->head_dim, max_keep)) {
     if (!workspace || !aligned16(workspace) || bytes < 4 * paged_evict_floats(A.P)) return ARKV_EINVAL;
   }
+  // Workgroups read lengths and tables while others have written their results.
+  const size_t B = A.P.B, n_kept = B * A.P.H * max_keep;
+  struct { const int32_t* p; size_t n; } in[] = {{A.P.kv_len, B}, {keep, B}, {A.P.table, B * A.P.width}, {dst_table, B * dst_width}};
+  for (const auto& i : in)
+    if (overlap(kept, n_kept, i.p, i.n) || overlap(new_len, B, i.p, i.n)) return ARKV_EINVAL;
+  if (overlap(kept, n_kept, new_len, B)) return ARKV_EINVAL;
   A.ws = (float*)workspace;
   A.keep = keep; A.dst_table = dst_table; A.kept = kept; A.new_len = new_len;
   A.max_keep = max_keep; A.sink = sink; A.recent = recent; A.dst_width = dst_width;

@@ -582,3 +582,21 @@ def test_the_example_keeps_its_requests_within_their_budget():
             pos = layer.pages.pos[held, h].reshape(-1)[:layer.rows[r]]
             assert (pos[1:] > pos[:-1]).all() and int(pos[-1]) == layer.seen[r] - 1   # in order, the latest there
             assert pos[:4].tolist() == [0, 1, 2, 3]                                    # and the first four
+
+
+def test_eviction_results_beside_its_lengths():
+    """new_len and kept right behind kv_len and keep in one array: neighbours are no overlap, and the lengths stay as they are."""
+    s = R.problem("cuda", BF, 8, 4, 64, 16, (0, 0, 0), (700, 90, 333), seed=80, spare_pages=30)
+    line = torch.full((9 + 3 * 4 * 100,), 77, dtype=torch.int32, device="cuda")
+    line[:3], line[6:9] = s.kv_len, torch.tensor([100, 80, 60], dtype=torch.int32, device="cuda")
+    s.kv_len, new_len, keep, kept = line[:3], line[3:6], line[6:9], line[9:].view(3, 4, 100)
+    pages, batch, ws = handles(s)
+    dst = torch.tensor(s.spare[:21], dtype=torch.int32, device="cuda").reshape(3, 7)
+    P.arkv_paged_evict(pages, batch, keep, dst, kept, new_len, workspace=ws)
+    ref, lens = R.evict(s, [100, 80, 60], 4, 32, 100)
+    assert new_len.tolist() == lens and torch.equal(kept.cpu(), ref)
+    assert s.kv_len.tolist() == [700, 90, 333] and keep.tolist() == [100, 80, 60]
+    for bad in (dict(new_len=s.kv_len), dict(new_len=keep), dict(kept=line[:1200].view(3, 4, 100))):
+        with pytest.raises(P.ArkvError) as e:
+            P.arkv_paged_evict(pages, batch, keep, dst, bad.get("kept", kept), bad.get("new_len", new_len), workspace=ws)
+        assert e.value.code == P.EINVAL

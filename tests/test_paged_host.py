@@ -223,3 +223,17 @@ def test_the_binding_takes_gpu_tensors_of_the_right_kind():
         P.arkv_page_batch(z(3, dtype=torch.int32), z(2, dtype=torch.int32), z(2, 4, dtype=torch.int32), 4)
     with pytest.raises(ValueError):
         P.arkv_rotary(z(32, dtype=torch.float64))
+
+
+def test_evictions_into_their_own_lengths_and_tables_are_refused():
+    """Workgroups read kv_len, keep and the tables while others store kept and new_len."""
+    # B = 2, 2 heads: kv_len and keep 8 bytes each, table 32, dst_table 16, kept [2][2][32] 512, new_len 8
+    lengths, keep, table, dst, kept, new_len = 0x10000, 0x20000, 0x30000, 0x40000, 0x50000, 0x60000
+    for bad in [dict(new_len=lengths), dict(new_len=lengths + 4), dict(new_len=lengths - 4), dict(new_len=keep), dict(new_len=table + 28),
+                dict(new_len=dst + 12), dict(kept=lengths), dict(kept=lengths - 508), dict(kept=keep + 4), dict(kept=table - 508),
+                dict(kept=dst), dict(kept=new_len), dict(kept=new_len - 508), dict(new_len=kept + 508)]:
+        a = _args()
+        a[1].kv_len, a[1].table = lengths, table
+        kw = dict(keep=keep, dst=dst, kept=kept, new_len=new_len)
+        kw.update(bad)
+        assert _call("evict", *a, **kw) == A.EINVAL, bad
