@@ -91,8 +91,9 @@ int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, con
                       void* hip_stream);
 
 /* Bytes of DEVICE workspace that the calls below need for this batch and any of their options (64 KiB or more).  HOST, pure.
- * The first 64 KiB must be zero before the workspace's first use; every call leaves them zero, so one workspace serves calls on
- * batches of any shape, one after the other.  Calls that may overlap in time need workspaces of their own. */
+ * The first 64 KiB must be zero before the workspace's first use; every call leaves them zero, so one workspace serves calls one
+ * after the other.  It is large enough for every batch of the same head_dim, H_kv and H_q whose batch, n_tokens, max_q and max_kv are none of them
+ * larger than here (up to 136 MB where chunks may meet long contexts at d = 128: few rows are cut finest).  Calls that may overlap in time need workspaces of their own. */
 int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, int32_t n_q_heads, size_t* bytes);
 
 /* out [n_tokens][H_q][d] (dense, DEVICE, of the pages' dtype) = softmax over the visible slots of x, times v.  lse DEVICE float

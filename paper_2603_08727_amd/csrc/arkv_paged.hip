@@ -217,6 +217,12 @@ size_t paged_evict_floats(const Paged& P) {
   const size_t units = (size_t)P.B * P.H;
   return kTicketFloats + units * (c.chunks > 1 ? (size_t)c.chunks * kEvictBins : 0) + 2 * units + 2 * units * c.blocks;
 }
+// For every batch of no more sequences and rows than P's: fewer units are counted by more workgroups each, 256 in all at most.
+size_t paged_evict_bound(const Paged& P) {
+  const size_t units = (size_t)P.B * P.H, steps = std::max(1, (P.max_kv + kEvictRows - 1) / kEvictRows);
+  return kTicketFloats + (steps > 1 ? std::min<size_t>(256, std::min<size_t>(128, units) * steps) * kEvictBins : 0) + 2 * units +
+         2 * units * evict_cut(P).blocks;
+}
 bool paged_evict_needs_workspace(const Paged& P, int D, int max_keep) {
   return (int64_t)max_keep * D > kSelectMoves || P.max_kv > kEvictRegs * kEvictRows;
 }

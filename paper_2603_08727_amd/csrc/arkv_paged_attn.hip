@@ -80,10 +80,33 @@ static size_t part_rows(const Paged& P, int Hq, const Cut& c, size_t& chunk0) {
   return chunk0 + (c.chunk_joined ? (size_t)c.blocks * P.H * c.n_chunk * kChunkRows : (size_t)c.n_chunk * P.N * Hq);
 }
 
+// Rows of partial results that suffice for every batch of no more sequences, tokens, new tokens and rows than P's: fewer of them
+// may be cut finer, so this bounds part_rows over all such batches.  With u units and want workgroups wanted, a cut whose pieces are
+// neither the shortest nor the longest allowed has at most ceil(want / u) of them, and u times that is below want + u.
+static size_t part_rows_bound(const Paged& P, int D, int Hq) {
+  auto parts = [](long long n, long long piece) { return (n + piece - 1) / piece; };
+  const long long kv = P.max_kv, units = (long long)P.B * P.H, rows = (long long)P.N * (Hq / P.H);
+  long long n = 0;
+  if (kv > 128)
+    n = kStepRows * std::min(units * parts(kv, 128), std::max({256 + units, units * parts(kv, kStepMaxPiece), std::min(units, 15ll) * parts(kv, kStepMaxPiece / 2)}));
+  if ((long long)P.max_q * (Hq / P.H) > kStepRows && kv > 256) {
+    // blocks of rows times heads: only fewer than want are cut.  a, b: pieces of the shortest length, of the two cuts in cut_of
+    const long long want = D == 64 ? 768 : 512, a = parts(kv, 256), b = parts(kv, D == 64 ? 512 : 1024);
+    const long long h = std::min(parts(rows, kChunkRows) * P.H, want - 1);
+    const long long pieces = std::max(std::min(a * h, 255 + h), std::min(b * h, want - 1 + h));
+    // those that are joined in the launch: a sequence's last block may be short, and there are at most 128 / 17 such blocks to a full one
+    const long long most = std::max(std::min(parts(256, P.H), a), std::min(parts(want, P.H), b));
+    const long long joined = std::min<long long>(kJoinBlocks, pieces + std::min(8 * pieces, units * most));
+    n += kChunkRows * std::max(pieces, joined);
+  }
+  return (size_t)n;
+}
+
 size_t paged_attention_floats(const Paged& P, int D, int Hq) {
   size_t chunk0;
   return kTicketFloats + part_rows(P, Hq, cut_of(P, D, Hq), chunk0) * (D + 2);
 }
+size_t paged_attention_bound(const Paged& P, int D, int Hq) { return kTicketFloats + part_rows_bound(P, D, Hq) * (D + 2); }
 
 // Partial results and tickets go past the L2 of one XCD: device-scope relaxed atomics.  A workgroup waits until its stores are
 // acknowledged before it draws its ticket, and the last one reads nothing that an L2 may hold from before.

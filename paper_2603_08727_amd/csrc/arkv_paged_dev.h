@@ -68,8 +68,11 @@ struct PagedAttnArgs {
   const float* carried;
   float* ws;
 };
+// Floats of workspace: _floats: of this batch, _bound: of any that is no larger.
 size_t paged_attention_floats(const Paged& P, int D, int Hq);
+size_t paged_attention_bound(const Paged& P, int D, int Hq);
 size_t paged_weights_floats(const Paged& P, int Hq);
+size_t paged_weights_bound(const Paged& P, int Hq);
 hipError_t launch_paged_attention(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
 hipError_t launch_paged_weights(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
 
@@ -81,6 +84,7 @@ struct EvictArgs {
   float* ws;           // null: none given
 };
 size_t paged_evict_floats(const Paged& P);
+size_t paged_evict_bound(const Paged& P);
 bool paged_evict_needs_workspace(const Paged& P, int D, int max_keep);
 hipError_t launch_paged_evict(int D, const EvictArgs& A, hipStream_t st);
 

@@ -52,9 +52,13 @@ static int check_heads(int n_q_heads, int H, int n_tokens, int& G) {
   return G > 16 || (int64_t)n_q_heads * n_tokens >= (1ll << 31) ? ARKV_EUNSUPPORTED : ARKV_OK;
 }
 
-// One size for all calls, so that a workspace serves every one of them.
+// One size for all calls, so that a workspace serves every one of them: what this batch's need ...
 static size_t workspace_bytes(const Paged& P, int D, int Hq) {
   return 4 * std::max({paged_attention_floats(P, D, Hq), paged_weights_floats(P, Hq), paged_evict_floats(P)});
+}
+// ... and what no smaller batch's exceed.
+static size_t workspace_bound(const Paged& P, int D, int Hq) {
+  return std::max(workspace_bytes(P, D, Hq), 4 * std::max({paged_attention_bound(P, D, Hq), paged_weights_bound(P, Hq), paged_evict_bound(P)}));
 }
 
 static int check_scores(const arkv_scores* s, Scores& out) {
@@ -102,7 +106,7 @@ int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, 
   if (!bytes) return ARKV_EINVAL;
   TRY(check(pages, batch, P));
   TRY(check_heads(n_q_heads, P.H, P.N, G));
-  *bytes = workspace_bytes(P, pages->head_dim, n_q_heads);
+  *bytes = workspace_bound(P, pages->head_dim, n_q_heads);
   return ARKV_OK;
 }
 

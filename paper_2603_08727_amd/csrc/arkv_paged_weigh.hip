@@ -336,6 +336,11 @@ size_t paged_weights_floats(const Paged& P, int Hq) {
   const int n = weigh_shares(P, Hq);
   return n == 1 ? 0 : kTicketFloats + (size_t)n * P.B * P.H * P.max_kv;
 }
+// For every batch of no more sequences, new tokens and rows than P's: shares times blocks are 512 at most, of 256 keys each.
+size_t paged_weights_bound(const Paged& P, int Hq) {
+  const size_t most = (size_t)P.max_q * (Hq / P.H) / (4 * kWeighRows);
+  return kTicketFloats + (most < 2 ? 0 : std::min<size_t>(512 * kWeighKeys, most * P.B * P.H * P.max_kv));
+}
 
 template <typename T, int D, int MODE>
 static hipError_t launch_weights(const PagedAttnArgs& A, hipStream_t st) {

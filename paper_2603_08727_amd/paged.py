@@ -198,14 +198,15 @@ def _check(rc, name):
 # ---- entry points, same names as the C ABI -----------------------------------------------------
 
 def arkv_paged_workspace_bytes(pages, batch, n_q_heads):
-    """Bytes of workspace that the calls below need for this batch."""
+    """Bytes of workspace that the calls below need for this batch, or any with no more sequences, tokens, new tokens or rows."""
     n = C.c_size_t()
     _check((_lib or load()).arkv_paged_workspace(pages.ref, batch.ref, n_q_heads, C.addressof(n)), "arkv_paged_workspace")
     return n.value
 
 
 def arkv_paged_workspace(pages, batch, n_q_heads):
-    """A workspace tensor for the calls below, its front zeroed as its first use wants it; one for the largest batch serves all."""
+    """A workspace tensor for the calls below, its front zeroed as its first use wants it; one for the largest of each of a batch's
+    bounds (sequences, n_tokens, max_q, max_kv) serves all."""
     torch = _TORCH or _torch()
     ws = torch.empty(arkv_paged_workspace_bytes(pages, batch, n_q_heads), dtype=torch.uint8, device=pages.device)
     ws[:TICKET_BYTES].zero_()

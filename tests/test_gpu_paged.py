@@ -600,3 +600,26 @@ def test_eviction_results_beside_its_lengths():
         with pytest.raises(P.ArkvError) as e:
             P.arkv_paged_evict(pages, batch, keep, dst, bad.get("kept", kept), bad.get("new_len", new_len), workspace=ws)
         assert e.value.code == P.EINVAL
+
+
+def test_a_workspace_for_the_largest_bounds_serves_every_call():
+    """Sized once for more sequences, tokens and rows than any of the batches has; single tokens and short chunks are cut finer."""
+    g = dict(dtype=BF, hq=8, hkv=2, d=128, page=16)
+    batches = [((600,) * 2, (4000, 2100)), ((1,), (6000,)), ((1,) * 12, (3000,) * 12), ((64,), (6000,)), ((20, 1, 1), (5000, 6000, 4000)), ((300,), (6000,))]
+    problems = [R.problem("cuda", q_len=q, kv_len=kv, seed=90 + i, **g) for i, (q, kv) in enumerate(batches)]
+    s = problems[0]
+    limits = P.arkv_page_batch(torch.zeros(13, dtype=torch.int32, device="cuda"), torch.zeros(12, dtype=torch.int32, device="cuda"),
+                               torch.zeros(12, 375, dtype=torch.int32, device="cuda"), 1200, 600, 6000)
+    ws = P.arkv_paged_workspace(P.arkv_pages(s.k, s.v, s.pos, s.weight), limits, 8)
+    for s in problems:
+        want, want_lse = attend(s)
+        pages, batch, _ = handles(s)
+        ws[TICKETS:].fill_(0xFF)
+        out, lse = torch.empty_like(want), torch.empty_like(want_lse)
+        P.arkv_paged_attention(pages, batch, s.q, s.scale, out, lse=lse, workspace=ws)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        ref, tol = R.weights(s, lse, 0.5, s.weight)
+        ws[TICKETS:].fill_(0xFF)
+        P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=0.5, workspace=ws)
+        R.close(s.weight, ref, tol, "weight")
+        assert not ws[:TICKETS].any()

@@ -237,3 +237,34 @@ def test_evictions_into_their_own_lengths_and_tables_are_refused():
         kw = dict(keep=keep, dst=dst, kept=kept, new_len=new_len)
         kw.update(bad)
         assert _call("evict", *a, **kw) == A.EINVAL, bad
+
+
+def _size(hq, hkv, d, batch, n_tokens, max_q, max_kv):
+    n = C.c_size_t()
+    pages = P._Pages(0, 100, 64, hkv, d, ADDR, ADDR, ADDR, ADDR)
+    b = P._Batch(batch, n_tokens, max_q, max_kv, 1 << 20, ADDR, ADDR, ADDR)
+    assert P.load().arkv_paged_workspace(C.byref(pages), C.byref(b), hq, C.byref(n)) == A.OK
+    return n.value
+
+
+@pytest.mark.parametrize("large,small", [
+    ((32, 32 * 2048, 2048, 16384), (32, 32, 1, 16384)), ((32, 32 * 2048, 2048, 16384), (1, 2048, 2048, 16384)),
+    ((32, 32 * 2048, 2048, 16384), (1, 128, 128, 16384)), ((64, 64, 1, 4096), (1, 1, 1, 4096)), ((200, 200, 1, 30000), (2, 2, 1, 30000))])
+def test_a_workspace_for_the_largest_batch_serves_smaller_ones(large, small):
+    """Fewer rows are cut finer: the size must not go by the batch's own cut alone."""
+    assert _size(32, 8, 128, *small) <= _size(32, 8, 128, *large)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (8, 8, 64), (16, 1, 128), (21, 3, 64), (64, 4, 128)])
+def test_workspaces_grow_with_each_bound(hq, hkv, d):
+    rng = np.random.default_rng(hq + d)
+    for _ in range(3000):
+        batch, n_tokens, max_kv = (int(np.exp(rng.uniform(0, np.log(hi)))) for hi in (2000, 100000, 1 << 20))
+        max_q = min(n_tokens, int(np.exp(rng.uniform(0, np.log(n_tokens + 1)))))
+        more = [x + int(rng.integers(0, 3)) * int(rng.integers(0, x + 2)) for x in (batch, n_tokens, max_q, max_kv)]
+        more[2] = min(more[2], more[1])
+        a, b = _size(hq, hkv, d, batch, n_tokens, max_q, max_kv), _size(hq, hkv, d, *more)
+        assert a <= b, (batch, n_tokens, max_q, max_kv, more)
+        few = [max(1, int(x * rng.uniform())) for x in (batch, n_tokens, max_q, max_kv)]
+        few[2] = min(few[2], few[1])
+        assert _size(hq, hkv, d, *few) <= a, (batch, n_tokens, max_q, max_kv, few)
