@@ -85,7 +85,8 @@ typedef struct {
 /* Turns q and k of the new tokens and stores k, v into their slots: q_out [n_tokens][H_q][d] (dense, DEVICE), rows k and v of
  * the pages, pos = positions[0][token], weight = 0.  positions DEVICE int32 [n_axes][n_tokens].  Angles are formed in 64
  * bits, products in 32, each result rounded once.  q.p may equal q_out (in place) if it is dense too.  q = NULL and q_out = NULL: keys and values only.
- * ARKV_EINVAL: null pointers, sizes, alignment, an axis >= n_axes.  ARKV_EUNSUPPORTED: head_dim, dtype, n_pages H_kv page_size >= 2^31. */
+ * ARKV_EINVAL: null pointers, sizes, alignment, an axis >= n_axes.  ARKV_EUNSUPPORTED: head_dim, dtype, n_pages H_kv page_size >= 2^31,
+ * n_tokens > 2^26 - 4. */
 int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_rotary* rotary, int32_t n_q_heads,
                       const arkv_rows* q, const arkv_rows* k, const arkv_rows* v, const int32_t* positions, void* q_out,
                       void* hip_stream);
@@ -101,7 +102,8 @@ int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, 
  * -infinity.  What lies in slots that a token does not see has no influence on its row, whatever bits it holds.
  * The new tokens' own rows must be in the pages already (arkv_paged_append).  G <= 16.
  * Probabilities are rounded to the pages' dtype in front of the product with v; sums, maxima and the denominator are fp32.  workspace 16-byte
- * aligned, as arkv_paged_workspace says. */
+ * aligned, as arkv_paged_workspace says.  ARKV_EUNSUPPORTED, besides the above: 2^24 workgroups or more (about n_tokens H_q / 128 +
+ * B H_kv max_kv / 2048; a sequence's last 128 rows may be a short block). */
 int arkv_paged_attention(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,
                          int32_t n_q_heads, const arkv_rows* q, void* out, float* lse, void* workspace, size_t bytes,
                          void* hip_stream);

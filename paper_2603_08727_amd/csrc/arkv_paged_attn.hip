@@ -786,33 +786,52 @@ __device__ __forceinline__ int find_seq(const int32_t* cu_q, int B, int t, int l
   return b;
 }
 
-// Joins the pieces of rows whose keys were split; rows that one workgroup finished are left alone.  32 lanes hold a row's
-// channels.  MANY pieces: the eight groups of 32 share a row's pieces; else each has a row of its own.
+// Joins the pieces of rows whose keys were split.  Rows of paged_step come first, `few_rows` of every unit (step_ids with them filled up
+// to eight), then all rows where those of paged_chunk are to be joined; rows that one workgroup finished are left alone.  32 lanes hold a
+// row's channels.  MANY pieces: the eight groups of 32 share a row's pieces; else each has a row of its own.
 template <typename T, int D, bool MANY>
-__global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs A, Cut cut, Parts parts) {
+__global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs A, Cut cut, Parts parts, int few_rows, int step_ids) {
   constexpr int C = D / 32;
   typedef float chan __attribute__((ext_vector_type(C)));
   __shared__ float s_acc[MANY ? 8 : 1][D];
   __shared__ float s_l[8];
   const Paged& P = A.P;
   const int lane = threadIdx.x & 63, c = threadIdx.x & 31, grp = threadIdx.x >> 5;
-  const int rows = P.N * A.Hq, want = MANY ? (int)blockIdx.x : (int)blockIdx.x * 8 + grp, id = min(want, rows - 1);
-  const int t = id / A.Hq, hq = id % A.Hq;
-  int b;
-  if constexpr (MANY) b = find_seq(P.cu_q, P.B, t, lane);
-  else {                                                           // (two rows in a wave)
-    const int t0 = __builtin_amdgcn_readlane(t, 0), t1 = __builtin_amdgcn_readlane(t, 32);
-    const int b0 = find_seq(P.cu_q, P.B, t0, lane), b1 = t1 == t0 ? b0 : find_seq(P.cu_q, P.B, t1, lane);
-    b = lane < 32 ? b0 : b1;
+  const int at = MANY ? (int)blockIdx.x : (int)blockIdx.x * 8 + grp;
+  const bool step = (MANY ? (int)blockIdx.x : (int)blockIdx.x * 8) < step_ids;   // (uniform)
+  int b, t, hq, r;
+  Seq s;
+  bool mine;                                                       // the row is one of the kind that is joined here
+  if (step) {
+    const int unit = at / few_rows;
+    r = at % few_rows;
+    b = min(unit / P.H, P.B - 1);
+    s = seq_of(P, b);
+    t = s.q0 + r / A.G;
+    hq = unit % P.H * A.G + r % A.G;
+    mine = unit < P.B * P.H && r < s.nq * A.G && s.nq * A.G <= kStepRows;
+  } else {
+    const int rows = P.N * A.Hq, want = at - step_ids, row = min(want, rows - 1);
+    t = row / A.Hq;
+    hq = row % A.Hq;
+    if constexpr (MANY) b = find_seq(P.cu_q, P.B, t, lane);
+    else {                                                         // (two rows in a wave)
+      const int t0 = __builtin_amdgcn_readlane(t, 0), t1 = __builtin_amdgcn_readlane(t, 32);
+      const int b0 = find_seq(P.cu_q, P.B, t0, lane), b1 = t1 == t0 ? b0 : find_seq(P.cu_q, P.B, t1, lane);
+      b = lane < 32 ? b0 : b1;
+    }
+    mine = want < rows && b < P.B;
+    b = min(b, P.B - 1);
+    s = seq_of(P, b);
+    const int i = t - s.q0;
+    r = i * A.G + hq % A.G;
+    mine = mine && i >= 0 && i < s.nq && s.nq * A.G > cut.w.few;
   }
-  const Seq s = seq_of(P, min(b, P.B - 1));
-  const int i = t - s.q0;
-  const int prefix = A.S.prefix ? A.S.prefix[min(b, P.B - 1)] : 0, R = s.nq * A.G, r = i * A.G + hq % A.G;
-  const bool step = R <= cut.w.few;
-  const int last = step ? s.nq - 1 : min(R - 1, r / kChunkRows * kChunkRows + kChunkRows - 1) / A.G;
+  const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
+  const int last = step ? s.nq - 1 : min(s.nq * A.G - 1, r / kChunkRows * kChunkRows + kChunkRows - 1) / A.G;
   const int piece = step ? cut.step_piece : cut.chunk_piece;
   int np = (row_end(s, last, prefix) + piece - 1) / piece;
-  if (want >= rows || b >= P.B || i < 0 || i >= s.nq || np <= 1 || (step ? cut.joined : cut.chunk_joined)) np = 0;
+  if (!mine || np <= 1) np = 0;
   if (MANY && np == 0) return;
   const size_t first = step ? (size_t)(b * P.H + hq / A.G) * cut.n_step * kStepRows + r : parts.chunk0 + (size_t)t * A.Hq + hq;
   const size_t stride = step ? kStepRows : (size_t)P.N * A.Hq;
@@ -847,30 +866,50 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs A, Cut cut, P
   }
   if (np == 0) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;                      // (NaN stays)
-  T* out = (T*)A.out + (size_t)id * D + C * c;
+  const size_t id = (size_t)t * A.Hq + hq;
+  T* out = (T*)A.out + id * D + C * c;
 #pragma unroll
   for (int e = 0; e < C; e += 2) *reinterpret_cast<uint32_t*>(out + e) = Mfma<T>::pack(acc[e] * inv, acc[e + 1] * inv);
   if (c == 0 && A.lse) A.lse[id] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+}
+
+// Workgroups of a call's launches.  merge: few_rows rows of every unit, if paged_step's pieces are not joined where they are made; then
+// all rows, if those of paged_chunk are not (they are cut only where they are few).  Rows of few pieces are little work, and eight fit a workgroup.
+struct Launches { long long chunk, step, merge; int few_rows, step_ids; bool many; };
+static Launches launches_of(const Paged& P, int Hq, const Cut& c) {
+  Launches l = {};
+  l.chunk = c.w.chunk ? (long long)c.blocks * P.H * c.n_chunk : 0;
+  l.step = c.w.step ? (long long)P.B * P.H * c.n_step : 0;
+  const bool join_step = l.step && c.n_step > 1 && !c.joined, join_chunk = l.chunk && c.n_chunk > 1 && !c.chunk_joined;
+  l.few_rows = (int)std::min<long long>(kStepRows, (long long)P.max_q * (Hq / P.H));
+  l.step_ids = join_step ? (P.B * P.H * l.few_rows + 7) / 8 * 8 : 0;
+  l.many = (join_chunk ? c.n_chunk : c.n_step) >= 8;
+  const long long ids = l.step_ids + (join_chunk ? (long long)P.N * Hq : 0);
+  l.merge = l.many ? ids : (ids + 7) / 8;
+  return l;
+}
+long long paged_attention_workgroups(const Paged& P, int D, int Hq) {
+  const Launches l = launches_of(P, Hq, cut_of(P, D, Hq));
+  return std::max(l.chunk + l.step, l.merge);
 }
 
 template <typename T, int D, int MODE>
 static hipError_t launch_attention(const PagedAttnArgs& A, hipStream_t st) {
   const Paged& P = A.P;
   const Cut c = cut_of(P, D, A.Hq);
+  const Launches l = launches_of(P, A.Hq, c);
   Parts parts = {};
   const size_t n = part_rows(P, A.Hq, c, parts.chunk0);
   parts.tickets = (int*)A.ws;
   parts.acc = A.ws + kTicketFloats;
   parts.ml = (float2*)(parts.acc + n * D);
-  const int chunk = c.w.chunk ? c.blocks * P.H * c.n_chunk : 0, step = c.w.step ? P.B * P.H * c.n_step : 0;
+  const int chunk = (int)l.chunk, step = (int)l.step;
   if (chunk && step) k_paged_attn<T, D, MODE, 3><<<chunk + step, 256, 0, st>>>(A, c, parts, chunk);
   else if (chunk) k_paged_attn<T, D, MODE, 1><<<chunk, 256, 0, st>>>(A, c, parts, chunk);
   else k_paged_attn<T, D, MODE, 2><<<step, 256, 0, st>>>(A, c, parts, 0);
-  if ((chunk && c.n_chunk > 1 && !c.chunk_joined) || (step && c.n_step > 1 && !c.joined)) {
-    const int rows = P.N * A.Hq;
-    // with few pieces a row is little work, and eight fit a workgroup
-    if ((chunk && !c.chunk_joined ? c.n_chunk : c.n_step) >= 8) k_paged_merge<T, D, true><<<rows, 256, 0, st>>>(A, c, parts);
-    else k_paged_merge<T, D, false><<<(rows + 7) / 8, 256, 0, st>>>(A, c, parts);
+  if (l.merge) {
+    if (l.many) k_paged_merge<T, D, true><<<(int)l.merge, 256, 0, st>>>(A, c, parts, l.few_rows, l.step_ids);
+    else k_paged_merge<T, D, false><<<(int)l.merge, 256, 0, st>>>(A, c, parts, l.few_rows, l.step_ids);
   }
   return hipGetLastError();
 }

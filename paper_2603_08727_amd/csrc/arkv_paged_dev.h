@@ -46,6 +46,9 @@ __host__ __device__ inline int slot_row(const int32_t* table_row, int n_pages, i
 constexpr int kJoinUnits = 1024, kTicketWords = 16;                // (a ticket has a cache line of its own)
 constexpr size_t kTicketFloats = (size_t)kJoinUnits * kTicketWords;
 
+// A launch takes fewer than 2^32 work-items in x.
+constexpr long long kMostWorkgroups = (1ll << 32) / 256 - 1;       // of 256
+
 struct AppendArgs {
   Paged P;
   Rows q, k, v;
@@ -73,6 +76,7 @@ size_t paged_attention_floats(const Paged& P, int D, int Hq);
 size_t paged_attention_bound(const Paged& P, int D, int Hq);
 size_t paged_weights_floats(const Paged& P, int Hq);
 size_t paged_weights_bound(const Paged& P, int Hq);
+long long paged_attention_workgroups(const Paged& P, int D, int Hq);   // of its largest launch
 hipError_t launch_paged_attention(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
 hipError_t launch_paged_weights(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
 

@@ -26,7 +26,7 @@ static int check(const arkv_pages* p, const arkv_page_batch* b, Paged& P) {
   if ((int64_t)p->n_pages * p->n_kv_heads >= (int64_t)(1u << 31) / p->page_size) return ARKV_EUNSUPPORTED;
   if (b->batch > 65535 || p->n_kv_heads > 65535 || b->n_tokens > (1 << 28)) return ARKV_EUNSUPPORTED;
   if ((int64_t)b->max_kv > (int64_t)b->table_width * p->page_size || b->max_q > b->n_tokens) return ARKV_EINVAL;
-  // (launches have fewer than 2^31 workgroups)
+  // (what the kernels count in 32 bits; how many workgroups a launch may have is checked where they are known)
   const int64_t units = (int64_t)b->batch * p->n_kv_heads;
   if (b->max_kv > (1 << 28) || units > (1 << 20) || units * b->max_kv > (1ll << 40)) return ARKV_EUNSUPPORTED;
   P.k = p->k; P.v = p->v; P.pos = p->pos; P.weight = p->weight;
@@ -97,6 +97,7 @@ int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, con
   A.freq = rotary->rot_dim ? rotary->freq : (const double*)pages->k;   // (read in any case, a branch would cost a round trip)
   A.half = rotary->rot_dim / 2; A.adjacent = rotary->adjacent; A.n_axes = rotary->n_axes;
   if (!A.P.N) return ARKV_OK;
+  if (A.P.N > 4 * kMostWorkgroups) return ARKV_EUNSUPPORTED;       // (four tokens a workgroup)
   LAUNCH(launch_paged_append(pages->dtype, pages->head_dim, A, (hipStream_t)hip_stream));
 }
 
@@ -131,6 +132,7 @@ int arkv_paged_attention(const arkv_pages* pages, const arkv_page_batch* batch, 
   if ((!out && A.P.N) || !aligned16(out)) return ARKV_EINVAL;
   A.out = out; A.lse = lse;
   if (!A.P.N || !A.P.max_q) return ARKV_OK;
+  if (paged_attention_workgroups(A.P, pages->head_dim, n_q_heads) > kMostWorkgroups) return ARKV_EUNSUPPORTED;
   LAUNCH(launch_paged_attention(pages->dtype, pages->head_dim, A, (hipStream_t)hip_stream));
 }
 

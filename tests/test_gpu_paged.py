@@ -623,3 +623,14 @@ def test_a_workspace_for_the_largest_bounds_serves_every_call():
         P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=0.5, workspace=ws)
         R.close(s.weight, ref, tol, "weight")
         assert not ws[:TICKETS].any()
+
+
+@pytest.mark.parametrize("q,kv,hq,hkv", [
+    ((1, 40, 0, 2) * 40, (5000, 70, 0, 300) + (33, 100, 9, 2100) * 39, 16, 8),      # 1280 units: too many for tickets, three pieces
+    ((1, 300, 2) * 45, (17000, 300, 2) + (64, 700, 2500) * 44, 8, 8),               # nine pieces
+    ((1100, 1, 1, 2), (1100, 40000, 33000, 2049), 16, 16),                          # more than sixteen, beside a chunk that is joined
+    ((17, 1, 0), (40000, 36000, 70), 2, 1)])                                        # both kinds of rows in many pieces
+def test_rows_of_split_sequences_are_joined_in_a_launch(q, kv, hq, hkv):
+    s = R.problem("cuda", BF, hq, hkv, 64, 16, q, kv, seed=17, extra_tokens=3)
+    check_attention(s)
+    check_attention(s, prefix=torch.tensor([t - a // 2 for a, t in zip(q, kv)], dtype=torch.int32, device="cuda"))

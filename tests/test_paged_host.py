@@ -268,3 +268,17 @@ def test_workspaces_grow_with_each_bound(hq, hkv, d):
         few = [max(1, int(x * rng.uniform())) for x in (batch, n_tokens, max_q, max_kv)]
         few[2] = min(few[2], few[1])
         assert _size(hq, hkv, d, *few) <= a, (batch, n_tokens, max_q, max_kv, few)
+
+
+@pytest.mark.parametrize("batch,hkv,hq,max_q,n_tokens,max_kv", [
+    (4096, 8, 8, 1, 4096, 1 << 20), (1024, 32, 32, 1, 1024, 1 << 20), (4096, 64, 64, 2, 8191, 1 << 18),
+    (65535, 1, 16, 2000, 1 << 27, 128)])
+def test_launches_that_cannot_be_made_are_refused_before_the_first(batch, hkv, hq, max_q, n_tokens, max_kv):
+    """2^32 work-items or more, within every other bound: of the attention's launch, not of the joining one behind it."""
+    pages, b, rows, rot, sc = _args()
+    pages.n_kv_heads, b.batch, b.n_tokens, b.max_q, b.max_kv, b.table_width = hkv, batch, n_tokens, max_q, max_kv, 1 << 16
+    if hq * n_tokens >= 1 << 31:                       # (that many tokens only without query heads)
+        pages.n_pages = 1
+        assert P.load().arkv_paged_append(C.byref(pages), C.byref(b), C.byref(rot), 0, None, C.byref(rows), C.byref(rows), ADDR, None, None) == A.EUNSUPPORTED
+    else:
+        assert _call("attention", pages, b, rows, rot, sc, hq=hq, size=1 << 50) == A.EUNSUPPORTED
