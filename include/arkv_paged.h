@@ -118,13 +118,13 @@ int arkv_paged_weights(const arkv_pages* pages, const arkv_page_batch* batch, co
                        void* workspace, size_t bytes, void* hip_stream);
 
 /* Every kv-head of sequence b keeps m = min(kv_len[b], keep[b]) of its rows: the first min(sink, m), the last
- * min(recent, m - that), and of the others those of the largest weight (equal weights: the lower slot; NaN: below
- * everything; -0 = +0).  The survivors' k, v, pos and weight are copied, in slot order, to the slots 0 .. m - 1 of the pages dst_table[b]
+ * min(recent, m - that), and of the others those of the largest weight (equal weights: the lower slot; -0 = +0; NaN
+ * and rows in absent pages, alike: below every number, the lower slot first).  The survivors' k, v, pos and weight are copied, in slot order, to the slots 0 .. m - 1 of the pages dst_table[b]
  * ([B][dst_width] DEVICE int32), which must be pages that no table of the batch names: the sources stay as they are, so
  * pages that other sequences share can be evicted from.  kept DEVICE int32 [B][H_kv][max_keep]: the survivors' former
  * slots, -1 behind them.  new_len DEVICE int32 [B] = m.  keep DEVICE int32 [B], cut to [0, max_keep].  cu_q and the new tokens play no
  * part.  kept and new_len must not overlap kv_len, keep, the tables or each other (lengths are read until the end of the call: copy new_len
- * over kv_len behind it).  A row in an absent page ranks below every other and is not copied.  workspace as arkv_paged_workspace says; NULL will do
+ * over kv_len behind it).  For a survivor in an absent page nothing is copied: its new slot holds what it held before.  workspace as arkv_paged_workspace says; NULL will do
  * where max_keep head_dim <= 32768 and max_kv <= 36864 (with one, few units of many rows are counted faster).
  * ARKV_EINVAL: as above, weight NULL, arrays that overlap, max_keep outside [1, dst_width * page_size], sink or recent negative, a workspace
  * that is too small, not aligned to 16 bytes, or missing. */

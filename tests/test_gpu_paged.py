@@ -634,3 +634,24 @@ def test_rows_of_split_sequences_are_joined_in_a_launch(q, kv, hq, hkv):
     s = R.problem("cuda", BF, hq, hkv, 64, 16, q, kv, seed=17, extra_tokens=3)
     check_attention(s)
     check_attention(s, prefix=torch.tensor([t - a // 2 for a, t in zip(q, kv)], dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("kv,keep", [(200, 130), (9000, 8700)])
+def test_rows_without_a_number_and_absent_rows_rank_alike(kv, keep):
+    """Both lie below every number, -infinity too, and among themselves the lower slot stays first."""
+    s = R.problem("cuda", BF, 2, 2, 64, 16, (0,), (kv,), seed=81, spare_pages=-(-keep // 16))
+    held = s.table[0].long()
+    s.weight[held] = torch.where(torch.rand(s.weight[held].shape, generator=torch.Generator().manual_seed(8)).cuda() < 0.5, math.nan, -math.inf)
+    s.table[0, 4] = -1                                 # slots 64 to 79, NaN before and behind them
+    dst = torch.tensor([s.spare], dtype=torch.int32, device="cuda")
+    pages, batch, ws = handles(s)
+    kept, lens = torch.empty((1, 2, keep), dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+    P.arkv_paged_evict(pages, batch, torch.tensor([keep], dtype=torch.int32, device="cuda"), dst, kept, lens, workspace=ws)
+    for h in range(2):
+        w = R.rows(s, s.weight, 0, h)[0]
+        number = ~torch.isnan(w)
+        number[64:80] = False
+        middle = torch.arange(4, kv - 32, device="cuda")
+        order = torch.cat([middle[number[4:kv - 32]], middle[~number[4:kv - 32]]])[:keep - 36]
+        want = torch.cat([torch.arange(4, device="cuda"), order.sort().values, torch.arange(kv - 32, kv, device="cuda")])
+        assert torch.equal(kept[0, h].long(), want)
