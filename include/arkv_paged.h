@@ -74,7 +74,8 @@ typedef struct {
 
 /* How a logit comes about: x = scale q.k; with cap > 0: x = cap tanh(x / cap); with slopes (DEVICE float [H_q]):
  * x -= slopes[h] |q_pos - pos|, q_pos DEVICE int32 [n_tokens], pos the cached row's.  New token i of sequence b sees the
- * slots up to its own, j <= ctx_b + i, and with prefix (DEVICE int32 [B]) every slot j < prefix[b]; all of them < kv_len[b]. */
+ * slots up to its own, j <= ctx_b + i, and with prefix (DEVICE int32 [B]) every slot j < prefix[b]; all of them < kv_len[b].
+ * The cap puts x off by 2^-22 cap at most; one above 256 by 2^-19 of x. */
 typedef struct {
   float scale, cap;
   const float* slopes;

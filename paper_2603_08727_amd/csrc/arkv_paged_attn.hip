@@ -151,7 +151,8 @@ template <int D> struct StepLds {
 
 template <typename T, int D, int MODE>
 __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, StepLds<D>& sm, int id) {
-  constexpr bool CAP = Mode<MODE>::cap, DIST = Mode<MODE>::dist;
+  constexpr int CAP = Mode<MODE>::cap;
+  constexpr bool DIST = Mode<MODE>::dist;
   constexpr int KK = D / 32, CB = D / 16, VI = 32 * D * 2 / 1024;   // k-steps, channel blocks, 1 KB loads of a value tile
   constexpr int RPI = 1024 / (2 * D), CPR = D / 8;                 // rows per load, 16-byte chunks per row
   const int piece_keys = cut.step_piece, n_pieces = cut.n_step;
@@ -461,7 +462,8 @@ template <int D> __device__ __forceinline__ int v_chunk(int row, int c) { return
 
 template <typename T, int D, int MODE>
 __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, ChunkLds<D>& sm, int id) {
-  constexpr bool CAP = Mode<MODE>::cap, DIST = Mode<MODE>::dist;
+  constexpr int CAP = Mode<MODE>::cap;
+  constexpr bool DIST = Mode<MODE>::dist;
   const int piece_keys = cut.chunk_piece;
   constexpr int KK = D / 16, CB = D / 32, CPR = D / 8, RPI = 64 / CPR, LPG = 16 / RPI;   // LPG: 1 KB loads of a granule
   const Paged& P = A.P;

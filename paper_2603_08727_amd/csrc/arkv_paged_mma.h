@@ -55,28 +55,31 @@ template <typename T> __device__ __forceinline__ uint32_t not_finite(uint32_t w)
   return ((w & Mfma<T>::kExp) == Mfma<T>::kExp ? 0xFFFFu : 0u) | ((w >> 16 & Mfma<T>::kExp) == Mfma<T>::kExp ? 0xFFFF0000u : 0u);
 }
 
-// What the kernels are built for: bit 0 of MODE: scores have a cap, bit 1: a bias by distance.
-template <int MODE> struct Mode { static constexpr bool cap = (MODE & 1) != 0, dist = (MODE & 2) != 0; };
-inline int mode_of(const Scores& S) { return (S.cap > 0.f ? 1 : 0) | (S.slopes ? 2 : 0); }
+// What the kernels are built for: bit 0 of MODE: scores have a cap, bit 1: a bias by distance, bit 2: a cap above kWideCap.
+template <int MODE> struct Mode { static constexpr int cap = MODE & 4 ? 2 : MODE & 1; static constexpr bool dist = (MODE & 2) != 0; };
+constexpr float kWideCap = 256.f;
+inline int mode_of(const Scores& S) { return (S.cap > kWideCap ? 4 : S.cap > 0.f ? 1 : 0) | (S.slopes ? 2 : 0); }
 
 // logit, times log2(e), of a raw dot product
 struct Logit {
-  float mul, inv_cap2, cap2;     // scale log2(e); 2 log2(e) scale / cap; cap log2(e)
+  float mul, inv_cap2, cap2, inv;     // scale log2(e); 2 log2(e) scale / cap; cap log2(e); scale / cap
   __device__ __forceinline__ Logit(const Scores& S) {
     mul = S.scale * kLog2e;
     cap2 = S.cap * kLog2e;
-    inv_cap2 = S.cap > 0.f ? 2.f * kLog2e * (S.scale / S.cap) : 0.f;
+    inv = S.cap > 0.f ? S.scale / S.cap : 0.f;
+    inv_cap2 = 2.f * kLog2e * inv;
   }
-  // tanh x = 1 - 2 / (1 + e^2x): off by a few 2^-24 of 1, for logits up to the cap in absolute terms
-  template <bool CAP> __device__ __forceinline__ float logit(float dot) const {
-    if (CAP) return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + exp2_hw(dot * inv_cap2)), cap2);
-    return dot * mul;
+  // the logit less ref.  CAP 1: tanh u = 1 - 2 / (1 + e^2u), which is off by a few 2^-24 of 1, the logit by 2^-22 of the cap, in absolute
+  // terms: 2^-14 at kWideCap.  CAP 2: a larger cap would drown small logits in that, so where |u| < 1 / 8 its series takes over (the first
+  // term left out is u^8 / 46 of u, below 2^-24), and the logit is off by 2^-19 of itself at most.
+  template <int CAP> __device__ __forceinline__ float above(float dot, float ref) const {
+    if (CAP == 0) return fmaf(dot, mul, -ref);
+    const float y = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + exp2_hw(dot * inv_cap2)), cap2 - ref);
+    if (CAP == 1) return y;
+    const float u = dot * inv, w = u * u;
+    return fabsf(u) < 0.125f ? fmaf(dot * mul, fmaf(w, fmaf(w, fmaf(w, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f), -ref) : y;
   }
-  // the same less ref
-  template <bool CAP> __device__ __forceinline__ float above(float dot, float ref) const {
-    if (CAP) return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + exp2_hw(dot * inv_cap2)), cap2 - ref);
-    return fmaf(dot, mul, -ref);
-  }
+  template <int CAP> __device__ __forceinline__ float logit(float dot) const { return CAP ? above<CAP>(dot, 0.f) : dot * mul; }
 };
 
 // Keeps a rare branch a branch: what depends on the result is not computed in front of it (the compiler would compute a tile's masks
@@ -128,7 +131,9 @@ template <typename T, int D, typename F> hipError_t dispatch_mode(int mode, F f)
     case 0: return f(TypeOf<T>(), Int<D>(), Int<0>());
     case 1: return f(TypeOf<T>(), Int<D>(), Int<1>());
     case 2: return f(TypeOf<T>(), Int<D>(), Int<2>());
-    default: return f(TypeOf<T>(), Int<D>(), Int<3>());
+    case 3: return f(TypeOf<T>(), Int<D>(), Int<3>());
+    case 4: return f(TypeOf<T>(), Int<D>(), Int<4>());
+    default: return f(TypeOf<T>(), Int<D>(), Int<6>());
   }
 }
 template <typename F> hipError_t dispatch(int dtype, int D, int mode, F f) {

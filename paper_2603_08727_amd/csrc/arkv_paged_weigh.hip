@@ -20,7 +20,8 @@ __device__ __forceinline__ void store_weight(const PagedAttnArgs& A, int row, fl
 // Few rows: bound by reading the keys (16 x 8192 rows x 8 heads: 50 us, 4.7 TB/s).  A wave takes wave_keys keys, 32 at a time (two granules), the next 32 in flight.
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(256) void k_weigh_step(PagedAttnArgs A, int wave_keys) {
-  constexpr bool CAP = Mode<MODE>::cap, DIST = Mode<MODE>::dist;
+  constexpr int CAP = Mode<MODE>::cap;
+  constexpr bool DIST = Mode<MODE>::dist;
   constexpr int KK = D / 32;
   const Paged& P = A.P;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -121,7 +122,8 @@ template <int D> struct WeighLds {
 
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(256, 2) void k_weigh_chunk(PagedAttnArgs A, int few, int n_shares) {
-  constexpr bool CAP = Mode<MODE>::cap, DIST = Mode<MODE>::dist;
+  constexpr int CAP = Mode<MODE>::cap;
+  constexpr bool DIST = Mode<MODE>::dist;
   constexpr int KK = D / 16, CPR = D / 8, RPI = 64 / CPR, LPW = kWeighRows / RPI / 4;    // LPW: 1 KB loads of a tile per wave
   __shared__ __align__(16) WeighLds<D> sm;
   const Paged& P = A.P;

@@ -655,3 +655,27 @@ def test_rows_without_a_number_and_absent_rows_rank_alike(kv, keep):
         order = torch.cat([middle[number[4:kv - 32]], middle[~number[4:kv - 32]]])[:keep - 36]
         want = torch.cat([torch.arange(4, device="cuda"), order.sort().values, torch.arange(kv - 32, kv, device="cuda")])
         assert torch.equal(kept[0, h].long(), want)
+
+
+@pytest.mark.parametrize("cap", [257.0, 3000.0, 1e5, 1e9, 3e38])
+@pytest.mark.parametrize("q,kv", [((1, 2), (700, 40)), ((60, 130), (800, 400))])
+@pytest.mark.parametrize("dtype,d,far", [(BF, 128, False), (FP, 64, True)])
+def test_wide_caps_do_not_drown_the_logits(dtype, d, far, q, kv, cap, monkeypatch):
+    """The wider the cap, the nearer the uncapped scores: off by 2^-19 of a logit, not by a share of the cap."""
+    plain = R.logits
+
+    def logits(s, b, hq, cap=0.0, **kw):
+        x, err = plain(s, b, hq, cap, **kw)
+        bare = plain(s, b, hq)[0]
+        return x, plain(s, b, hq, **kw)[1] + 2.0 ** -19 * float(bare[torch.isfinite(bare)].abs().max())
+
+    monkeypatch.setattr(R, "logits", logits)
+    s = R.problem("cuda", dtype, 8, 2, d, 16, q, kv, seed=18, hot=20.0)
+    kw = dict(cap=cap)
+    if far:
+        kw["slopes"], kw["q_pos"] = slopes_of(s)
+    _, lse = check_attention(s, **kw)
+    pages, batch, ws = handles(s)
+    ref, tol = R.weights(s, lse, 1.0, s.weight, **kw)
+    P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, workspace=ws, **kw)
+    R.close(s.weight, ref, tol, "weight")
