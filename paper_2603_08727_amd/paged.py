@@ -82,6 +82,13 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+def _int32(**numbers):
+    """Python's numbers have no end; ctypes would pass on their lowest 32 bits."""
+    for what, x in numbers.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{what}: {x} does not fit 32 bits")
+
+
 def _dense(t, shape, dtype, what, index=None):
     """Address of a contiguous GPU tensor (on GPU `index`) of that shape and type."""
     at = t.get_device()
@@ -122,7 +129,9 @@ class arkv_page_batch:
         self.cu_q, self.kv_len, self.table = cu_q, kv_len, table
         self.device, self.index, self.B, self.n_tokens = table.device, table.get_device(), B, n_tokens
         _need(max_kv is not None or page_size is not None, "max_kv or page_size is needed")
-        self.c = _Batch(B, n_tokens, n_tokens if max_q is None else max_q, width * page_size if max_kv is None else max_kv, width,
+        max_q, max_kv = n_tokens if max_q is None else max_q, width * page_size if max_kv is None else max_kv
+        _int32(n_tokens=n_tokens, max_q=max_q, max_kv=max_kv)
+        self.c = _Batch(B, n_tokens, max_q, max_kv, width,
                         _dense(cu_q, (B + 1,), torch.int32, "cu_q", self.index), _dense(kv_len, (B,), torch.int32, "kv_len", self.index),
                         _dense(table, (B, width), torch.int32, "table"))
         self.ref = C.addressof(self.c)
@@ -138,6 +147,7 @@ class arkv_rotary:
         _need(half <= 64, "at most 64 pairs")
         axis = [0] * half if axis is None else [int(a) for a in axis]
         _need(len(axis) == half and all(0 <= a < 256 for a in axis), "axis: one entry per pair")
+        _int32(n_axes=n_axes)
         self.freq, self.n_axes, self.index = freq, n_axes, None if freq is None else freq.get_device()
         self.c = _Rotary(2 * half, n_axes, 1 if adjacent else 0, (C.c_uint8 * 64)(*axis),
                          None if freq is None else _dense(freq, (half,), torch.float64, "freq"))
@@ -284,6 +294,7 @@ def arkv_paged_evict(pages, batch, keep, dst_table, kept, new_len, sink=4, recen
     stream = _current(pages, batch)
     B, at, i32 = batch.B, pages.index, torch.int32
     _need(dst_table.dim() == 2 and kept.dim() == 3, "dst_table: [B][pages]; kept: [B][H_kv][max_keep]")
+    _int32(sink=sink, recent=recent)
     width, max_keep = dst_table.size(1), kept.size(2)
     ws, size = _workspace(workspace, pages)
     rc = (_lib or load()).arkv_paged_evict(
@@ -295,6 +306,7 @@ def arkv_paged_evict(pages, batch, keep, dst_table, kept, new_len, sink=4, recen
 def arkv_debug_paged_row(table_row, n_pages, page_size, n_kv_heads, kv_head, length, slot):
     """Row of [n_pages][H_kv][page_size] in which the kernels look for a slot, -1: none.  table_row: NumPy int32."""
     import numpy as np
+    _int32(n_pages=n_pages, page_size=page_size, n_kv_heads=n_kv_heads, kv_head=kv_head, length=length, slot=slot)
     t = np.ascontiguousarray(table_row, dtype=np.int32)
     row = C.c_int64()
     _check((_lib or load()).arkv_debug_paged_row(t.ctypes.data, len(t), n_pages, page_size, n_kv_heads, kv_head, length, slot, C.addressof(row)),

@@ -679,3 +679,14 @@ def test_wide_caps_do_not_drown_the_logits(dtype, d, far, q, kv, cap, monkeypatc
     ref, tol = R.weights(s, lse, 1.0, s.weight, **kw)
     P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, workspace=ws, **kw)
     R.close(s.weight, ref, tol, "weight")
+
+
+@pytest.mark.parametrize("kw", [dict(sink=1 << 32), dict(recent=(1 << 32) + 8), dict(sink=-(1 << 32))])
+def test_evictions_whose_numbers_do_not_fit_32_bits_are_refused(kw):
+    s = R.problem("cuda", BF, 2, 2, 64, 16, (0,), (100,), seed=82, spare_pages=4)
+    pages, batch, ws = handles(s)
+    kept, lens = torch.full((1, 2, 50), 9, dtype=torch.int32, device="cuda"), torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="32 bits"):
+        P.arkv_paged_evict(pages, batch, torch.tensor([50], dtype=torch.int32, device="cuda"), torch.tensor([s.spare], dtype=torch.int32, device="cuda"),
+                           kept, lens, workspace=ws, **kw)
+    assert (kept == 9).all() and int(lens) == 9

@@ -282,3 +282,19 @@ def test_launches_that_cannot_be_made_are_refused_before_the_first(batch, hkv, h
         assert P.load().arkv_paged_append(C.byref(pages), C.byref(b), C.byref(rot), 0, None, C.byref(rows), C.byref(rows), ADDR, None, None) == A.EUNSUPPORTED
     else:
         assert _call("attention", pages, b, rows, rot, sc, hq=hq, size=1 << 50) == A.EUNSUPPORTED
+
+
+def test_numbers_that_do_not_fit_32_bits_are_refused():
+    """ctypes passes on the lowest 32 bits of a number: 2^32 + 64 rows would be 64."""
+    big, z = (1 << 32) + 64, torch.zeros
+    cu, lens, table = z(3, dtype=torch.int32), z(2, dtype=torch.int32), z(2, 4, dtype=torch.int32)
+    for kw in [dict(n_tokens=big, max_q=1, max_kv=64), dict(n_tokens=4, max_q=big, max_kv=64), dict(n_tokens=4, max_q=1, max_kv=big),
+               dict(n_tokens=4, max_q=1, page_size=1 << 30)]:
+        with pytest.raises(ValueError, match="32 bits"):
+            P.arkv_page_batch(cu, lens, table, **kw)
+    with pytest.raises(ValueError, match="32 bits"):
+        P.arkv_rotary(None, n_axes=(1 << 32) + 1)
+    kw = dict(n_pages=4, page_size=16, n_kv_heads=1, kv_head=0, length=64, slot=0)
+    for name in kw:
+        with pytest.raises(ValueError, match="32 bits"):
+            P.arkv_debug_paged_row(np.zeros(4, np.int32), **{**kw, name: kw[name] + (1 << 32)})
