@@ -19,7 +19,10 @@ class PagedLayer:
 
     def __init__(self, n_requests, hidden=512, n_q_heads=8, n_kv_heads=2, head_dim=64, page_size=16, n_pages=256, limit=256,
                  budget=128, max_tokens=256, dtype=torch.bfloat16, seed=0, device="cuda"):
+        if not 0 < budget <= limit:
+            raise ValueError(f"budget {budget}: a request over the limit of {limit} rows is cut to 1 .. limit of them")
         g = torch.Generator(device=device).manual_seed(seed)
+        self.max_tokens = max_tokens                   # of a request in one step
         self.hq, self.hkv, self.d, self.page, self.limit, self.budget, self.device = n_q_heads, n_kv_heads, head_dim, page_size, limit, budget, device
         # a chunk can bring a request over its limit before it is cut
         self.width = -(-(limit + max_tokens) // page_size)
@@ -39,8 +42,6 @@ class PagedLayer:
         self.workspace = None
 
     def _take(self, n):
-        if n > len(self.free):
-            raise RuntimeError(f"out of pages: {n} wanted, {len(self.free)} free")
         got, self.free = self.free[:n], self.free[n:]
         return got
 
@@ -57,9 +58,21 @@ class PagedLayer:
             self.workspace = P.arkv_paged_workspace(self.pages, batch, self.hq)
         return batch
 
+    def _check_step(self, n, q_len):
+        if len(q_len) != len(self.rows) or sum(q_len) != n or not all(0 <= a <= self.max_tokens for a in q_len):
+            raise ValueError(f"{n} tokens as {q_len}: one count of 0 to {self.max_tokens} for each of {len(self.rows)} requests")
+        rows = [have + a for have, a in zip(self.rows, q_len)]
+        need = sum(-(-m // self.page) - len(held) for m, held in zip(rows, self.held))
+        need += sum(m > self.limit for m in rows) * -(-self.budget // self.page)       # (the old pages return behind the eviction)
+        if need > len(self.free):
+            raise RuntimeError(f"out of pages: {need} wanted, {len(self.free)} free")
+
     def step(self, x, q_len):
-        """x [sum(q_len)][hidden], request after request: the layer's output for the new tokens."""
+        """x [sum(q_len)][hidden], request after request: the layer's output for the new tokens.  A step that is refused (too many
+        tokens, not enough pages) changes nothing."""
         n, hq, hkv, d = x.shape[0], self.hq, self.hkv, self.d
+        self._check_step(n, q_len)
+        qkv = (x @ self.w_qkv).view(n, hq + 2 * hkv, d)
         positions = []
         for r, a in enumerate(q_len):
             positions += range(self.seen[r], self.seen[r] + a)
@@ -68,7 +81,6 @@ class PagedLayer:
             self.held[r] += self._take(-(-self.rows[r] // self.page) - len(self.held[r]))
         batch = self._batch(q_len)
         positions = torch.tensor([positions], dtype=torch.int32, device=self.device)
-        qkv = (x @ self.w_qkv).view(n, hq + 2 * hkv, d)
         q, out, lse = (torch.empty(n, hq, d, dtype=x.dtype, device=self.device), torch.empty(n, hq, d, dtype=x.dtype, device=self.device),
                        torch.empty(n, hq, device=self.device))
         scale = 1.0 / math.sqrt(d)

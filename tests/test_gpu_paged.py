@@ -690,3 +690,28 @@ def test_evictions_whose_numbers_do_not_fit_32_bits_are_refused(kw):
         P.arkv_paged_evict(pages, batch, torch.tensor([50], dtype=torch.int32, device="cuda"), torch.tensor([s.spare], dtype=torch.int32, device="cuda"),
                            kept, lens, workspace=ws, **kw)
     assert (kept == 9).all() and int(lens) == 9
+
+
+def test_a_refused_step_of_the_example_changes_nothing():
+    """Out of pages for the rows, or for the eviction behind them, or too many tokens: the next step goes on as if it had not been tried."""
+    from paper_2603_08727_amd.paged_example import PagedLayer
+    layers = [PagedLayer(2, n_pages=12, limit=96, budget=64, max_tokens=64) for _ in range(2)]
+    g = torch.Generator(device="cuda").manual_seed(5)
+
+    def rows(n):
+        return torch.randn(n, 512, generator=g, device="cuda").to(BF)
+
+    for q_len, bad in [([60, 20], [(RuntimeError, [64, 64])]),         # 14 pages for the rows alone
+                       ([30, 30], [(RuntimeError, [64, 1]), (ValueError, [65, 0]), (ValueError, [1]), (ValueError, [2, -1])]),
+                       ([1, 1], [(RuntimeError, [10, 1])])]:           # 101 rows have their pages, but not the 4 to cut them into
+        x = rows(sum(q_len))
+        want = layers[0].step(x, list(q_len))
+        assert torch.equal(layers[1].step(x, list(q_len)), want)
+        for error, refused in bad:
+            state = [str(getattr(layers[1], n)) for n in ("free", "held", "rows", "seen")] + [layers[1].table.clone(), layers[1].pages.k.clone()]
+            with pytest.raises(error):
+                layers[1].step(rows(max(0, sum(refused))), refused)
+            assert state[:4] == [str(getattr(layers[1], n)) for n in ("free", "held", "rows", "seen")]
+            assert torch.equal(state[4], layers[1].table) and torch.equal(state[5], layers[1].pages.k)
+    x = rows(2)
+    assert torch.equal(layers[0].step(x, [1, 1]), layers[1].step(x, [1, 1]))

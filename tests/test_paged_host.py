@@ -298,3 +298,11 @@ def test_numbers_that_do_not_fit_32_bits_are_refused():
     for name in kw:
         with pytest.raises(ValueError, match="32 bits"):
             P.arkv_debug_paged_row(np.zeros(4, np.int32), **{**kw, name: kw[name] + (1 << 32)})
+
+
+@pytest.mark.parametrize("budget", [0, -1, 65])
+def test_the_example_refuses_budgets_that_no_cut_can_meet(budget):
+    """With a budget above the limit a request would count rows that it never had."""
+    from paper_2603_08727_amd.paged_example import PagedLayer
+    with pytest.raises(ValueError, match="budget"):
+        PagedLayer(1, limit=64, budget=budget, device="cpu")
