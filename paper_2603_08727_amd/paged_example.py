@@ -39,7 +39,9 @@ class PagedLayer:
         self.seen = [0] * n_requests                   # tokens it has had: the next one's position
         # the step's arrays live as long as the server: a captured step would find them where they were
         self.table = torch.full((n_requests, self.width), -1, dtype=torch.int32, device=device)
-        self.workspace = None
+        lengths = torch.zeros(n_requests + 1, dtype=torch.int32, device=device)
+        largest = P.arkv_page_batch(lengths, lengths[1:], self.table, n_requests * max_tokens, max_tokens, self.width * page_size)
+        self.workspace = P.arkv_paged_workspace(self.pages, largest, n_q_heads)        # serves every smaller batch
 
     def _take(self, n):
         got, self.free = self.free[:n], self.free[n:]
@@ -51,12 +53,8 @@ class PagedLayer:
             if held:
                 self.table[r, :len(held)] = torch.tensor(held, dtype=torch.int32, device=dev)
         cu = torch.tensor([sum(q_len[:i]) for i in range(len(q_len) + 1)], dtype=torch.int32, device=dev)
-        batch = P.arkv_page_batch(cu, torch.tensor(self.rows, dtype=torch.int32, device=dev), self.table, sum(q_len),
-                                  max(q_len), max(self.rows))
-        need = P.arkv_paged_workspace_bytes(self.pages, batch, self.hq)
-        if self.workspace is None or self.workspace.numel() < need:
-            self.workspace = P.arkv_paged_workspace(self.pages, batch, self.hq)
-        return batch
+        return P.arkv_page_batch(cu, torch.tensor(self.rows, dtype=torch.int32, device=dev), self.table, sum(q_len), max(q_len),
+                                 max(self.rows))
 
     def _check_step(self, n, q_len):
         if len(q_len) != len(self.rows) or sum(q_len) != n or not all(0 <= a <= self.max_tokens for a in q_len):
