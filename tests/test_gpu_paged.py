@@ -715,3 +715,93 @@ def test_a_refused_step_of_the_example_changes_nothing():
             assert torch.equal(state[4], layers[1].table) and torch.equal(state[5], layers[1].pages.k)
     x = rows(2)
     assert torch.equal(layers[0].step(x, [1, 1]), layers[1].step(x, [1, 1]))
+
+
+def ragged(chunks, many):
+    """130 sequences: single tokens and a chunk now and then, empty ones and absent ones around the 64th and the 128th."""
+    q = [0 if b in (0, 62, 64, 127) else chunks[b % len(chunks)] if b in (1, 61, 63, 65, 100, 126, 128, 129) else 1 for b in range(130)]
+    kv = [0 if b in (64, 101) else a + 5 + 37 * b % 211 for b, a in enumerate(q)]
+    if many:
+        kv[3], kv[66], kv[129] = 17001, 3000, 2500     # nine pieces: joined by a launch
+    return q, kv
+
+
+@pytest.mark.parametrize("chunks,many", [((2, 40, 150), False), ((3, 1, 300), True), ((1, 2), False), ((2,), True)])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(BF, 16, 8, 64), (FP, 6, 2, 128)])
+def test_batches_of_more_than_64_sequences(dtype, hq, hkv, d, chunks, many):
+    """Searches for a token's sequence go round more than once, in append, attention and its joins; weights of all sequences."""
+    q, kv = ragged(chunks, many)
+    s = R.problem("cuda", dtype, hq, hkv, d, 16, q, kv, seed=83, extra_tokens=2, fused=True)
+    s.table[5, 0] = -1
+    g = torch.Generator().manual_seed(6)
+    freq = (10000.0 ** (-torch.arange(d // 2, dtype=torch.float64) / (d // 2))).cuda()
+    positions = torch.randint(0, 100000, (1, s.n), generator=g, dtype=torch.int32).cuda()
+    new = torch.randn(s.n, 2 * hkv, d, generator=g).to(dtype).cuda()
+    pages, batch, ws = handles(s)
+    want = {n: getattr(s, n).clone() for n in ("k", "v", "pos", "weight")}
+    q_out = torch.full((s.n, hq, d), 7.0, dtype=dtype, device="cuda")
+    P.arkv_paged_append(pages, batch, P.arkv_rotary(freq), s.q, new[:, :hkv], new[:, hkv:], positions, q_out)
+    n = sum(q)
+    check_append(s, want, new[:, :hkv], new[:, hkv:], positions, freq, [0] * (d // 2), False, q_out)
+    assert (q_out[n:] == 7).all()
+    _, lse = check_attention(s)
+    ref, tol = R.weights(s, lse, 0.5, s.weight)
+    P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=0.5, workspace=ws)
+    R.close(s.weight, ref, tol, "weight")
+
+
+def check_append(s, before, kn, vn, positions, freq, axis, adjacent, q_out):
+    """Turned queries, and pools that differ from `before` in the new tokens' slots alone."""
+    n = sum(s.q_len)
+    (rq, tq), (rk, tk) = (R.rotate(x[:n], positions[:, :n], freq, axis, adjacent) for x in (s.q, kn))
+    R.close(q_out[:n], rq, tq, "q")
+    b = torch.repeat_interleave(torch.arange(s.B), torch.tensor(s.q_len))
+    i = torch.cat([torch.arange(a) for a in s.q_len])
+    slot = (torch.tensor(s.kv_len_list) - torch.tensor(s.q_len))[b] + i
+    page = s.table.cpu()[b, slot.clamp(min=0) // s.page].long()
+    there = (slot >= 0) & (page >= 0) & (page < s.n_pages)
+    t, page, off = torch.arange(n)[there].cuda(), page[there].cuda(), (slot[there] % s.page).cuda()
+    R.close(s.k[page, :, off], rk[t], tk[t], "k")
+    before["k"][page, :, off] = s.k[page, :, off]
+    before["v"][page, :, off] = vn[t]
+    before["pos"][page, :, off] = positions[0, t][:, None].expand(-1, s.hkv)
+    before["weight"][page, :, off] = 0.0
+    for name, want in before.items():
+        assert torch.equal(getattr(s, name).view(torch.uint8), want.view(torch.uint8)), name
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("q,kv", [((1,) * 16, tuple(range(1, 1600, 100))), ((5, 11), (5, 900)), ((2100,), (2131,)), ((700, 1400, 3), (700, 1500, 40))])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(BF, 32, 8, 128), (FP, 40, 5, 64), (BF, 64, 8, 128)])
+def test_appends_whose_tokens_are_several_waves_or_rounds(dtype, hq, hkv, d, q, kv, adjacent):
+    """Few tokens are dealt out over waves by their heads, many (from 2048 on) are one wave's each, in several rounds."""
+    s = R.problem("cuda", dtype, hq, hkv, d, 16, q, kv, seed=84, fused=True)
+    g = torch.Generator().manual_seed(7)
+    freq = (10000.0 ** (-torch.arange(d // 2, dtype=torch.float64) / (d // 2))).cuda()
+    axis = [i % 3 for i in range(d // 2)]
+    positions = torch.randint(0, 1 << 20, (3, s.n), generator=g, dtype=torch.int32).cuda()
+    new = torch.randn(s.n, 2 * hkv, d, generator=g).to(dtype).cuda()
+    want = {n: getattr(s, n).clone() for n in ("k", "v", "pos", "weight")}
+    pages, batch, _ = handles(s)
+    q_out = torch.empty((s.n, hq, d), dtype=dtype, device="cuda")
+    P.arkv_paged_append(pages, batch, P.arkv_rotary(freq, axis, 3, adjacent), s.q, new[:, :hkv], new[:, hkv:], positions, q_out)
+    check_append(s, want, new[:, :hkv], new[:, hkv:], positions, freq, axis, adjacent, q_out)
+
+
+@pytest.mark.parametrize("q,d,page", [(1, 64, 64), (1, 128, 16), (4, 64, 16)])
+@pytest.mark.parametrize("far", [False, True])
+def test_weights_of_many_rows_per_wave(q, d, page, far):
+    """16 x 8 units of thousands of rows: five to nine tiles a wave, lengths that end inside one, absent pages."""
+    kv = [9001 if d == 64 else 5003] + [4000 + 331 * b for b in range(14)] + [70]
+    s = R.problem("cuda", BF, 32, 8, d, page, (q,) * 16, kv, seed=85)
+    s.table[1, 7], s.table[2, 30] = -1, s.n_pages
+    kw = {}
+    if far:
+        kw["slopes"], kw["q_pos"] = slopes_of(s)
+    _, lse = attend(s, **kw)
+    pages, batch, ws = handles(s)
+    for decay, other in [(0.75, False), (1.0, True), (0.0, False)]:
+        carried = torch.rand_like(s.weight) if other else s.weight.clone()
+        ref, tol = R.weights(s, lse, decay, carried, **kw)
+        P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=decay, carried=carried if other else None, workspace=ws, **kw)
+        R.close(s.weight, ref, tol, "weight")
