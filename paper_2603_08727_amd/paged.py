@@ -179,6 +179,10 @@ def _rows(to, t, n, pages, what):
             to.token_stride, to.head_stride, channel = t.stride()
             if channel != 1:
                 raise ValueError(f"{what}: channels must be adjacent")
+            if tokens == 1:                            # (a stride that nothing is multiplied by can be any number in torch)
+                to.token_stride = 0
+            if heads == 1:
+                to.head_stride = 0
             to.p = t.data_ptr()
             return heads
     raise ValueError(f"{what}: expected {pages.dtype} [{n}][heads][{pages.d}] on {pages.device}, got {t.dtype} {tuple(shape)} on {t.device}")

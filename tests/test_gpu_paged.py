@@ -805,3 +805,24 @@ def test_weights_of_many_rows_per_wave(q, d, page, far):
         ref, tol = R.weights(s, lse, decay, carried, **kw)
         P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=decay, carried=carried if other else None, workspace=ws, **kw)
         R.close(s.weight, ref, tol, "weight")
+
+
+@pytest.mark.parametrize("n,h", [(1, 8), (5, 1), (1, 1)])
+def test_strides_of_a_single_token_or_head_do_not_matter(n, h):
+    """torch gives such axes any stride: here 1, which no row could have."""
+    s = R.problem("cuda", BF, h, 1, 64, 16, (n,), (90,), seed=86)
+    new = torch.randn(n, 1, 64, device="cuda").to(BF)
+    q, out = s.q, []
+    for odd in (False, True):
+        if odd:
+            strides = (1 if n == 1 else q.stride(0), 1 if h == 1 else q.stride(1), 1)
+            s.q, new = q.as_strided(q.shape, strides), new.as_strided(new.shape, (1 if n == 1 else 64, 1, 1))
+        pages, batch, ws = handles(s)
+        turned = torch.empty_like(q)
+        P.arkv_paged_append(pages, batch, P.arkv_rotary(None), s.q, new, new, torch.arange(n, dtype=torch.int32, device="cuda")[None].contiguous(), turned)
+        o, lse = check_attention(s)
+        P.arkv_paged_weights(pages, batch, s.q, s.scale, lse, decay=0.0, workspace=ws)
+        out.append([turned, o, lse, s.k.nan_to_num(5.0), s.weight.nan_to_num(5.0)])
+        out[-1] = [x.clone() for x in out[-1]]
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
