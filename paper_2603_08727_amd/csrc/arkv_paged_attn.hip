@@ -290,13 +290,16 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
       return sum;
     };
     float sum = probs();
-    if (__any(!(sum <= kSumLimit))) {
+    uint64_t big = __ballot(!(sum <= kSumLimit));
+    if (big) {
+      big |= big >> 32;                                            // of the four lanes of a row any one: that row alone moves
+      big |= big >> 16;
       float top = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i >> 2][i & 3] * mul);
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float mn = fmaxf(m, top), f = exp2_hw(m - mn);         // every lane of a row moves alike
+      const float mn = big >> n & 1 ? fmaxf(m, top) : m, f = exp2_hw(m - mn);
       m = mn;
       l *= f;
 #pragma unroll

@@ -826,3 +826,17 @@ def test_strides_of_a_single_token_or_head_do_not_matter(n, h):
         out[-1] = [x.clone() for x in out[-1]]
     for a, b in zip(*out):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("what", [math.nan, 40.0])
+@pytest.mark.parametrize("q,kv", [((2,), (8190,)), ((4,), (20001,)), ((40,), (5000,))])
+def test_rows_are_independent_to_the_bit(q, kv, what, dtype):
+    """A key that the last token alone sees, in a tile behind a wave's first: the rounding of the other tokens' rows does not change either."""
+    s = R.problem("cuda", dtype, 8, 2, 64, 16, q, kv, seed=87)
+    clean, clean_lse = attend(s)
+    last = kv[0] - 1
+    s.k[int(s.table[0, last // 16]), :, last % 16] = what if what != what else s.q[-1, ::4] * what
+    out, lse = attend(s)
+    assert not torch.equal(out[-1], clean[-1])
+    assert torch.equal(out[:-1], clean[:-1]) and torch.equal(lse[:-1], clean_lse[:-1])
