@@ -73,7 +73,7 @@ typedef struct {
 } arkv_rotary;
 
 /* How a logit comes about: x = scale q.k; with cap > 0: x = cap tanh(x / cap); with slopes (DEVICE float [H_q]):
- * x -= slopes[h] |q_pos - pos|, q_pos DEVICE int32 [n_tokens], pos the cached row's.  New token i of sequence b sees the
+ * x -= slopes[h] |q_pos - pos|, q_pos DEVICE int32 [n_tokens], pos the cached row's (less than 2^31 apart).  New token i of sequence b sees the
  * slots up to its own, j <= ctx_b + i, and with prefix (DEVICE int32 [B]) every slot j < prefix[b]; all of them < kv_len[b].
  * The cap puts x off by 2^-22 cap at most; one above 256 by 2^-19 of x. */
 typedef struct {
@@ -94,8 +94,9 @@ int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, con
 
 /* Bytes of DEVICE workspace that the calls below need for this batch and any of their options (64 KiB or more).  HOST, pure.
  * The first 64 KiB must be zero before the workspace's first use; every call leaves them zero, so one workspace serves calls one
- * after the other.  It is large enough for every batch of the same head_dim, H_kv and H_q whose batch, n_tokens, max_q and max_kv are none of them
- * larger than here (up to 136 MB where chunks may meet long contexts at d = 128: few rows are cut finest).  Calls that may overlap in time need workspaces of their own. */
+ * after the other.  It is large enough for every batch of the same head_dim, H_kv and H_q whose batch, n_tokens, max_q and max_kv are none of
+ * them larger than here: at most 136 MB for chunks (fewer rows are cut finer), and 8 KB for each 2048 rows of a kv-head for single tokens.
+ * Calls that may overlap in time need workspaces of their own. */
 int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, int32_t n_q_heads, size_t* bytes);
 
 /* out [n_tokens][H_q][d] (dense, DEVICE, of the pages' dtype) = softmax over the visible slots of x, times v.  lse DEVICE float

@@ -27,7 +27,7 @@ constexpr int kAppendWaves = 4, kAppendItems = 3;
 // One wave per new token (or a share of its heads).  The wave's lanes form the token's angles (position times frequency in turns, in 64 bits: at
 // position 2^17 a 32-bit product is off by up to 2^-8 turns; the fraction that is left fits 32), then walk its heads'
 // 16-byte chunks in pairs: item i of a row is the pair of chunks whose channels turn together.  A generated token is bound by
-// round trips to memory: its lengths, angles and rows are requested together, the page behind them, then it stores (16 tokens: 4.5 us);
+// round trips to memory: its lengths, angles and rows are requested together, the page behind them, then it stores (16 tokens: 5.1 us);
 // many by memory itself (7817 tokens of 32 + 2 x 8 heads: 43 us, 4.5 TB/s).
 template <typename T, int D>
 __global__ __launch_bounds__(64 * kAppendWaves) void k_paged_append(AppendArgs A, int per_wave) {
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_paged_append(AppendArgs A
 
 hipError_t launch_paged_append(int dtype, int D, const AppendArgs& A, hipStream_t st) {
   // A token is one wave's work where there are tokens for the whole chip; fewer are dealt out, one load of each lane's at a
-  // time (16 tokens of 32 + 2 x 8 heads: 6.9 us as one wave each, 5.3 as two).
+  // time (16 tokens of 32 + 2 x 8 heads: 7.0 us as one wave each, 5.1 as two).
   const int n_all = (A.Hq + 2 * A.P.H) * (D / 16), once = 64 * kAppendItems;
   const int per_wave = A.P.N >= 2048 ? n_all : once;
   const dim3 grid((A.P.N + kAppendWaves - 1) / kAppendWaves, (n_all + per_wave - 1) / per_wave), block(64 * kAppendWaves);
@@ -529,7 +529,7 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs A, Evi
 }
 
 // Lists the survivors among 256 slots, a slot per lane, and copies them: the units' slots are spread over the whole chip (8192 of 32768
-// rows of 32 units, 272 MB: 62 us, 4.4 TB/s).
+// rows of 32 units, 272 MB: 63 us, 4.3 TB/s).
 template <int D>
 __global__ __launch_bounds__(kEvictSlots) void k_evict_move(EvictArgs A, EvictCut cut, EvictParts parts) {
   constexpr int NW = kEvictSlots / 64, RPW = kEvictSlots / (D / 8);
@@ -594,7 +594,7 @@ static hipError_t launch_evict(const EvictArgs& A, hipStream_t st) {
     }
     k_evict_select<N, 0><<<grid, kEvictThreads, 0, st>>>(A, cut, parts);
   };
-  // (8 x 2 units of 1000 rows: 9.5 us; with the code of nine steps, which has to come from memory, 14.0)
+  // (8 x 2 units of 1000 rows: 9.2 us; with the code of nine steps, which has to come from memory, 11.9)
   if (P.max_kv <= kEvictRows) select(std::integral_constant<int, 1>());
   else if (P.max_kv <= kEvictRegs * kEvictRows) select(std::integral_constant<int, kEvictRegs>());
   else select(std::integral_constant<int, 0>());

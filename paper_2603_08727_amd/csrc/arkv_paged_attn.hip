@@ -5,7 +5,7 @@
 //   paged_step   up to 16 rows (a generated token, a few drafted ones): bound by reading the pages (4 x 131071 rows x 8 heads in
 //                377 us, 5.7 TB/s; 31 requests of up to 16384 rows in 184 us, 4.9 TB/s)
 //   paged_chunk  more rows: bound by the matrix cores and the exponentials between them (2 x 2048 tokens of 16384, 32 heads, in
-//                950 us, 1.08 PFLOP/s)
+//                917 to 938 us, 1.10 to 1.12 PFLOP/s)
 // Both split a sequence's keys over workgroups where that fills the chip.  The last workgroup to finish joins up to 16 pieces, a
 // launch of k_paged_merge more than that.
 //
@@ -13,6 +13,9 @@
 // probabilities are, as they lie, the B operand of O^T = V^T P^T once the contraction index is read in their order; the
 // matching A operand comes out of row-major values in LDS by transposing reads (ds_read_b64_tr_b16: sixteen lanes read a
 // 4 x 16 block, four lanes a row, and get a column each).
+// Probabilities are rounded to the pages' type on the way into the second product, whose operands have that type: off by half a step each,
+// in either direction, as the output's own rounding is once; the denominator sums them as they were (16384 rows in bf16: outputs 2.0e-3 from
+// 64 bits, of which 1.7e-3 is the output's rounding).
 // The softmax reference of a row is lazy: probabilities are taken against the row's present reference, which moves to the
 // tile's maximum only when a lane's sum shows that they grew large (or when it is unset).
 // Pages are at least 16 slots, so the 16 rows from a multiple of 16 on (a granule) lie in one page, whose id is uniform.

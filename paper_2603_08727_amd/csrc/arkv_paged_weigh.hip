@@ -17,7 +17,7 @@ __device__ __forceinline__ void store_weight(const PagedAttnArgs& A, int row, fl
   A.P.weight[row] = (A.decay == 0.f ? 0.f : A.decay * A.carried[row]) + sum;
 }
 
-// Few rows: bound by reading the keys (16 x 8192 rows x 8 heads: 50 us, 4.7 TB/s).  A wave takes wave_keys keys, 32 at a time (two granules), the next 32 in flight.
+// Few rows: bound by reading the keys (16 requests of 5960 to 8192 rows x 8 heads, 233 MB: 50 us, 4.7 TB/s).  A wave takes wave_keys keys, 32 at a time (two granules), the next 32 in flight.
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(256) void k_weigh_step(PagedAttnArgs A, int wave_keys) {
   constexpr int CAP = Mode<MODE>::cap;
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void k_weigh_step(PagedAttnArgs A, int wave_ke
 // Many rows: bound by the matrix cores and the exponentials.  One workgroup = 256 keys of a (sequence, kv-head), 64 per wave,
 // held in registers as B operands, and a share of the rows that see them; rows come through LDS, 64 at a time, the next 64
 // on their way.  The logits' MFMAs of the next 32 rows stand between the exponentials of these (2 x 1024 tokens over 8191 rows, 32 heads:
-// 144 us, 0.9 PFLOP/s; with the two one behind the other 188).
+// 146 us, 0.9 PFLOP/s; with the two one behind the other, as with a cap or a bias, 169).
 constexpr int kWeighBufs = 3;           // rows in use, the next ones (their first half is ahead), the ones on their way
 template <int D> struct WeighLds {
   uint16_t q[kWeighBufs][kWeighRows * D];
