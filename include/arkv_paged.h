@@ -86,7 +86,7 @@ typedef struct {
 /* Turns q and k of the new tokens and stores k, v into their slots: q_out [n_tokens][H_q][d] (dense, DEVICE), rows k and v of
  * the pages, pos = positions[0][token], weight = 0.  positions DEVICE int32 [n_axes][n_tokens].  Angles are formed in 64
  * bits, products in 32, each result rounded once.  q.p may equal q_out (in place) if it is dense too.  q = NULL and q_out = NULL: keys and values only.
- * ARKV_EINVAL: null pointers, sizes, alignment, an axis >= n_axes.  ARKV_EUNSUPPORTED: head_dim, dtype, n_pages H_kv page_size >= 2^31,
+ * ARKV_EINVAL: null pointers, sizes, alignment, an axis >= n_axes, q.p = q_out with other strides.  ARKV_EUNSUPPORTED: head_dim, dtype, n_pages H_kv page_size >= 2^31,
  * n_tokens > 2^26 - 4. */
 int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_rotary* rotary, int32_t n_q_heads,
                       const arkv_rows* q, const arkv_rows* k, const arkv_rows* v, const int32_t* positions, void* q_out,

@@ -91,6 +91,9 @@ int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, con
     if (n_q_heads < 1 || !aligned16(q_out)) return ARKV_EINVAL;
     TRY(check_rows(q, A.P.N, A.q));
     if (n_q_heads > 65535) return ARKV_EUNSUPPORTED;
+    // in place, every row has to lie where it is stored: other rows are still to be read
+    const int64_t d = pages->head_dim;
+    if (q->p && q->p == q_out && ((A.P.N > 1 && q->token_stride != n_q_heads * d) || (n_q_heads > 1 && q->head_stride != d))) return ARKV_EINVAL;
     A.Hq = n_q_heads;
   }
   A.q_out = q_out; A.positions = positions;

@@ -306,3 +306,12 @@ def test_the_example_refuses_budgets_that_no_cut_can_meet(budget):
     from paper_2603_08727_amd.paged_example import PagedLayer
     with pytest.raises(ValueError, match="budget"):
         PagedLayer(1, limit=64, budget=budget, device="cpu")
+
+
+@pytest.mark.parametrize("token_stride,head_stride", [(768, 64), (512, 128), (256, 64), (512, 0)])
+def test_appends_in_place_of_rows_that_are_not_dense_are_refused(token_stride, head_stride):
+    """Stored rows would lie over rows that are still to be read."""
+    pages, batch, rows, rot, sc = _args()
+    kv, q = P._Rows(0x100000, 128, 64), P._Rows(0x200000, token_stride, head_stride)
+    assert P.load().arkv_paged_append(C.byref(pages), C.byref(batch), C.byref(rot), 8, C.byref(q), C.byref(kv), C.byref(kv), ADDR, 0x200000,
+                                      None) == A.EINVAL
