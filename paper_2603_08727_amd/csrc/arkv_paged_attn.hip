@@ -5,7 +5,7 @@
 //   paged_step   up to 16 rows (a generated token, a few drafted ones): bound by reading the pages (4 x 131071 rows x 8 heads in
 //                377 us, 5.7 TB/s; 31 requests of up to 16384 rows in 184 us, 4.9 TB/s)
 //   paged_chunk  more rows: bound by the matrix cores and the exponentials between them (2 x 2048 tokens of 16384, 32 heads, in
-//                917 to 938 us, 1.10 to 1.12 PFLOP/s)
+//                917 to 946 us, 1.09 to 1.12 PFLOP/s)
 // Both split a sequence's keys over workgroups where that fills the chip.  The last workgroup to finish joins up to 16 pieces, a
 // launch of k_paged_merge more than that.
 //
