@@ -114,7 +114,8 @@ int arkv_paged_attention(const arkv_pages* pages, const arkv_page_batch* batch, 
  * use (slots of no sequence are left alone).  carried: DEVICE, laid out as weight; NULL or weight itself: in place; another
  * array: e.g. the weights before drafted tokens that may be rejected.  With decay = 0 carried is not read.  lse DEVICE float [n_tokens][H_q], what
  * arkv_paged_attention returned for the same batch, scores and q.  Pages that several sequences of the batch share would be updated
- * by each: their weight is the last writer's.  Sums are fp32, in an order that the sizes alone fix. */
+ * by each: their weight is the last writer's.  Sums are fp32, in an order that the sizes alone fix;
+ * terms below 2^-126 count as zero. */
 int arkv_paged_weights(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,
                        int32_t n_q_heads, const arkv_rows* q, const float* lse, float decay, const float* carried,
                        void* workspace, size_t bytes, void* hip_stream);
