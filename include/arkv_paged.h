@@ -1,7 +1,8 @@
 /*
  * libarkv, operators around a paged cache - for servers that keep many requests' rows in pages of one pool: rotary
  * positions on the way into the pages, attention of the requests' new tokens over them, the attention weight that every
- * cached row collected, and eviction by that weight.
+ * cached row collected, and eviction by that weight.  Pages may hold rows of 16 bits, or packed ones of 8 or 4 bits a channel
+ * (arkv_packed_*); tokens may see all rows up to their own, or those that a window or a tree of drafted tokens leaves (arkv_sight).
  *
  * C ABI, the conventions of arkv.h: every call returns 0 or a negative ARKV_E* code, nothing throws, every call is
  * asynchronous on hip_stream (a hipStream_t as void*, NULL = the default stream).  Here the caller owns all memory: no
@@ -83,6 +84,29 @@ typedef struct {
   const int32_t* prefix;
 } arkv_scores;
 
+/* Which slots new token i of sequence b sees, where that is not all up to its own, p = ctx_b + i.  window w > 0: the slots j <= p with
+ * j > p - w or j < sink.  tree (DEVICE uint64 [n_tokens][tree_words], 8-byte aligned, tree_words >= max_q / 64): bit t of the token's words says
+ * whether it sees new token t, itself among them; the slots below ctx_b it sees all, or with a window as a token at p = ctx_b + (new tokens it
+ * sees) - 1 (the window takes no new token away).  Bits from q_len[b] on count for nothing.  A prefix of the scores is seen besides.  All zero: no limits. */
+typedef struct {
+  int32_t window, sink, tree_words;
+  const uint64_t* tree;
+} arkv_sight;
+
+/* One layer's packed pages: k, v DEVICE [n_pages][H_kv][page_size][d bits / 8], k_scale, v_scale DEVICE uint8 [n_pages][H_kv][page_size][d / 32],
+ * pos as in arkv_pages.  A row's channels lie in blocks of 32, each with a scale byte s; a channel is its code's value times 2^(s - 127).
+ * bits = 8: a code is a byte: sign, 4 bits of exponent (bias 7), 3 of mantissa, 127 and 255 NaN, the largest value 448; 4: half a byte (an even
+ * channel's the low half): sign, 2 bits of exponent (bias 1), 1 of mantissa, the largest value 6.  s = 255: NaN, the whole block.
+ * dtype: of the rows that go in and come out, and of q.  All five 16-byte aligned; sizes as in arkv_pages. */
+typedef struct {
+  int32_t dtype, bits, n_pages, page_size, n_kv_heads, head_dim;
+  void* k;
+  void* v;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int32_t* pos;
+} arkv_packed_pages;
+
 /* Turns q and k of the new tokens and stores k, v into their slots: q_out [n_tokens][H_q][d] (dense, DEVICE), rows k and v of
  * the pages, pos = positions[0][token], weight = 0.  positions DEVICE int32 [n_axes][n_tokens].  Angles are formed in 64
  * bits, products in 32, each result rounded once.  q.p may equal q_out (in place) if it is dense too.  q = NULL and q_out = NULL: keys and values only.
@@ -109,6 +133,33 @@ int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, 
 int arkv_paged_attention(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,
                          int32_t n_q_heads, const arkv_rows* q, void* out, float* lse, void* workspace, size_t bytes,
                          void* hip_stream);
+
+/* The same, a token seeing the slots that sight says (NULL: arkv_paged_attention). What no token sees is not read, whole granules of 16
+ * slots at a time.  ARKV_EINVAL, besides: window or sink negative, tree_words too small, tree not aligned. */
+int arkv_paged_attention_sight(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,
+                               const arkv_sight* sight, int32_t n_q_heads, const arkv_rows* q, void* out, float* lse,
+                               void* workspace, size_t bytes, void* hip_stream);
+
+/* arkv_paged_append into packed pages.  k is turned in 64 bits, so that a code does not depend on how its angle was rounded; q_out is what
+ * arkv_paged_append gives.  A block's s is the smallest from 1 on with max|x| <= 448 (6) times 2^(s - 127); codes are the nearest ones, ties to
+ * the even one.  Channels that are not finite, or beyond the type's range once turned, count for nothing in max|x|; with 8 bits they are
+ * stored as NaN, with 4 their block is.  Where the nearest code's value would be beyond the type's range, the largest one that is not is stored. */
+int arkv_packed_append(const arkv_packed_pages* pages, const arkv_page_batch* batch, const arkv_rotary* rotary, int32_t n_q_heads,
+                       const arkv_rows* q, const arkv_rows* k, const arkv_rows* v, const int32_t* positions, void* q_out,
+                       void* hip_stream);
+
+/* The rows of the batch's new tokens (the last q_len[b] slots of each sequence: all of them, where q_len = kv_len) as their values:
+ * k, v [n_tokens][H_kv][d] (dense, DEVICE, of dtype, 16-byte aligned; either may be NULL).  Nothing is rounded, but values below the type's
+ * normal range.  A row without a slot, or in an absent page, is zeros. */
+int arkv_packed_read(const arkv_packed_pages* pages, const arkv_page_batch* batch, void* k, void* v, void* hip_stream);
+
+/* arkv_paged_workspace for arkv_packed_attention. */
+int arkv_packed_workspace(const arkv_packed_pages* pages, const arkv_page_batch* batch, int32_t n_q_heads, size_t* bytes);
+
+/* arkv_paged_attention over the values of packed rows; sight as in arkv_paged_attention_sight, or NULL. */
+int arkv_packed_attention(const arkv_packed_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,
+                          const arkv_sight* sight, int32_t n_q_heads, const arkv_rows* q, void* out, float* lse,
+                          void* workspace, size_t bytes, void* hip_stream);
 
 /* weight = decay * carried + sum of exp(x - lse) over the G heads of the row's group and the new tokens that see it, for every slot in
  * use (slots of no sequence are left alone).  carried: DEVICE, laid out as weight; NULL or weight itself: in place; another

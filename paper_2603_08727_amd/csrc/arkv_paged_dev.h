@@ -21,6 +21,9 @@ struct Rows { const void* p; int64_t ts, hs; };
 
 struct Scores { float scale, cap; const float* slopes; const int32_t *q_pos, *prefix; };
 
+// Which slots a token sees, where that is not all up to its own.  prefixed: the scores have a prefix.
+struct Sight { int window, sink, words; bool prefixed; const uint64_t* tree; };
+
 // One sequence, cut to what the launch was announced: nothing behind these numbers reaches outside the arrays.
 struct Seq { int q0, nq, kv; };
 __host__ __device__ inline Seq clamp_seq(int a, int e, int kv, int N, int max_q, int max_kv) {
@@ -60,6 +63,11 @@ struct AppendArgs {
 };
 hipError_t launch_paged_append(int dtype, int D, const AppendArgs& A, hipStream_t st);
 
+// Packed pages' scale bytes; where arkv_packed_read puts rows.
+struct PackedArgs { uint8_t *k_scale, *v_scale; void *k, *v; };
+hipError_t launch_packed_append(int dtype, int D, int bits, const AppendArgs& A, const PackedArgs& X, hipStream_t st);
+hipError_t launch_packed_read(int dtype, int D, int bits, const Paged& P, const PackedArgs& X, hipStream_t st);
+
 struct PagedAttnArgs {
   Paged P;
   Scores S;
@@ -70,14 +78,19 @@ struct PagedAttnArgs {
   float decay;
   const float* carried;
   float* ws;
+  Sight V;
+  const uint8_t *k_scale, *v_scale;   // of packed pages
 };
 // Floats of workspace: _floats: of this batch, _bound: of any that is no larger.
-size_t paged_attention_floats(const Paged& P, int D, int Hq);
+size_t paged_attention_floats(const Paged& P, const Sight& V, int D, int Hq);
 size_t paged_attention_bound(const Paged& P, int D, int Hq);
 size_t paged_weights_floats(const Paged& P, int Hq);
 size_t paged_weights_bound(const Paged& P, int Hq);
-long long paged_attention_workgroups(const Paged& P, int D, int Hq);   // of its largest launch
+long long paged_attention_workgroups(const Paged& P, const Sight& V, int D, int Hq);   // of its largest launch
 hipError_t launch_paged_attention(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
+hipError_t launch_paged_attention_sight(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
+hipError_t launch_packed_attention8(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
+hipError_t launch_packed_attention4(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
 hipError_t launch_paged_weights(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
 
 struct EvictArgs {

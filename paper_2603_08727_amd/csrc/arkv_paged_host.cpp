@@ -38,6 +38,14 @@ static int check(const arkv_pages* p, const arkv_page_batch* b, Paged& P) {
   return ARKV_OK;
 }
 
+// The same for packed pages: what they share with others is checked as theirs.
+static int check_packed(const arkv_packed_pages* p, const arkv_page_batch* b, Paged& P) {
+  if (!p || !p->k_scale || !p->v_scale || !aligned16(p->k_scale) || !aligned16(p->v_scale)) return ARKV_EINVAL;
+  if (p->bits != 8 && p->bits != 4) return ARKV_EUNSUPPORTED;
+  const arkv_pages shared = {p->dtype, p->n_pages, p->page_size, p->n_kv_heads, p->head_dim, p->k, p->v, p->pos, nullptr};
+  return check(&shared, b, P);
+}
+
 // (n: how many there are; arrays of none may have no address)
 static int check_rows(const arkv_rows* r, int n, Rows& out) {
   if (!r || (!r->p && n) || !aligned16(r->p) || r->token_stride < 0 || r->head_stride < 0 || r->token_stride % 8 || r->head_stride % 8)
@@ -54,7 +62,7 @@ static int check_heads(int n_q_heads, int H, int n_tokens, int& G) {
 
 // One size for all calls, so that a workspace serves every one of them: what this batch's need ...
 static size_t workspace_bytes(const Paged& P, int D, int Hq) {
-  return 4 * std::max({paged_attention_floats(P, D, Hq), paged_weights_floats(P, Hq), paged_evict_floats(P)});
+  return 4 * std::max({paged_attention_floats(P, {}, D, Hq), paged_weights_floats(P, Hq), paged_evict_floats(P)});
 }
 // ... and what no smaller batch's exceed.
 static size_t workspace_bound(const Paged& P, int D, int Hq) {
@@ -67,18 +75,28 @@ static int check_scores(const arkv_scores* s, Scores& out) {
   return ARKV_OK;
 }
 
+// s may be null: no limits.  Numbers that no slot reaches are cut, so that sums with them fit 32 bits.
+static int check_sight(const arkv_sight* s, const Paged& P, const Scores& x, Sight& out) {
+  out = {};
+  out.prefixed = x.prefix != nullptr;
+  if (!s) return ARKV_OK;
+  if (s->window < 0 || s->sink < 0) return ARKV_EINVAL;
+  if (s->tree && (s->tree_words < 1 || (int64_t)s->tree_words * 64 < P.max_q || ((uintptr_t)s->tree & 7))) return ARKV_EINVAL;
+  out.window = std::min(s->window, 1 << 29);
+  out.sink = s->window ? std::min(s->sink, 1 << 28) : 0;
+  out.tree = s->tree;
+  out.words = s->tree ? s->tree_words : 0;
+  return ARKV_OK;
+}
+
 #define TRY(expr) do { const int rc_ = (expr); if (rc_ != ARKV_OK) return rc_; } while (0)
 #define LAUNCH(expr) do { const hipError_t e_ = (expr); return e_ == hipSuccess ? ARKV_OK : hip_failure(e_, #expr); } while (0)
 
-extern "C" {
-
-int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_rotary* rotary, int32_t n_q_heads,
-                      const arkv_rows* q, const arkv_rows* k, const arkv_rows* v, const int32_t* positions, void* q_out,
-                      void* hip_stream) {
-  AppendArgs A = {};
-  TRY(check(pages, batch, A.P));
+// (A.P is filled already; d: channels of a row)
+static int append_args(int d, const arkv_rotary* rotary, int32_t n_q_heads, const arkv_rows* q, const arkv_rows* k, const arkv_rows* v,
+                       const int32_t* positions, void* q_out, AppendArgs& A) {
   if (!rotary || (!positions && A.P.N) || (!q != !q_out && A.P.N)) return ARKV_EINVAL;
-  if (rotary->rot_dim < 0 || rotary->rot_dim % 16 || rotary->rot_dim > pages->head_dim || rotary->n_axes < 1 || rotary->n_axes > 4 ||
+  if (rotary->rot_dim < 0 || rotary->rot_dim % 16 || rotary->rot_dim > d || rotary->n_axes < 1 || rotary->n_axes > 4 ||
       (rotary->adjacent != 0 && rotary->adjacent != 1) || (rotary->rot_dim && !rotary->freq))
     return ARKV_EINVAL;
   for (int i = 0; i < rotary->rot_dim / 2; ++i) {
@@ -92,16 +110,47 @@ int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, con
     TRY(check_rows(q, A.P.N, A.q));
     if (n_q_heads > 65535) return ARKV_EUNSUPPORTED;
     // in place, every row has to lie where it is stored: other rows are still to be read
-    const int64_t d = pages->head_dim;
-    if (q->p && q->p == q_out && ((A.P.N > 1 && q->token_stride != n_q_heads * d) || (n_q_heads > 1 && q->head_stride != d))) return ARKV_EINVAL;
+    if (q->p && q->p == q_out && ((A.P.N > 1 && q->token_stride != (int64_t)n_q_heads * d) || (n_q_heads > 1 && q->head_stride != d))) return ARKV_EINVAL;
     A.Hq = n_q_heads;
   }
   A.q_out = q_out; A.positions = positions;
-  A.freq = rotary->rot_dim ? rotary->freq : (const double*)pages->k;   // (read in any case, a branch would cost a round trip)
+  A.freq = rotary->rot_dim ? rotary->freq : (const double*)A.P.k;   // (read in any case, a branch would cost a round trip)
   A.half = rotary->rot_dim / 2; A.adjacent = rotary->adjacent; A.n_axes = rotary->n_axes;
-  if (!A.P.N) return ARKV_OK;
   if (A.P.N > 4 * kMostWorkgroups) return ARKV_EUNSUPPORTED;       // (four tokens a workgroup)
+  return ARKV_OK;
+}
+
+extern "C" {
+
+int arkv_paged_append(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_rotary* rotary, int32_t n_q_heads,
+                      const arkv_rows* q, const arkv_rows* k, const arkv_rows* v, const int32_t* positions, void* q_out,
+                      void* hip_stream) {
+  AppendArgs A = {};
+  TRY(check(pages, batch, A.P));
+  TRY(append_args(pages->head_dim, rotary, n_q_heads, q, k, v, positions, q_out, A));
+  if (!A.P.N) return ARKV_OK;
   LAUNCH(launch_paged_append(pages->dtype, pages->head_dim, A, (hipStream_t)hip_stream));
+}
+
+int arkv_packed_append(const arkv_packed_pages* pages, const arkv_page_batch* batch, const arkv_rotary* rotary, int32_t n_q_heads,
+                       const arkv_rows* q, const arkv_rows* k, const arkv_rows* v, const int32_t* positions, void* q_out,
+                       void* hip_stream) {
+  AppendArgs A = {};
+  TRY(check_packed(pages, batch, A.P));
+  TRY(append_args(pages->head_dim, rotary, n_q_heads, q, k, v, positions, q_out, A));
+  if (!A.P.N) return ARKV_OK;
+  const PackedArgs X = {pages->k_scale, pages->v_scale, nullptr, nullptr};
+  LAUNCH(launch_packed_append(pages->dtype, pages->head_dim, pages->bits, A, X, (hipStream_t)hip_stream));
+}
+
+int arkv_packed_read(const arkv_packed_pages* pages, const arkv_page_batch* batch, void* k, void* v, void* hip_stream) {
+  Paged P;
+  TRY(check_packed(pages, batch, P));
+  if (!aligned16(k) || !aligned16(v)) return ARKV_EINVAL;
+  if ((int64_t)P.N > 4 * kMostWorkgroups) return ARKV_EUNSUPPORTED;
+  if (!P.N || (!k && !v)) return ARKV_OK;
+  const PackedArgs X = {pages->k_scale, pages->v_scale, k, v};
+  LAUNCH(launch_packed_read(pages->dtype, pages->head_dim, pages->bits, P, X, (hipStream_t)hip_stream));
 }
 
 int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, int32_t n_q_heads, size_t* bytes) {
@@ -111,6 +160,16 @@ int arkv_paged_workspace(const arkv_pages* pages, const arkv_page_batch* batch, 
   TRY(check(pages, batch, P));
   TRY(check_heads(n_q_heads, P.H, P.N, G));
   *bytes = workspace_bound(P, pages->head_dim, n_q_heads);
+  return ARKV_OK;
+}
+
+int arkv_packed_workspace(const arkv_packed_pages* pages, const arkv_page_batch* batch, int32_t n_q_heads, size_t* bytes) {
+  Paged P;
+  int G;
+  if (!bytes) return ARKV_EINVAL;
+  TRY(check_packed(pages, batch, P));
+  TRY(check_heads(n_q_heads, P.H, P.N, G));
+  *bytes = 4 * std::max(paged_attention_floats(P, {}, pages->head_dim, n_q_heads), paged_attention_bound(P, pages->head_dim, n_q_heads));
   return ARKV_OK;
 }
 
@@ -135,8 +194,50 @@ int arkv_paged_attention(const arkv_pages* pages, const arkv_page_batch* batch, 
   if ((!out && A.P.N) || !aligned16(out)) return ARKV_EINVAL;
   A.out = out; A.lse = lse;
   if (!A.P.N || !A.P.max_q) return ARKV_OK;
-  if (paged_attention_workgroups(A.P, pages->head_dim, n_q_heads) > kMostWorkgroups) return ARKV_EUNSUPPORTED;
+  if (paged_attention_workgroups(A.P, {}, pages->head_dim, n_q_heads) > kMostWorkgroups) return ARKV_EUNSUPPORTED;
   LAUNCH(launch_paged_attention(pages->dtype, pages->head_dim, A, (hipStream_t)hip_stream));
+}
+
+// (A.P is filled already.)  done: there is nothing to launch.
+static int sight_args(int d, const arkv_scores* scores, const arkv_sight* sight, int32_t n_q_heads, const arkv_rows* q, void* out, float* lse,
+                      void* workspace, size_t bytes, PagedAttnArgs& A, bool& done) {
+  TRY(check_heads(n_q_heads, A.P.H, A.P.N, A.G));
+  TRY(check_scores(scores, A.S));
+  TRY(check_sight(sight, A.P, A.S, A.V));
+  TRY(check_rows(q, A.P.N, A.q));
+  A.Hq = n_q_heads;
+  if (!workspace || !aligned16(workspace) || bytes < 4 * paged_attention_floats(A.P, A.V, d, n_q_heads)) return ARKV_EINVAL;
+  A.ws = (float*)workspace;
+  if ((!out && A.P.N) || !aligned16(out)) return ARKV_EINVAL;
+  A.out = out; A.lse = lse;
+  done = !A.P.N || !A.P.max_q;
+  return !done && paged_attention_workgroups(A.P, A.V, d, n_q_heads) > kMostWorkgroups ? ARKV_EUNSUPPORTED : ARKV_OK;
+}
+
+int arkv_paged_attention_sight(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,
+                               const arkv_sight* sight, int32_t n_q_heads, const arkv_rows* q, void* out, float* lse,
+                               void* workspace, size_t bytes, void* hip_stream) {
+  if (!sight || (!sight->window && !sight->tree && sight->sink >= 0))
+    return arkv_paged_attention(pages, batch, scores, n_q_heads, q, out, lse, workspace, bytes, hip_stream);
+  PagedAttnArgs A = {};
+  bool done;
+  TRY(check(pages, batch, A.P));
+  TRY(sight_args(pages->head_dim, scores, sight, n_q_heads, q, out, lse, workspace, bytes, A, done));
+  if (done) return ARKV_OK;
+  LAUNCH(launch_paged_attention_sight(pages->dtype, pages->head_dim, A, (hipStream_t)hip_stream));
+}
+
+int arkv_packed_attention(const arkv_packed_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,
+                          const arkv_sight* sight, int32_t n_q_heads, const arkv_rows* q, void* out, float* lse,
+                          void* workspace, size_t bytes, void* hip_stream) {
+  PagedAttnArgs A = {};
+  bool done;
+  TRY(check_packed(pages, batch, A.P));
+  TRY(sight_args(pages->head_dim, scores, sight, n_q_heads, q, out, lse, workspace, bytes, A, done));
+  if (done) return ARKV_OK;
+  A.k_scale = pages->k_scale; A.v_scale = pages->v_scale;
+  const auto launch = pages->bits == 8 ? launch_packed_attention8 : launch_packed_attention4;
+  LAUNCH(launch(pages->dtype, pages->head_dim, A, (hipStream_t)hip_stream));
 }
 
 int arkv_paged_weights(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,

@@ -15,6 +15,7 @@ from .binding import ArkvError, EINVAL, EUNSUPPORTED, EHIP, OK  # noqa: F401
 TICKET_BYTES = 1 << 16                             # of a workspace's front, zero between calls
 
 EXPORTED = ["arkv_paged_append", "arkv_paged_workspace", "arkv_paged_attention", "arkv_paged_weights", "arkv_paged_evict",
+            "arkv_paged_attention_sight", "arkv_packed_append", "arkv_packed_read", "arkv_packed_workspace", "arkv_packed_attention",
             "arkv_debug_paged_row"]
 
 
@@ -41,6 +42,16 @@ class _Scores(C.Structure):
     _fields_ = [("scale", C.c_float), ("cap", C.c_float), ("slopes", C.c_void_p), ("q_pos", C.c_void_p), ("prefix", C.c_void_p)]
 
 
+class _Sight(C.Structure):
+    _fields_ = [("window", C.c_int32), ("sink", C.c_int32), ("tree_words", C.c_int32), ("tree", C.c_void_p)]
+
+
+class _Packed(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("bits", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("pos", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -57,6 +68,11 @@ def load():
             "arkv_paged_attention": [pg, bt, sc, i32, rw, vp, vp, vp, C.c_size_t, vp],
             "arkv_paged_weights": [pg, bt, sc, i32, rw, vp, C.c_float, vp, vp, C.c_size_t, vp],
             "arkv_paged_evict": [pg, bt, vp, i32, i32, i32, vp, i32, vp, vp, vp, C.c_size_t, vp],
+            "arkv_paged_attention_sight": [pg, bt, sc, vp, i32, rw, vp, vp, vp, C.c_size_t, vp],
+            "arkv_packed_append": [pg, bt, rt, i32, rw, rw, rw, vp, vp, vp],
+            "arkv_packed_read": [pg, bt, vp, vp, vp],
+            "arkv_packed_workspace": [pg, bt, i32, vp],
+            "arkv_packed_attention": [pg, bt, sc, vp, i32, rw, vp, vp, vp, C.c_size_t, vp],
             "arkv_debug_paged_row": [vp] + [i32] * 7 + [vp],
         }
         for name, args in sig.items():
@@ -115,6 +131,44 @@ class arkv_pages:
                         _dense(k, k.shape, k.dtype, "k"), _dense(v, k.shape, k.dtype, "v", dev),
                         _dense(pos, k.shape[:3], torch.int32, "pos", dev),
                         None if weight is None else _dense(weight, k.shape[:3], torch.float32, "weight", dev))
+        self.ref = C.addressof(self.c)
+
+
+class arkv_packed_pages:
+    """One layer's packed pages: k, v uint8 [n_pages][H_kv][page_size][d * bits / 8], k_scale, v_scale uint8
+    [n_pages][H_kv][page_size][d / 32] (their width says d, and with it bits), pos int32 [n_pages][H_kv][page_size]; dtype: bf16 or
+    fp16, of the rows that go in and come out."""
+
+    def __init__(self, k, v, k_scale, v_scale, pos, dtype):
+        torch = _TORCH or _torch()
+        _need(k.dim() == 4 and k_scale.dim() == 4, "k: [n_pages][H_kv][page_size][bytes], k_scale: [n_pages][H_kv][page_size][d / 32]")
+        _need(dtype in (torch.bfloat16, torch.float16), f"dtype: bf16 or fp16, got {dtype}")
+        self.k, self.v, self.k_scale, self.v_scale, self.pos = k, v, k_scale, v_scale, pos
+        self.device, self.dtype, self.index = k.device, dtype, k.get_device()
+        self.n_pages, self.H, self.page_size, width = k.shape
+        self.rows, self.d = k.shape[:3], 32 * k_scale.size(3)
+        _need(width in (self.d, self.d // 2), f"k: {width} bytes for {self.d} channels: 8 or 4 bits each")
+        self.bits = 8 if width == self.d else 4
+        dev, u8, scales = self.index, torch.uint8, (*self.rows, self.d // 32)
+        self.c = _Packed(0 if dtype == torch.bfloat16 else 1, self.bits, self.n_pages, self.page_size, self.H, self.d,
+                         _dense(k, k.shape, u8, "k"), _dense(v, k.shape, u8, "v", dev), _dense(k_scale, scales, u8, "k_scale", dev),
+                         _dense(v_scale, scales, u8, "v_scale", dev), _dense(pos, self.rows, torch.int32, "pos", dev))
+        self.ref = C.addressof(self.c)
+
+
+class arkv_sight:
+    """Which slots a new token sees: window rows back (0: all) and the first `sink`; of the new tokens those whose bits in tree say so
+    (int64 or uint64 [n_tokens][words] on the GPU; None: those up to itself)."""
+
+    def __init__(self, window=0, sink=0, tree=None):
+        torch = _TORCH or _torch()
+        _int32(window=window, sink=sink)
+        words = 0
+        if tree is not None:
+            _need(tree.dim() == 2 and tree.dtype in (torch.int64, torch.uint64), f"tree: int64 or uint64 [n_tokens][words], got {tree.dtype} {tuple(tree.shape)}")
+            words = tree.size(1)
+        self.tree, self.n_tokens, self.index = tree, None if tree is None else tree.size(0), None if tree is None else tree.get_device()
+        self.c = _Sight(window, sink, words, None if tree is None else _dense(tree, tree.shape, tree.dtype, "tree"))
         self.ref = C.addressof(self.c)
 
 
@@ -227,10 +281,7 @@ def arkv_paged_workspace(pages, batch, n_q_heads):
     return ws
 
 
-def arkv_paged_append(pages, batch, rotary, q, k, v, positions, q_out):
-    """q [n][H_q][d], k, v [n][H_kv][d] (strided), positions int32 [n_axes][n]; q and q_out may both be None."""
-    torch = _TORCH or _torch()
-    stream = _current(pages, batch)
+def _append(name, torch, stream, pages, batch, rotary, q, k, v, positions, q_out):
     n, H, o = batch.n_tokens, pages.H, _own.set
     if rotary.index != pages.index and rotary.index is not None:
         raise ValueError("freq: on another device than the pages")
@@ -242,9 +293,15 @@ def arkv_paged_append(pages, batch, rotary, q, k, v, positions, q_out):
     if q is not None:
         hq, rq = _rows(o.q, q, n, pages, "q"), o.rq
         to = _dense(q_out, (n, hq, pages.d), pages.dtype, "q_out", pages.index)
-    rc = (_lib or load()).arkv_paged_append(pages.ref, batch.ref, rotary.ref, hq, rq, o.rk, o.rv,
-                                            _dense(positions, (rotary.n_axes, n), torch.int32, "positions", pages.index), to, stream)
-    _check(rc, "arkv_paged_append")
+    rc = getattr(_lib or load(), name)(pages.ref, batch.ref, rotary.ref, hq, rq, o.rk, o.rv,
+                                       _dense(positions, (rotary.n_axes, n), torch.int32, "positions", pages.index), to, stream)
+    _check(rc, name)
+
+
+def arkv_paged_append(pages, batch, rotary, q, k, v, positions, q_out):
+    """q [n][H_q][d], k, v [n][H_kv][d] (strided), positions int32 [n_axes][n]; q and q_out may both be None."""
+    torch = _TORCH or _torch()
+    _append("arkv_paged_append", torch, _current(pages, batch), pages, batch, rotary, q, k, v, positions, q_out)
 
 
 def _scores(o, pages, batch, hq, scale, cap, slopes, q_pos, prefix):
@@ -275,6 +332,72 @@ def arkv_paged_attention(pages, batch, q, scale, out, lse=None, cap=0.0, slopes=
         _dense(out, (n, hq, pages.d), pages.dtype, "out", at), None if lse is None else _dense(lse, (n, hq), torch.float32, "lse", at),
         ws, size, stream)
     _check(rc, "arkv_paged_attention")
+
+
+def _sight(sight, pages, batch):
+    if sight is None:
+        return None
+    if sight.tree is not None and (sight.n_tokens != batch.n_tokens or sight.index != pages.index):
+        raise ValueError(f"tree: expected {batch.n_tokens} tokens on {pages.device}, got {sight.n_tokens} on {sight.tree.device}")
+    return sight.ref
+
+
+def arkv_paged_attention_sight(pages, batch, sight, q, scale, out, lse=None, cap=0.0, slopes=None, q_pos=None, prefix=None, workspace=None):
+    """arkv_paged_attention with an arkv_sight."""
+    torch = _TORCH or _torch()
+    stream = _current(pages, batch)
+    n, o, at = batch.n_tokens, _own.set, pages.index
+    hq = _rows(o.q, q, n, pages, "q")
+    ws, size = _workspace(workspace, pages)
+    rc = (_lib or load()).arkv_paged_attention_sight(
+        pages.ref, batch.ref, _scores(o, pages, batch, hq, scale, cap, slopes, q_pos, prefix), _sight(sight, pages, batch), hq, o.rq,
+        _dense(out, (n, hq, pages.d), pages.dtype, "out", at), None if lse is None else _dense(lse, (n, hq), torch.float32, "lse", at),
+        ws, size, stream)
+    _check(rc, "arkv_paged_attention_sight")
+
+
+def arkv_packed_append(pages, batch, rotary, q, k, v, positions, q_out):
+    """arkv_paged_append into packed pages."""
+    torch = _TORCH or _torch()
+    _append("arkv_packed_append", torch, _current(pages, batch), pages, batch, rotary, q, k, v, positions, q_out)
+
+
+def arkv_packed_read(pages, batch, k, v):
+    """k, v [n][H_kv][d] (out; either may be None): the values of the batch's new tokens' rows."""
+    _TORCH or _torch()
+    stream = _current(pages, batch)
+    shape = (batch.n_tokens, pages.H, pages.d)
+    k, v = (None if x is None else _dense(x, shape, pages.dtype, what, pages.index) for x, what in ((k, "k"), (v, "v")))
+    _check((_lib or load()).arkv_packed_read(pages.ref, batch.ref, k, v, stream), "arkv_packed_read")
+
+
+def arkv_packed_workspace_bytes(pages, batch, n_q_heads):
+    """Bytes of workspace that arkv_packed_attention needs for this batch, or any with no more sequences, tokens, new tokens or rows."""
+    n = C.c_size_t()
+    _check((_lib or load()).arkv_packed_workspace(pages.ref, batch.ref, n_q_heads, C.addressof(n)), "arkv_packed_workspace")
+    return n.value
+
+
+def arkv_packed_workspace(pages, batch, n_q_heads):
+    """A workspace tensor for arkv_packed_attention, as arkv_paged_workspace makes one."""
+    torch = _TORCH or _torch()
+    ws = torch.empty(arkv_packed_workspace_bytes(pages, batch, n_q_heads), dtype=torch.uint8, device=pages.device)
+    ws[:TICKET_BYTES].zero_()
+    return ws
+
+
+def arkv_packed_attention(pages, batch, q, scale, out, lse=None, cap=0.0, slopes=None, q_pos=None, prefix=None, sight=None, workspace=None):
+    """arkv_paged_attention over the values of packed rows; sight: an arkv_sight, or None."""
+    torch = _TORCH or _torch()
+    stream = _current(pages, batch)
+    n, o, at = batch.n_tokens, _own.set, pages.index
+    hq = _rows(o.q, q, n, pages, "q")
+    ws, size = _workspace(workspace, pages)
+    rc = (_lib or load()).arkv_packed_attention(
+        pages.ref, batch.ref, _scores(o, pages, batch, hq, scale, cap, slopes, q_pos, prefix), _sight(sight, pages, batch), hq, o.rq,
+        _dense(out, (n, hq, pages.d), pages.dtype, "out", at), None if lse is None else _dense(lse, (n, hq), torch.float32, "lse", at),
+        ws, size, stream)
+    _check(rc, "arkv_packed_attention")
 
 
 def arkv_paged_weights(pages, batch, q, scale, lse, decay=1.0, carried=None, cap=0.0, slopes=None, q_pos=None, prefix=None,
