@@ -121,17 +121,99 @@ template <typename T> __device__ __forceinline__ void store4(T* p, float a, floa
 // layout; values in whole rows, through LDS of the wave's own.  A tile's loads are in flight while the tile before it
 // is worked on.
 template <int D> struct StepLds {
-  uint16_t v[kStepWaves][32][D + 16];     // (the pitch: transposing reads of 16 rows meet each bank twice, as they must)
-  float acc[kStepWaves][kStepRows][D + 4];
+  union {                                 // a wave's values while it works, its sums behind that
+    uint16_t v[32][D + 16];               // (the pitch: transposing reads of 16 rows meet each bank twice, as they must)
+    float acc[kStepRows][D + 4];
+  } w[kStepWaves];
   float2 ml[kStepWaves][kStepRows];
   int last;                               // whether this workgroup's piece was the last one to be finished
 };
 
-template <typename T, int D, int MODE, int BITS, bool SIGHT>
+// The waves' results of a piece together: the row's output where the piece is the only one, else into the workspace, from where the
+// last workgroup of the sequence's head joins them.
+template <typename T, int D>
+__device__ __forceinline__ void step_finish(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, StepLds<D>& sm, const Seq& s, int h, int unit,
+                                            int piece, int np, const f32x4g (&acc)[D / 16], float m, float l) {
+  constexpr int CB = D / 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, gq = lane >> 4, R = s.nq * A.G, n_pieces = cut.n_step;
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+#pragma unroll
+  for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4g*>(&sm.w[wave].acc[n][16 * c + 4 * gq]) = acc[c];
+  if (gq == 0) sm.ml[wave][n] = make_float2(m, l);
+  __syncthreads();
+  auto finish = [&](int r, int c, f32x4g o, float mm, float ll) {  // four channels of a row's result
+    const size_t orow = (size_t)(s.q0 + r / A.G) * A.Hq + h * A.G + r % A.G;
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;                  // (NaN stays)
+    store4((T*)A.out + orow * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    if (c == 0 && A.lse) A.lse[orow] = ll == 0.f ? -INFINITY : kLn2 * (mm + log2f(ll));
+  };
+  // the waves' parts: thread = four channels of a row
+  for (int it = threadIdx.x; it < R * (D / 4); it += 64 * kStepWaves) {
+    const int r = it / (D / 4), c = 4 * (it % (D / 4));
+    float mm = kUnset, ll = 0.f;
+#pragma unroll
+    for (int w = 0; w < kStepWaves; ++w) mm = fmaxf(mm, sm.ml[w][r].x);
+    f32x4g o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kStepWaves; ++w) {
+      const float f = exp2_hw(sm.ml[w][r].x - mm);
+      ll += f * sm.ml[w][r].y;
+      o += f * *reinterpret_cast<const f32x4g*>(&sm.w[w].acc[r][c]);
+    }
+    if (np > 1) {
+      const size_t pr = ((size_t)unit * n_pieces + piece) * kStepRows + r;
+      put4(parts.acc + pr * D + c, o);
+      if (c == 0) put2(parts.ml + pr, mm, ll);
+    } else {
+      finish(r, c, o, mm, ll);
+    }
+  }
+  if (np == 1 || !cut.joined) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                 // this wave's stores are where everyone sees them
+  __syncthreads();
+  int* ticket = parts.tickets + unit * kTicketWords;
+  if (threadIdx.x == 0) {
+    const int drawn = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    sm.last = drawn == np - 1;
+    if (sm.last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call wants it
+  }
+  __syncthreads();
+  if (!sm.last) return;
+  for (int it = threadIdx.x; it < R * (D / 4); it += 64 * kStepWaves) {
+    const int r = it / (D / 4), c = 4 * (it % (D / 4));
+    const size_t first = (size_t)unit * n_pieces * kStepRows + r;
+    float2 ml[kJoinPieces];
+    f32x4g x[kJoinPieces];
+#pragma unroll
+    for (int p = 0; p < kJoinPieces; ++p) {
+      if (p < np) {
+        ml[p] = take2(parts.ml + first + p * kStepRows);
+        x[p] = take4(parts.acc + (first + p * kStepRows) * D + c);
+      }
+    }
+    float mm = kUnset, ll = 0.f;
+#pragma unroll
+    for (int p = 0; p < kJoinPieces; ++p)
+      if (p < np) mm = fmaxf(mm, ml[p].x);
+    f32x4g o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < kJoinPieces; ++p)
+      if (p < np) {
+        const float f = exp2_hw(ml[p].x - mm);
+        ll += f * ml[p].y;
+        o += f * x[p];
+      }
+    finish(r, c, o, mm, ll);
+  }
+}
+
+template <typename T, int D, int MODE, bool SIGHT>
 __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, StepLds<D>& sm, int id) {
   constexpr int CAP = Mode<MODE>::cap;
   constexpr bool DIST = Mode<MODE>::dist;
-  typedef PoolRow<T, D, BITS> Row;
+  typedef PoolRow<T, D, 16> Row;
   constexpr int KK = D / 32, CB = D / 16;                          // k-steps, channel blocks
   constexpr int CPR = Row::kLanes, RPI = 64 / CPR, VI = 32 / RPI;  // lanes per row, rows per load, loads of a value tile
   const int piece_keys = cut.step_piece, n_pieces = cut.n_step;
@@ -261,7 +343,7 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
     for (int i = 0; i < VI; ++i)
 #pragma unroll
       for (int o = 0; o < Row::kOut; ++o)
-        *reinterpret_cast<u32x4g*>(&sm.v[wave][RPI * i + lane / CPR][8 * (Row::kOut * (lane % CPR) + o)]) = vw[i][o];
+        *reinterpret_cast<u32x4g*>(&sm.w[wave].v[RPI * i + lane / CPR][8 * (Row::kOut * (lane % CPR) + o)]) = vw[i][o];
     if (t + 1 < nt) load_v(t + 1);
     float p[8];
     auto probs = [&]() {
@@ -294,8 +376,8 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
     const u32x4g pb = {Mfma<T>::pack(p[0], p[1]), Mfma<T>::pack(p[2], p[3]), Mfma<T>::pack(p[4], p[5]), Mfma<T>::pack(p[6], p[7])};
 #pragma unroll
     for (int c = 0; c < CB; ++c) {
-      const s16x4g a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.v[wave][4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
-      const s16x4g a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.v[wave][16 + 4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
+      const s16x4g a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.w[wave].v[4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
+      const s16x4g a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.w[wave].v[16 + 4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
       const u32x2g w0_ = __builtin_bit_cast(u32x2g, a0), w1_ = __builtin_bit_cast(u32x2g, a1);
       acc[c] = Mfma<T>::m16(u32x4g{w0_[0], w0_[1], w1_[0], w1_[1]}, pb, acc[c]);
     }
@@ -331,76 +413,210 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
       }
     }
   }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
+  step_finish<T, D>(A, cut, parts, sm, s, h, unit, piece, np, acc, m, l);
+}
+
+// The same over packed rows, 64 keys at a time: a tile's codes are few registers, and are requested again as soon as they are
+// expanded, so that most of a tile's time lies between request and use (8 bits: 17 KB a wave under way, 4 bits: 9 KB).  A lane's keys of a
+// row are whole chunks of it (PoolRow::channel).
+template <typename T, int D, int MODE, int BITS>
+__device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, StepLds<D>& sm, int id) {
+  constexpr int CAP = Mode<MODE>::cap;
+  constexpr bool DIST = Mode<MODE>::dist;
+  typedef PoolRow<T, D, BITS> Row;
+  constexpr int KK = D / 32, CB = D / 16;                          // k-steps, channel blocks
+  constexpr int CPR = Row::kLanes, RPI = 64 / CPR, VI = 32 / RPI;  // lanes per row, rows per load, loads of half a tile's values
+  const int piece_keys = cut.step_piece;
+  const Paged& P = A.P;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, gq = lane >> 4;
+  const int unit = id % (P.B * P.H), piece = id / (P.B * P.H), h = unit % P.H, b = unit / P.H;
+  const Seq s = seq_of(P, b);
+  const int R = s.nq * A.G;
+  if (R == 0 || R > kStepRows) return;
+  const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
+  const Keys<true> keys(A.V, s, prefix, 0, s.nq - 1);
+  const int np = max(1, (keys.end + piece_keys - 1) / piece_keys);
+  if (piece >= np) return;
+  const int row = n < R ? n : 0;
+  const RowView<true> view(A.V, s, prefix, row / A.G, n < R);
+  const int hq = h * A.G + row % A.G, tok = s.q0 + row / A.G;
+  const Logit lg(A.S);
+  const float slope = DIST ? A.S.slopes[hq] * kLog2e : 0.f;
+  const int qp = DIST ? A.S.q_pos[tok] : 0;
+
+  u32x4g q[KK];
+  {
+    const T* p = (const T*)A.q.p + (size_t)tok * A.q.ts + (size_t)hq * A.q.hs;
 #pragma unroll
-  for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4g*>(&sm.acc[wave][n][16 * c + 4 * gq]) = acc[c];
-  if (gq == 0) sm.ml[wave][n] = make_float2(m, l);
-  __syncthreads();
-  auto finish = [&](int r, int c, f32x4g o, float mm, float ll) {  // four channels of a row's result
-    const size_t orow = (size_t)(s.q0 + r / A.G) * A.Hq + h * A.G + r % A.G;
-    const float inv = ll == 0.f ? 0.f : 1.f / ll;                  // (NaN stays)
-    store4((T*)A.out + orow * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-    if (c == 0 && A.lse) A.lse[orow] = ll == 0.f ? -INFINITY : kLn2 * (mm + log2f(ll));
+    for (int kk = 0; kk < KK; ++kk) q[kk] = *reinterpret_cast<const u32x4g*>(p + Row::channel(gq, kk));
+  }
+  // this wave's keys: [w0, w1), a multiple of 32 from p0 on
+  const int p0 = piece * piece_keys, p1 = min(p0 + piece_keys, keys.end);
+  const int halves = (p1 - p0 + 31) / 32, per = (halves + kStepWaves - 1) / kStepWaves;
+  const int w0 = min(p0 + 32 * per * wave, p1), w1 = min(w0 + 32 * per, p1), nt = (w1 - w0 + 63) / 64;
+  // lane i holds the page id of granule i from w0 on; one that is not there, or not this wave's, becomes page 0, whose rows nobody sees
+  int my_page;
+  bool page_ok;
+  {
+    const int j = w0 + 16 * lane;
+    my_page = j < w1 ? P.table[(size_t)b * P.width + (keys.slot(j) >> P.lg_page)] : -1;
+    page_ok = (unsigned)my_page < (unsigned)P.n_pages;
+    if (!page_ok) my_page = 0;
+  }
+  const uint64_t ok_mask = __ballot(page_ok);
+  const int in_page = (1 << P.lg_page) - 1;
+  auto granule_row = [&](int g) {                                  // first row of granule g
+    const int page = __builtin_amdgcn_readlane(my_page, g);
+    return (size_t)(unsigned)(((page * P.H + h) << P.lg_page) + (keys.slot(w0 + 16 * g) & in_page));
   };
-  // the waves' parts: thread = four channels of a row
-  for (int it = threadIdx.x; it < R * (D / 4); it += 64 * kStepWaves) {
-    const int r = it / (D / 4), c = 4 * (it % (D / 4));
-    float mm = kUnset, ll = 0.f;
+
+  typename Row::Keys kr[4];
+  typename Row::Chunk vr[2][VI];
+  auto load_k = [&](int t) {
 #pragma unroll
-    for (int w = 0; w < kStepWaves; ++w) mm = fmaxf(mm, sm.ml[w][r].x);
-    f32x4g o = {0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < 4; ++g) Row::load_keys(A, granule_row(4 * t + g), n, gq, kr[g]);
+  };
+  auto load_v = [&](int t, int half) {
 #pragma unroll
-    for (int w = 0; w < kStepWaves; ++w) {
-      const float f = exp2_hw(sm.ml[w][r].x - mm);
-      ll += f * sm.ml[w][r].y;
-      o += f * *reinterpret_cast<const f32x4g*>(&sm.acc[w][r][c]);
+    for (int i = 0; i < VI; ++i) {
+      const int first = RPI * i + lane / CPR;                      // (a load's rows lie in one granule)
+      Row::load_chunk(P.v, A.v_scale, granule_row(4 * t + 2 * half + RPI * i / 16) + (first & 15), lane % CPR, vr[half][i]);
     }
-    if (np > 1) {
-      const size_t pr = ((size_t)unit * n_pieces + piece) * kStepRows + r;
-      put4(parts.acc + pr * D + c, o);
-      if (c == 0) put2(parts.ml + pr, mm, ll);
-    } else {
-      finish(r, c, o, mm, ll);
-    }
-  }
-  if (np == 1 || !cut.joined) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                 // this wave's stores are where everyone sees them
-  __syncthreads();
-  int* ticket = parts.tickets + unit * kTicketWords;
-  if (threadIdx.x == 0) {
-    const int drawn = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    sm.last = drawn == np - 1;
-    if (sm.last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call wants it
-  }
-  __syncthreads();
-  if (!sm.last) return;
-  for (int it = threadIdx.x; it < R * (D / 4); it += 64 * kStepWaves) {
-    const int r = it / (D / 4), c = 4 * (it % (D / 4));
-    const size_t first = (size_t)unit * n_pieces * kStepRows + r;
-    float2 ml[kJoinPieces];
-    f32x4g x[kJoinPieces];
+  };
+  f32x4g acc[CB];
 #pragma unroll
-    for (int p = 0; p < kJoinPieces; ++p) {
-      if (p < np) {
-        ml[p] = take2(parts.ml + first + p * kStepRows);
-        x[p] = take4(parts.acc + (first + p * kStepRows) * D + c);
+  for (int c = 0; c < CB; ++c) acc[c] = f32x4g{0.f, 0.f, 0.f, 0.f};
+  float m = kUnset, l = 0.f;
+  if (nt > 0) {
+    load_k(0);
+    load_v(0, 0);
+    load_v(0, 1);
+  }
+  for (int t = 0; t < nt; ++t) {
+    const int j0 = w0 + 64 * t;
+    f32x4g x[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      x[g] = f32x4g{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) x[g] = Mfma<T>::m16(Row::operand(kr[g], gq, kk), q[kk], x[g]);
+    }
+    if (t + 1 < nt) load_k(t + 1);
+    const bool masked = !keys.all_seen(j0, 64) || (ok_mask >> (4 * t) & 15) != 15;
+    float mul = lg.mul;
+    if (CAP || DIST) {
+      mul = 1.f;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[g][i] = lg.logit<CAP>(x[g][i]);
+        if (DIST) {
+          const int4 kp = *reinterpret_cast<const int4*>(P.pos + granule_row(4 * t + g) + 4 * gq);
+          x[g][0] = fmaf(-slope, fabsf((float)(qp - kp.x)), x[g][0]);
+          x[g][1] = fmaf(-slope, fabsf((float)(qp - kp.y)), x[g][1]);
+          x[g][2] = fmaf(-slope, fabsf((float)(qp - kp.z)), x[g][2]);
+          x[g][3] = fmaf(-slope, fabsf((float)(qp - kp.w)), x[g][3]);
+        }
       }
     }
-    float mm = kUnset, ll = 0.f;
+    if (masked) {
 #pragma unroll
-    for (int p = 0; p < kJoinPieces; ++p)
-      if (p < np) mm = fmaxf(mm, ml[p].x);
-    f32x4g o = {0.f, 0.f, 0.f, 0.f};
+      for (int g = 0; g < 4; ++g) {
+        const auto seen = view.granule(keys.slot(j0 + 16 * g), ok_mask >> (4 * t + g) & 1, 4 * gq);
 #pragma unroll
-    for (int p = 0; p < kJoinPieces; ++p)
-      if (p < np) {
-        const float f = exp2_hw(ml[p].x - mm);
-        ll += f * ml[p].y;
-        o += f * x[p];
+        for (int i = 0; i < 4; ++i) x[g][i] = seen.at(i) ? x[g][i] * mul : -INFINITY;
       }
-    finish(r, c, o, mm, ll);
+      mul = 1.f;
+    }
+    float p[16];
+    auto probs = [&]() {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i] = exp2_hw(fmaf(x[i >> 2][i & 3], mul, -m));
+        sum += p[i];
+      }
+      return sum;
+    };
+    float sum = probs();
+    uint64_t big = __ballot(!(sum <= kSumLimit));
+    if (big) {
+      big |= big >> 32;                                            // of the four lanes of a row any one: that row alone moves
+      big |= big >> 16;
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i >> 2][i & 3] * mul);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = big >> n & 1 ? fmaxf(m, top) : m, f = exp2_hw(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < CB; ++c) acc[c] *= f;
+      sum = probs();
+    }
+    l += sum;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const u32x4g pb = {Mfma<T>::pack(p[8 * half], p[8 * half + 1]), Mfma<T>::pack(p[8 * half + 2], p[8 * half + 3]),
+                         Mfma<T>::pack(p[8 * half + 4], p[8 * half + 5]), Mfma<T>::pack(p[8 * half + 6], p[8 * half + 7])};
+      uint32_t odd = 0;                                            // keys of this half whose values are not all finite
+#pragma unroll
+      for (int i = 0; i < VI; ++i) {
+        u32x4g w[Row::kOut];
+        Row::expand(vr[half][i], w);
+        if (masked) {
+          // a value that is not finite would spoil the rows that do not see it: it leaves the product, and is added below
+          uint32_t any = 0;
+#pragma unroll
+          for (int o = 0; o < Row::kOut; ++o)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t f = not_finite<T>(w[o][e]);
+              w[o][e] &= ~f;
+              any |= f;
+            }
+          const uint64_t who = __ballot(any != 0);
+#pragma unroll
+          for (int r = 0; r < RPI; ++r)
+            if (who >> (CPR * r) & ((1ull << CPR) - 1)) odd |= 1u << (RPI * i + r);
+        }
+#pragma unroll
+        for (int o = 0; o < Row::kOut; ++o)
+          *reinterpret_cast<u32x4g*>(&sm.w[wave].v[RPI * i + lane / CPR][8 * (Row::kOut * (lane % CPR) + o)]) = w[o];
+      }
+      if (t + 1 < nt) load_v(t + 1, half);
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        const s16x4g a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.w[wave].v[4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
+        const s16x4g a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.w[wave].v[16 + 4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
+        const u32x2g w0_ = __builtin_bit_cast(u32x2g, a0), w1_ = __builtin_bit_cast(u32x2g, a1);
+        acc[c] = Mfma<T>::m16(u32x4g{w0_[0], w0_[1], w1_[0], w1_[1]}, pb, acc[c]);
+      }
+      while (odd) {                                                // (uniform; hardly ever)
+        const int j = __builtin_ctz(odd);
+        odd &= odd - 1;
+        const int g = j >> 4, i = j & 3, from = (j & 12) >> 2;
+        float pj = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e == 4 * g + i) pj = Mfma<T>::get(opaque(pb[e / 2]), e & 1);
+        pj = __shfl(pj, n + 16 * from);
+        const int granule = 4 * t + 2 * half + g;
+        const bool seen = view.granule(keys.slot(w0 + 16 * granule), ok_mask >> granule & 1, 0).at(j & 15);
+        const size_t vrow = granule_row(granule) + (j & 15);
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float w = Row::value(A, vrow, 16 * c + 4 * gq + e);
+            if (seen && !(fabsf(w) < INFINITY)) acc[c][e] += pj * w;
+          }
+      }
+    }
   }
+  step_finish<T, D>(A, cut, parts, sm, s, h, unit, piece, np, acc, m, l);
 }
 
 // ---- many rows ----------------------------------------------------------------------------------------
@@ -558,7 +774,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
   // The row's softmax reference; rows that see none of this piece need none.
-  float m = view.end > keys.slot(p0) ? kUnset : 0.f, l = 0.f;
+  float m = view.end() > keys.slot(p0) ? kUnset : 0.f, l = 0.f;
   load_pages(0, 0);
   if (nt > 0) {
     fetch(0, 0, 0);
@@ -602,6 +818,10 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
       __syncthreads();
       odd = (uint64_t)sm.odd[1] << 32 | sm.odd[0];
     }
+    if (SIGHT && r0 + 32 * wave >= R) {                            // no rows of this wave's: it only fetches
+      if (t + 1 < nt) put(buf ^ 1);
+      return;
+    }
     f32x16g x[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g)
@@ -636,7 +856,8 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
     if (masked) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {                                // granules
-        const auto seen = view.granule(keys.slot(j0 + 16 * g), ok >> g & 1, 4 * hh, true);   // (what depends on it stays in this branch)
+        auto seen = view.granule(keys.slot(j0 + 16 * g), ok >> g & 1, 4 * hh);
+        if constexpr (!SIGHT) seen.left = (int)opaque(seen.left);  // (what depends on it stays in this branch)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           if (!seen.at(8 * (i >> 2) + (i & 3))) x[g >> 1][8 * (g & 1) + i] = -INFINITY;
@@ -706,7 +927,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
     }
     if (t + 1 < nt) put(buf ^ 1);
   };
-  if constexpr (DIST || D == 64) {                                 // (two copies of the tile do not fit the registers of two and three waves per SIMD)
+  if constexpr (DIST || D == 64 || (BITS != 16 && CAP)) {                                 // (two copies of the tile do not fit the registers of two and three waves per SIMD)
     for (int t = 0; t < nt; ++t) tile(t, t & 1);
   } else {
     for (int t = 0; t < nt; t += 2) {
@@ -790,14 +1011,18 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
 // few (unit by unit, piece by piece).  One launch for both: a prompt's chunk and the other requests' tokens share the chip.
 // KIND: bit 0: there are the former, bit 1: the latter.
 template <typename T, int D, int MODE, int KIND, int BITS, bool SIGHT>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_paged_attn(PagedAttnArgs A, Cut cut, Parts parts, int chunk_wgs) {
+__global__ __launch_bounds__(256, D == 64 || (BITS == 4 && KIND == 2) ? 3 : 2) void k_paged_attn(PagedAttnArgs A, Cut cut, Parts parts, int chunk_wgs) {
   constexpr size_t kMost = sizeof(ChunkLds<D>) > sizeof(StepLds<D>) ? sizeof(ChunkLds<D>) : sizeof(StepLds<D>);
   __shared__ __align__(16) char lds[KIND == 1 ? sizeof(ChunkLds<D>) : KIND == 2 ? sizeof(StepLds<D>) : kMost];
   const int id = (int)blockIdx.x;
   if ((KIND & 1) && (KIND == 1 || id < chunk_wgs)) {
     if constexpr (KIND & 1) paged_chunk<T, D, MODE, BITS, SIGHT>(A, cut, parts, *reinterpret_cast<ChunkLds<D>*>(lds), id);
   } else {
-    if constexpr (KIND & 2) paged_step<T, D, MODE, BITS, SIGHT>(A, cut, parts, *reinterpret_cast<StepLds<D>*>(lds), id - chunk_wgs);
+    if constexpr (KIND & 2) {
+      StepLds<D>& sm = *reinterpret_cast<StepLds<D>*>(lds);
+      if constexpr (BITS == 16) paged_step<T, D, MODE, SIGHT>(A, cut, parts, sm, id - chunk_wgs);
+      else packed_step<T, D, MODE, BITS>(A, cut, parts, sm, id - chunk_wgs);
+    }
   }
 }
 

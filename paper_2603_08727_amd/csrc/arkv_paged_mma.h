@@ -136,16 +136,6 @@ template <typename T, int D, typename F> hipError_t dispatch_mode(int mode, F f)
     default: return f(TypeOf<T>(), Int<D>(), Int<6>());
   }
 }
-// the same with one build for caps of any width
-template <typename T, int D, typename F> hipError_t dispatch_cap(int mode, F f) {
-  const bool cap = mode & 5;
-  if (mode & 2) return cap ? f(TypeOf<T>(), Int<D>(), Int<6>()) : f(TypeOf<T>(), Int<D>(), Int<2>());
-  return cap ? f(TypeOf<T>(), Int<D>(), Int<4>()) : f(TypeOf<T>(), Int<D>(), Int<0>());
-}
-template <typename F> hipError_t dispatch_any_cap(int dtype, int D, int mode, F f) {
-  if (dtype == ARKV_DTYPE_BF16) return D == 64 ? dispatch_cap<__bf16, 64>(mode, f) : dispatch_cap<__bf16, 128>(mode, f);
-  return D == 64 ? dispatch_cap<_Float16, 64>(mode, f) : dispatch_cap<_Float16, 128>(mode, f);
-}
 template <typename F> hipError_t dispatch(int dtype, int D, int mode, F f) {
   if (dtype == ARKV_DTYPE_BF16) return D == 64 ? dispatch_mode<__bf16, 64>(mode, f) : dispatch_mode<__bf16, 128>(mode, f);
   return D == 64 ? dispatch_mode<_Float16, 64>(mode, f) : dispatch_mode<_Float16, 128>(mode, f);

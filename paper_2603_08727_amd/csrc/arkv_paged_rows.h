@@ -124,66 +124,69 @@ template <> struct Keys<true> {
   }
 };
 
-// What one row (a token) sees.  granule(first slot, whether it is there, off): which of its slots from `off` on, at(i): slot off + i.
-// live: whether the lane has a row at all.
+// What one row (a token) sees.  granule(first slot, whether it is there, off): which of its slots from `off` on, at(i): slot off + i; end(): no
+// slot from there on.  live: whether the lane has a row at all.
 template <bool SIGHT> struct RowView;
 template <> struct RowView<false> {
-  int end;                                // slots below are seen, no others
-  __device__ __forceinline__ RowView(const Sight&, const Seq& s, int prefix, int i, bool live) : end(live ? row_end(s, i, prefix) : 0) {}
+  int last;                               // slots below are seen, no others
+  __device__ __forceinline__ RowView(const Sight&, const Seq& s, int prefix, int i, bool live) : last(live ? row_end(s, i, prefix) : 0) {}
+  __device__ __forceinline__ int end() const { return last; }
   struct Seen {
     int left;
     __device__ __forceinline__ bool at(int i) const { return i < left; }
   };
-  // (apart: nothing that depends on the result is computed in front of a branch)
-  __device__ __forceinline__ Seen granule(int slot, bool there, int off, bool apart = false) const {
-    const int left = there ? end - slot - off : 0;
-    return {apart ? (int)opaque(left) : left};
-  }
+  __device__ __forceinline__ Seen granule(int slot, bool there, int off) const { return {there ? last - slot - off : 0}; }
 };
 template <> struct RowView<true> {
-  int end;                                // no slot from here on is seen
-  int own, lo, sink, pre, ctx, nq;        // slots below own and from lo on or below sink; new ones by their bits; all below pre
-  bool window;
-  const uint64_t* bits;                   // null: no tree
-  __device__ __forceinline__ RowView(const Sight& V, const Seq& s, int prefix, int i, bool live) {
-    ctx = s.kv - s.nq;
-    const bool has = live && ctx + i >= 0;                         // its slot, that is
-    nq = has ? s.nq : 0;
-    pre = live ? max(0, min(prefix, s.kv)) : 0;
-    own = !has ? 0 : V.tree ? max(ctx, 0) : ctx + i + 1;
-    bits = V.tree ? V.tree + (size_t)(s.q0 + i) * V.words : nullptr;
-    sink = V.sink;
-    window = V.window != 0;
-    lo = ctx + i - V.window + 1;
-    if (bits && window) {                                          // its place is behind the tokens above it
-      int n = 0;
-      for (int w = 0; 64 * w < nq; ++w) n += __popcll(bits[w] & (nq - 64 * w < 64 ? (1ull << (nq - 64 * w)) - 1 : ~0ull));
-      lo = ctx + max(n - 1, 0) - V.window + 1;
+  // (the numbers of the sequence are uniform; a lane keeps two words of its own, and works the others out where a tile is masked)
+  const Sight& V;
+  const Seq& s;
+  int i, lo, pre;                         // its token (-1: no row), the first slot of its window, the slots below which all see
+  __device__ __forceinline__ RowView(const Sight& V, const Seq& s, int prefix, int token, bool live) : V(V), s(s) {
+    i = live ? token : -1;
+    pre = max(0, min(prefix, s.kv));
+    const int ctx = s.kv - s.nq;
+    lo = 0;
+    if (V.window) {
+      int above = token;                                           // its place is behind the tokens above it
+      if (V.tree && live) {
+        const uint64_t* bits = V.tree + (size_t)(s.q0 + token) * V.words;
+        int n = 0;
+        for (int w = 0; 64 * w < s.nq; ++w) n += __popcll(bits[w] & (s.nq - 64 * w < 64 ? (1ull << (s.nq - 64 * w)) - 1 : ~0ull));
+        above = max(n - 1, 0);
+      }
+      lo = ctx + above - V.window + 1;
     }
-    end = max(pre, bits && has ? s.kv : own);
   }
-  // bits t .. t + 15, t from -15 on
-  __device__ __forceinline__ uint32_t tree16(int t) const {
-    if (t <= -16 || t >= nq) return 0;
+  __device__ __forceinline__ bool has_slot(int t) const { return t >= 0 && s.kv - s.nq + t >= 0; }
+  // no slot from here on is seen
+  __device__ __forceinline__ int end() const {
+    return i < 0 ? 0 : max(pre, !has_slot(i) ? 0 : V.tree ? s.kv : s.kv - s.nq + i + 1);
+  }
+  // bits t .. t + 15 of the token's, t from -15 on
+  __device__ __forceinline__ uint32_t tree16(int token, int t) const {
+    if (t <= -16 || t >= s.nq) return 0;
+    const uint64_t* bits = V.tree + (size_t)(s.q0 + token) * V.words;
     uint64_t x;
     if (t < 0) x = bits[0] << -t;
     else {
       x = bits[t >> 6] >> (t & 63);
-      if ((t & 63) > 48 && ((t >> 6) + 1) * 64 < nq) x |= bits[(t >> 6) + 1] << (64 - (t & 63));
+      if ((t & 63) > 48 && ((t >> 6) + 1) * 64 < s.nq) x |= bits[(t >> 6) + 1] << (64 - (t & 63));
     }
-    return (uint32_t)x & first16(nq - t) & (t < 0 ? ~first16(-t) : ~0u) & 0xFFFFu;
+    return (uint32_t)x & first16(s.nq - t) & 0xFFFFu;
   }
   struct Seen {
     uint32_t mask;
     __device__ __forceinline__ bool at(int i) const { return mask >> i & 1; }
   };
-  __device__ __forceinline__ Seen granule(int slot, bool there, int off, bool apart = false) const {
-    uint32_t m = first16(own - slot);
-    if (window) m &= ~first16(lo - slot) | first16(sink - slot);
-    if (bits) m |= tree16(slot - ctx);
-    m |= first16(pre - slot);
-    m = there ? m >> off : 0;
-    return {apart ? opaque(m) : m};
+  __device__ __forceinline__ Seen granule(int slot, bool there, int off) const {
+    const int t = (int)opaque(i), ctx = s.kv - s.nq;
+    const bool has = has_slot(t);
+    uint32_t m = has ? first16((V.tree ? max(ctx, 0) : ctx + t + 1) - slot) : 0;
+    if (V.window) m &= ~first16(lo - slot) | first16(V.sink - slot);
+    if (V.tree && has) m |= tree16(t, slot - ctx);
+    if (t >= 0) m |= first16(pre - slot);
+    return {there ? m >> off : 0};
   }
 };
 
