@@ -69,143 +69,220 @@ template <typename T, int BITS> __device__ __forceinline__ uint32_t quantise(con
 
 constexpr int kPackWaves = 4;
 
-// The sequence of token t (of the wave), its new tokens' first row and their number, the token's slot; b < 0: none.
-struct Place { int b, slot, row0; };      // row0: its row of kv-head 0, -1: none
-__device__ __forceinline__ Place place_of(const Paged& P, int t, int lane) {
-  Place o = {-1, 0, -1};
+// A token's sequence, its slot, and the sequence's rows.
+struct Place { int b, slot, kv; };        // b < 0: a row of no sequence
+// Of a wave's token, out of the lengths of 64 sequences (from `at` on, a lane each) that it holds already, and of those behind them.
+__device__ __forceinline__ Place place_of(const Paged& P, int t, int lane, int sq0, int sq1, int skv) {
   for (int i = 0; i < P.B; i += 64) {
-    const int at = min(i + lane, P.B - 1);
-    const int sq0 = P.cu_q[at], sq1 = P.cu_q[at + 1], skv = P.kv_len[at];
+    if (i) {
+      const int at = min(i + lane, P.B - 1);
+      sq0 = P.cu_q[at]; sq1 = P.cu_q[at + 1]; skv = P.kv_len[at];
+    }
     const uint64_t hit = __ballot(i + lane < P.B && sq1 > t);
     if (!hit) continue;
     const int l = __builtin_ctzll(hit);
     const Seq s = clamp_seq(__builtin_amdgcn_readlane(sq0, l), __builtin_amdgcn_readlane(sq1, l), __builtin_amdgcn_readlane(skv, l), P.N, P.max_q, P.max_kv);
-    if (t < s.q0 || t >= s.q0 + s.nq) return o;                    // a row of no sequence
-    o.b = i + l;
-    o.slot = s.kv - s.nq + t - s.q0;
-    o.row0 = slot_row(P.table + (size_t)o.b * P.width, P.n_pages, P.H, 0, P.lg_page, s.kv, o.slot);
-    return o;
+    if (t < s.q0 || t >= s.q0 + s.nq) break;
+    return {i + l, s.kv - s.nq + t - s.q0, s.kv};
   }
-  return o;
+  return {-1, 0, 0};
+}
+__device__ __forceinline__ int row_of(const Paged& P, const Place& o) {
+  return o.b < 0 ? -1 : slot_row(P.table + (size_t)o.b * P.width, P.n_pages, P.H, 0, P.lg_page, o.kv, o.slot);
 }
 
-// One wave per new token.  Its lanes form the token's angles, then walk its query heads in pairs of 16-byte chunks whose channels turn
-// together, and its keys and values a chunk a lane (a key's partner chunk is read again: it comes out of the cache), so that four
-// adjacent lanes hold a block.
+// Rounds of 64 lanes that a wave has under way together: chunks of keys and values, and pairs of chunks of queries.
+constexpr int kPackKv = 4, kPackQ = 3;
+__host__ __device__ constexpr int kv_batches(int H, int D) { return (2 * H * (D / 8) + 64 * kPackKv - 1) / (64 * kPackKv); }
+__host__ __device__ constexpr int q_batches(int Hq, int D) { return (Hq * (D / 16) + 64 * kPackQ - 1) / (64 * kPackQ); }
+
+// One wave per new token, or a share of its batches.  Its lanes form the token's angles, then walk its keys and values a 16-byte chunk a lane (a key's
+// partner chunk is read again: it comes out of the cache), so that four adjacent lanes hold a block, and its query heads in pairs of
+// chunks whose channels turn together.  The first batch's rows are requested with the lengths and angles, the page behind them.  Many tokens are bound
+// by memory (7817 tokens of 32 + 2 x 8 heads to 4 bits: 39 us, 4.3 TB/s), few by round trips (16 tokens: 5.6 us).
 template <typename T, int D, int BITS>
-__global__ __launch_bounds__(64 * kPackWaves) void k_packed_append(AppendArgs A, PackedArgs X) {
+__global__ __launch_bounds__(64 * kPackWaves) void k_packed_append(AppendArgs A, PackedArgs X, int per_wave) {
   __shared__ float2 turn[kPackWaves][64];
   __shared__ double2 turn64[kPackWaves][64];
+  constexpr int CPR = D / 8, IPR = D / 16;                         // chunks, pairs of chunks of a row
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = blockIdx.x * kPackWaves + wave;
   const Paged& P = A.P;
   if (t >= P.N) return;
-  const Place place = place_of(P, t, lane);
-  if (place.b < 0) return;
-  const int row0 = place.row0;
-  if (lane < A.half) {
-    const double turns = (double)A.positions[(size_t)A.axis[lane] * P.N + t] * (A.freq[lane] * 0.15915494309189533577);
-    const double rest = turns - rint(turns);
-    float sn, cs;
-    sincospif(2.0f * (float)rest, &sn, &cs);
-    turn[wave][lane] = make_float2(cs, sn);                        // (read by this wave alone)
-    double sn64, cs64;
-    sincospi(2.0 * rest, &sn64, &cs64);
-    turn64[wave][lane] = make_double2(cs64, sn64);
-  }
-  constexpr int CPR = D / 8, IPR = D / 16;                         // chunks, pairs of chunks of a row
   const int rot = A.half / 8;                                      // pairs that turn
-  for (int it = lane; it < A.Hq * IPR; it += 64) {
-    const int h = it / IPR, i = it % IPR;
-    const bool turns = i < rot, halves = turns && !A.adjacent;
-    const int c0 = halves ? i : 2 * i, c1 = halves ? i + rot : 2 * i + 1;
-    const T* from = (const T*)A.q.p + (size_t)t * A.q.ts + A.q.hs * h;
-    u32x4g x = *reinterpret_cast<const u32x4g*>(from + 8 * c0), y = *reinterpret_cast<const u32x4g*>(from + 8 * c1);
-    if (turns) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float ax = Mfma<T>::get(x[e], 0), ay = Mfma<T>::get(x[e], 1), zx = Mfma<T>::get(y[e], 0), zy = Mfma<T>::get(y[e], 1);
-        if (!A.adjacent) {
-          const float2 t0 = turn[wave][8 * i + 2 * e], t1 = turn[wave][8 * i + 2 * e + 1];
-          x[e] = Mfma<T>::pack(ax * t0.x - zx * t0.y, ay * t1.x - zy * t1.y);
-          y[e] = Mfma<T>::pack(zx * t0.x + ax * t0.y, zy * t1.x + ay * t1.y);
-        } else {
-          const float2 t0 = turn[wave][8 * i + e], t1 = turn[wave][8 * i + 4 + e];
-          x[e] = Mfma<T>::pack(ax * t0.x - ay * t0.y, ay * t0.x + ax * t0.y);
-          y[e] = Mfma<T>::pack(zx * t1.x - zy * t1.y, zy * t1.x + zx * t1.y);
-        }
+  const int n_kv = 2 * P.H * CPR, n_q = A.Hq * IPR, kvb = kv_batches(P.H, D), all = kvb + q_batches(A.Hq, D);
+  const int first = (int)blockIdx.y * per_wave, last = min(first + per_wave, all);
+  const int at0 = min(lane, P.B - 1);
+  int sq0 = P.cu_q[at0], sq1 = P.cu_q[at0 + 1], skv = P.kv_len[at0];
+  const int axis = A.axis[lane], pos0 = A.positions[t];
+  const double freq = A.freq[min(lane, max(A.half, 1) - 1)];
+  const int pos = A.positions[(size_t)min(axis, A.n_axes - 1) * P.N + t];
+  int row0 = -1;
+  bool placed = false;
+  const T *qp = (const T*)A.q.p + (size_t)t * A.q.ts, *kp = (const T*)A.k.p + (size_t)t * A.k.ts, *vp = (const T*)A.v.p + (size_t)t * A.v.ts;
+  // whether the token is a sequence's; what its rows turn by
+  auto place = [&]() {
+    asm volatile("" : "+v"(sq0), "+v"(sq1), "+v"(skv));            // (requested above, not where they turn out to be needed)
+    const Place o = place_of(P, t, lane, sq0, sq1, skv);
+    row0 = row_of(P, o);
+    if (lane < A.half) {
+      const double turns = (double)pos * (freq * 0.15915494309189533577), rest = turns - rint(turns);
+      if (last > kvb) {
+        float sn, cs;
+        sincospif(2.0f * (float)rest, &sn, &cs);
+        turn[wave][lane] = make_float2(cs, sn);                    // (read by this wave alone)
+      }
+      if (first < kvb) {
+        double sn, cs;
+        sincospi(2.0 * rest, &sn, &cs);
+        turn64[wave][lane] = make_double2(cs, sn);
       }
     }
-    T* to = (T*)A.q_out + ((size_t)t * A.Hq + h) * D;
-    *reinterpret_cast<u32x4g*>(to + 8 * c0) = x;
-    *reinterpret_cast<u32x4g*>(to + 8 * c1) = y;
-  }
-  if (row0 < 0) return;
-  for (int h = lane; h < P.H; h += 64) P.pos[(size_t)row0 + ((size_t)h << P.lg_page)] = A.positions[t];
-  for (int it = lane; it < 2 * P.H * CPR; it += 64) {              // (whole blocks: CPR is a multiple of 4)
-    const int h = it / CPR, c = it % CPR, hs = h < P.H ? h : h - P.H;
-    const bool key = h < P.H;
-    const T* from = key ? (const T*)A.k.p + (size_t)t * A.k.ts + A.k.hs * hs : (const T*)A.v.p + (size_t)t * A.v.ts + A.v.hs * hs;
-    const u32x4g x = *reinterpret_cast<const u32x4g*>(from + 8 * c);
-    float y[8];
+    placed = true;
+    return o.b >= 0;
+  };
+  for (int batch = first; batch < min(last, kvb); ++batch) {
+    const int it0 = batch * 64 * kPackKv + lane;
+    u32x4g x[kPackKv], o[kPackKv];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = Mfma<T>::get(x[e / 2], e & 1);
-    if (key && c < 2 * rot) {
-      if (A.adjacent) {
+    for (int u = 0; u < kPackKv; ++u) {
+      const int it = min(it0 + 64 * u, n_kv - 1), h = it / CPR, c = it % CPR;
+      const T* from = h < P.H ? kp + A.k.hs * h : vp + A.v.hs * (h - P.H);
+      x[u] = *reinterpret_cast<const u32x4g*>(from + 8 * c);
+      const int partner = h < P.H && !A.adjacent && c < 2 * rot ? (c < rot ? c + rot : c - rot) : c;
+      o[u] = *reinterpret_cast<const u32x4g*>(from + 8 * partner);
+    }
+    if (!placed) {
+      if (!place()) return;
+      if (row0 >= 0 && batch == 0)
+        for (int h = lane; h < P.H; h += 64) P.pos[(size_t)row0 + ((size_t)h << P.lg_page)] = pos0;
+    }
+    if (row0 < 0) continue;
+#pragma unroll
+    for (int u = 0; u < kPackKv; ++u) {
+      const int it = it0 + 64 * u, h = it / CPR, c = it % CPR;     // (a block's four lanes are in or out together)
+      if (it >= n_kv) continue;
+      const bool key = h < P.H;
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = Mfma<T>::get(x[u][e / 2], e & 1);
+      if (key && c < 2 * rot) {
+        if (A.adjacent) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const double2 w = turn64[wave][4 * c + e];
+            const double a = y[2 * e], z = y[2 * e + 1];
+            y[2 * e] = round_to_odd(fma(a, w.x, -(z * w.y)));
+            y[2 * e + 1] = round_to_odd(fma(z, w.x, a * w.y));
+          }
+        } else {
+          const bool front = c < rot;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const double2 w = turn64[wave][8 * (front ? c : c - rot) + e];
+            const double z = Mfma<T>::get(o[u][e / 2], e & 1);
+            y[e] = round_to_odd(fma((double)y[e], w.x, front ? -(z * w.y) : z * w.y));
+          }
+        }
+      }
+      uint32_t code[BITS / 4];
+      const uint32_t s = quantise<T, BITS>(y, code);
+      const size_t row = (size_t)row0 + ((size_t)(key ? h : h - P.H) << P.lg_page);
+      uint8_t* to = (uint8_t*)(key ? P.k : P.v) + row * (D * BITS / 8) + c * BITS;
+      if constexpr (BITS == 8) *reinterpret_cast<u32x2g*>(to) = u32x2g{code[0], code[1]};
+      else *reinterpret_cast<uint32_t*>(to) = code[0];
+      if ((c & 3) == 0) (key ? X.k_scale : X.v_scale)[row * (D / 32) + c / 4] = (uint8_t)s;
+    }
+  }
+  for (int batch = max(first, kvb); batch < last; ++batch) {
+    const int it0 = (batch - kvb) * 64 * kPackQ + lane;
+    u32x4g x[kPackQ], y[kPackQ];
+    // with halves, chunk i turns with chunk i + rot; else (and behind rot_dim) two adjacent ones
+    auto chunk0 = [&](int i) { return i < rot && !A.adjacent ? i : 2 * i; };
+    auto chunk1 = [&](int i) { return i < rot && !A.adjacent ? i + rot : 2 * i + 1; };
+#pragma unroll
+    for (int u = 0; u < kPackQ; ++u) {
+      const int it = min(it0 + 64 * u, n_q - 1), h = it / IPR, i = it % IPR;
+      x[u] = *reinterpret_cast<const u32x4g*>(qp + A.q.hs * h + 8 * chunk0(i));
+      y[u] = *reinterpret_cast<const u32x4g*>(qp + A.q.hs * h + 8 * chunk1(i));
+    }
+    if (!placed && !place()) return;
+#pragma unroll
+    for (int u = 0; u < kPackQ; ++u) {
+      const int it = it0 + 64 * u, h = it / IPR, i = it % IPR;
+      if (it >= n_q) continue;
+      if (i < rot) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const double2 u = turn64[wave][4 * c + e];
-          const double a = y[2 * e], z = y[2 * e + 1];
-          y[2 * e] = round_to_odd(fma(a, u.x, -(z * u.y)));
-          y[2 * e + 1] = round_to_odd(fma(z, u.x, a * u.y));
-        }
-      } else {
-        const bool first = c < rot;
-        const u32x4g o = *reinterpret_cast<const u32x4g*>(from + 8 * (first ? c + rot : c - rot));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const double2 u = turn64[wave][8 * (first ? c : c - rot) + e];
-          const double z = Mfma<T>::get(o[e / 2], e & 1);
-          y[e] = round_to_odd(fma((double)y[e], u.x, first ? -(z * u.y) : z * u.y));
+          const float ax = Mfma<T>::get(x[u][e], 0), ay = Mfma<T>::get(x[u][e], 1), zx = Mfma<T>::get(y[u][e], 0), zy = Mfma<T>::get(y[u][e], 1);
+          if (!A.adjacent) {
+            const float2 t0 = turn[wave][8 * i + 2 * e], t1 = turn[wave][8 * i + 2 * e + 1];
+            x[u][e] = Mfma<T>::pack(ax * t0.x - zx * t0.y, ay * t1.x - zy * t1.y);
+            y[u][e] = Mfma<T>::pack(zx * t0.x + ax * t0.y, zy * t1.x + ay * t1.y);
+          } else {
+            const float2 t0 = turn[wave][8 * i + e], t1 = turn[wave][8 * i + 4 + e];
+            x[u][e] = Mfma<T>::pack(ax * t0.x - ay * t0.y, ay * t0.x + ax * t0.y);
+            y[u][e] = Mfma<T>::pack(zx * t1.x - zy * t1.y, zy * t1.x + zx * t1.y);
+          }
         }
       }
+      T* to = (T*)A.q_out + ((size_t)t * A.Hq + h) * D;
+      *reinterpret_cast<u32x4g*>(to + 8 * chunk0(i)) = x[u];
+      *reinterpret_cast<u32x4g*>(to + 8 * chunk1(i)) = y[u];
     }
-    uint32_t code[BITS / 4];
-    const uint32_t s = quantise<T, BITS>(y, code);
-    const size_t row = (size_t)row0 + ((size_t)hs << P.lg_page);
-    uint8_t* to = (uint8_t*)(key ? P.k : P.v) + row * (D * BITS / 8) + c * BITS;
-    if constexpr (BITS == 8) *reinterpret_cast<u32x2g*>(to) = u32x2g{code[0], code[1]};
-    else *reinterpret_cast<uint32_t*>(to) = code[0];
-    if ((c & 3) == 0) (key ? X.k_scale : X.v_scale)[row * (D / 32) + c / 4] = (uint8_t)s;
   }
 }
 
-// One wave per token: a lane takes a chunk of codes at a time.
-template <typename T, int D, int BITS>
+// TOKENS adjacent tokens to a wave; a lane takes a chunk of codes at a time, kReadRounds of them under way.  Bound by memory (55591 rows of 8 x 128
+// channels, 8 bits, four tokens a wave: 74 us, 4.7 TB/s; one: 77).  From kReadMany tokens on there are waves enough for four, and more is stored
+// than the caches hold: the stores pass them by (74 us; with ordinary ones 90).  Fewer are left in the caches for whom they are read for (7817
+// tokens of 4 bits: 15 us; past the caches 26).
+constexpr int kReadRounds = 4, kReadMany = 16384;
+template <typename T, int D, int BITS, int TOKENS>
 __global__ __launch_bounds__(64 * kPackWaves) void k_packed_read(Paged P, PackedArgs X) {
   typedef PoolRow<T, D, BITS> Row;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t = blockIdx.x * kPackWaves + wave;
-  if (t >= P.N) return;
-  const Place place = place_of(P, t, lane);
-  if (place.b < 0) return;
-  for (int it = lane; it < 2 * P.H * Row::kLanes; it += 64) {
-    const int h = it / Row::kLanes, c = it % Row::kLanes, hs = h < P.H ? h : h - P.H;
-    const bool key = h < P.H;
-    T* out = (T*)(key ? X.k : X.v);
-    if (!out) continue;
-    u32x4g w[Row::kOut];
-    if (place.row0 >= 0) {
-      typename Row::Chunk chunk;
-      Row::load_chunk(key ? P.k : P.v, key ? X.k_scale : X.v_scale, (size_t)place.row0 + ((size_t)hs << P.lg_page), c, chunk);
-      Row::expand(chunk, w);
-    } else {
+  const int t0 = (blockIdx.x * kPackWaves + wave) * TOKENS;
+  if (t0 >= P.N) return;
+  const int at0 = min(lane, P.B - 1), sq0 = P.cu_q[at0], sq1 = P.cu_q[at0 + 1], skv = P.kv_len[at0];
+  Place o[TOKENS];
+  int row0[TOKENS];
 #pragma unroll
-      for (int o = 0; o < Row::kOut; ++o) w[o] = u32x4g{0, 0, 0, 0};
+  for (int i = 0; i < TOKENS; ++i) o[i] = t0 + i < P.N ? place_of(P, t0 + i, lane, sq0, sq1, skv) : Place{-1, 0, 0};
+#pragma unroll
+  for (int i = 0; i < TOKENS; ++i) row0[i] = row_of(P, o[i]);
+  const int per = 2 * P.H * Row::kLanes;                           // chunks of a token
+  for (int it0 = lane; it0 < TOKENS * per; it0 += 64 * kReadRounds) {
+    typename Row::Chunk chunk[kReadRounds];
+    int row[kReadRounds], to[kReadRounds], in[kReadRounds];        // row, and its output's among the token's keys (values: from P.H on); -1: none
+#pragma unroll
+    for (int u = 0; u < kReadRounds; ++u) {
+      const int it = it0 + 64 * u, i = TOKENS == 1 ? 0 : min(it / per, TOKENS - 1), left = it - i * per, h = left / Row::kLanes;
+      int r0 = row0[0], b = o[0].b;
+#pragma unroll
+      for (int e = 1; e < TOKENS; ++e)
+        if (i == e) { r0 = row0[e]; b = o[e].b; }
+      in[u] = left % Row::kLanes;
+      to[u] = left < per && b >= 0 && (h < P.H ? X.k : X.v) ? 2 * P.H * i + h : -1;
+      row[u] = r0 < 0 || to[u] < 0 ? -1 : r0 + ((h < P.H ? h : h - P.H) << P.lg_page);
+      if (row[u] >= 0) Row::load_chunk(h < P.H ? P.k : P.v, h < P.H ? X.k_scale : X.v_scale, (size_t)row[u], in[u], chunk[u]);
     }
-    u32x4g* to = reinterpret_cast<u32x4g*>(out + ((size_t)t * P.H + hs) * D) + Row::kOut * c;
 #pragma unroll
-    for (int o = 0; o < Row::kOut; ++o) to[o] = w[o];
+    for (int u = 0; u < kReadRounds; ++u) {
+      if (to[u] < 0) continue;
+      u32x4g w[Row::kOut];
+#pragma unroll
+      for (int e = 0; e < Row::kOut; ++e) w[e] = u32x4g{0, 0, 0, 0};
+      if (row[u] >= 0) Row::expand(chunk[u], row[u], in[u], w);
+      const int i = to[u] / (2 * P.H), h = to[u] % (2 * P.H);
+      T* out = (h < P.H ? (T*)X.k : (T*)X.v) + ((size_t)(t0 + i) * P.H + (h < P.H ? h : h - P.H)) * D;
+#pragma unroll
+      for (int e = 0; e < Row::kOut; ++e) {
+        u32x4g* at = reinterpret_cast<u32x4g*>(out) + Row::kOut * in[u] + e;
+        if constexpr (TOKENS > 1) __builtin_nontemporal_store(w[e], at);
+        else *at = w[e];
+      }
+    }
   }
 }
 
@@ -216,15 +293,22 @@ template <typename F> static hipError_t dispatch_packed(int dtype, int D, int bi
 }
 
 hipError_t launch_packed_append(int dtype, int D, int bits, const AppendArgs& A, const PackedArgs& X, hipStream_t st) {
+  // A wave takes two batches of a token where there are tokens for the whole chip, of fewer one (7817 tokens: 41 us by ones, 38 by twos, 39 by threes).
+  const int all = kv_batches(A.P.H, D) + q_batches(A.Hq, D), per_wave = A.P.N >= 2048 ? 2 : 1;
+  const dim3 grid((A.P.N + kPackWaves - 1) / kPackWaves, (all + per_wave - 1) / per_wave);
   return dispatch_packed(dtype, D, bits, [&](auto t, auto d, auto b) {
-    k_packed_append<typename decltype(t)::type, decltype(d)::value, decltype(b)::value><<<(A.P.N + kPackWaves - 1) / kPackWaves, 64 * kPackWaves, 0, st>>>(A, X);
+    k_packed_append<typename decltype(t)::type, decltype(d)::value, decltype(b)::value><<<grid, 64 * kPackWaves, 0, st>>>(A, X, per_wave);
     return hipGetLastError();
   });
 }
 
 hipError_t launch_packed_read(int dtype, int D, int bits, const Paged& P, const PackedArgs& X, hipStream_t st) {
   return dispatch_packed(dtype, D, bits, [&](auto t, auto d, auto b) {
-    k_packed_read<typename decltype(t)::type, decltype(d)::value, decltype(b)::value><<<(P.N + kPackWaves - 1) / kPackWaves, 64 * kPackWaves, 0, st>>>(P, X);
+    constexpr int D_ = decltype(d)::value, B_ = decltype(b)::value, many = 4;
+    typedef typename decltype(t)::type T;
+    auto groups = [&](int tokens) { return (P.N + kPackWaves * tokens - 1) / (kPackWaves * tokens); };
+    if (P.N >= kReadMany) k_packed_read<T, D_, B_, many><<<groups(many), 64 * kPackWaves, 0, st>>>(P, X);
+    else k_packed_read<T, D_, B_, 1><<<groups(1), 64 * kPackWaves, 0, st>>>(P, X);
     return hipGetLastError();
   });
 }

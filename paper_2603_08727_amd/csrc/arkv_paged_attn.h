@@ -34,8 +34,12 @@ constexpr int kChunkRows = 128, kChunkKeys = 64;
 // How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
 // blocks: of kChunkRows rows, of all sequences, at most.  joined: the last workgroup of a (sequence, kv-head), chunk_joined: of a block
 // and kv-head joins its pieces (tickets from chunk_ticket0 on), no launch is needed for that.
-struct Cut { int step_piece, n_step, chunk_piece, n_chunk, blocks, chunk_ticket0; bool joined, chunk_joined; Which w; };
+struct Cut { int step_piece, n_step, groups, chunk_piece, n_chunk, blocks, places, chunk_ticket0; bool joined, chunk_joined, chunk_spread; Which w; };
 constexpr int kJoinPieces = 16;         // at most: a lane has all pieces' loads under way at once
+// Limited sight and packed rows: sequences of more than kStepRows rows are paged_step's too, in groups of kStepRows, where all groups' tiles of 64
+// keys are this few (25 drafts, 4 heads a group, 2100 rows: 14 us, as blocks 20; 8 x 16 drafts: 23 and 32; 64 drafts on 8192 rows, 17408 tiles of 16 bits:
+// 47 and 34); and pieces of blocks are joined by a launch from more than kFewPieces on (9 pieces: 27 us joined in the launch, 20 by another).
+constexpr int kGroupTiles = 8192, kGroupWorkgroups = 256, kFewPieces = 4;
 constexpr int kJoinBlocks = 2048;       // pieces of blocks that are joined in the launch, at most (they take 67 KB of workspace each)
 
 inline Cut cut_of(const Paged& P, const Sight& V, int D, int Hq) {
@@ -48,7 +52,8 @@ inline Cut cut_of(const Paged& P, const Sight& V, int D, int Hq) {
     piece = (int)std::min<long long>(most, std::max<long long>(least, (p + unit - 1) / unit * unit));
     n = std::max(1, (kv + piece - 1) / piece);
   };
-  const int kv_step = most_keys(P, V, kStepRows / G), kv_chunk = most_keys(P, V, (kChunkRows - 1) / G + 2);
+  int kv_step = most_keys(P, V, kStepRows / G);
+  const int kv_chunk = most_keys(P, V, (kChunkRows - 1) / G + 2);
   // A workgroup for each CU, and no more pieces than the last workgroup joins (8 heads x 1024 rows: 6.6 us in pieces of 128
   // keys, 9.6 of 512, 12.4 in one; x 8192: 13.7 us in pieces of 128 and a launch that joins them, 11.9 of 512; 32 heads x
   // 8192: 29.6 us in pieces of 512, 28.7 of 1024), but no large ones: sequences differ in length, and the last round of
@@ -65,6 +70,19 @@ inline Cut cut_of(const Paged& P, const Sight& V, int D, int Hq) {
   pieces(kv_chunk, blocks, 256, 256, 1 << 28, kChunkKeys, alone, n_alone);
   pieces(kv_chunk, blocks, D == 64 ? 768 : 512, D == 64 ? 512 : 1024, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
   if (alone < c.chunk_piece) { c.chunk_piece = alone; c.n_chunk = n_alone; }
+  if (V.on && c.w.chunk) {
+    const long long groups = rows / kStepRows + std::min<long long>(P.B, rows), keys = most_keys(P, V, (kStepRows - 1) / G + 2);
+    int piece, n;
+    pieces((int)keys, groups * P.H, kGroupWorkgroups, std::max(128, ((int)keys + 2047) / 2048 * 128), kStepMaxPiece, 128, piece, n);
+    if (groups * P.H <= kJoinUnits && groups * P.H * ((keys + 63) / 64) <= kGroupTiles && n <= kJoinPieces) {
+      c.groups = (int)groups;
+      c.step_piece = piece;
+      c.n_step = n;
+      c.w = {true, false, kStepRows};
+      c.joined = true;
+      return c;
+    }
+  }
   c.joined = c.n_step <= kJoinPieces && units <= kJoinUnits;
   // (a sequence that is the chunk kernel's has more rows than the step kernel takes)
   c.blocks = (int)(rows / kChunkRows + std::min<long long>(P.B, c.w.step ? rows / (kStepRows + 1) : P.B));
@@ -72,18 +90,30 @@ inline Cut cut_of(const Paged& P, const Sight& V, int D, int Hq) {
   // (512 tokens on 4100 rows, 16 heads, beside 7 single tokens: 60 us, with a launch that joins 70)
   c.chunk_joined = c.n_chunk <= kJoinPieces && (long long)c.blocks * P.H + c.chunk_ticket0 <= kJoinUnits &&
                    (long long)c.blocks * P.H * c.n_chunk <= kJoinBlocks;
+  if (V.on) {
+    // the kernel may find that pieces down to half as long fit the chip at once
+    const int half = std::max(D == 64 ? 256 : 512, c.chunk_piece / 2 / kChunkKeys * kChunkKeys), n = (kv_chunk + half - 1) / half;
+    if (c.n_chunk > 1 && P.B <= 64 && (long long)c.blocks * P.H * n <= kJoinBlocks && half < c.chunk_piece) {
+      c.chunk_piece = half;
+      c.n_chunk = n;
+      c.places = 256 * (D == 64 ? 3 : 2);
+    }
+    c.chunk_joined = c.chunk_joined && c.n_chunk <= kFewPieces;
+    c.chunk_spread = c.w.chunk && !c.chunk_joined && c.n_chunk > 1 && (long long)c.blocks * P.H * c.n_chunk <= kJoinBlocks;
+  }
   return c;
 }
 
 // Pieces' results: sums [row][D] and (reference, denominator) [row].  Rows of paged_step: ((unit * n_step + piece) * 16 +
 // row), behind them rows of paged_chunk: (piece * N + token) * Hq + head, or, where its workgroups join them, kChunkRows rows of
 // ((block * H + head) * n_chunk + piece), each wave's as they lie in its lanes.
-struct Parts { float* acc; float2* ml; int* tickets; size_t chunk0; };
+// split: what k_chunk_join needs of each block of rows and kv-head: pieces, first token, tokens, which block of the sequence's.
+struct Parts { float* acc; float2* ml; int* tickets; size_t chunk0; int4* split; };
 
 inline size_t part_rows(const Paged& P, int Hq, const Cut& c, size_t& chunk0) {
-  chunk0 = c.w.step && c.n_step > 1 ? (size_t)P.B * P.H * c.n_step * kStepRows : 0;
+  chunk0 = c.w.step && c.n_step > 1 ? (size_t)(c.groups ? c.groups : P.B) * P.H * c.n_step * kStepRows : 0;
   if (!c.w.chunk || c.n_chunk == 1) return chunk0;
-  return chunk0 + (c.chunk_joined ? (size_t)c.blocks * P.H * c.n_chunk * kChunkRows : (size_t)c.n_chunk * P.N * Hq);
+  return chunk0 + (c.chunk_joined || c.chunk_spread ? (size_t)c.blocks * P.H * c.n_chunk * kChunkRows : (size_t)c.n_chunk * P.N * Hq);
 }
 
 // Partial results and tickets go past the L2 of one XCD: device-scope relaxed atomics.  A workgroup waits until its stores are
@@ -114,12 +144,61 @@ template <typename T> __device__ __forceinline__ void store4(T* p, float a, floa
   *reinterpret_cast<u32x2g*>(p) = u32x2g{Mfma<T>::pack(a, b), Mfma<T>::pack(c, d)};
 }
 
+// Blocks of ROWS rows that a sequence of more than `few` makes.
+template <int ROWS> __host__ __device__ __forceinline__ int row_blocks(int nq, int G, int few) { return nq * G <= few ? 0 : (nq * G + ROWS - 1) / ROWS; }
+
+// Sequence and block of the rank-th block of a launch; the lanes of a wave look at 64 sequences at a time.
+template <int ROWS>
+__device__ __forceinline__ bool find_block(const Paged& P, int G, int few, int rank, int lane, int& b, int& blk, Seq& s) {
+  for (int i = 0; i < P.B; i += 64) {
+    const Seq own = seq_of(P, min(i + lane, P.B - 1));
+    const int mine = i + lane < P.B ? row_blocks<ROWS>(own.nq, G, few) : 0;
+    int sum = mine;                                                // blocks up to and with this lane's sequence
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int below = __shfl_up(sum, o);
+      if (lane >= o) sum += below;
+    }
+    const uint64_t hit = __ballot(sum > rank);
+    if (hit) {
+      const int first = __builtin_ctzll(hit);
+      b = i + first;
+      const int n = __builtin_amdgcn_readlane(mine, first);
+      blk = n - 1 - (rank - (__builtin_amdgcn_readlane(sum, first) - n));   // the block that sees most comes first
+      s = {__builtin_amdgcn_readlane(own.q0, first), __builtin_amdgcn_readlane(own.nq, first), __builtin_amdgcn_readlane(own.kv, first)};
+      return true;
+    }
+    rank -= __builtin_amdgcn_readlane(sum, 63);
+  }
+  return false;
+}
+
 // ---- few rows -----------------------------------------------------------------------------------------
 
 // One workgroup = one piece of a (sequence, kv-head); its waves take a quarter of the piece each, 32 keys at a time, with
 // 16x16x32 MFMAs (lane: row lane % 16, keys 4 (lane / 16) .. + 3 of each granule).  Keys come from memory in operand
 // layout; values in whole rows, through LDS of the wave's own.  A tile's loads are in flight while the tile before it
 // is worked on.
+// Pages of a wave's granules, from key w0 on, of which there are 64 at most: lane i holds the page of granule i.  One that is not there, or lies
+// behind the keys below `end`, becomes page 0, whose rows nobody sees.
+template <bool SIGHT> struct GranulePages {
+  const Paged& P;
+  const Keys<SIGHT>& keys;
+  int h, w0, page;
+  uint64_t there;
+  __device__ __forceinline__ GranulePages(const Paged& P, const Keys<SIGHT>& keys, int b, int h, int w0, int end, int lane) : P(P), keys(keys), h(h), w0(w0) {
+    const int j = w0 + 16 * lane;
+    page = j < end ? P.table[(size_t)b * P.width + (keys.slot(j) >> P.lg_page)] : -1;
+    const bool ok = (unsigned)page < (unsigned)P.n_pages;
+    there = __ballot(ok);
+    if (!ok) page = 0;
+  }
+  __device__ __forceinline__ size_t row(int g) const {             // first row of granule g
+    const int p = __builtin_amdgcn_readlane(page, g);
+    return (size_t)(unsigned)(((p * P.H + h) << P.lg_page) + (keys.slot(w0 + 16 * g) & ((1 << P.lg_page) - 1)));
+  }
+};
+
 template <int D> struct StepLds {
   union {                                 // a wave's values while it works, its sums behind that
     uint16_t v[32][D + 16];               // (the pitch: transposing reads of 16 rows meet each bank twice, as they must)
@@ -129,14 +208,18 @@ template <int D> struct StepLds {
   int last;                               // whether this workgroup's piece was the last one to be finished
 };
 
+// One of the np pieces that a (sequence, kv-head) is cut into; first: rows of the workspace in front of its first piece's.  ticket: of the
+// launch that joins its pieces itself; null: another launch does.
+struct Piece { int np, index; size_t first; int* ticket; };
+
 // The waves' results of a piece together: the row's output where the piece is the only one, else into the workspace, from where the
 // last workgroup of the sequence's head joins them.
 template <typename T, int D>
-__device__ __forceinline__ void step_finish(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, StepLds<D>& sm, const Seq& s, int h, int unit,
-                                            int piece, int np, const f32x4g (&acc)[D / 16], float m, float l) {
+__device__ __forceinline__ void step_finish(const PagedAttnArgs& A, const Parts& parts, StepLds<D>& sm, const Seq& s, int r0, int h, const Piece& pc,
+                                            const f32x4g (&acc)[D / 16], float m, float l) {
   constexpr int CB = D / 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 15, gq = lane >> 4, R = s.nq * A.G, n_pieces = cut.n_step;
+  const int n = lane & 15, gq = lane >> 4, R = min(s.nq * A.G - r0, kStepRows), np = pc.np;
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
 #pragma unroll
@@ -144,7 +227,7 @@ __device__ __forceinline__ void step_finish(const PagedAttnArgs& A, const Cut& c
   if (gq == 0) sm.ml[wave][n] = make_float2(m, l);
   __syncthreads();
   auto finish = [&](int r, int c, f32x4g o, float mm, float ll) {  // four channels of a row's result
-    const size_t orow = (size_t)(s.q0 + r / A.G) * A.Hq + h * A.G + r % A.G;
+    const size_t orow = (size_t)(s.q0 + (r0 + r) / A.G) * A.Hq + h * A.G + (r0 + r) % A.G;
     const float inv = ll == 0.f ? 0.f : 1.f / ll;                  // (NaN stays)
     store4((T*)A.out + orow * D + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
     if (c == 0 && A.lse) A.lse[orow] = ll == 0.f ? -INFINITY : kLn2 * (mm + log2f(ll));
@@ -163,34 +246,33 @@ __device__ __forceinline__ void step_finish(const PagedAttnArgs& A, const Cut& c
       o += f * *reinterpret_cast<const f32x4g*>(&sm.w[w].acc[r][c]);
     }
     if (np > 1) {
-      const size_t pr = ((size_t)unit * n_pieces + piece) * kStepRows + r;
+      const size_t pr = pc.first + pc.index * kStepRows + r;
       put4(parts.acc + pr * D + c, o);
       if (c == 0) put2(parts.ml + pr, mm, ll);
     } else {
       finish(r, c, o, mm, ll);
     }
   }
-  if (np == 1 || !cut.joined) return;
+  if (np == 1 || !pc.ticket) return;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                 // this wave's stores are where everyone sees them
   __syncthreads();
-  int* ticket = parts.tickets + unit * kTicketWords;
   if (threadIdx.x == 0) {
-    const int drawn = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int drawn = __hip_atomic_fetch_add(pc.ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sm.last = drawn == np - 1;
-    if (sm.last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call wants it
+    if (sm.last) __hip_atomic_store(pc.ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call wants it
   }
   __syncthreads();
   if (!sm.last) return;
   for (int it = threadIdx.x; it < R * (D / 4); it += 64 * kStepWaves) {
     const int r = it / (D / 4), c = 4 * (it % (D / 4));
-    const size_t first = (size_t)unit * n_pieces * kStepRows + r;
     float2 ml[kJoinPieces];
     f32x4g x[kJoinPieces];
 #pragma unroll
     for (int p = 0; p < kJoinPieces; ++p) {
       if (p < np) {
-        ml[p] = take2(parts.ml + first + p * kStepRows);
-        x[p] = take4(parts.acc + (first + p * kStepRows) * D + c);
+        const size_t pr = pc.first + p * kStepRows + r;
+        ml[p] = take2(parts.ml + pr);
+        x[p] = take4(parts.acc + pr * D + c);
       }
     }
     float mm = kUnset, ll = 0.f;
@@ -210,26 +292,17 @@ __device__ __forceinline__ void step_finish(const PagedAttnArgs& A, const Cut& c
 }
 
 template <typename T, int D, int MODE, bool SIGHT>
-__device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, StepLds<D>& sm, int id) {
+__device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Parts& parts, StepLds<D>& sm, const Seq& s, int b, int r0, int h, int prefix,
+                                           const Keys<SIGHT>& keys, int p0, int p1, const Piece& pc) {
   constexpr int CAP = Mode<MODE>::cap;
   constexpr bool DIST = Mode<MODE>::dist;
   typedef PoolRow<T, D, 16> Row;
   constexpr int KK = D / 32, CB = D / 16;                          // k-steps, channel blocks
   constexpr int CPR = Row::kLanes, RPI = 64 / CPR, VI = 32 / RPI;  // lanes per row, rows per load, loads of a value tile
-  const int piece_keys = cut.step_piece, n_pieces = cut.n_step;
   const Paged& P = A.P;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 15, gq = lane >> 4;
-  const int unit = id % (P.B * P.H), piece = id / (P.B * P.H), h = unit % P.H, b = unit / P.H;
-  const Seq s = seq_of(P, b);
-  const int R = s.nq * A.G;
-  if (R == 0 || R > kStepRows) return;
-  const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
-  const Keys<SIGHT> keys(A.V, s, prefix, 0, s.nq - 1);
-  const int end = keys.end;
-  const int np = max(1, (end + piece_keys - 1) / piece_keys);
-  if (piece >= np) return;
-  const int row = n < R ? n : 0;
+  const int n = lane & 15, gq = lane >> 4, R = min(s.nq * A.G - r0, kStepRows);
+  const int row = r0 + (n < R ? n : 0);
   const RowView<SIGHT> view(A.V, s, prefix, row / A.G, n < R);
   const int hq = h * A.G + row % A.G, tok = s.q0 + row / A.G;
   const Logit lg(A.S);
@@ -242,26 +315,12 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) q[kk] = *reinterpret_cast<const u32x4g*>(p + Row::channel(gq, kk));
   }
-  // this wave's keys: [w0, w1), whole tiles
-  const int p0 = piece * piece_keys, p1 = min(p0 + piece_keys, end);
+  // this wave's of the piece's keys p0 .. p1 - 1: [w0, w1), whole tiles
   const int tiles = (p1 - p0 + 31) / 32, per = (tiles + kStepWaves - 1) / kStepWaves;
   const int t0 = min(per * wave, tiles), t1 = min(t0 + per, tiles);
   const int w0 = p0 + 32 * t0;
-  // lane i holds the page id of granule i from w0 on; one that is not there becomes page 0, whose rows nobody sees
-  int my_page;
-  bool page_ok;
-  {
-    const int j = w0 + 16 * lane;
-    my_page = j < p1 ? P.table[(size_t)b * P.width + (keys.slot(j) >> P.lg_page)] : 0;
-    page_ok = (unsigned)my_page < (unsigned)P.n_pages;
-    if (!page_ok) my_page = 0;
-  }
-  const uint64_t ok_mask = __ballot(page_ok);
-  const int in_page = (1 << P.lg_page) - 1;
-  auto granule_row = [&](int g) {                                  // first row of granule g
-    const int page = __builtin_amdgcn_readlane(my_page, g);
-    return (size_t)(unsigned)(((page * P.H + h) << P.lg_page) + (keys.slot(w0 + 16 * g) & in_page));
-  };
+  const GranulePages<SIGHT> pages(P, keys, b, h, w0, p1, lane);
+  auto granule_row = [&](int g) { return pages.row(g); };
 
   typename Row::Keys kb[2][2];
   typename Row::Chunk vb[VI];
@@ -290,9 +349,10 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
     for (int g = 0; g < 2; ++g) {
       x[g] = f32x4g{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) x[g] = Mfma<T>::m16(Row::operand(kc[g], gq, kk), q[kk], x[g]);
+      for (int kk = 0; kk < KK; ++kk) x[g] = Mfma<T>::m16(Row::operand(kc[g], n, gq, kk), q[kk], x[g]);
     }
-    const bool masked = !keys.all_seen(j0, 32) || (ok_mask >> (2 * t) & 3) != 3;
+    const uint32_t ok = (uint32_t)(pages.there >> (2 * t)) & 3;
+    const bool masked = !keys.all_seen(j0, 32) || ok != 3;
     float mul = lg.mul;
     if (CAP || DIST) {
       mul = 1.f;
@@ -312,11 +372,11 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
     uint32_t odd = 0;                                              // keys of this tile whose values are not all finite
     u32x4g vw[VI][Row::kOut];                                      // values, as the product takes them
 #pragma unroll
-    for (int i = 0; i < VI; ++i) Row::expand(vb[i], vw[i]);
+    for (int i = 0; i < VI; ++i) Row::expand(vb[i], 0, 0, vw[i]);
     if (masked) {
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        const auto seen = view.granule(keys.slot(j0 + 16 * g), ok_mask >> (2 * t + g) & 1, 4 * gq);
+        const auto seen = view.granule(keys.slot(j0 + 16 * g), ok >> g & 1, 4 * gq);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[g][i] = seen.at(i) ? x[g][i] * mul : -INFINITY;
       }
@@ -390,7 +450,7 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
       for (int e = 0; e < 8; ++e)
         if (e == 4 * g + i) pj = Mfma<T>::get(opaque(pb[e / 2]), e & 1);
       pj = __shfl(pj, n + 16 * from);
-      const bool seen = view.granule(keys.slot(j0 + 16 * g), ok_mask >> (2 * t + g) & 1, 0).at(j & 15);
+      const bool seen = view.granule(keys.slot(j0 + 16 * g), ok >> g & 1, 0).at(j & 15);
       const size_t vrow = granule_row(2 * t + g) + (j & 15);
 #pragma unroll
       for (int c = 0; c < CB; ++c)
@@ -413,32 +473,24 @@ __device__ __forceinline__ void paged_step(const PagedAttnArgs& A, const Cut& cu
       }
     }
   }
-  step_finish<T, D>(A, cut, parts, sm, s, h, unit, piece, np, acc, m, l);
+  step_finish<T, D>(A, parts, sm, s, r0, h, pc, acc, m, l);
 }
 
 // The same over packed rows, 64 keys at a time: a tile's codes are few registers, and are requested again as soon as they are
 // expanded, so that most of a tile's time lies between request and use (8 bits: 17 KB a wave under way, 4 bits: 9 KB).  A lane's keys of a
 // row are whole chunks of it (PoolRow::channel).
 template <typename T, int D, int MODE, int BITS>
-__device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, StepLds<D>& sm, int id) {
+__device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Parts& parts, StepLds<D>& sm, const Seq& s, int b, int r0, int h, int prefix,
+                                            const Keys<true>& keys, int p0, int p1, const Piece& pc) {
   constexpr int CAP = Mode<MODE>::cap;
   constexpr bool DIST = Mode<MODE>::dist;
   typedef PoolRow<T, D, BITS> Row;
   constexpr int KK = D / 32, CB = D / 16;                          // k-steps, channel blocks
   constexpr int CPR = Row::kLanes, RPI = 64 / CPR, VI = 32 / RPI;  // lanes per row, rows per load, loads of half a tile's values
-  const int piece_keys = cut.step_piece;
   const Paged& P = A.P;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 15, gq = lane >> 4;
-  const int unit = id % (P.B * P.H), piece = id / (P.B * P.H), h = unit % P.H, b = unit / P.H;
-  const Seq s = seq_of(P, b);
-  const int R = s.nq * A.G;
-  if (R == 0 || R > kStepRows) return;
-  const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
-  const Keys<true> keys(A.V, s, prefix, 0, s.nq - 1);
-  const int np = max(1, (keys.end + piece_keys - 1) / piece_keys);
-  if (piece >= np) return;
-  const int row = n < R ? n : 0;
+  const int n = lane & 15, gq = lane >> 4, R = min(s.nq * A.G - r0, kStepRows);
+  const int row = r0 + (n < R ? n : 0);
   const RowView<true> view(A.V, s, prefix, row / A.G, n < R);
   const int hq = h * A.G + row % A.G, tok = s.q0 + row / A.G;
   const Logit lg(A.S);
@@ -451,37 +503,22 @@ __device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Cut& c
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) q[kk] = *reinterpret_cast<const u32x4g*>(p + Row::channel(gq, kk));
   }
-  // this wave's keys: [w0, w1), a multiple of 32 from p0 on
-  const int p0 = piece * piece_keys, p1 = min(p0 + piece_keys, keys.end);
+  // this wave's of the piece's keys p0 .. p1 - 1: [w0, w1), a multiple of 32 from p0 on
   const int halves = (p1 - p0 + 31) / 32, per = (halves + kStepWaves - 1) / kStepWaves;
   const int w0 = min(p0 + 32 * per * wave, p1), w1 = min(w0 + 32 * per, p1), nt = (w1 - w0 + 63) / 64;
-  // lane i holds the page id of granule i from w0 on; one that is not there, or not this wave's, becomes page 0, whose rows nobody sees
-  int my_page;
-  bool page_ok;
-  {
-    const int j = w0 + 16 * lane;
-    my_page = j < w1 ? P.table[(size_t)b * P.width + (keys.slot(j) >> P.lg_page)] : -1;
-    page_ok = (unsigned)my_page < (unsigned)P.n_pages;
-    if (!page_ok) my_page = 0;
-  }
-  const uint64_t ok_mask = __ballot(page_ok);
-  const int in_page = (1 << P.lg_page) - 1;
-  auto granule_row = [&](int g) {                                  // first row of granule g
-    const int page = __builtin_amdgcn_readlane(my_page, g);
-    return (size_t)(unsigned)(((page * P.H + h) << P.lg_page) + (keys.slot(w0 + 16 * g) & in_page));
-  };
+  const GranulePages<true> pages(P, keys, b, h, w0, w1, lane);
 
   typename Row::Keys kr[4];
   typename Row::Chunk vr[2][VI];
   auto load_k = [&](int t) {
 #pragma unroll
-    for (int g = 0; g < 4; ++g) Row::load_keys(A, granule_row(4 * t + g), n, gq, kr[g]);
+    for (int g = 0; g < 4; ++g) Row::load_keys(A, pages.row(4 * t + g), n, gq, kr[g]);
   };
   auto load_v = [&](int t, int half) {
 #pragma unroll
     for (int i = 0; i < VI; ++i) {
       const int first = RPI * i + lane / CPR;                      // (a load's rows lie in one granule)
-      Row::load_chunk(P.v, A.v_scale, granule_row(4 * t + 2 * half + RPI * i / 16) + (first & 15), lane % CPR, vr[half][i]);
+      Row::load_chunk(P.v, A.v_scale, pages.row(4 * t + 2 * half + RPI * i / 16) + (first & 15), lane % CPR, vr[half][i]);
     }
   };
   f32x4g acc[CB];
@@ -500,10 +537,11 @@ __device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Cut& c
     for (int g = 0; g < 4; ++g) {
       x[g] = f32x4g{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) x[g] = Mfma<T>::m16(Row::operand(kr[g], gq, kk), q[kk], x[g]);
+      for (int kk = 0; kk < KK; ++kk) x[g] = Mfma<T>::m16(Row::operand(kr[g], n, gq, kk), q[kk], x[g]);
     }
-    if (t + 1 < nt) load_k(t + 1);
-    const bool masked = !keys.all_seen(j0, 64) || (ok_mask >> (4 * t) & 15) != 15;
+    load_k(t + 1);                                                 // (behind the last tile: rows of page 0.  A branch here would be waited for)
+    const uint32_t ok = (uint32_t)(pages.there >> (4 * t)) & 15;
+    const bool masked = !keys.all_seen(j0, 64) || ok != 15;
     float mul = lg.mul;
     if (CAP || DIST) {
       mul = 1.f;
@@ -512,7 +550,7 @@ __device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Cut& c
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[g][i] = lg.logit<CAP>(x[g][i]);
         if (DIST) {
-          const int4 kp = *reinterpret_cast<const int4*>(P.pos + granule_row(4 * t + g) + 4 * gq);
+          const int4 kp = *reinterpret_cast<const int4*>(P.pos + pages.row(4 * t + g) + 4 * gq);
           x[g][0] = fmaf(-slope, fabsf((float)(qp - kp.x)), x[g][0]);
           x[g][1] = fmaf(-slope, fabsf((float)(qp - kp.y)), x[g][1]);
           x[g][2] = fmaf(-slope, fabsf((float)(qp - kp.z)), x[g][2]);
@@ -523,7 +561,7 @@ __device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Cut& c
     if (masked) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const auto seen = view.granule(keys.slot(j0 + 16 * g), ok_mask >> (4 * t + g) & 1, 4 * gq);
+        const auto seen = view.granule(keys.slot(j0 + 16 * g), ok >> g & 1, 4 * gq);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[g][i] = seen.at(i) ? x[g][i] * mul : -INFINITY;
       }
@@ -565,7 +603,7 @@ __device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Cut& c
 #pragma unroll
       for (int i = 0; i < VI; ++i) {
         u32x4g w[Row::kOut];
-        Row::expand(vr[half][i], w);
+        Row::expand(vr[half][i], lane / CPR, lane % CPR, w);
         if (masked) {
           // a value that is not finite would spoil the rows that do not see it: it leaves the product, and is added below
           uint32_t any = 0;
@@ -586,7 +624,7 @@ __device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Cut& c
         for (int o = 0; o < Row::kOut; ++o)
           *reinterpret_cast<u32x4g*>(&sm.w[wave].v[RPI * i + lane / CPR][8 * (Row::kOut * (lane % CPR) + o)]) = w[o];
       }
-      if (t + 1 < nt) load_v(t + 1, half);
+      load_v(t + 1, half);
 #pragma unroll
       for (int c = 0; c < CB; ++c) {
         const s16x4g a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.w[wave].v[4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);
@@ -604,8 +642,8 @@ __device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Cut& c
           if (e == 4 * g + i) pj = Mfma<T>::get(opaque(pb[e / 2]), e & 1);
         pj = __shfl(pj, n + 16 * from);
         const int granule = 4 * t + 2 * half + g;
-        const bool seen = view.granule(keys.slot(w0 + 16 * granule), ok_mask >> granule & 1, 0).at(j & 15);
-        const size_t vrow = granule_row(granule) + (j & 15);
+        const bool seen = view.granule(keys.slot(w0 + 16 * granule), ok >> (2 * half + g) & 1, 0).at(j & 15);
+        const size_t vrow = pages.row(granule) + (j & 15);
 #pragma unroll
         for (int c = 0; c < CB; ++c)
 #pragma unroll
@@ -616,38 +654,40 @@ __device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Cut& c
       }
     }
   }
-  step_finish<T, D>(A, cut, parts, sm, s, h, unit, piece, np, acc, m, l);
+  step_finish<T, D>(A, parts, sm, s, r0, h, pc, acc, m, l);
+}
+
+// The keys of a row of 16-bit pages, or of packed ones.
+template <typename T, int D, int MODE, int BITS, bool SIGHT, typename... Rest>
+__device__ __forceinline__ void few_rows(const PagedAttnArgs& A, const Parts& parts, StepLds<D>& sm, const Rest&... rest) {
+  if constexpr (BITS == 16) paged_step<T, D, MODE, SIGHT>(A, parts, sm, rest...);
+  else packed_step<T, D, MODE, BITS>(A, parts, sm, rest...);
+}
+
+// Workgroup id of a launch for few rows: unit by unit, piece by piece.  In groups: a unit is kStepRows rows of a sequence's, of as many as it has.
+template <typename T, int D, int MODE, int BITS, bool SIGHT>
+__device__ __forceinline__ void cut_step(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, StepLds<D>& sm, int id) {
+  const Paged& P = A.P;
+  const bool grouped = SIGHT && cut.groups;
+  const int units = (grouped ? cut.groups : P.B) * P.H, unit = id % units, piece = id / units, h = unit % P.H;
+  int b = unit / P.H, group = 0;
+  Seq s;
+  if (grouped) {
+    if (!find_block<kStepRows>(P, A.G, 0, b, threadIdx.x & 63, b, group, s)) return;
+  } else {
+    s = seq_of(P, b);
+    if (s.nq == 0 || s.nq * A.G > kStepRows) return;
+  }
+  const int r0 = group * kStepRows, prefix = A.S.prefix ? A.S.prefix[b] : 0;
+  const Keys<SIGHT> keys(A.V, s, prefix, r0 / A.G, grouped ? min(s.nq * A.G - 1, r0 + kStepRows - 1) / A.G : s.nq - 1);
+  const int np = max(1, (keys.end + cut.step_piece - 1) / cut.step_piece);
+  if (piece >= np) return;
+  const int p0 = piece * cut.step_piece, p1 = min(p0 + cut.step_piece, keys.end);
+  const Piece pc = {np, piece, (size_t)unit * cut.n_step * kStepRows, cut.joined ? parts.tickets + unit * kTicketWords : nullptr};
+  few_rows<T, D, MODE, BITS, SIGHT>(A, parts, sm, s, b, r0, h, prefix, keys, p0, p1, pc);
 }
 
 // ---- many rows ----------------------------------------------------------------------------------------
-
-// Blocks of kChunkRows rows that paged_chunk makes of a sequence.
-__host__ __device__ __forceinline__ int chunk_blocks(int nq, int G, int few) { return nq * G <= few ? 0 : (nq * G + kChunkRows - 1) / kChunkRows; }
-
-// Sequence and block of the rank-th block of a launch; the lanes of a wave look at 64 sequences at a time.
-__device__ __forceinline__ bool find_block(const Paged& P, int G, int few, int rank, int lane, int& b, int& blk, Seq& s) {
-  for (int i = 0; i < P.B; i += 64) {
-    const Seq own = seq_of(P, min(i + lane, P.B - 1));
-    const int mine = i + lane < P.B ? chunk_blocks(own.nq, G, few) : 0;
-    int sum = mine;                                                // blocks up to and with this lane's sequence
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int below = __shfl_up(sum, o);
-      if (lane >= o) sum += below;
-    }
-    const uint64_t hit = __ballot(sum > rank);
-    if (hit) {
-      const int first = __builtin_ctzll(hit);
-      b = i + first;
-      const int n = __builtin_amdgcn_readlane(mine, first);
-      blk = n - 1 - (rank - (__builtin_amdgcn_readlane(sum, first) - n));   // the block that sees most comes first
-      s = {__builtin_amdgcn_readlane(own.q0, first), __builtin_amdgcn_readlane(own.nq, first), __builtin_amdgcn_readlane(own.kv, first)};
-      return true;
-    }
-    rank -= __builtin_amdgcn_readlane(sum, 63);
-  }
-  return false;
-}
 
 // One workgroup = 128 rows of a (sequence, kv-head) and a piece of the keys they see; a wave takes 32 rows with 32x32x16
 // MFMAs (lane: row lane % 32, keys 8 (i / 4) + 4 (lane / 32) + i % 4 of each half of a 64-key tile).  Keys and values of
@@ -663,27 +703,19 @@ template <int D> struct ChunkLds {
 };
 template <int D> __device__ __forceinline__ int v_chunk(int row, int c) { return D == 128 ? c ^ (row & 3) << 2 : c ^ (row >> 1 & 1) << 2; }
 
-template <typename T, int D, int MODE, int BITS, bool SIGHT>
-__device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, ChunkLds<D>& sm, int id) {
+// combine(sums, reference, denominator, token's row): what becomes of a lane's part of a row; whether the result is the row's now.
+template <typename T, int D, int MODE, int BITS, bool SIGHT, typename F>
+__device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, ChunkLds<D>& sm, const Seq& s, int b, int blk, int h, int prefix,
+                                            const Keys<SIGHT>& keys, int p0, int p1, F combine) {
   constexpr int CAP = Mode<MODE>::cap;
   constexpr bool DIST = Mode<MODE>::dist;
-  const int piece_keys = cut.chunk_piece;
   typedef PoolRow<T, D, BITS> Row;
   constexpr int KK = D / 16, CB = D / 32, CPR = D / 8;
   constexpr int RPI = 64 / Row::kLanes, LPG = 16 / RPI;            // rows per load, loads of a granule
   const Paged& P = A.P;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, hh = lane >> 5;
-  const int h = id % P.H, piece = id / (cut.blocks * P.H), bh = id % (cut.blocks * P.H);
-  int b, blk;
-  Seq s;
-  if (!find_block(P, A.G, cut.w.few, bh / P.H, lane, b, blk, s)) return;
-  const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
-  const int R = s.nq * A.G, r0 = blk * kChunkRows;
-  const Keys<SIGHT> keys(A.V, s, prefix, r0 / A.G, min(R - 1, r0 + kChunkRows - 1) / A.G);
-  const int end = keys.end;
-  const int np = max(1, (end + piece_keys - 1) / piece_keys);
-  if (piece >= np) return;
+  const int R = s.nq * A.G, r0 = blk * kChunkRows, end = keys.end;
   const int r = r0 + 32 * wave + n;
   const int rc = min(r, R - 1);
   const RowView<SIGHT> view(A.V, s, prefix, rc / A.G, r < R);
@@ -698,7 +730,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) q[kk] = *reinterpret_cast<const u32x4g*>(p + 16 * kk);
   }
-  const int p0 = piece * piece_keys, p1 = min(p0 + piece_keys, end), nt = (p1 - p0 + kChunkKeys - 1) / kChunkKeys;
+  const int nt = (p1 - p0 + kChunkKeys - 1) / kChunkKeys;
   const int32_t* table = P.table + (size_t)b * P.width;
   const int in_page = (1 << P.lg_page) - 1;
 
@@ -740,10 +772,10 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
         uint16_t* const kt = sm.k[buf] + wave * 16 * D + rr * D;
         uint16_t* const vt = sm.v[buf] + wave * 16 * D + rr * D;
         u32x4g w[Row::kOut];
-        Row::expand(kr[i], w);
+        Row::expand(kr[i], rr, in, w);
 #pragma unroll
         for (int o = 0; o < Row::kOut; ++o) *reinterpret_cast<u32x4g*>(kt + 8 * k_chunk<D>(rr, Row::kOut * in + o)) = w[o];
-        Row::expand(vr[i], w);
+        Row::expand(vr[i], rr, in, w);
 #pragma unroll
         for (int o = 0; o < Row::kOut; ++o) *reinterpret_cast<u32x4g*>(vt + 8 * v_chunk<D>(rr, Row::kOut * in + o)) = w[o];
       }
@@ -765,7 +797,8 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
 #pragma unroll
       for (int i = 0; i < LPG; ++i) Row::load_chunk(P.v, A.v_scale, row + RPI * i + lane / Row::kLanes, lane % Row::kLanes, vr[i]);
     }
-    if (DIST && lane < 16) load_lds4(P.pos + row + lane, lds_pos + 4 * (buf * kChunkKeys + 16 * wave));
+    const uint32_t at_pos = __builtin_amdgcn_readfirstlane(lds_pos + 4 * (buf * kChunkKeys + 16 * wave));
+    if (DIST && lane < 16) load_lds4(P.pos + row + lane, at_pos);
   };
 
   f32x16g acc[CB];
@@ -938,64 +971,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
   l += __shfl_xor(l, 32);
   if (l == 0.f) m = kUnset;
   const size_t orow = (size_t)tok * A.Hq + hq;
-  if (np > 1 && !cut.chunk_joined) {
-    if (r >= R) return;
-    const size_t pr = parts.chunk0 + (size_t)piece * P.N * A.Hq + orow;
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<f32x4g*>(parts.acc + pr * D + 32 * c + 8 * e + 4 * hh) =
-            f32x4g{acc[c][4 * e], acc[c][4 * e + 1], acc[c][4 * e + 2], acc[c][4 * e + 3]};
-    if (hh == 0) parts.ml[pr] = make_float2(m, l);
-    return;
-  }
-  if (np > 1) {
-    // 8 bytes per lane, adjacent lanes adjacent: where wave w's two channels i, i + 1 of block c lie in a piece's rows
-    const size_t row0 = parts.chunk0 + (size_t)bh * cut.n_chunk * kChunkRows + 32 * wave;
-    const uint32_t at = 8 * (uint32_t)lane;                        // (beside a uniform address: 64 bits a lane would not fit the registers)
-    auto sums = [&](int p, int c, int i) {
-      return reinterpret_cast<float2*>(reinterpret_cast<char*>(parts.acc + (row0 + (size_t)p * kChunkRows) * D) + (8 * c + i / 2) * 512 + at);
-    };
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) put2(sums(piece, c, i), acc[c][i], acc[c][i + 1]);
-    if (hh == 0) put2(parts.ml + row0 + (size_t)piece * kChunkRows + n, m, l);
-    vm_wait();                                                     // this wave's stores are where everyone sees them
-    __syncthreads();
-    int* ticket = parts.tickets + (cut.chunk_ticket0 + bh) * kTicketWords;
-    if (tid == 0) {
-      sm.last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == np - 1;
-      if (sm.last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call wants it
-    }
-    __syncthreads();
-    if (!sm.last) return;
-    m = kUnset;
-    l = 0.f;
-    for (int p = 0; p < np; ++p) m = fmaxf(m, take2(parts.ml + row0 + (size_t)p * kChunkRows + n).x);
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
-    for (int p = 0; p < np; ++p) {                                 // (always in this order, whoever is last)
-      const float2 z = take2(parts.ml + row0 + (size_t)p * kChunkRows + n);
-      float2 x[CB * 8];
-#pragma unroll
-      for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) x[8 * c + i / 2] = take2(sums(p, c, i));
-      const float f = exp2_hw(z.x - m);
-      l += f * z.y;
-#pragma unroll
-      for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          acc[c][i] += f * x[8 * c + i / 2].x;
-          acc[c][i + 1] += f * x[8 * c + i / 2].y;
-        }
-    }
-  }
+  if (!combine(acc, m, l, r < R, orow)) return;
   if (r >= R) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;                      // (NaN stays)
 #pragma unroll
@@ -1007,6 +983,119 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, const Cut& c
   if (hh == 0 && A.lse) A.lse[orow] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
 }
 
+// Keys of a piece.  The host knows bounds of the lengths alone; where it leaves the choice (cut.places), the pieces are the shortest, from
+// cut.chunk_piece on, with which all of them are on the chip at once (eight requests of 25 to 64 drafts, 4472 to 8192 rows of 8 bits: 1408
+// keys, which the bounds give, make 536 workgroups, 83 us; 1536 make 504, 69 us).
+__device__ __forceinline__ int chunk_piece(const PagedAttnArgs& A, const Cut& cut, int lane) {
+  if (!cut.places) return cut.chunk_piece;
+  const Paged& P = A.P;
+  const int b = min(lane, P.B - 1), prefix = A.S.prefix ? A.S.prefix[b] : 0;
+  const Seq s = seq_of(P, b);
+  const int R = s.nq * A.G, blocks = lane < P.B ? row_blocks<kChunkRows>(s.nq, A.G, cut.w.few) * P.H : 0;
+  const int tiles = (Keys<true>(A.V, s, prefix, max(0, R - 1) / kChunkRows * kChunkRows / A.G, s.nq - 1).end + kChunkKeys - 1) / kChunkKeys;
+  auto sum = [](int x) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+    return __builtin_amdgcn_readfirstlane(x);
+  };
+  int piece = max(cut.chunk_piece / kChunkKeys, (int)min((sum(min(blocks * (tiles >> 4), 1 << 24)) * 16ll) / cut.places, 1ll << 24));
+  for (int i = 0; i < 24 && sum(blocks * ((tiles + piece - 1) / piece)) > cut.places; ++i) piece += (piece + 15) / 16;
+  return piece * kChunkKeys;
+}
+
+// Workgroup id of a launch that is cut: blocks of each kv-head, piece by piece.
+template <typename T, int D, int MODE, int BITS, bool SIGHT>
+__device__ __forceinline__ void cut_chunk(const PagedAttnArgs& A, const Cut& cut, const Parts& parts, ChunkLds<D>& sm, int id) {
+  constexpr int CB = D / 32;
+  const Paged& P = A.P;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int h = id % P.H, piece = id / (cut.blocks * P.H), bh = id % (cut.blocks * P.H);
+  int b, blk;
+  Seq s;
+  const bool split = SIGHT && cut.chunk_spread && piece == 0 && tid == 0;
+  if (!find_block<kChunkRows>(P, A.G, cut.w.few, bh / P.H, lane, b, blk, s)) {
+    if (split) parts.split[bh] = int4{0, 0, 0, 0};
+    return;
+  }
+  const int prefix = A.S.prefix ? A.S.prefix[b] : 0;
+  const int r0 = blk * kChunkRows;
+  const Keys<SIGHT> keys(A.V, s, prefix, r0 / A.G, min(s.nq * A.G - 1, r0 + kChunkRows - 1) / A.G);
+  const int length = SIGHT ? chunk_piece(A, cut, lane) : cut.chunk_piece, np = max(1, (keys.end + length - 1) / length);
+  if (piece >= np) return;
+  if (split) parts.split[bh] = int4{np, s.q0, s.nq, blk};
+  const int p0 = piece * length, p1 = min(p0 + length, keys.end);
+  paged_chunk<T, D, MODE, BITS, SIGHT>(A, sm, s, b, blk, h, prefix, keys, p0, p1, [&](f32x16g (&acc)[CB], float& m, float& l, bool live, size_t orow) {
+    if (np > 1 && !cut.chunk_joined && !cut.chunk_spread) {
+      if (!live) return false;
+      const size_t pr = parts.chunk0 + (size_t)piece * P.N * A.Hq + orow;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<f32x4g*>(parts.acc + pr * D + 32 * c + 8 * e + 4 * hh) =
+              f32x4g{acc[c][4 * e], acc[c][4 * e + 1], acc[c][4 * e + 2], acc[c][4 * e + 3]};
+      if (hh == 0) parts.ml[pr] = make_float2(m, l);
+      return false;
+    }
+    if (np > 1) {
+      // 8 bytes per lane, adjacent lanes adjacent: where wave w's two channels i, i + 1 of block c lie in a piece's rows
+      const size_t row0 = parts.chunk0 + (size_t)bh * cut.n_chunk * kChunkRows + 32 * wave;
+      const uint32_t at = 8 * (uint32_t)lane;                        // (beside a uniform address: 64 bits a lane would not fit the registers)
+      auto sums = [&](int p, int c, int i) {
+        return reinterpret_cast<float2*>(reinterpret_cast<char*>(parts.acc + (row0 + (size_t)p * kChunkRows) * D) + (8 * c + i / 2) * 512 + at);
+      };
+      if (SIGHT && cut.chunk_spread) {                             // (k_chunk_join is another launch: ordinary stores will do)
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) *sums(piece, c, i) = make_float2(acc[c][i], acc[c][i + 1]);
+        if (hh == 0) parts.ml[row0 + (size_t)piece * kChunkRows + n] = make_float2(m, l);
+        return false;
+      }
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) put2(sums(piece, c, i), acc[c][i], acc[c][i + 1]);
+      if (hh == 0) put2(parts.ml + row0 + (size_t)piece * kChunkRows + n, m, l);
+      vm_wait();                                                     // this wave's stores are where everyone sees them
+      __syncthreads();
+      int* ticket = parts.tickets + (cut.chunk_ticket0 + bh) * kTicketWords;
+      if (tid == 0) {
+        sm.last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == np - 1;
+        if (sm.last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call wants it
+      }
+      __syncthreads();
+      if (!sm.last) return false;
+      m = kUnset;
+      l = 0.f;
+      for (int p = 0; p < np; ++p) m = fmaxf(m, take2(parts.ml + row0 + (size_t)p * kChunkRows + n).x);
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
+      for (int p = 0; p < np; ++p) {                                 // (always in this order, whoever is last)
+        const float2 z = take2(parts.ml + row0 + (size_t)p * kChunkRows + n);
+        float2 x[CB * 8];
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) x[8 * c + i / 2] = take2(sums(p, c, i));
+        const float f = exp2_hw(z.x - m);
+        l += f * z.y;
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            acc[c][i] += f * x[8 * c + i / 2].x;
+            acc[c][i + 1] += f * x[8 * c + i / 2].y;
+          }
+      }
+    }
+    return true;
+  });
+}
+
 // A launch: chunk_wgs workgroups for sequences of many rows (cut.blocks blocks of each kv-head, piece by piece), behind them those for
 // few (unit by unit, piece by piece).  One launch for both: a prompt's chunk and the other requests' tokens share the chip.
 // KIND: bit 0: there are the former, bit 1: the latter.
@@ -1016,13 +1105,9 @@ __global__ __launch_bounds__(256, D == 64 || (BITS == 4 && KIND == 2) ? 3 : 2) v
   __shared__ __align__(16) char lds[KIND == 1 ? sizeof(ChunkLds<D>) : KIND == 2 ? sizeof(StepLds<D>) : kMost];
   const int id = (int)blockIdx.x;
   if ((KIND & 1) && (KIND == 1 || id < chunk_wgs)) {
-    if constexpr (KIND & 1) paged_chunk<T, D, MODE, BITS, SIGHT>(A, cut, parts, *reinterpret_cast<ChunkLds<D>*>(lds), id);
+    if constexpr (KIND & 1) cut_chunk<T, D, MODE, BITS, SIGHT>(A, cut, parts, *reinterpret_cast<ChunkLds<D>*>(lds), id);
   } else {
-    if constexpr (KIND & 2) {
-      StepLds<D>& sm = *reinterpret_cast<StepLds<D>*>(lds);
-      if constexpr (BITS == 16) paged_step<T, D, MODE, SIGHT>(A, cut, parts, sm, id - chunk_wgs);
-      else packed_step<T, D, MODE, BITS>(A, cut, parts, sm, id - chunk_wgs);
-    }
+    if constexpr (KIND & 2) cut_step<T, D, MODE, BITS, SIGHT>(A, cut, parts, *reinterpret_cast<StepLds<D>*>(lds), id - chunk_wgs);
   }
 }
 
@@ -1122,14 +1207,43 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs A, Cut cut, P
   if (c == 0 && A.lse) A.lse[id] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
 }
 
+// Joins the pieces of cut_chunk's blocks, in order: blockIdx.y: block and kv-head, 16 (D = 128) or 8 workgroups each.  A lane has four channels of a
+// row, as paged_chunk's had them.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_chunk_join(PagedAttnArgs A, Cut cut, Parts parts) {
+  constexpr int CB = D / 32;
+  const Paged& P = A.P;
+  const int at = (int)blockIdx.x * 256 + (int)threadIdx.x, lane = at & 63, e = at >> 6 & 3, c = at / 256 % CB, wave = at / (256 * CB);
+  const int4 split = parts.split[blockIdx.y];
+  const int np = split.x, h = (int)blockIdx.y % P.H, r = split.w * kChunkRows + 32 * wave + (lane & 31);
+  if (np <= 1 || r >= split.z * A.G) return;
+  const size_t row0 = parts.chunk0 + (size_t)blockIdx.y * cut.n_chunk * kChunkRows + 32 * wave;
+  float m = kUnset, l = 0.f;
+#pragma unroll 8
+  for (int p = 0; p < np; ++p) m = fmaxf(m, parts.ml[row0 + (size_t)p * kChunkRows + (lane & 31)].x);
+  f32x4g o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int p = 0; p < np; ++p) {
+    const float2* from = reinterpret_cast<const float2*>(parts.acc + (row0 + (size_t)p * kChunkRows) * D) + (8 * c + 2 * e) * 64 + lane;
+    const float2 z = parts.ml[row0 + (size_t)p * kChunkRows + (lane & 31)], x = from[0], y = from[64];
+    const float f = exp2_hw(z.x - m);
+    l += f * z.y;
+    o += f * f32x4g{x.x, x.y, y.x, y.y};
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;                      // (NaN stays)
+  const size_t orow = (size_t)(split.y + r / A.G) * A.Hq + h * A.G + r % A.G;
+  store4((T*)A.out + orow * D + 32 * c + 8 * e + 4 * (lane >> 5), o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+  if (c == 0 && e == 0 && lane < 32 && A.lse) A.lse[orow] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+}
+
 // Workgroups of a call's launches.  merge: few_rows rows of every unit, if paged_step's pieces are not joined where they are made; then
 // all rows, if those of paged_chunk are not (they are cut only where they are few).  Rows of few pieces are little work, and eight fit a workgroup.
 struct Launches { long long chunk, step, merge; int few_rows, step_ids; bool many; };
 inline Launches launches_of(const Paged& P, int Hq, const Cut& c) {
   Launches l = {};
   l.chunk = c.w.chunk ? (long long)c.blocks * P.H * c.n_chunk : 0;
-  l.step = c.w.step ? (long long)P.B * P.H * c.n_step : 0;
-  const bool join_step = l.step && c.n_step > 1 && !c.joined, join_chunk = l.chunk && c.n_chunk > 1 && !c.chunk_joined;
+  l.step = c.w.step ? (long long)(c.groups ? c.groups : P.B) * P.H * c.n_step : 0;
+  const bool join_step = l.step && c.n_step > 1 && !c.joined, join_chunk = l.chunk && c.n_chunk > 1 && !c.chunk_joined && !c.chunk_spread;
   l.few_rows = (int)std::min<long long>(kStepRows, (long long)P.max_q * (Hq / P.H));
   l.step_ids = join_step ? (P.B * P.H * l.few_rows + 7) / 8 * 8 : 0;
   l.many = (join_chunk ? c.n_chunk : c.n_step) >= 8;
@@ -1147,10 +1261,13 @@ hipError_t launch_attention(const PagedAttnArgs& A, hipStream_t st) {
   parts.tickets = (int*)A.ws;
   parts.acc = A.ws + kTicketFloats;
   parts.ml = (float2*)(parts.acc + n * D);
+  parts.split = (int4*)(parts.ml + (n + 1) / 2 * 2);
   const int chunk = (int)l.chunk, step = (int)l.step;
   if (chunk && step) k_paged_attn<T, D, MODE, 3, BITS, SIGHT><<<chunk + step, 256, 0, st>>>(A, c, parts, chunk);
   else if (chunk) k_paged_attn<T, D, MODE, 1, BITS, SIGHT><<<chunk, 256, 0, st>>>(A, c, parts, chunk);
   else k_paged_attn<T, D, MODE, 2, BITS, SIGHT><<<step, 256, 0, st>>>(A, c, parts, 0);
+  if constexpr (SIGHT)
+    if (chunk && c.chunk_spread) k_chunk_join<T, D><<<dim3(D / 8, (unsigned)(c.blocks * P.H)), 256, 0, st>>>(A, c, parts);
   if (l.merge) {
     if (l.many) k_paged_merge<T, D, true, SIGHT><<<(int)l.merge, 256, 0, st>>>(A, c, parts, l.few_rows, l.step_ids);
     else k_paged_merge<T, D, false, SIGHT><<<(int)l.merge, 256, 0, st>>>(A, c, parts, l.few_rows, l.step_ids);

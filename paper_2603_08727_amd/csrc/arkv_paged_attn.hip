@@ -9,9 +9,9 @@ namespace arkv {
 static size_t part_rows_bound(const Paged& P, int D, int Hq) {
   auto parts = [](long long n, long long piece) { return (n + piece - 1) / piece; };
   const long long kv = P.max_kv, units = (long long)P.B * P.H, rows = (long long)P.N * (Hq / P.H);
-  long long n = 0;
+  long long n = 0, step = 0;
   if (kv > 128)
-    n = kStepRows * std::min(units * parts(kv, 128), std::max({256 + units, units * parts(kv, kStepMaxPiece), std::min(units, 15ll) * parts(kv, kStepMaxPiece / 2)}));
+    n = step = kStepRows * std::min(units * parts(kv, 128), std::max({256 + units, units * parts(kv, kStepMaxPiece), std::min(units, 15ll) * parts(kv, kStepMaxPiece / 2)}));
   if ((long long)P.max_q * (Hq / P.H) > kStepRows && kv > 256) {
     // blocks of rows times heads: only fewer than want are cut.  a, b: pieces of the shortest length, of the two cuts in cut_of
     const long long want = D == 64 ? 768 : 512, a = parts(kv, 256), b = parts(kv, D == 64 ? 512 : 1024);
@@ -22,14 +22,26 @@ static size_t part_rows_bound(const Paged& P, int D, int Hq) {
     const long long joined = std::min<long long>(kJoinBlocks, pieces + std::min(8 * pieces, units * most));
     n += kChunkRows * std::max(pieces, joined);
   }
+  if ((long long)P.max_q * (Hq / P.H) > kStepRows) {
+    const long long sequences = std::min<long long>(P.B, rows);
+    // groups of kStepRows rows, of which no more than kGroupWorkgroups are wanted with their pieces, which are of 128 keys at least
+    const long long groups = (rows / kStepRows + sequences) * P.H;
+    if (kv > 128) n = std::max(n, kStepRows * std::min(groups * parts(kv, 128), kGroupWorkgroups + std::min<long long>(groups, kJoinUnits)));
+    // blocks whose pieces may be halved: of 256 keys at least
+    if (kv > 256) n = std::max(n, step + kChunkRows * std::min<long long>(kJoinBlocks, (rows / kChunkRows + sequences) * P.H * parts(kv, 256)));
+  }
   return (size_t)n;
 }
 
 size_t paged_attention_floats(const Paged& P, const Sight& V, int D, int Hq) {
   size_t chunk0;
-  return kTicketFloats + part_rows(P, Hq, cut_of(P, V, D, Hq), chunk0) * (D + 2);
+  const Cut c = cut_of(P, V, D, Hq);
+  const size_t rows = part_rows(P, Hq, c, chunk0);
+  return kTicketFloats + rows * (D + 2) + (c.chunk_spread ? 2 + 4 * (size_t)c.blocks * P.H : 0);
 }
-size_t paged_attention_bound(const Paged& P, int D, int Hq) { return kTicketFloats + part_rows_bound(P, D, Hq) * (D + 2); }
+size_t paged_attention_bound(const Paged& P, int D, int Hq) {
+  return kTicketFloats + part_rows_bound(P, D, Hq) * (D + 2) + ((long long)P.max_q * (Hq / P.H) > kStepRows && P.max_kv > 256 ? 2 + 4 * kJoinBlocks : 0);
+}
 
 long long paged_attention_workgroups(const Paged& P, const Sight& V, int D, int Hq) {
   const Launches l = launches_of(P, Hq, cut_of(P, V, D, Hq));

@@ -78,6 +78,7 @@ static int check_scores(const arkv_scores* s, Scores& out) {
 // s may be null: no limits.  Numbers that no slot reaches are cut, so that sums with them fit 32 bits.
 static int check_sight(const arkv_sight* s, const Paged& P, const Scores& x, Sight& out) {
   out = {};
+  out.on = true;
   out.prefixed = x.prefix != nullptr;
   if (!s) return ARKV_OK;
   if (s->window < 0 || s->sink < 0) return ARKV_EINVAL;

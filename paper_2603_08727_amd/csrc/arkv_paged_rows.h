@@ -25,12 +25,19 @@ __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_floa
 
 // A row of D channels.  A chunk is what one lane loads of it at a time (kLanes of them a row), kOut times eight channels.  The logits'
 // contraction may run over the channels in any order that q follows: channel() is the first of the eight that lane group gq
-// (of four) takes in k-step kk, so that a lane's keys are whole chunks.
+// (of four) takes in k-step kk, so that a lane's keys are whole chunks.  Scale bytes are loaded as words, those of one row (D = 128) or of two,
+// and shifted where they are used: a byte would be cut out where it arrives, at the end of a loop, and waited for there.
 template <typename T, int D, int BITS> struct PoolRow {
   static constexpr int kRow = D * BITS / 8, kBytes = kRow / 4 < 16 ? kRow / 4 : 16, kWords = kBytes / 4;
   static constexpr int kLanes = kRow / kBytes, kOut = kBytes / BITS, kParts = kRow / 4 / kBytes;
-  struct Chunk { uint32_t w[kWords], scale; };
-  struct Keys { uint32_t w[kParts * kWords], scale; };
+  struct Chunk { uint32_t w[kWords], scales; };
+  struct Keys { uint32_t w[kParts * kWords], scales; };
+  static __device__ __forceinline__ uint32_t scales_of(const uint8_t* scale, size_t row) {
+    return *reinterpret_cast<const uint32_t*>(scale + (D == 128 ? 4 * row : 2 * (row & ~(size_t)1)));
+  }
+  static __device__ __forceinline__ float scale(uint32_t scales, int row, int channel) {
+    return scale_of(scales >> (8 * (channel / 32) + (D == 128 ? 0 : 16 * (row & 1))) & 255);
+  }
   static __device__ __forceinline__ int channel(int gq, int kk) { return kk / kOut * (32 * kOut) + gq * (8 * kOut) + 8 * (kk % kOut); }
   static __device__ __forceinline__ void load(const uint8_t* p, uint32_t* w) {
     if constexpr (kBytes == 16) {
@@ -45,21 +52,20 @@ template <typename T, int D, int BITS> struct PoolRow {
     const uint8_t* p = (const uint8_t*)A.P.k + (row0 + n) * kRow + gq * kBytes;
 #pragma unroll
     for (int i = 0; i < kParts; ++i) load(p + 4 * kBytes * i, to.w + kWords * i);
-    const uint8_t* s = A.k_scale + (row0 + n) * (D / 32);
-    to.scale = D == 128 ? *reinterpret_cast<const uint32_t*>(s) : *reinterpret_cast<const uint16_t*>(s);
+    to.scales = scales_of(A.k_scale, row0 + n);
   }
-  static __device__ __forceinline__ u32x4g operand(const Keys& k, int gq, int kk) {
-    const int block = channel(gq, kk / kOut * kOut) / 32;
-    return unpack8<T, BITS>(k.w + kk / kOut * kWords + kk % kOut * (BITS / 4), scale_of(k.scale >> 8 * block & 255));
+  static __device__ __forceinline__ u32x4g operand(const Keys& k, int n, int gq, int kk) {
+    return unpack8<T, BITS>(k.w + kk / kOut * kWords + kk % kOut * (BITS / 4), scale(k.scales, n, channel(gq, kk / kOut * kOut)));
   }
   static __device__ __forceinline__ void load_chunk(const void* base, const uint8_t* scale, size_t row, int c, Chunk& to) {
     load((const uint8_t*)base + row * kRow + c * kBytes, to.w);
-    to.scale = scale[row * (D / 32) + c * kOut / 4];
+    to.scales = scales_of(scale, row);
   }
-  static __device__ __forceinline__ void expand(const Chunk& c, u32x4g (&to)[kOut]) {
-    const float scale = scale_of(c.scale);
+  // (row, c: which chunk it is; of the row its last bit matters)
+  static __device__ __forceinline__ void expand(const Chunk& chunk, int row, int c, u32x4g (&to)[kOut]) {
+    const float s = scale(chunk.scales, row, 8 * kOut * c);
 #pragma unroll
-    for (int o = 0; o < kOut; ++o) to[o] = unpack8<T, BITS>(c.w + o * (BITS / 4), scale);
+    for (int o = 0; o < kOut; ++o) to[o] = unpack8<T, BITS>(chunk.w + o * (BITS / 4), s);
   }
   static __device__ __forceinline__ float value(const PagedAttnArgs& A, size_t row, int ch) {
     const uint32_t byte = ((const uint8_t*)A.P.v)[row * kRow + ch * BITS / 8];
@@ -76,17 +82,18 @@ template <typename T, int D> struct PoolRow<T, D, 16> {
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) to.w[kk] = *reinterpret_cast<const u32x4g*>(p + 32 * kk);
   }
-  static __device__ __forceinline__ u32x4g operand(const Keys& k, int, int kk) { return k.w[kk]; }
+  static __device__ __forceinline__ u32x4g operand(const Keys& k, int, int, int kk) { return k.w[kk]; }
   static __device__ __forceinline__ void load_chunk(const void* base, const uint8_t*, size_t row, int c, Chunk& to) {
     to = *reinterpret_cast<const u32x4g*>((const T*)base + row * D + 8 * c);
   }
-  static __device__ __forceinline__ void expand(const Chunk& c, u32x4g (&to)[1]) { to[0] = c; }
+  static __device__ __forceinline__ void expand(const Chunk& chunk, int, int, u32x4g (&to)[1]) { to[0] = chunk; }
   static __device__ __forceinline__ float value(const PagedAttnArgs& A, size_t row, int ch) { return (float)((const T*)A.P.v)[row * D + ch]; }
 };
 
 // ---- which rows are seen ----------------------------------------------------------------------------
 
-// The first n of 16 bits.
+// The first n of 64 bits, n > 0; of 16, any n.
+__device__ __forceinline__ uint64_t low64(int n) { return n < 64 ? (1ull << n) - 1 : ~0ull; }
 __device__ __forceinline__ uint32_t first16(int n) { return (1u << max(0, min(n, 16))) - 1; }
 
 // The slots that any of a sequence's tokens first .. last sees, as keys 0 .. end - 1: slot(j) of key j.  Under a window, granules between the
@@ -142,17 +149,18 @@ template <> struct RowView<true> {
   const Sight& V;
   const Seq& s;
   int i, lo, pre;                         // its token (-1: no row), the first slot of its window, the slots below which all see
+  uint64_t drawn;                         // its bits of the first 64 new tokens: requested in front of the work, not where they are needed
   __device__ __forceinline__ RowView(const Sight& V, const Seq& s, int prefix, int token, bool live) : V(V), s(s) {
     i = live ? token : -1;
     pre = max(0, min(prefix, s.kv));
     const int ctx = s.kv - s.nq;
     lo = 0;
+    drawn = V.tree ? V.tree[(size_t)(s.q0 + token) * V.words] : 0;
     if (V.window) {
       int above = token;                                           // its place is behind the tokens above it
-      if (V.tree && live) {
-        const uint64_t* bits = V.tree + (size_t)(s.q0 + token) * V.words;
-        int n = 0;
-        for (int w = 0; 64 * w < s.nq; ++w) n += __popcll(bits[w] & (s.nq - 64 * w < 64 ? (1ull << (s.nq - 64 * w)) - 1 : ~0ull));
+      if (V.tree) {
+        int n = __popcll(drawn & low64(s.nq));
+        for (int w = 1; 64 * w < s.nq; ++w) n += __popcll(V.tree[(size_t)(s.q0 + token) * V.words + w] & low64(s.nq - 64 * w));
         above = max(n - 1, 0);
       }
       lo = ctx + above - V.window + 1;
@@ -165,13 +173,16 @@ template <> struct RowView<true> {
   }
   // bits t .. t + 15 of the token's, t from -15 on
   __device__ __forceinline__ uint32_t tree16(int token, int t) const {
-    if (t <= -16 || t >= s.nq) return 0;
-    const uint64_t* bits = V.tree + (size_t)(s.q0 + token) * V.words;
+    if (t <= -16 || t >= s.nq) return 0;                           // (uniform, as t is)
     uint64_t x;
-    if (t < 0) x = bits[0] << -t;
+    if (t < 0) x = drawn << -t;
+    else if (s.nq <= 64) x = drawn >> t;
     else {
-      x = bits[t >> 6] >> (t & 63);
-      if ((t & 63) > 48 && ((t >> 6) + 1) * 64 < s.nq) x |= bits[(t >> 6) + 1] << (64 - (t & 63));
+      const uint64_t* bits = V.tree + (size_t)(s.q0 + token) * V.words;
+      const int w = t >> 6;
+      const uint64_t here = bits[w], next = bits[min(w + 1, (s.nq - 1) >> 6)];
+      x = here >> (t & 63);
+      if (t & 63) x |= next << (64 - (t & 63));                    // (of the last word once more: behind the tokens, and cut off)
     }
     return (uint32_t)x & first16(s.nq - t) & 0xFFFFu;
   }
