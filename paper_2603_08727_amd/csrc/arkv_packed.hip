@@ -233,55 +233,39 @@ __global__ __launch_bounds__(64 * kPackWaves) void k_packed_append(AppendArgs A,
   }
 }
 
-// TOKENS adjacent tokens to a wave; a lane takes a chunk of codes at a time, kReadRounds of them under way.  Bound by memory (55591 rows of 8 x 128
-// channels, 8 bits, four tokens a wave: 74 us, 4.7 TB/s; one: 77).  From kReadMany tokens on there are waves enough for four, and more is stored
-// than the caches hold: the stores pass them by (74 us; with ordinary ones 90).  Fewer are left in the caches for whom they are read for (7817
-// tokens of 4 bits: 15 us; past the caches 26).
-constexpr int kReadRounds = 4, kReadMany = 16384;
-template <typename T, int D, int BITS, int TOKENS>
+// One wave per token; a lane takes a chunk of codes at a time, kReadRounds of them under way.  Bound by memory (55591 rows of 8 x 128 channels, 8 bits:
+// 77 us, 4.5 TB/s; four tokens a wave, and stores past the caches: 83; 7817 tokens of 4 bits: 15 us, with such stores 26).
+constexpr int kReadRounds = 4;
+template <typename T, int D, int BITS>
 __global__ __launch_bounds__(64 * kPackWaves) void k_packed_read(Paged P, PackedArgs X) {
   typedef PoolRow<T, D, BITS> Row;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t0 = (blockIdx.x * kPackWaves + wave) * TOKENS;
-  if (t0 >= P.N) return;
-  const int at0 = min(lane, P.B - 1), sq0 = P.cu_q[at0], sq1 = P.cu_q[at0 + 1], skv = P.kv_len[at0];
-  Place o[TOKENS];
-  int row0[TOKENS];
-#pragma unroll
-  for (int i = 0; i < TOKENS; ++i) o[i] = t0 + i < P.N ? place_of(P, t0 + i, lane, sq0, sq1, skv) : Place{-1, 0, 0};
-#pragma unroll
-  for (int i = 0; i < TOKENS; ++i) row0[i] = row_of(P, o[i]);
-  const int per = 2 * P.H * Row::kLanes;                           // chunks of a token
-  for (int it0 = lane; it0 < TOKENS * per; it0 += 64 * kReadRounds) {
+  const int t = blockIdx.x * kPackWaves + wave;
+  if (t >= P.N) return;
+  const int at0 = min(lane, P.B - 1);
+  const Place o = place_of(P, t, lane, P.cu_q[at0], P.cu_q[at0 + 1], P.kv_len[at0]);
+  if (o.b < 0) return;
+  const int row0 = row_of(P, o), n = 2 * P.H * Row::kLanes;        // chunks of the token
+  for (int it0 = lane; it0 < n; it0 += 64 * kReadRounds) {
     typename Row::Chunk chunk[kReadRounds];
-    int row[kReadRounds], to[kReadRounds], in[kReadRounds];        // row, and its output's among the token's keys (values: from P.H on); -1: none
+    auto row = [&](int h) { return (size_t)row0 + ((size_t)(h < P.H ? h : h - P.H) << P.lg_page); };
 #pragma unroll
     for (int u = 0; u < kReadRounds; ++u) {
-      const int it = it0 + 64 * u, i = TOKENS == 1 ? 0 : min(it / per, TOKENS - 1), left = it - i * per, h = left / Row::kLanes;
-      int r0 = row0[0], b = o[0].b;
-#pragma unroll
-      for (int e = 1; e < TOKENS; ++e)
-        if (i == e) { r0 = row0[e]; b = o[e].b; }
-      in[u] = left % Row::kLanes;
-      to[u] = left < per && b >= 0 && (h < P.H ? X.k : X.v) ? 2 * P.H * i + h : -1;
-      row[u] = r0 < 0 || to[u] < 0 ? -1 : r0 + ((h < P.H ? h : h - P.H) << P.lg_page);
-      if (row[u] >= 0) Row::load_chunk(h < P.H ? P.k : P.v, h < P.H ? X.k_scale : X.v_scale, (size_t)row[u], in[u], chunk[u]);
+      const int it = it0 + 64 * u, h = it / Row::kLanes, c = it % Row::kLanes;
+      if (it < n && row0 >= 0) Row::load_chunk(h < P.H ? P.k : P.v, h < P.H ? X.k_scale : X.v_scale, row(h), c, chunk[u]);
     }
 #pragma unroll
     for (int u = 0; u < kReadRounds; ++u) {
-      if (to[u] < 0) continue;
+      const int it = it0 + 64 * u, h = it / Row::kLanes, c = it % Row::kLanes;
+      T* out = h < P.H ? (T*)X.k : (T*)X.v;
+      if (it >= n || !out) continue;
       u32x4g w[Row::kOut];
 #pragma unroll
       for (int e = 0; e < Row::kOut; ++e) w[e] = u32x4g{0, 0, 0, 0};
-      if (row[u] >= 0) Row::expand(chunk[u], row[u], in[u], w);
-      const int i = to[u] / (2 * P.H), h = to[u] % (2 * P.H);
-      T* out = (h < P.H ? (T*)X.k : (T*)X.v) + ((size_t)(t0 + i) * P.H + (h < P.H ? h : h - P.H)) * D;
+      if (row0 >= 0) Row::expand(chunk[u], (int)row(h), c, w);
+      u32x4g* to = reinterpret_cast<u32x4g*>(out + ((size_t)t * P.H + (h < P.H ? h : h - P.H)) * D) + Row::kOut * c;
 #pragma unroll
-      for (int e = 0; e < Row::kOut; ++e) {
-        u32x4g* at = reinterpret_cast<u32x4g*>(out) + Row::kOut * in[u] + e;
-        if constexpr (TOKENS > 1) __builtin_nontemporal_store(w[e], at);
-        else *at = w[e];
-      }
+      for (int e = 0; e < Row::kOut; ++e) to[e] = w[e];
     }
   }
 }
@@ -304,11 +288,7 @@ hipError_t launch_packed_append(int dtype, int D, int bits, const AppendArgs& A,
 
 hipError_t launch_packed_read(int dtype, int D, int bits, const Paged& P, const PackedArgs& X, hipStream_t st) {
   return dispatch_packed(dtype, D, bits, [&](auto t, auto d, auto b) {
-    constexpr int D_ = decltype(d)::value, B_ = decltype(b)::value, many = 4;
-    typedef typename decltype(t)::type T;
-    auto groups = [&](int tokens) { return (P.N + kPackWaves * tokens - 1) / (kPackWaves * tokens); };
-    if (P.N >= kReadMany) k_packed_read<T, D_, B_, many><<<groups(many), 64 * kPackWaves, 0, st>>>(P, X);
-    else k_packed_read<T, D_, B_, 1><<<groups(1), 64 * kPackWaves, 0, st>>>(P, X);
+    k_packed_read<typename decltype(t)::type, decltype(d)::value, decltype(b)::value><<<(P.N + kPackWaves - 1) / kPackWaves, 64 * kPackWaves, 0, st>>>(P, X);
     return hipGetLastError();
   });
 }

@@ -809,6 +809,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, ChunkLds<D>&
   // The row's softmax reference; rows that see none of this piece need none.
   float m = view.end() > keys.slot(p0) ? kUnset : 0.f, l = 0.f;
   load_pages(0, 0);
+  if (SIGHT && tid < 2) sm.odd[tid] = 0;
   if (nt > 0) {
     fetch(0, 0, 0);
     put(0);
@@ -828,9 +829,24 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, ChunkLds<D>&
     uint64_t odd = 0;
     if (masked) {
       // Values that are not finite would spoil the rows that do not see them: they leave the product, and are added below.
-      if (tid < 2) sm.odd[tid] = 0;
-      __syncthreads();
+      // (Under a window a quarter of the tiles is masked.  There the words are zero from before, and a chunk is first looked at as a whole.)
+      if constexpr (!SIGHT) {
+        if (tid < 2) sm.odd[tid] = 0;
+        __syncthreads();
+      }
       constexpr int PT = kChunkKeys * CPR / 256;                   // chunks per thread
+      bool look = true;
+      if constexpr (SIGHT) {
+        u16x2g most = {0, 0};
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+          const u32x4g w = *reinterpret_cast<const u32x4g*>(&sm.v[buf][8 * (tid + 256 * i)]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2g, w[e] & 0x7FFF7FFFu));
+        }
+        look = most[0] >= Mfma<T>::kExp || most[1] >= Mfma<T>::kExp;
+      }
+      if (look)
 #pragma unroll
       for (int i = 0; i < PT; ++i) {
         const int at = tid + 256 * i, rr = at / CPR;
@@ -850,6 +866,10 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, ChunkLds<D>&
       }
       __syncthreads();
       odd = (uint64_t)sm.odd[1] << 32 | sm.odd[0];
+      if (SIGHT && odd) {
+        __syncthreads();
+        if (tid < 2) sm.odd[tid] = 0;
+      }
     }
     if (SIGHT && r0 + 32 * wave >= R) {                            // no rows of this wave's: it only fetches
       if (t + 1 < nt) put(buf ^ 1);
@@ -892,8 +912,11 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, ChunkLds<D>&
         auto seen = view.granule(keys.slot(j0 + 16 * g), ok >> g & 1, 4 * hh);
         if constexpr (!SIGHT) seen.left = (int)opaque(seen.left);  // (what depends on it stays in this branch)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (!seen.at(8 * (i >> 2) + (i & 3))) x[g >> 1][8 * (g & 1) + i] = -INFINITY;
+        for (int i = 0; i < 8; ++i) {
+          const int e = 8 * (g & 1) + i;
+          if constexpr (SIGHT) x[g >> 1][e] = seen.pick(8 * (i >> 2) + (i & 3), x[g >> 1][e]);
+          else if (!seen.at(8 * (i >> 2) + (i & 3))) x[g >> 1][e] = -INFINITY;
+        }
       }
     }
     u32x4g pb[4];                                                  // probabilities of keys 16 i .. 16 i + 15, eight per lane

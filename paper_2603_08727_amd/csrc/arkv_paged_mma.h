@@ -11,6 +11,7 @@ template <int N> using Int = std::integral_constant<int, N>;
 
 typedef uint32_t u32x4g __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2g __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2g __attribute__((ext_vector_type(2)));
 typedef float f32x4g __attribute__((ext_vector_type(4)));
 typedef float f32x16g __attribute__((ext_vector_type(16)));
 typedef short s16x4g __attribute__((ext_vector_type(4)));

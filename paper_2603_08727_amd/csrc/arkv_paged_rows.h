@@ -189,6 +189,10 @@ template <> struct RowView<true> {
   struct Seen {
     uint32_t mask;
     __device__ __forceinline__ bool at(int i) const { return mask >> i & 1; }
+    __device__ __forceinline__ float pick(int i, float x) const {  // x, or -infinity
+      const uint32_t on = (uint32_t)((int)(mask << (31 - i)) >> 31);
+      return __uint_as_float((__float_as_uint(x) & on) | (0xFF800000u & ~on));
+    }
   };
   __device__ __forceinline__ Seen granule(int slot, bool there, int off) const {
     const int t = (int)opaque(i), ctx = s.kv - s.nq;
