@@ -85,7 +85,7 @@ typedef struct {
 } arkv_scores;
 
 /* Which slots new token i of sequence b sees, where that is not all up to its own, p = ctx_b + i.  window w > 0: the slots j <= p with
- * j > p - w or j < sink.  tree (DEVICE uint64 [n_tokens][tree_words], 8-byte aligned, tree_words >= max_q / 64): bit t of the token's words says
+ * j > p - w or j < sink.  tree (DEVICE uint64 [n_tokens][tree_words], 8-byte aligned, 64 tree_words >= max_q): bit t of the token's words says
  * whether it sees new token t, itself among them; the slots below ctx_b it sees all, or with a window as a token at p = ctx_b + (new tokens it
  * sees) - 1 (the window takes no new token away).  Bits from q_len[b] on count for nothing.  A prefix of the scores is seen besides.  All zero: no limits. */
 typedef struct {
@@ -134,8 +134,10 @@ int arkv_paged_attention(const arkv_pages* pages, const arkv_page_batch* batch, 
                          int32_t n_q_heads, const arkv_rows* q, void* out, float* lse, void* workspace, size_t bytes,
                          void* hip_stream);
 
-/* The same, a token seeing the slots that sight says (NULL: arkv_paged_attention). What no token sees is not read, whole granules of 16
- * slots at a time.  ARKV_EINVAL, besides: window or sink negative, tree_words too small, tree not aligned. */
+/* The same, a token seeing the slots that sight says (NULL: arkv_paged_attention).  What no token of a workgroup sees in front of its window is not
+ * read, nor its table entries, whole granules of 16 slots at a time.  The lengths choose how long sequences are cut: a row's last bits may differ with
+ * the batch that it is in.  After drafting, the accepted tokens' rows are appended once more, kv_len cut to them: their slots are the first drafts'.
+ * ARKV_EINVAL, besides: window or sink negative, tree_words too small, tree not aligned. */
 int arkv_paged_attention_sight(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,
                                const arkv_sight* sight, int32_t n_q_heads, const arkv_rows* q, void* out, float* lse,
                                void* workspace, size_t bytes, void* hip_stream);

@@ -589,3 +589,52 @@ def test_arguments_on_the_gpu_are_checked():
         P.arkv_packed_read(pages, batch, out, None)
     with pytest.raises(ValueError):
         P.arkv_packed_pages(s.k_codes, s.v_codes, s.k_scale[..., :1].contiguous(), s.v_scale, s.pos, BF)
+
+
+# ---- a run of them together ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("bits,dtype", [(8, BF), (4, BF), (8, FP)])
+def test_rounds_of_drafts_leave_what_their_accepted_tokens_would(bits, dtype):
+    """Drafting, attending and accepting, against a twin that never drafted: the same rows, to the bit, and the same outputs."""
+    from paper_2603_08727_amd.paged_drafts_example import DraftedLayer
+    make = lambda: DraftedLayer(3, hidden=128, bits=bits, rows=192, window=40, sink=4, max_tokens=70, dtype=dtype, seed=3)  # noqa: E731
+    layer, twin = make(), make()
+    g = torch.Generator().manual_seed(1)
+    new = lambda n: torch.randn(n, 128, generator=g).to(dtype).cuda()  # noqa: E731
+    x = new(50 + 3 + 70)
+    assert torch.equal(layer.prompt(x, [50, 3, 70]), twin.prompt(x, [50, 3, 70]))
+    chosen = [[[-1, 0, 0, 1, 2, 4], [0, 2, 4]], [[-1, 0], []], [[-1, -1, 1, 2], [1, 2]]]
+    for turn in range(3):
+        parents, paths = [c[0] for c in chosen], [c[1] for c in chosen]
+        q_len = [len(p) for p in parents]
+        x = new(sum(q_len))
+        y = layer.draft(x, parents)
+        layer.accept(paths)
+        picked = [sum(q_len[:r]) + i for r, path in enumerate(paths) for i in path]
+        z = twin.prompt(x[picked], [len(p) for p in paths])
+        # An accepted draft saw what the accepted token sees.  On either side an output is off by its rounding and by those of the probabilities, 2 U
+        # of the largest value, and 2^-12 of it covers sums and logits in 32 bits; the projection rounds once more.
+        most = float(max(K.values(c.cpu(), s.cpu(), bits).abs().max() for c, s in ((twin.pages.v, twin.pages.v_scale),)))
+        off = 2 * (2 * R.U[dtype] + 2.0 ** -12) * most * math.sqrt(len(picked) * twin.hq * twin.d)
+        w = float(torch.linalg.matrix_norm(twin.w_out.float(), 2))
+        assert (y[picked].float() - z.float()).norm() <= w * off + 3 * R.U[dtype] * z.float().norm()
+        assert layer.have == twin.have
+        kv = torch.tensor(layer.have, dtype=torch.int32, device="cuda")
+        cu = torch.tensor([sum(layer.have[:r]) for r in range(4)], dtype=torch.int32, device="cuda")
+        n = sum(layer.have)
+        rows = []
+        for each in (layer, twin):
+            k, v = (torch.empty(n, each.hkv, each.d, dtype=dtype, device="cuda") for _ in "kv")
+            P.arkv_packed_read(each.pages, P.arkv_page_batch(cu, kv, each.table, n, max(layer.have), max(layer.have)), k, v)
+            rows.append((k, v))
+        assert torch.equal(rows[0][0], rows[1][0]) and torch.equal(rows[0][1], rows[1][1])
+    x = new(3)
+    assert torch.equal(layer.prompt(x, [1, 1, 1]), twin.prompt(x, [1, 1, 1]))
+    with pytest.raises(ValueError, match="follows"):
+        layer.draft(new(2), [[0], [-1], []])
+
+
+def test_the_drafts_example_runs(capsys):
+    from paper_2603_08727_amd import paged_drafts_example
+    paged_drafts_example.main()
+    assert "round 7" in capsys.readouterr().out

@@ -114,8 +114,8 @@ def test_a_workspace_serves_every_window(hq, hkv, d):
         for pages, size, call in ((plain, lib.arkv_paged_workspace, lib.arkv_paged_attention_sight), (packed, lib.arkv_packed_workspace, lib.arkv_packed_attention)):
             assert size(C.byref(pages), C.byref(b), hq, C.byref(n)) == A.OK
             # (refused for its output alone, which is checked behind the workspace: with one that is too small too)
-            for s in (P._Sight(window, sink, 0, None), P._Sight(window, sink, 1 << 10, ADDR)):
-                args = (C.byref(pages), C.byref(b), C.byref(sc), C.byref(s), hq, C.byref(rows))
+            for s in (None, P._Sight(window, sink, 0, None), P._Sight(window, sink, 1 << 10, ADDR)):
+                args = (C.byref(pages), C.byref(b), C.byref(sc), s if s is None else C.byref(s), hq, C.byref(rows))
                 assert call(*args, ADDR, None, ADDR, 0, None) == A.EINVAL
                 need = _need(call, args, n.value)
                 assert need <= n.value, (batch, n_tokens, max_q, max_kv, window, sink)
