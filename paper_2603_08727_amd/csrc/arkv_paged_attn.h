@@ -28,7 +28,7 @@
 namespace arkv {
 
 constexpr int kStepWaves = 4;
-constexpr int kStepMaxPiece = 2048;     // (at most 4096: a lane holds the page of one granule)
+constexpr int kStepMaxPiece = 2048;     // (twice that at most: a lane holds the page of one granule)
 constexpr int kChunkRows = 128, kChunkKeys = 64;
 
 // How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
@@ -60,7 +60,10 @@ inline Cut cut_of(const Paged& P, const Sight& V, int D, int Hq) {
   // workgroups should end with the others (32 requests of 800 to 16384 rows x 8 heads: 177 us in pieces of 2048, 182 of
   // 4096; four of 131071 rows: 362 and 354).  Fewer than 16 heads do not fill the chip in 16 pieces.
   const long long units = (long long)P.B * P.H;
-  pieces(kv_step, units, std::min(256ll, kJoinPieces * units), 128, units < 16 ? kStepMaxPiece / 2 : kStepMaxPiece, 128, c.step_piece, c.n_step);
+  // Rows of 4 bits are read in half the time (31 requests of 800 to 16384 rows x 8 heads: 66 us in pieces of 2048 keys, 61 of 4096; of 8 bits, four of 131071
+  // rows: 209 and 210).
+  const int longest = V.bits == 4 ? 2 * kStepMaxPiece : kStepMaxPiece;
+  pieces(kv_step, units, std::min(256ll, kJoinPieces * units), 128, units < 16 ? longest / 2 : longest, 128, c.step_piece, c.n_step);
   // One workgroup for each CU; then for every place on the chip, at d = 64 three to a CU, in larger pieces (1686 tokens on up to 3001
   // rows, 12 heads: 46 us in pieces of 1024 keys, 42 of 512; d = 128, 512 tokens on 4100 rows, 16 heads, 7 single tokens: 66 us in pieces of
   // 1024, 70 of 768, 82 of 512; 128 tokens on 1024 rows: 28 us in one piece, 22 in
@@ -70,7 +73,7 @@ inline Cut cut_of(const Paged& P, const Sight& V, int D, int Hq) {
   pieces(kv_chunk, blocks, 256, 256, 1 << 28, kChunkKeys, alone, n_alone);
   pieces(kv_chunk, blocks, D == 64 ? 768 : 512, D == 64 ? 512 : 1024, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
   if (alone < c.chunk_piece) { c.chunk_piece = alone; c.n_chunk = n_alone; }
-  if (V.on && c.w.chunk) {
+  if (V.bits && c.w.chunk) {
     const long long groups = rows / kStepRows + std::min<long long>(P.B, rows), keys = most_keys(P, V, (kStepRows - 1) / G + 2);
     int piece, n;
     pieces((int)keys, groups * P.H, kGroupWorkgroups, std::max(128, ((int)keys + 2047) / 2048 * 128), kStepMaxPiece, 128, piece, n);
@@ -90,7 +93,7 @@ inline Cut cut_of(const Paged& P, const Sight& V, int D, int Hq) {
   // (512 tokens on 4100 rows, 16 heads, beside 7 single tokens: 60 us, with a launch that joins 70)
   c.chunk_joined = c.n_chunk <= kJoinPieces && (long long)c.blocks * P.H + c.chunk_ticket0 <= kJoinUnits &&
                    (long long)c.blocks * P.H * c.n_chunk <= kJoinBlocks;
-  if (V.on) {
+  if (V.bits) {
     // the kernel may find that pieces down to half as long fit the chip at once
     const int half = std::max(D == 64 ? 256 : 512, c.chunk_piece / 2 / kChunkKeys * kChunkKeys), n = (kv_chunk + half - 1) / half;
     if (c.n_chunk > 1 && P.B <= 64 && (long long)c.blocks * P.H * n <= kJoinBlocks && half < c.chunk_piece) {
@@ -539,7 +542,8 @@ __device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Parts&
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) x[g] = Mfma<T>::m16(Row::operand(kr[g], n, gq, kk), q[kk], x[g]);
     }
-    load_k(t + 1);                                                 // (behind the last tile: rows of page 0.  A branch here would be waited for)
+    const int next = min(t + 1, nt - 1);                           // (behind the last tile that one again: a branch here would be waited for)
+    load_k(next);
     const uint32_t ok = (uint32_t)(pages.there >> (4 * t)) & 15;
     const bool masked = !keys.all_seen(j0, 64) || ok != 15;
     float mul = lg.mul;
@@ -624,7 +628,7 @@ __device__ __forceinline__ void packed_step(const PagedAttnArgs& A, const Parts&
         for (int o = 0; o < Row::kOut; ++o)
           *reinterpret_cast<u32x4g*>(&sm.w[wave].v[RPI * i + lane / CPR][8 * (Row::kOut * (lane % CPR) + o)]) = w[o];
       }
-      load_v(t + 1, half);
+      load_v(next, half);
 #pragma unroll
       for (int c = 0; c < CB; ++c) {
         const s16x4g a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sm.w[wave].v[4 * gq + (n >> 2)][16 * c + 4 * (n & 3)]);

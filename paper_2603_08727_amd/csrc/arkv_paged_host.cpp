@@ -76,9 +76,9 @@ static int check_scores(const arkv_scores* s, Scores& out) {
 }
 
 // s may be null: no limits.  Numbers that no slot reaches are cut, so that sums with them fit 32 bits.
-static int check_sight(const arkv_sight* s, const Paged& P, const Scores& x, Sight& out) {
+static int check_sight(const arkv_sight* s, int bits, const Paged& P, const Scores& x, Sight& out) {
   out = {};
-  out.on = true;
+  out.bits = bits;
   out.prefixed = x.prefix != nullptr;
   if (!s) return ARKV_OK;
   if (s->window < 0 || s->sink < 0) return ARKV_EINVAL;
@@ -200,11 +200,11 @@ int arkv_paged_attention(const arkv_pages* pages, const arkv_page_batch* batch, 
 }
 
 // (A.P is filled already.)  done: there is nothing to launch.
-static int sight_args(int d, const arkv_scores* scores, const arkv_sight* sight, int32_t n_q_heads, const arkv_rows* q, void* out, float* lse,
+static int sight_args(int d, int bits, const arkv_scores* scores, const arkv_sight* sight, int32_t n_q_heads, const arkv_rows* q, void* out, float* lse,
                       void* workspace, size_t bytes, PagedAttnArgs& A, bool& done) {
   TRY(check_heads(n_q_heads, A.P.H, A.P.N, A.G));
   TRY(check_scores(scores, A.S));
-  TRY(check_sight(sight, A.P, A.S, A.V));
+  TRY(check_sight(sight, bits, A.P, A.S, A.V));
   TRY(check_rows(q, A.P.N, A.q));
   A.Hq = n_q_heads;
   if (!workspace || !aligned16(workspace) || bytes < 4 * paged_attention_floats(A.P, A.V, d, n_q_heads)) return ARKV_EINVAL;
@@ -223,7 +223,7 @@ int arkv_paged_attention_sight(const arkv_pages* pages, const arkv_page_batch* b
   PagedAttnArgs A = {};
   bool done;
   TRY(check(pages, batch, A.P));
-  TRY(sight_args(pages->head_dim, scores, sight, n_q_heads, q, out, lse, workspace, bytes, A, done));
+  TRY(sight_args(pages->head_dim, 16, scores, sight, n_q_heads, q, out, lse, workspace, bytes, A, done));
   if (done) return ARKV_OK;
   LAUNCH(launch_paged_attention_sight(pages->dtype, pages->head_dim, A, (hipStream_t)hip_stream));
 }
@@ -234,7 +234,7 @@ int arkv_packed_attention(const arkv_packed_pages* pages, const arkv_page_batch*
   PagedAttnArgs A = {};
   bool done;
   TRY(check_packed(pages, batch, A.P));
-  TRY(sight_args(pages->head_dim, scores, sight, n_q_heads, q, out, lse, workspace, bytes, A, done));
+  TRY(sight_args(pages->head_dim, pages->bits, scores, sight, n_q_heads, q, out, lse, workspace, bytes, A, done));
   if (done) return ARKV_OK;
   A.k_scale = pages->k_scale; A.v_scale = pages->v_scale;
   const auto launch = pages->bits == 8 ? launch_packed_attention8 : launch_packed_attention4;

@@ -321,7 +321,8 @@ def test_absent_packed_pages(q, bits):
 
 
 @pytest.mark.parametrize("bits,hq,hkv,d,q,kv", [(8, 8, 1, 128, (1, 1), (40001, 9)), (4, 16, 2, 64, (1, 3), (30000, 17000)), (8, 4, 2, 128, (40,), (20001,)),
-                                               (4, 8, 8, 128, (1,) * 3, (9000, 1, 8191))])
+                                               (4, 8, 8, 128, (1,) * 3, (9000, 1, 8191)),
+                                               (4, 8, 8, 64, (1,) * 8, (17000, 1, 90, 0, 4097, 300, 2, 8192))])
 def test_pieces_of_packed_rows_are_joined(bits, hq, hkv, d, q, kv):
     s = K.problem("cuda", bits, BF, hq=hq, hkv=hkv, d=d, page=64, q_len=q, kv_len=kv, seed=9)
     out, lse = check(s)
