@@ -1,11 +1,13 @@
-// Attention of new tokens over a paged cache, and the weight that the cached rows collect from them.
+// Attention of new tokens over a paged cache: rows of 16 bits or packed ones (PoolRow), all slots up to a token's own or those that a window or
+// a tree of drafts leaves (Keys, RowView).
 //
 // The rows of a (sequence, kv-head) are its new tokens times the G query heads of the group: row r is token r / G, head
 // r % G, so the heads of a group share every key and value that is fetched.  Two kernels divide the sequences between them:
 //   paged_step   up to 16 rows (a generated token, a few drafted ones): bound by reading the pages (4 x 131071 rows x 8 heads in
 //                377 us, 5.7 TB/s; 31 requests of up to 16384 rows in 184 us, 4.9 TB/s)
 //   paged_chunk  more rows: bound by the matrix cores and the exponentials between them (2 x 2048 tokens of 16384, 32 heads, in
-//                917 to 946 us, 1.09 to 1.12 PFLOP/s)
+//                917 to 946 us, 1.09 to 1.12 PFLOP/s; rows of 8 bits, which pass through registers on their way to LDS: 1000 to 1060 us)
+//   packed_step  paged_step over packed rows (4 x 131071 rows of 8 bits in 209 us, 5.3 TB/s; the 31 requests' rows of 4 bits in 61 us)
 // Both split a sequence's keys over workgroups where that fills the chip.  The last workgroup to finish joins up to 16 pieces, a
 // launch of k_paged_merge more than that.
 //

