@@ -1125,11 +1125,17 @@ __device__ __forceinline__ void cut_chunk(const PagedAttnArgs& A, const Cut& cut
   });
 }
 
+// Waves per SIMD that a build's registers are for.  Single tokens' rows of 4 bits fit three; chunks of such rows at d = 64 do not without spills, which
+// the exponentials of a cap hide (2 x 2048 tokens of 16384: 663 us with three, 634 with two, with a cap 907 and 943; of 8 bits 660 and 658, 907 and 945).
+__host__ __device__ constexpr int waves_of(int D, int MODE, int KIND, int BITS) {
+  return KIND == 2 ? (D == 64 || BITS == 4 ? 3 : 2) : (D == 64 && (BITS != 4 || (MODE & 5)) ? 3 : 2);
+}
+
 // A launch: chunk_wgs workgroups for sequences of many rows (cut.blocks blocks of each kv-head, piece by piece), behind them those for
 // few (unit by unit, piece by piece).  One launch for both: a prompt's chunk and the other requests' tokens share the chip.
 // KIND: bit 0: there are the former, bit 1: the latter.
 template <typename T, int D, int MODE, int KIND, int BITS, bool SIGHT>
-__global__ __launch_bounds__(256, D == 64 || (BITS == 4 && KIND == 2) ? 3 : 2) void k_paged_attn(PagedAttnArgs A, Cut cut, Parts parts, int chunk_wgs) {
+__global__ __launch_bounds__(256, waves_of(D, MODE, KIND, BITS)) void k_paged_attn(PagedAttnArgs A, Cut cut, Parts parts, int chunk_wgs) {
   constexpr size_t kMost = sizeof(ChunkLds<D>) > sizeof(StepLds<D>) ? sizeof(ChunkLds<D>) : sizeof(StepLds<D>);
   __shared__ __align__(16) char lds[KIND == 1 ? sizeof(ChunkLds<D>) : KIND == 2 ? sizeof(StepLds<D>) : kMost];
   const int id = (int)blockIdx.x;

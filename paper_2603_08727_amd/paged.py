@@ -167,6 +167,7 @@ class arkv_sight:
         if tree is not None:
             _need(tree.dim() == 2 and tree.dtype in (torch.int64, torch.uint64), f"tree: int64 or uint64 [n_tokens][words], got {tree.dtype} {tuple(tree.shape)}")
             words = tree.size(1)
+            _need(words >= 1, "tree: at least one word a token")       # (a tensor of nothing has no address: it would be no tree)
         self.tree, self.n_tokens, self.index = tree, None if tree is None else tree.size(0), None if tree is None else tree.get_device()
         self.c = _Sight(window, sink, words, None if tree is None else _dense(tree, tree.shape, tree.dtype, "tree"))
         self.ref = C.addressof(self.c)

@@ -484,6 +484,28 @@ def test_batches_of_more_than_64_sequences(bits, hq, hkv, d):
                 assert torch.equal(v[sum(q[:b]):sum(q[:b]) + a, h], R.rows(s, s.v, b, h)[0][kv[b] - a:])
 
 
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("q,kv", [((1, 1, 1), (700, 3, 90)), ((5, 0, 2), (300, 8, 2)), ((40, 3), (900, 40)), ((150, 1), (2000, 1500))])
+def test_bounds_may_be_loose(q, kv, bits):
+    """What is announced shapes the launches, not the results: tokens and rows of sequences far below their bounds."""
+    make = dict(hq=16, hkv=2, d=128, page=32, q_len=q, kv_len=kv, seed=4, width=200)
+    s = R.problem("cuda", BF, **make) if bits == 16 else K.problem("cuda", bits, BF, **make)
+    tree = K.drafts(s)
+    for window, drafted, max_kv in [(0, True, 6400), (50, False, 6400), (50, True, 4000), (0, True, max(kv))]:
+        ref, rl, tol, ltol = K.attention(s, window, 4, tree if drafted else None)
+        pages, batch, ws = handles(s, max_q=s.n, max_kv=max_kv)
+        out, lse = torch.empty(s.n, s.hq, s.d, dtype=BF, device="cuda"), torch.empty(s.n, s.hq, device="cuda")
+        wide = torch.zeros(s.n, -(-s.n // 64) * 64, dtype=torch.bool)
+        wide[:, :tree.shape[1]] = tree
+        sight = P.arkv_sight(window, 4, K.words(wide).cuda() if drafted else None)
+        if bits == 16:
+            P.arkv_paged_attention_sight(pages, batch, sight, s.q, s.scale, out, lse=lse, workspace=ws)
+        else:
+            P.arkv_packed_attention(pages, batch, s.q, s.scale, out, lse=lse, sight=sight, workspace=ws)
+        R.close(out, ref, tol, "out")
+        R.close(lse, rl, ltol, "lse")
+
+
 def test_one_workspace_serves_every_batch_bits_and_sight():
     s0 = K.problem("cuda", 8, BF, hq=16, hkv=4, d=128, page=16, q_len=(300,) * 6, kv_len=(3000,) * 6, seed=1)
     ws = handles(s0)[2]

@@ -143,6 +143,8 @@ def test_the_binding_checks_packed_pages_and_sights():
     for kw in [dict(window=1 << 32), dict(sink=1 << 31)]:
         with pytest.raises(ValueError, match="32 bits"):
             P.arkv_sight(**kw)
+    with pytest.raises(ValueError, match="word"):
+        P.arkv_sight(tree=z(4, 0, dtype=torch.int64))
     for tree in [z(4, 1), z(4, dtype=torch.int64), z(4, 1, dtype=i32), z(4, 1, dtype=torch.int64)]:     # (the last: on the CPU)
         with pytest.raises(ValueError):
             P.arkv_sight(tree=tree)
