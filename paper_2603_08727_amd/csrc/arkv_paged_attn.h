@@ -35,7 +35,9 @@ constexpr int kChunkRows = 128, kChunkKeys = 64;
 
 // How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
 // blocks: of kChunkRows rows, of all sequences, at most.  joined: the last workgroup of a (sequence, kv-head), chunk_joined: of a block
-// and kv-head joins its pieces (tickets from chunk_ticket0 on), no launch is needed for that.
+// and kv-head joins its pieces (tickets from chunk_ticket0 on), no launch is needed for that; chunk_spread: k_chunk_join does, else k_paged_merge.
+// groups: of kStepRows rows, of all sequences, at most: all rows are paged_step's, group by group (0: sequences of few rows alone are, each a unit).
+// places: workgroups that the chip holds, where the kernel chooses its pieces itself (chunk_piece: the shortest), else 0.
 struct Cut { int step_piece, n_step, groups, chunk_piece, n_chunk, blocks, places, chunk_ticket0; bool joined, chunk_joined, chunk_spread; Which w; };
 constexpr int kJoinPieces = 16;         // at most: a lane has all pieces' loads under way at once
 // Limited sight and packed rows: sequences of more than kStepRows rows are paged_step's too, in groups of kStepRows, where all groups' tiles of 64
@@ -110,7 +112,7 @@ inline Cut cut_of(const Paged& P, const Sight& V, int D, int Hq) {
 }
 
 // Pieces' results: sums [row][D] and (reference, denominator) [row].  Rows of paged_step: ((unit * n_step + piece) * 16 +
-// row), behind them rows of paged_chunk: (piece * N + token) * Hq + head, or, where its workgroups join them, kChunkRows rows of
+// row), behind them rows of paged_chunk: (piece * N + token) * Hq + head, or, where its workgroups or k_chunk_join join them, kChunkRows rows of
 // ((block * H + head) * n_chunk + piece), each wave's as they lie in its lanes.
 // split: what k_chunk_join needs of each block of rows and kv-head: pieces, first token, tokens, which block of the sequence's.
 struct Parts { float* acc; float2* ml; int* tickets; size_t chunk0; int4* split; };
