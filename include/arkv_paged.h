@@ -97,7 +97,7 @@ typedef struct {
  * pos as in arkv_pages.  A row's channels lie in blocks of 32, each with a scale byte s; a channel is its code's value times 2^(s - 127).
  * bits = 8: a code is a byte: sign, 4 bits of exponent (bias 7), 3 of mantissa, 127 and 255 NaN, the largest value 448; 4: half a byte (an even
  * channel's the low half): sign, 2 bits of exponent (bias 1), 1 of mantissa, the largest value 6.  s = 255: NaN, the whole block.
- * dtype: of the rows that go in and come out, and of q.  All five 16-byte aligned; sizes as in arkv_pages. */
+ * dtype: of the rows that go in and come out, and of q.  All five 16-byte aligned; sizes as in arkv_pages.  Other bits: ARKV_EUNSUPPORTED. */
 typedef struct {
   int32_t dtype, bits, n_pages, page_size, n_kv_heads, head_dim;
   void* k;

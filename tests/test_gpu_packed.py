@@ -263,6 +263,23 @@ def test_rows_are_read_from_far_behind_4_gb():
     P.arkv_packed_read(pages, batch, k, None)
     rows = [R.rows(far, far.k, b, 0)[0][-a:] for b, a in enumerate(far.q_len)]
     assert torch.equal(k[:, 0], torch.cat(rows))
+    # rows appended there, against a small pool's
+    g = torch.Generator().manual_seed(1)
+    kn, vn = (torch.randn(s.n, hkv, d, generator=g).to(BF).cuda() for _ in "kv")
+    freq = (10000.0 ** (-torch.arange(64, dtype=torch.float64) / 64)).cuda()
+    positions = torch.arange(s.n, dtype=torch.int32, device="cuda")[None]
+    scale_v, codes_v = torch.empty_like(scale), torch.empty_like(codes)
+    there = P.arkv_packed_pages(codes, codes_v, scale, scale_v, pos, BF)
+    near, near_batch, _ = handles(far)
+    near = P.arkv_packed_pages(torch.zeros_like(far.k_codes), torch.zeros_like(far.k_codes), torch.zeros_like(far.k_scale), torch.zeros_like(far.k_scale),
+                               torch.zeros_like(far.pos), BF)
+    got = []
+    for p, b in ((there, batch), (near, near_batch)):
+        P.arkv_packed_append(p, b, P.arkv_rotary(freq), None, kn, vn, positions, None)
+        read = [torch.empty(s.n, hkv, d, dtype=BF, device="cuda") for _ in "kv"]
+        P.arkv_packed_read(p, b, *read)
+        got.append(read)
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
 
 
 # ---- attention over packed pages ------------------------------------------------------------------
