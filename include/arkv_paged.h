@@ -194,6 +194,15 @@ int arkv_paged_evict(const arkv_pages* pages, const arkv_page_batch* batch, cons
 int arkv_debug_paged_row(const int32_t* table_row, int32_t table_width, int32_t n_pages, int32_t page_size,
                          int32_t n_kv_heads, int32_t kv_head, int32_t len, int32_t slot, int64_t* row);
 
+/* Parity hook, HOST, pure: how arkv_packed_attention, or with bits = 16 arkv_paged_attention_sight, divides a batch.  HOST arrays here: the batch's cu_q and
+ * kv_len, the scores' prefix; no other address is followed.  cut HOST int32 [9]: [0] bit 0: blocks of 128 rows (a row: a new token and a query
+ * head of the group) are launched, bit 1: groups of up to 16; [1] groups that sequences of more rows are divided into, at most (0: into blocks); [2] keys
+ * of a group's piece; [3] pieces of a group, the most; [4] keys of a block's piece; [5] pieces of a block, the most; [6] where a block has more than
+ * one, they are joined by 1: the last workgroup to finish, 2: a launch of blocks, 3: a launch of rows; [7] pieces of all blocks and kv-heads;
+ * [8] workgroups that the chip holds at once, which [4] is chosen for (0: by the batch's bounds alone).  ARKV_EINVAL, ARKV_EUNSUPPORTED: as those calls. */
+int arkv_debug_attention_cut(const arkv_packed_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores, const arkv_sight* sight,
+                             int32_t n_q_heads, int32_t* cut);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1017,21 +1017,34 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, ChunkLds<D>&
 // Keys of a piece.  The host knows bounds of the lengths alone; where it leaves the choice (cut.places), the pieces are the shortest, from
 // cut.chunk_piece on, with which all of them are on the chip at once (eight requests of 25 to 64 drafts, 4472 to 8192 rows of 8 bits: 1408
 // keys, which the bounds give, make 536 workgroups, 83 us; 1536 make 504, 69 us).
+// sum(f): of f(blocks, tiles) over the sequences, up to 64 of them.
+template <typename Sum> __host__ __device__ __forceinline__ int chosen_piece(const Cut& cut, Sum sum) {
+  const int most = 1 << 24, whole = sum([](int blocks, int tiles) { const int n = blocks * (tiles >> 4); return n < 1 << 24 ? n : 1 << 24; });
+  const long long even = whole * 16ll / cut.places;
+  int piece = even < most ? (int)even : most;
+  if (piece < cut.chunk_piece / kChunkKeys) piece = cut.chunk_piece / kChunkKeys;
+  for (int i = 0; i < 24 && sum([=](int blocks, int tiles) { return blocks * ((tiles + piece - 1) / piece); }) > cut.places; ++i) piece += (piece + 15) / 16;
+  return piece * kChunkKeys;
+}
+// A sequence's blocks, of all kv-heads, and their 64-key tiles.
+struct Load { int blocks, tiles; };
+__host__ __device__ __forceinline__ Load load_of(const Paged& P, const Sight& V, const Seq& s, int prefix, int G, int few) {
+  const int R = s.nq * G, blocks = row_blocks<kChunkRows>(s.nq, G, few);
+  const int tiles = (Keys<true>(V, s, prefix, (R > 1 ? R - 1 : 0) / kChunkRows * kChunkRows / G, s.nq - 1).end + kChunkKeys - 1) / kChunkKeys;
+  return {blocks * P.H, tiles};
+}
 __device__ __forceinline__ int chunk_piece(const PagedAttnArgs& A, const Cut& cut, int lane) {
   if (!cut.places) return cut.chunk_piece;
   const Paged& P = A.P;
-  const int b = min(lane, P.B - 1), prefix = A.S.prefix ? A.S.prefix[b] : 0;
-  const Seq s = seq_of(P, b);
-  const int R = s.nq * A.G, blocks = lane < P.B ? row_blocks<kChunkRows>(s.nq, A.G, cut.w.few) * P.H : 0;
-  const int tiles = (Keys<true>(A.V, s, prefix, max(0, R - 1) / kChunkRows * kChunkRows / A.G, s.nq - 1).end + kChunkKeys - 1) / kChunkKeys;
-  auto sum = [](int x) {
+  const int b = min(lane, P.B - 1);
+  const Load own = load_of(P, A.V, seq_of(P, b), A.S.prefix ? A.S.prefix[b] : 0, A.G, cut.w.few);
+  const int blocks = lane < P.B ? own.blocks : 0, tiles = own.tiles;
+  return chosen_piece(cut, [=](auto f) {
+    int x = f(blocks, tiles);
 #pragma unroll
     for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
     return __builtin_amdgcn_readfirstlane(x);
-  };
-  int piece = max(cut.chunk_piece / kChunkKeys, (int)min((sum(min(blocks * (tiles >> 4), 1 << 24)) * 16ll) / cut.places, 1ll << 24));
-  for (int i = 0; i < 24 && sum(blocks * ((tiles + piece - 1) / piece)) > cut.places; ++i) piece += (piece + 15) / 16;
-  return piece * kChunkKeys;
+  });
 }
 
 // Workgroup id of a launch that is cut: blocks of each kv-head, piece by piece.

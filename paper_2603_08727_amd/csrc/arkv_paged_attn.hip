@@ -1,4 +1,6 @@
 // Attention over 16-bit pages, every new token seeing all slots up to its own: its builds, and the sizes of workspaces and launches.
+#include <iterator>
+
 #include "arkv_paged_attn.h"
 
 namespace arkv {
@@ -46,6 +48,41 @@ size_t paged_attention_bound(const Paged& P, int D, int Hq) {
 long long paged_attention_workgroups(const Paged& P, const Sight& V, int D, int Hq) {
   const Launches l = launches_of(P, Hq, cut_of(P, V, D, Hq));
   return std::max(l.chunk + l.step, l.merge);
+}
+
+void paged_attention_cut(const Paged& P, const Scores& S, const Sight& V, int D, int Hq, int32_t* cut) {
+  const Cut c = cut_of(P, V, D, Hq);
+  const int G = Hq / P.H;
+  const auto seq = [&](int b) { return clamp_seq(P.cu_q[b], P.cu_q[b + 1], P.kv_len[b], P.N, P.max_q, P.max_kv); };
+  const auto prefix = [&](int b) { return S.prefix ? S.prefix[b] : 0; };
+  const int length = !c.places ? c.chunk_piece : chosen_piece(c, [&](auto f) {
+    int x = 0;
+    for (int b = 0; b < P.B; ++b) {
+      const Load l = load_of(P, V, seq(b), prefix(b), G, c.w.few);
+      x += f(l.blocks, l.tiles);
+    }
+    return x;
+  });
+  int step = 1, chunk = 1;
+  long long chunks = 0;
+  for (int b = 0; b < P.B; ++b) {
+    const Seq s = seq(b);
+    const int R = s.nq * G, blocks = row_blocks<kChunkRows>(s.nq, G, c.w.few);
+    const auto pieces = [&](int r0, int rows, int piece) {
+      return std::max(1, (Keys<true>(V, s, prefix(b), r0 / G, (std::min(R, r0 + rows) - 1) / G).end + piece - 1) / piece);
+    };
+    if (c.w.chunk)
+      for (int i = 0; i < blocks; ++i) {
+        const int n = pieces(i * kChunkRows, kChunkRows, length);
+        chunk = std::max(chunk, n);
+        chunks += (long long)n * P.H;
+      }
+    if (c.w.step && (c.groups || R <= kStepRows))
+      for (int r0 = 0; r0 < R; r0 += kStepRows) step = std::max(step, pieces(r0, kStepRows, c.step_piece));
+  }
+  const int joined = chunk == 1 ? 0 : c.chunk_joined ? 1 : c.chunk_spread ? 2 : 3;
+  const int32_t got[] = {(c.w.chunk ? 1 : 0) | (c.w.step ? 2 : 0), c.groups, c.step_piece, step, length, chunk, joined, (int32_t)std::min(chunks, 1ll << 30), c.places};
+  std::copy(std::begin(got), std::end(got), cut);
 }
 
 hipError_t launch_paged_attention(int dtype, int D, const PagedAttnArgs& A, hipStream_t st) {

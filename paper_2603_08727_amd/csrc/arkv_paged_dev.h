@@ -88,6 +88,8 @@ size_t paged_attention_bound(const Paged& P, int D, int Hq);
 size_t paged_weights_floats(const Paged& P, int Hq);
 size_t paged_weights_bound(const Paged& P, int Hq);
 long long paged_attention_workgroups(const Paged& P, const Sight& V, int D, int Hq);   // of its largest launch
+// What arkv_debug_attention_cut says (P's and S's arrays: HOST).
+void paged_attention_cut(const Paged& P, const Scores& S, const Sight& V, int D, int Hq, int32_t* cut);
 hipError_t launch_paged_attention(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
 hipError_t launch_paged_attention_sight(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);
 hipError_t launch_packed_attention8(int dtype, int D, const PagedAttnArgs& A, hipStream_t st);

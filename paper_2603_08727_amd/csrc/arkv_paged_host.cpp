@@ -287,4 +287,22 @@ int arkv_debug_paged_row(const int32_t* table_row, int32_t table_width, int32_t 
   return ARKV_OK;
 }
 
+int arkv_debug_attention_cut(const arkv_packed_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores, const arkv_sight* sight,
+                             int32_t n_q_heads, int32_t* cut) {
+  Paged P;
+  Scores S;
+  Sight V;
+  int G;
+  if (!pages || !cut) return ARKV_EINVAL;
+  arkv_packed_pages p = *pages;
+  if (p.bits == 16) p.bits = 8;
+  TRY(check_packed(&p, batch, P));
+  TRY(check_heads(n_q_heads, P.H, P.N, G));
+  TRY(check_scores(scores, S));
+  TRY(check_sight(sight, pages->bits, P, S, V));
+  if (pages->bits == 16 && !V.window && !V.tree) V = {};           // (arkv_paged_attention's)
+  paged_attention_cut(P, S, V, pages->head_dim, n_q_heads, cut);
+  return ARKV_OK;
+}
+
 }  // extern "C"

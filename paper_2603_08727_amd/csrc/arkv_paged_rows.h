@@ -113,7 +113,7 @@ template <> struct Keys<false> {
 };
 template <> struct Keys<true> {
   int end, all_end, front, gap, lo, sink, pre;   // all tokens see slots lo .. all_end - 1, those of them below sink, and all below pre
-  __device__ __forceinline__ Keys(const Sight& V, const Seq& s, int prefix, int first, int last) {
+  __host__ __device__ __forceinline__ Keys(const Sight& V, const Seq& s, int prefix, int first, int last) {
     const int ctx = s.kv - s.nq;
     pre = max(0, min(prefix, s.kv));
     sink = V.sink;
@@ -128,8 +128,8 @@ template <> struct Keys<true> {
       lo = ctx + (V.tree ? s.nq - 1 : last) - V.window + 1;
     }
   }
-  __device__ __forceinline__ int slot(int j) const { return j < front ? j : j + gap; }
-  __device__ __forceinline__ bool all_seen(int j, int n) const {
+  __host__ __device__ __forceinline__ int slot(int j) const { return j < front ? j : j + gap; }
+  __host__ __device__ __forceinline__ bool all_seen(int j, int n) const {
     const int at = slot(j);
     if (at + n - 1 != slot(j + n - 1)) return false;
     return (at + n <= all_end && (at >= lo || at + n <= sink)) || at + n <= pre;

@@ -16,7 +16,7 @@ TICKET_BYTES = 1 << 16                             # of a workspace's front, zer
 
 EXPORTED = ["arkv_paged_append", "arkv_paged_workspace", "arkv_paged_attention", "arkv_paged_weights", "arkv_paged_evict",
             "arkv_paged_attention_sight", "arkv_packed_append", "arkv_packed_read", "arkv_packed_workspace", "arkv_packed_attention",
-            "arkv_debug_paged_row"]
+            "arkv_debug_paged_row", "arkv_debug_attention_cut"]
 
 
 class _Pages(C.Structure):
@@ -74,6 +74,7 @@ def load():
             "arkv_packed_workspace": [pg, bt, i32, vp],
             "arkv_packed_attention": [pg, bt, sc, vp, i32, rw, vp, vp, vp, C.c_size_t, vp],
             "arkv_debug_paged_row": [vp] + [i32] * 7 + [vp],
+            "arkv_debug_attention_cut": [pg, bt, sc, vp, i32, vp],
         }
         for name, args in sig.items():
             fn = getattr(lib, name)
@@ -440,3 +441,20 @@ def arkv_debug_paged_row(table_row, n_pages, page_size, n_kv_heads, kv_head, len
     _check((_lib or load()).arkv_debug_paged_row(t.ctypes.data, len(t), n_pages, page_size, n_kv_heads, kv_head, length, slot, C.addressof(row)),
            "arkv_debug_paged_row")
     return row.value
+
+
+def arkv_debug_attention_cut(cu_q, kv_len, n_tokens, max_q, max_kv, n_q_heads, n_kv_heads, head_dim, bits, window=0, sink=0, tree_words=0, cap=0.0,
+                             prefix=None):
+    """How an attention call over pages of 16-, 8- or 4-bit rows divides a batch: the nine numbers of the header's text.  cu_q, kv_len, prefix: NumPy
+    int32; tree_words: 0 without a tree."""
+    import numpy as np
+    _int32(n_tokens=n_tokens, max_q=max_q, max_kv=max_kv, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, window=window, sink=sink)
+    cu_q, kv_len, prefix = (None if x is None else np.ascontiguousarray(x, dtype=np.int32) for x in (cu_q, kv_len, prefix))
+    B, cut, none = len(kv_len), (C.c_int32 * 9)(), 16      # (an address that is not followed)
+    _need(len(cu_q) == B + 1 and (prefix is None or len(prefix) == B), "cu_q: [B + 1], kv_len, prefix: [B]")
+    pages = _Packed(0, bits, 1, 16, n_kv_heads, head_dim, none, none, none, none, none)
+    batch = _Batch(B, n_tokens, max_q, max_kv, max(1, -(-max_kv // 16)), cu_q.ctypes.data, kv_len.ctypes.data, none)
+    scores = _Scores(1.0, cap, None, None, None if prefix is None else prefix.ctypes.data)
+    sight = _Sight(window, sink, tree_words, none if tree_words else None)
+    _check((_lib or load()).arkv_debug_attention_cut(*(C.addressof(x) for x in (pages, batch, scores, sight)), n_q_heads, cut), "arkv_debug_attention_cut")
+    return list(cut)

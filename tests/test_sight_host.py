@@ -1,0 +1,55 @@
+"""CPU checks of how attention over packed pages, under a window or for drafted trees, is divided, and of the tests' matrices of what tokens see."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_08727_amd import binding as A
+from paper_2603_08727_amd import paged as P
+import packed_ref as K
+import sight_ref as S
+
+
+def cut(q, kv, hq, hkv, d, bits, window=0, sink=0, tree=False, n_tokens=None, max_q=None, max_kv=None, **kw):
+    return S.Cut(P.arkv_debug_attention_cut(np.cumsum([0, *q]), kv, n_tokens or sum(q), max_q or max(q), max_kv or max(kv), hq, hkv, d, bits, window, sink,
+                                            -(-(max_q or max(q)) // 64) if tree else 0, **kw))
+
+
+def test_what_is_seen_is_the_same_as_whole_matrices():
+    g = torch.Generator().manual_seed(1)
+    pick = lambda hi: int(torch.randint(0, hi, (1,), generator=g))  # noqa: E731
+    for _ in range(300):
+        q = [pick(9) for _ in range(3)]
+        kv = [pick(40) for _ in range(3)]
+        s = K.R.problem("cpu", hq=2, hkv=1, d=2, page=16, q_len=q, kv_len=kv, seed=pick(1 << 20))
+        s.table[pick(3), 0] = -1
+        tree = None if pick(2) else torch.rand(s.n, 12, generator=g) < 0.4
+        prefix = None if pick(2) else [pick(50) - 5 for _ in range(3)]
+        window, sink = pick(2) * (1 + pick(20)), pick(2) * pick(20)
+        for b in range(3):
+            assert torch.equal(S.sight(s, b, prefix, window, sink, tree), K.sight(s, b, prefix, window, sink, tree))
+
+
+def test_cuts_by_hand():
+    """One request whose 64 new tokens are 512 rows of 8 heads' groups: 4 blocks, 32 groups."""
+    one = cut([64], [300], 8, 1, 128, 16)
+    assert one.blocks and not one.few and not one.groups and one.piece == 256 and one.pieces == 2 and one.join == 1
+    assert one.workgroups == 1 + 2 + 2 + 2             # (the first block's tokens see 252 rows, the second's 268)
+    few = cut([1, 2], [300, 40], 8, 1, 128, 16)
+    assert few.few and not few.blocks and few.step_piece == 128 and few.step_pieces == 3 and few.workgroups == 0
+    grouped = cut([64], [300], 8, 1, 128, 8)           # (one request's groups: 32, and one for a sequence's rest)
+    assert grouped.groups == 33 and not grouped.blocks
+    both = cut([64, 1], [300, 40], 8, 1, 128, 16)
+    assert both.blocks and both.few
+    # under a window of 100 of 5000 rows the longest has 16 slots of its page, 100, and 15 of other blocks' tokens
+    assert cut([1], [5000], 8, 1, 128, 16, window=100, sink=4).step_pieces == 1 and cut([1], [5000], 8, 1, 128, 16).step_pieces > 8
+
+
+def test_refusals_of_the_hook():
+    for bad in [dict(bits=5), dict(d=32), dict(hq=7), dict(hq=34), dict(window=-1), dict(max_kv=-1), dict(cap=-1.0)]:
+        kw = dict(q=[3], kv=[30], hq=8, hkv=2, d=64, bits=8)
+        kw.update(bad)
+        with pytest.raises(A.ArkvError):
+            cut(**kw)
+    assert P.load().arkv_debug_attention_cut(None, None, None, None, 8, None) == A.EINVAL
+    with pytest.raises(ValueError):
+        P.arkv_debug_attention_cut([0, 1], [3, 4], 1, 1, 4, 8, 2, 64, 8)
