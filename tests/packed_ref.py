@@ -95,6 +95,14 @@ def quick_pack(x, bits):
     return codes.contiguous(), (e + 127).to(torch.uint8)
 
 
+def every_pair(bits, d):
+    """Rows' bytes [rows][d bits / 8] and scale bytes [rows][d / 32]: every byte of codes in a block of every scale."""
+    per = 32 * bits // 8
+    codes = torch.arange(256, dtype=torch.int32).reshape(1, -1, per).expand(256, -1, -1)
+    scale = torch.arange(256, dtype=torch.int32)[:, None].expand(-1, 256 // per)
+    return codes.reshape(-1, d * bits // 8).to(torch.uint8), scale.reshape(-1, d // 32).to(torch.uint8)
+
+
 def problem(dev, bits, dtype=torch.bfloat16, **kw):
     """paged_ref.problem with packed pages: s.k and s.v are what the codes stand for; unused slots hold NaN."""
     s = R.problem("cpu", dtype, **kw)

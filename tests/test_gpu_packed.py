@@ -118,6 +118,27 @@ def test_every_code_and_scale_is_read_as_its_value(bits, d, dtype):
         assert torch.equal(got[ok], want[ok])
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_every_pair_of_code_and_scale_is_read(bits, d, dtype):
+    """All of them in rows of the batch: keys in order, values the other way round."""
+    codes, scale = K.every_pair(bits, d)
+    n, page = len(codes), 64
+    pages = pool(bits, n // page, 1, page, d, dtype)
+    for x, y in ((pages.k, codes), (pages.v, codes.flip(0)), (pages.k_scale, scale), (pages.v_scale, scale.flip(0))):
+        x.copy_(y.reshape(x.shape))
+    one = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    batch = P.arkv_page_batch(one([0, n]), one([n]), one([list(range(n // page))]), n, n, n)
+    k, v = (torch.full((n, 1, d), 7.0, dtype=dtype, device="cuda") for _ in "kv")
+    P.arkv_packed_read(pages, batch, k, v)
+    want = K.values(codes, scale, bits).float().to(dtype)              # (codes' values fit 32 bits)
+    for got, ref in ((k, want), (v, want.flip(0))):
+        got = got[:, 0].cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(ref))
+        assert torch.equal(got[~torch.isnan(ref)], ref[~torch.isnan(ref)])
+
+
 def check_append(pages, batch, s, kn, vn, positions, rotary, freq, axis, adjacent, q=None, q_out=None):
     """Appends, and compares every byte of the pool."""
     before = [x.clone().cpu() for x in (pages.k, pages.v, pages.k_scale, pages.v_scale, pages.pos)]

@@ -195,3 +195,12 @@ def test_sights_by_the_book():
     assert see(tree=tree) == [[0, 1, 2, 3, 4, 5], [0, 1, 2, 3, 4, 5, 6], [0, 1, 2, 3, 4, 5, 7]]
     assert see(tree=tree, window=3) == [[3, 4, 5], [4, 5, 6], [4, 5, 7]]
     assert see(window=1, prefix=[3]) == [[0, 1, 2, 5], [0, 1, 2, 6], [0, 1, 2, 7]]
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("d", [64, 128])
+def test_every_pair_of_code_and_scale_is_there(bits, d):
+    codes, scale = K.every_pair(bits, d)
+    assert len(codes) == len(scale)
+    pairs = {(int(s), int(c)) for row, of in zip(codes, scale) for c, s in zip(row, of.repeat_interleave(32 * bits // 8))}
+    assert pairs == {(s, c) for s in range(256) for c in range(256)}
