@@ -33,6 +33,14 @@ constexpr int kStepWaves = 4;
 constexpr int kStepMaxPiece = 2048;     // (twice that at most: a lane holds the page of one granule)
 constexpr int kChunkRows = 128, kChunkKeys = 64;
 
+// Waves per SIMD that a build's registers are for, and with that workgroups to a CU.  Single tokens' rows of 4 bits fit three; chunks of such rows at
+// d = 64 do not without spills, which the exponentials of a cap hide (2 x 2048 tokens of 16384: 663 us with three, 634 with two, with a cap 907 and
+// 943; of 8 bits 660 and 658, 907 and 945).
+__host__ __device__ constexpr int chunk_waves(int D, int bits, bool capped) { return D == 64 && (bits != 4 || capped) ? 3 : 2; }
+__host__ __device__ constexpr int waves_of(int D, int MODE, int KIND, int BITS) {
+  return KIND == 2 ? (D == 64 || BITS == 4 ? 3 : 2) : chunk_waves(D, BITS, MODE & 5);
+}
+
 // How a launch is cut.  step_piece, chunk_piece: keys per workgroup; the counts: pieces of the longest sequence.
 // blocks: of kChunkRows rows, of all sequences, at most.  joined: the last workgroup of a (sequence, kv-head), chunk_joined: of a block
 // and kv-head joins its pieces (tickets from chunk_ticket0 on), no launch is needed for that; chunk_spread: k_chunk_join does, else k_paged_merge.
@@ -68,14 +76,15 @@ inline Cut cut_of(const Paged& P, const Sight& V, int D, int Hq) {
   // rows: 209 and 210).
   const int longest = V.bits == 4 ? 2 * kStepMaxPiece : kStepMaxPiece;
   pieces(kv_step, units, std::min(256ll, kJoinPieces * units), 128, units < 16 ? longest / 2 : longest, 128, c.step_piece, c.n_step);
-  // One workgroup for each CU; then for every place on the chip, at d = 64 three to a CU, in larger pieces (1686 tokens on up to 3001
+  // One workgroup for each CU; then for every place on the chip, two or three to a CU, in larger pieces (1686 tokens on up to 3001
   // rows, 12 heads: 46 us in pieces of 1024 keys, 42 of 512; d = 128, 512 tokens on 4100 rows, 16 heads, 7 single tokens: 66 us in pieces of
   // 1024, 70 of 768, 82 of 512; 128 tokens on 1024 rows: 28 us in one piece, 22 in
   // pieces of 256).
   const long long rows = (long long)P.N * G, blocks = (rows + kChunkRows - 1) / kChunkRows * P.H;
+  const int places = 256 * chunk_waves(D, V.bits, V.capped);
   int alone, n_alone;
   pieces(kv_chunk, blocks, 256, 256, 1 << 28, kChunkKeys, alone, n_alone);
-  pieces(kv_chunk, blocks, D == 64 ? 768 : 512, D == 64 ? 512 : 1024, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
+  pieces(kv_chunk, blocks, places, D == 64 ? 512 : 1024, 1 << 28, kChunkKeys, c.chunk_piece, c.n_chunk);
   if (alone < c.chunk_piece) { c.chunk_piece = alone; c.n_chunk = n_alone; }
   if (V.bits && c.w.chunk) {
     const long long groups = rows / kStepRows + std::min<long long>(P.B, rows), keys = most_keys(P, V, (kStepRows - 1) / G + 2);
@@ -103,7 +112,7 @@ inline Cut cut_of(const Paged& P, const Sight& V, int D, int Hq) {
     if (c.n_chunk > 1 && P.B <= 64 && (long long)c.blocks * P.H * n <= kJoinBlocks && half < c.chunk_piece) {
       c.chunk_piece = half;
       c.n_chunk = n;
-      c.places = 256 * (D == 64 ? 3 : 2);
+      c.places = places;
     }
     c.chunk_joined = c.chunk_joined && c.n_chunk <= kFewPieces;
     c.chunk_spread = c.w.chunk && !c.chunk_joined && c.n_chunk > 1 && (long long)c.blocks * P.H * c.n_chunk <= kJoinBlocks;
@@ -1138,12 +1147,6 @@ __device__ __forceinline__ void cut_chunk(const PagedAttnArgs& A, const Cut& cut
     }
     return true;
   });
-}
-
-// Waves per SIMD that a build's registers are for.  Single tokens' rows of 4 bits fit three; chunks of such rows at d = 64 do not without spills, which
-// the exponentials of a cap hide (2 x 2048 tokens of 16384: 663 us with three, 634 with two, with a cap 907 and 943; of 8 bits 660 and 658, 907 and 945).
-__host__ __device__ constexpr int waves_of(int D, int MODE, int KIND, int BITS) {
-  return KIND == 2 ? (D == 64 || BITS == 4 ? 3 : 2) : (D == 64 && (BITS != 4 || (MODE & 5)) ? 3 : 2);
 }
 
 // A launch: chunk_wgs workgroups for sequences of many rows (cut.blocks blocks of each kv-head, piece by piece), behind them those for

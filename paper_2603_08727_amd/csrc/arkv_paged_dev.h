@@ -22,8 +22,8 @@ struct Rows { const void* p; int64_t ts, hs; };
 struct Scores { float scale, cap; const float* slopes; const int32_t *q_pos, *prefix; };
 
 // Which slots a token sees, where that is not all up to its own.  bits: of a row's channels, where a build for that is called (0: the one without);
-// prefixed: the scores have a prefix.
-struct Sight { int window, sink, words, bits; bool prefixed; const uint64_t* tree; };
+// prefixed, capped: the scores have a prefix, a cap.
+struct Sight { int window, sink, words, bits; bool prefixed, capped; const uint64_t* tree; };
 
 // One sequence, cut to what the launch was announced: nothing behind these numbers reaches outside the arrays.
 struct Seq { int q0, nq, kv; };

@@ -80,6 +80,7 @@ static int check_sight(const arkv_sight* s, int bits, const Paged& P, const Scor
   out = {};
   out.bits = bits;
   out.prefixed = x.prefix != nullptr;
+  out.capped = x.cap > 0.f;
   if (!s) return ARKV_OK;
   if (s->window < 0 || s->sink < 0) return ARKV_EINVAL;
   if (s->tree && (s->tree_words < 1 || (int64_t)s->tree_words * 64 < P.max_q || ((uintptr_t)s->tree & 7))) return ARKV_EINVAL;

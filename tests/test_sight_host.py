@@ -1,4 +1,6 @@
 """CPU checks of how attention over packed pages, under a window or for drafted trees, is divided, and of the tests' matrices of what tokens see."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -53,3 +55,32 @@ def test_refusals_of_the_hook():
     assert P.load().arkv_debug_attention_cut(None, None, None, None, 8, None) == A.EINVAL
     with pytest.raises(ValueError):
         P.arkv_debug_attention_cut([0, 1], [3, 4], 1, 1, 4, 8, 2, 64, 8)
+
+
+@pytest.mark.parametrize("d,bits,cap,places", [(128, 8, 0.0, 512), (128, 4, 0.0, 512), (128, 16, 30.0, 512), (64, 16, 0.0, 768), (64, 8, 0.0, 768), (64, 8, 30.0, 768),
+                                               (64, 4, 30.0, 768), (64, 4, 300.0, 768), (64, 4, 0.0, 512)])
+def test_pieces_are_planned_for_the_places_of_the_build_that_runs(d, bits, cap, places):
+    """Workgroups of four waves: three or two to each of 256 CUs, by the registers that the build leaves a wave."""
+    window = 3000 if bits == 16 else 0
+    c = cut([700, 700, 300], [5000, 4000, 6000], 16, 4, d, bits, window=window, cap=cap)
+    assert c.blocks and c.pieces > 1 and c.places == places and c.workgroups <= places
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (8, 8, 64), (16, 1, 64), (21, 3, 64), (4, 4, 64)])
+def test_a_workspace_of_4_bit_pages_serves_every_window_and_cap(hq, hkv, d):
+    """Their builds have other places than those of 8 bits, and others with a cap: no call may need more than the workspace's size."""
+    if torch.cuda.is_available():
+        pytest.skip("would launch")                    # (without a GPU a call that passes its checks fails in the launch)
+    rng = np.random.default_rng(hq + d)
+    lib, n, r, at = P.load(), C.c_size_t(), C.byref, 0x1000
+    pages, rows = P._Packed(0, 4, 100, 64, hkv, d, at, at, at, at, at), P._Rows(at, hq * d, d)
+    for _ in range(1500):
+        batch, n_tokens, max_kv, window = (int(np.exp(rng.uniform(0, np.log(hi)))) for hi in (500, 30000, 1 << 20, 1 << 20))
+        max_q = min(n_tokens, int(np.exp(rng.uniform(0, np.log(n_tokens + 1)))))
+        b = P._Batch(batch, n_tokens, max_q, max_kv, 1 << 20, at, at, at)
+        assert lib.arkv_packed_workspace(r(pages), r(b), hq, r(n)) == A.OK
+        for cap in (0.0, 30.0):
+            for s in (None, P._Sight(window, 4, 0, None), P._Sight(window, 0, 1 << 10, at)):
+                args = (r(pages), r(b), r(P._Scores(0.125, cap, None, None, None)), s if s is None else r(s), hq, r(rows), at, None, at)
+                assert lib.arkv_packed_attention(*args, 0, None) == A.EINVAL
+                assert lib.arkv_packed_attention(*args, n.value, None) in (A.EHIP, A.EUNSUPPORTED), (batch, n_tokens, max_q, max_kv, window, cap)
