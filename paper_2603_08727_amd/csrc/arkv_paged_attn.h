@@ -1024,7 +1024,7 @@ __device__ __forceinline__ void paged_chunk(const PagedAttnArgs& A, ChunkLds<D>&
 }
 
 // Keys of a piece.  The host knows bounds of the lengths alone; where it leaves the choice (cut.places), the pieces are the shortest, from
-// cut.chunk_piece on, with which all of them are on the chip at once (eight requests of 25 to 64 drafts, 4472 to 8192 rows of 8 bits: 1408
+// cut.chunk_piece on, with which all blocks' are on the chip at once, by load_of's count (eight requests of 25 to 64 drafts, 4472 to 8192 rows of 8 bits: 1408
 // keys, which the bounds give, make 536 workgroups, 83 us; 1536 make 504, 69 us).
 // sum(f): of f(blocks, tiles) over the sequences, up to 64 of them.
 template <typename Sum> __host__ __device__ __forceinline__ int chosen_piece(const Cut& cut, Sum sum) {
@@ -1035,11 +1035,15 @@ template <typename Sum> __host__ __device__ __forceinline__ int chosen_piece(con
   for (int i = 0; i < 24 && sum([=](int blocks, int tiles) { return blocks * ((tiles + piece - 1) / piece); }) > cut.places; ++i) piece += (piece + 15) / 16;
   return piece * kChunkKeys;
 }
-// A sequence's blocks, of all kv-heads, and their 64-key tiles.
+// A sequence's blocks, of all kv-heads, and 64-key tiles of the one with most: the last one, or under a window, where that is short, the one in
+// front of it.  The others count as much, so the pieces may be longer than they need to be (causal blocks in front see fewer keys), or a few more than the
+// places (blocks begin elsewhere in a granule); workgroups for few rows in the same launch are not counted.
 struct Load { int blocks, tiles; };
 __host__ __device__ __forceinline__ Load load_of(const Paged& P, const Sight& V, const Seq& s, int prefix, int G, int few) {
-  const int R = s.nq * G, blocks = row_blocks<kChunkRows>(s.nq, G, few);
-  const int tiles = (Keys<true>(V, s, prefix, (R > 1 ? R - 1 : 0) / kChunkRows * kChunkRows / G, s.nq - 1).end + kChunkKeys - 1) / kChunkKeys;
+  const int R = s.nq * G, blocks = row_blocks<kChunkRows>(s.nq, G, few), last = (R > 1 ? R - 1 : 0) / kChunkRows * kChunkRows;
+  const int end = Keys<true>(V, s, prefix, last / G, s.nq - 1).end;
+  const int before = last ? Keys<true>(V, s, prefix, (last - kChunkRows) / G, (last - 1) / G).end : 0;
+  const int tiles = ((end > before ? end : before) + kChunkKeys - 1) / kChunkKeys;
   return {blocks * P.H, tiles};
 }
 __device__ __forceinline__ int chunk_piece(const PagedAttnArgs& A, const Cut& cut, int lane) {

@@ -84,3 +84,12 @@ def test_a_workspace_of_4_bit_pages_serves_every_window_and_cap(hq, hkv, d):
                 args = (r(pages), r(b), r(P._Scores(0.125, cap, None, None, None)), s if s is None else r(s), hq, r(rows), at, None, at)
                 assert lib.arkv_packed_attention(*args, 0, None) == A.EINVAL
                 assert lib.arkv_packed_attention(*args, n.value, None) in (A.EHIP, A.EUNSUPPORTED), (batch, n_tokens, max_q, max_kv, window, cap)
+
+
+@pytest.mark.parametrize("q,kv,hq,hkv,d,bits,window", [
+    ([3, 46, 1, 40, 494, 14, 1917], [3514, 6832, 157, 3426, 7817, 1857, 4591], 24, 8, 128, 8, 1990), ([3, 10, 2478], [1875, 6397, 4064], 32, 8, 64, 8, 536),
+    ([2196, 60, 101, 181], [9849, 3010, 7089, 1188], 24, 8, 64, 4, 1413), ([129] * 40, [5000] * 40, 4, 4, 128, 16, 1600)])
+def test_a_short_last_block_does_not_decide_for_those_before_it(q, kv, hq, hkv, d, bits, window):
+    """Under a window a sequence's last block, of few tokens, has fewer keys than the others: they do not become two pieces each beyond the places."""
+    c = cut(q, kv, hq, hkv, d, bits, window=window, sink=4)
+    assert c.places and c.workgroups <= c.places
