@@ -34,7 +34,7 @@ class DraftedLayer:
         self.rotary = P.arkv_rotary(10000.0 ** (-torch.arange(half, dtype=torch.float64, device=device) / half))
         self.table = torch.randperm(n_requests * width, generator=g, device=device).to(torch.int32).reshape(n_requests, width)
         self.have = [0] * n_requests                   # accepted rows
-        self.drafted = None                            # the round's keys and values, until some of them are accepted
+        self.drafted = None                            # the round's keys, values and trees, until some of them are accepted
         lengths = torch.zeros(n_requests + 1, dtype=torch.int32, device=device)
         largest = P.arkv_page_batch(lengths, lengths[1:], self.table, n_requests * max_tokens, max_tokens, rows)
         self.workspace = P.arkv_packed_workspace(self.pages, largest, n_q_heads)       # serves every smaller batch
@@ -60,6 +60,7 @@ class DraftedLayer:
     def prompt(self, x, q_len):
         """x [sum(q_len)][hidden], request after request: accepted tokens, each of which sees those before it."""
         y, _, _ = self._step(x, q_len, [h + i for h, a in zip(self.have, q_len) for i in range(a)], None)
+        self.drafted = None                            # (of a round that nothing was accepted of: the prompt's rows are in its place)
         self.have = [h + a for h, a in zip(self.have, q_len)]
         return y
 
@@ -79,13 +80,22 @@ class DraftedLayer:
             bits += [[w - (1 << 64) if w >> 63 else w for w in (s >> 64 * j & (1 << 64) - 1 for j in range(words))] for s in seen]
         tree = torch.tensor(bits, dtype=torch.int64, device=self.device).reshape(-1, words)
         y, k, v = self._step(x, q_len, [h + i for h, at in zip(self.have, depth) for i in at], tree)
-        self.drafted = (k, v, q_len)
+        self.drafted = (k, v, [list(p) for p in parents])
         return y
 
     def accept(self, paths):
-        """The drafts of every request that are accepted, from the accepted rows on: their rows take the drafts' place."""
-        k, v, q_len = self.drafted
-        self.drafted = None
+        """The drafts of every request that are accepted, from the accepted rows on, each following the one before it: their rows take
+        the drafts' place."""
+        if self.drafted is None:
+            raise ValueError("nothing is drafted")
+        k, v, parents = self.drafted
+        if len(paths) != len(parents):
+            raise ValueError(f"{len(paths)} paths for {len(parents)} requests")
+        for path, p in zip(paths, parents):
+            for at, i in zip([-1, *path], path):
+                if not 0 <= i < len(p) or p[i] != at:
+                    raise ValueError(f"path {path}: draft {i} does not follow {at}")
+        self.drafted, q_len = None, [len(p) for p in parents]
         picked = torch.tensor([sum(q_len[:r]) + i for r, path in enumerate(paths) for i in path], dtype=torch.int64, device=self.device)
         counts = [len(p) for p in paths]
         positions = torch.tensor([[h + i for h, a in zip(self.have, counts) for i in range(a)]], dtype=torch.int32, device=self.device)
