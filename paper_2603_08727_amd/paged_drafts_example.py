@@ -66,7 +66,7 @@ class DraftedLayer:
 
     def draft(self, x, parents):
         """A tree of drafted tokens of every request: parents[r][i] is the draft that draft i follows, -1 the accepted rows.  The layer's
-        output for each; nothing is accepted yet."""
+        output for each; nothing is accepted yet.  A window counts from a draft's place but takes no drafts away: trees are less deep than it."""
         q_len, depth, bits = [len(p) for p in parents], [], []
         words = max(1, -(-max(q_len) // 64))
         for p in parents:
@@ -76,6 +76,8 @@ class DraftedLayer:
                     raise ValueError(f"draft {i} follows {up}: one before it, or -1")
                 seen.append((seen[up] if up >= 0 else 0) | 1 << i)
                 at.append(at[up] + 1 if up >= 0 else 0)
+                if 0 < self.window <= at[i]:
+                    raise ValueError(f"draft {i} follows {at[i]} others: its window of {self.window} would end within them")
             depth.append(at)
             bits += [[w - (1 << 64) if w >> 63 else w for w in (s >> 64 * j & (1 << 64) - 1 for j in range(words))] for s in seen]
         tree = torch.tensor(bits, dtype=torch.int64, device=self.device).reshape(-1, words)

@@ -28,3 +28,11 @@ def test_drafts_are_accepted_once():
     assert x.have == [40, 7]
     with pytest.raises(ValueError, match="drafted"):
         x.accept([[], []])
+
+
+def test_trees_that_reach_behind_the_window_are_refused():
+    """A window takes no drafts away: a draft at its depth would see a first one, which decoding would not."""
+    x = layer(window=3)
+    with pytest.raises(ValueError, match="window"):
+        x.draft(None, [[-1, 0, 1, 2], [-1]])
+    assert x.have == [40, 7] and x.drafted is not None
