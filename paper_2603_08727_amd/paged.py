@@ -244,8 +244,15 @@ def _rows(to, t, n, pages, what):
     raise ValueError(f"{what}: expected {pages.dtype} [{n}][heads][{pages.d}] on {pages.device}, got {t.dtype} {tuple(shape)} on {t.device}")
 
 
-def _current(pages, batch):
+def _kind(pages, kind):
+    """A struct of the other kind of pages would be read with its fields moved."""
+    if not isinstance(pages, kind):
+        raise ValueError(f"pages: expected {kind.__name__}, got {type(pages).__name__}")
+
+
+def _current(pages, batch, kind):
     """Handle of torch's current stream on the device where everything has to be."""
+    _kind(pages, kind)
     at = pages.index
     if batch.index != at or at != _b._device():
         raise ValueError(f"pages on {pages.device}, batch on {batch.device}: both must be on the current device")
@@ -269,6 +276,7 @@ def _check(rc, name):
 
 def arkv_paged_workspace_bytes(pages, batch, n_q_heads):
     """Bytes of workspace that the calls below need for this batch, or any with no more sequences, tokens, new tokens or rows."""
+    _kind(pages, arkv_pages)
     n = C.c_size_t()
     _check((_lib or load()).arkv_paged_workspace(pages.ref, batch.ref, n_q_heads, C.addressof(n)), "arkv_paged_workspace")
     return n.value
@@ -303,7 +311,7 @@ def _append(name, torch, stream, pages, batch, rotary, q, k, v, positions, q_out
 def arkv_paged_append(pages, batch, rotary, q, k, v, positions, q_out):
     """q [n][H_q][d], k, v [n][H_kv][d] (strided), positions int32 [n_axes][n]; q and q_out may both be None."""
     torch = _TORCH or _torch()
-    _append("arkv_paged_append", torch, _current(pages, batch), pages, batch, rotary, q, k, v, positions, q_out)
+    _append("arkv_paged_append", torch, _current(pages, batch, arkv_pages), pages, batch, rotary, q, k, v, positions, q_out)
 
 
 def _scores(o, pages, batch, hq, scale, cap, slopes, q_pos, prefix):
@@ -325,7 +333,7 @@ def _scores(o, pages, batch, hq, scale, cap, slopes, q_pos, prefix):
 def arkv_paged_attention(pages, batch, q, scale, out, lse=None, cap=0.0, slopes=None, q_pos=None, prefix=None, workspace=None):
     """q [n][H_q][d] (strided), out [n][H_q][d], lse fp32 [n][H_q] or None; the other arguments as arkv_scores."""
     torch = _TORCH or _torch()
-    stream = _current(pages, batch)
+    stream = _current(pages, batch, arkv_pages)
     n, o, at = batch.n_tokens, _own.set, pages.index
     hq = _rows(o.q, q, n, pages, "q")
     ws, size = _workspace(workspace, pages)
@@ -347,7 +355,7 @@ def _sight(sight, pages, batch):
 def arkv_paged_attention_sight(pages, batch, sight, q, scale, out, lse=None, cap=0.0, slopes=None, q_pos=None, prefix=None, workspace=None):
     """arkv_paged_attention with an arkv_sight."""
     torch = _TORCH or _torch()
-    stream = _current(pages, batch)
+    stream = _current(pages, batch, arkv_pages)
     n, o, at = batch.n_tokens, _own.set, pages.index
     hq = _rows(o.q, q, n, pages, "q")
     ws, size = _workspace(workspace, pages)
@@ -361,13 +369,13 @@ def arkv_paged_attention_sight(pages, batch, sight, q, scale, out, lse=None, cap
 def arkv_packed_append(pages, batch, rotary, q, k, v, positions, q_out):
     """arkv_paged_append into packed pages."""
     torch = _TORCH or _torch()
-    _append("arkv_packed_append", torch, _current(pages, batch), pages, batch, rotary, q, k, v, positions, q_out)
+    _append("arkv_packed_append", torch, _current(pages, batch, arkv_packed_pages), pages, batch, rotary, q, k, v, positions, q_out)
 
 
 def arkv_packed_read(pages, batch, k, v):
     """k, v [n][H_kv][d] (out; either may be None): the values of the batch's new tokens' rows."""
     _TORCH or _torch()
-    stream = _current(pages, batch)
+    stream = _current(pages, batch, arkv_packed_pages)
     shape = (batch.n_tokens, pages.H, pages.d)
     k, v = (None if x is None else _dense(x, shape, pages.dtype, what, pages.index) for x, what in ((k, "k"), (v, "v")))
     _check((_lib or load()).arkv_packed_read(pages.ref, batch.ref, k, v, stream), "arkv_packed_read")
@@ -375,6 +383,7 @@ def arkv_packed_read(pages, batch, k, v):
 
 def arkv_packed_workspace_bytes(pages, batch, n_q_heads):
     """Bytes of workspace that arkv_packed_attention needs for this batch, or any with no more sequences, tokens, new tokens or rows."""
+    _kind(pages, arkv_packed_pages)
     n = C.c_size_t()
     _check((_lib or load()).arkv_packed_workspace(pages.ref, batch.ref, n_q_heads, C.addressof(n)), "arkv_packed_workspace")
     return n.value
@@ -391,7 +400,7 @@ def arkv_packed_workspace(pages, batch, n_q_heads):
 def arkv_packed_attention(pages, batch, q, scale, out, lse=None, cap=0.0, slopes=None, q_pos=None, prefix=None, sight=None, workspace=None):
     """arkv_paged_attention over the values of packed rows; sight: an arkv_sight, or None."""
     torch = _TORCH or _torch()
-    stream = _current(pages, batch)
+    stream = _current(pages, batch, arkv_packed_pages)
     n, o, at = batch.n_tokens, _own.set, pages.index
     hq = _rows(o.q, q, n, pages, "q")
     ws, size = _workspace(workspace, pages)
@@ -406,7 +415,7 @@ def arkv_paged_weights(pages, batch, q, scale, lse, decay=1.0, carried=None, cap
                        workspace=None):
     """Adds the tokens' probabilities to pages.weight (decay * carried + sum); carried None: pages.weight itself."""
     torch = _TORCH or _torch()
-    stream = _current(pages, batch)
+    stream = _current(pages, batch, arkv_pages)
     n, o, at = batch.n_tokens, _own.set, pages.index
     hq = _rows(o.q, q, n, pages, "q")
     ws, size = _workspace(workspace, pages)
@@ -420,7 +429,7 @@ def arkv_paged_weights(pages, batch, q, scale, lse, decay=1.0, carried=None, cap
 def arkv_paged_evict(pages, batch, keep, dst_table, kept, new_len, sink=4, recent=32, workspace=None):
     """keep int32 [B], dst_table int32 [B][pages], kept int32 [B][H_kv][max_keep] (out), new_len int32 [B] (out)."""
     torch = _TORCH or _torch()
-    stream = _current(pages, batch)
+    stream = _current(pages, batch, arkv_pages)
     B, at, i32 = batch.B, pages.index, torch.int32
     _need(dst_table.dim() == 2 and kept.dim() == 3, "dst_table: [B][pages]; kept: [B][H_kv][max_keep]")
     _int32(sink=sink, recent=recent)

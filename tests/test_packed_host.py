@@ -204,3 +204,32 @@ def test_every_pair_of_code_and_scale_is_there(bits, d):
     assert len(codes) == len(scale)
     pairs = {(int(s), int(c)) for row, of in zip(codes, scale) for c, s in zip(row, of.repeat_interleave(32 * bits // 8))}
     assert pairs == {(s, c) for s in range(256) for c in range(256)}
+
+
+@pytest.mark.parametrize("hkv", [2, 64, 128])
+def test_each_entry_point_takes_its_own_kind_of_pages(hkv):
+    """A struct of the other kind would be read with its fields moved: 64 kv-heads as 64 channels, the scale bytes as weights."""
+    batch = P._Batch(2, 10, 5, 64, 4, ADDR, ADDR, ADDR)
+    packed = P._Packed(0, 8, 64, 16, hkv, 64, ADDR, ADDR, ADDR, ADDR, ADDR)
+    plain = P._Pages(0, 64, 16, hkv, 64, ADDR, ADDR, ADDR, ADDR)
+
+    class Held:
+        def __init__(self, c):
+            self.c, self.ref, self.index, self.device = c, C.addressof(c), 0, "cuda:0"
+
+    def kind(cls, c):
+        x = cls.__new__(cls)
+        Held.__init__(x, c)
+        return x
+
+    b, pk, pl = Held(batch), kind(P.arkv_packed_pages, packed), kind(P.arkv_pages, plain)
+    for call in [lambda: P.arkv_paged_workspace_bytes(pk, b, 2 * hkv), lambda: P.arkv_paged_workspace(pk, b, 2 * hkv),
+                 lambda: P.arkv_paged_append(pk, b, None, None, None, None, None, None), lambda: P.arkv_paged_attention(pk, b, None, 1.0, None),
+                 lambda: P.arkv_paged_attention_sight(pk, b, None, None, 1.0, None), lambda: P.arkv_paged_weights(pk, b, None, 1.0, None),
+                 lambda: P.arkv_paged_evict(pk, b, None, None, None, None),
+                 lambda: P.arkv_packed_workspace_bytes(pl, b, 2 * hkv), lambda: P.arkv_packed_workspace(pl, b, 2 * hkv),
+                 lambda: P.arkv_packed_append(pl, b, None, None, None, None, None, None), lambda: P.arkv_packed_read(pl, b, None, None),
+                 lambda: P.arkv_packed_attention(pl, b, None, 1.0, None)]:
+        with pytest.raises(ValueError, match="pages: expected"):
+            call()
+    assert P.arkv_packed_workspace_bytes(pk, b, 2 * hkv) >= 1 << 16 and P.arkv_paged_workspace_bytes(pl, b, 2 * hkv) >= 1 << 16
