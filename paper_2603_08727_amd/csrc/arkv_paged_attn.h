@@ -1035,15 +1035,13 @@ template <typename Sum> __host__ __device__ __forceinline__ int chosen_piece(con
   for (int i = 0; i < 24 && sum([=](int blocks, int tiles) { return blocks * ((tiles + piece - 1) / piece); }) > cut.places; ++i) piece += (piece + 15) / 16;
   return piece * kChunkKeys;
 }
-// A sequence's blocks, of all kv-heads, and 64-key tiles of the one with most: the last one, or under a window, where that is short, the one in
-// front of it.  The others count as much, so the pieces may be longer than they need to be (causal blocks in front see fewer keys), or a few more than the
-// places (blocks begin elsewhere in a granule); workgroups for few rows in the same launch are not counted.
+// A sequence's blocks, of all kv-heads, and 64-key tiles of its last kChunkRows rows: as many as any block has, also under a window, where a short
+// last block sees fewer, and other blocks begin elsewhere in a granule or a token.  All count as much, so the pieces may be longer than they need to be
+// (causal blocks in front see fewer keys); workgroups for few rows in the same launch are not counted.
 struct Load { int blocks, tiles; };
 __host__ __device__ __forceinline__ Load load_of(const Paged& P, const Sight& V, const Seq& s, int prefix, int G, int few) {
-  const int R = s.nq * G, blocks = row_blocks<kChunkRows>(s.nq, G, few), last = (R > 1 ? R - 1 : 0) / kChunkRows * kChunkRows;
-  const int end = Keys<true>(V, s, prefix, last / G, s.nq - 1).end;
-  const int before = last ? Keys<true>(V, s, prefix, (last - kChunkRows) / G, (last - 1) / G).end : 0;
-  const int tiles = ((end > before ? end : before) + kChunkKeys - 1) / kChunkKeys;
+  const int R = s.nq * G, blocks = row_blocks<kChunkRows>(s.nq, G, few);
+  const int tiles = (Keys<true>(V, s, prefix, (R > kChunkRows ? R - kChunkRows : 0) / G - 16, s.nq - 1).end + kChunkKeys - 1) / kChunkKeys;
   return {blocks * P.H, tiles};
 }
 __device__ __forceinline__ int chunk_piece(const PagedAttnArgs& A, const Cut& cut, int lane) {

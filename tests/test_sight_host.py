@@ -93,3 +93,17 @@ def test_a_short_last_block_does_not_decide_for_those_before_it(q, kv, hq, hkv, 
     """Under a window a sequence's last block, of few tokens, has fewer keys than the others: they do not become two pieces each beyond the places."""
     c = cut(q, kv, hq, hkv, d, bits, window=window, sink=4)
     assert c.places and c.workgroups <= c.places
+
+
+def test_pieces_fit_the_places_wherever_whole_blocks_do():
+    rng, chosen = np.random.default_rng(5), 0
+    for _ in range(6000):
+        B, hkv, G = int(rng.integers(1, 9)), int(rng.choice([1, 2, 4, 8])), int(rng.choice([1, 2, 3, 4, 7, 8]))
+        q = [int(np.exp(rng.uniform(0, np.log(2500)))) for _ in range(B)]
+        kv = [a + int(rng.integers(0, 8000)) for a in q]
+        window = int(rng.integers(0, 2)) * int(np.exp(rng.uniform(3, 8)))
+        c = cut(q, kv, hkv * G, hkv, int(rng.choice([64, 128])), int(rng.choice([16, 8, 4])), window=window, sink=int(rng.integers(0, 70)), tree=bool(rng.integers(0, 2)))
+        if c.places and sum(-(-a * G // 128) * hkv for a in q if a * G > 16) <= c.places:
+            chosen += 1
+            assert c.workgroups <= c.places, (q, kv, hkv, G, window, vars(c))
+    assert chosen > 500
