@@ -302,6 +302,7 @@ int arkv_debug_attention_cut(const arkv_packed_pages* pages, const arkv_page_bat
   TRY(check_scores(scores, S));
   TRY(check_sight(sight, pages->bits, P, S, V));
   if (pages->bits == 16 && !V.window && !V.tree) V = {};           // (arkv_paged_attention's)
+  if (paged_attention_workgroups(P, V, pages->head_dim, n_q_heads) > kMostWorkgroups) return ARKV_EUNSUPPORTED;
   paged_attention_cut(P, S, V, pages->head_dim, n_q_heads, cut);
   return ARKV_OK;
 }
