@@ -87,7 +87,9 @@ typedef struct {
 /* Which slots new token i of sequence b sees, where that is not all up to its own, p = ctx_b + i.  window w > 0: the slots j <= p with
  * j > p - w or j < sink.  tree (DEVICE uint64 [n_tokens][tree_words], 8-byte aligned, 64 tree_words >= max_q): bit t of the token's words says
  * whether it sees new token t, itself among them; the slots below ctx_b it sees all, or with a window as a token at p = ctx_b + (new tokens it
- * sees) - 1 (the window takes no new token away).  Bits from q_len[b] on count for nothing.  A prefix of the scores is seen besides.  All zero: no limits. */
+ * sees) - 1, at ctx_b where it sees none.  The window takes no new token away: a draft that w or more others come before sees first ones that it
+ * would not see once they are accepted, so trees should be less deep than the window.  Bits from q_len[b] on count for nothing.  A prefix of the scores is
+ * seen besides.  All zero: no limits. */
 typedef struct {
   int32_t window, sink, tree_words;
   const uint64_t* tree;
@@ -136,16 +138,17 @@ int arkv_paged_attention(const arkv_pages* pages, const arkv_page_batch* batch, 
 
 /* The same, a token seeing the slots that sight says (NULL: arkv_paged_attention).  What no token of a workgroup sees in front of its window is not
  * read, nor its table entries, whole granules of 16 slots at a time.  The lengths choose how long sequences are cut: a row's last bits may differ with
- * the batch that it is in.  After drafting, the accepted tokens' rows are appended once more, kv_len cut to them: their slots are the first drafts'.
- * ARKV_EINVAL, besides: window or sink negative, tree_words too small, tree not aligned. */
+ * the batch that it is in.  lse is no input for arkv_paged_weights, which knows of no sight.  After drafting, the accepted tokens' rows are appended once
+ * more, kv_len cut to them: their slots are the first drafts'.  ARKV_EINVAL, besides: window or sink negative, tree_words too small, tree not aligned. */
 int arkv_paged_attention_sight(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,
                                const arkv_sight* sight, int32_t n_q_heads, const arkv_rows* q, void* out, float* lse,
                                void* workspace, size_t bytes, void* hip_stream);
 
-/* arkv_paged_append into packed pages.  k is turned in 64 bits, so that a code does not depend on how its angle was rounded; q_out is what
- * arkv_paged_append gives.  A block's s is the smallest from 1 on with max|x| <= 448 (6) times 2^(s - 127); codes are the nearest ones, ties to
- * the even one.  Channels that are not finite, or beyond the type's range once turned, count for nothing in max|x|; with 8 bits they are
- * stored as NaN, with 4 their block is.  Where the nearest code's value would be beyond the type's range, the largest one that is not is stored. */
+/* arkv_paged_append into packed pages.  k is turned in 64 bits, by an angle that is off by 2^-51 of position * freq and a few 2^-53 at most: a code or a
+ * scale is the next one only where the turned key lies that close to a border between them; q_out is what arkv_paged_append gives.  A block's s is the
+ * smallest from 1 on with max|x| <= 448 (6) times 2^(s - 127); codes are the nearest ones, ties to the even one.  Channels that are not finite, or beyond
+ * the type's range once turned, count for nothing in max|x|; with 8 bits they are stored as NaN, with 4 their block is.  Where the nearest code's value
+ * would be beyond the type's range, the largest one that is not is stored. */
 int arkv_packed_append(const arkv_packed_pages* pages, const arkv_page_batch* batch, const arkv_rotary* rotary, int32_t n_q_heads,
                        const arkv_rows* q, const arkv_rows* k, const arkv_rows* v, const int32_t* positions, void* q_out,
                        void* hip_stream);
@@ -166,7 +169,8 @@ int arkv_packed_attention(const arkv_packed_pages* pages, const arkv_page_batch*
 /* weight = decay * carried + sum of exp(x - lse) over the G heads of the row's group and the new tokens that see it, for every slot in
  * use (slots of no sequence are left alone).  carried: DEVICE, laid out as weight; NULL or weight itself: in place; another
  * array: e.g. the weights before drafted tokens that may be rejected.  With decay = 0 carried is not read.  lse DEVICE float [n_tokens][H_q], what
- * arkv_paged_attention returned for the same batch, scores and q.  Pages that several sequences of the batch share would be updated
+ * arkv_paged_attention returned for the same batch, scores and q (one of a call with a sight is accepted, but then rows that the sight hid collect
+ * weight; packed pages keep none).  Pages that several sequences of the batch share would be updated
  * by each: their weight is the last writer's.  Sums are fp32, in an order that the sizes alone fix;
  * terms below 2^-126 count as zero. */
 int arkv_paged_weights(const arkv_pages* pages, const arkv_page_batch* batch, const arkv_scores* scores,

@@ -3,7 +3,8 @@
 // A row's channels lie in blocks of 32 that share a power of two, 2^(s - 127): what a code stands for is exact in the rows' type, so the
 // attention's conversion instructions, which take such scales, add no rounding.  s is the smallest with max|x| <= 448 (6) 2^(s - 127): none of a
 // block saturates.  Codes are rounded once: keys are turned in 64 bits and go to 32 by rounding to odd, which leaves every later comparison and
-// rounding to fewer bits as it would have been from 64.
+// rounding to fewer bits as it would have been from 64.  What is left is the angle's own error: freq / 2 pi and its product with the position are rounded
+// to 64 bits, 2^-51 of the angle, so that a key within that of a border between codes (1e-9 radians at 2^20, 1e-6 at 2^31) may get the next one.
 #include <algorithm>
 #include <type_traits>
 
@@ -233,8 +234,9 @@ __global__ __launch_bounds__(64 * kPackWaves) void k_packed_append(AppendArgs A,
   }
 }
 
-// One wave per token; a lane takes a chunk of codes at a time, kReadRounds of them under way.  Bound by memory (55591 rows of 8 x 128 channels, 8 bits:
-// 77 us, 4.5 TB/s; four tokens a wave, and stores past the caches: 83; 7817 tokens of 4 bits: 15 us, with such stores 26).
+// One wave per token; a lane takes a chunk of codes at a time, up to kReadRounds of them under way.  Bound by memory where there are many (55591 rows of
+// 8 x 128 channels, 8 bits: 77 us, 4.5 TB/s).  A token of 8 x 128 channels of 4 bits is one chunk a lane behind three round trips, and 7817 of them take
+// 15 us where their bytes take 8.  Two changes were measured together, four tokens a wave and stores past the caches: 83 us, and 26; not each by itself.
 constexpr int kReadRounds = 4;
 template <typename T, int D, int BITS>
 __global__ __launch_bounds__(64 * kPackWaves) void k_packed_read(Paged P, PackedArgs X) {

@@ -252,7 +252,8 @@ def _kind(pages, kind):
 
 def _current(pages, batch, kind):
     """Handle of torch's current stream on the device where everything has to be."""
-    _kind(pages, kind)
+    if not isinstance(pages, kind):
+        _kind(pages, kind)
     at = pages.index
     if batch.index != at or at != _b._device():
         raise ValueError(f"pages on {pages.device}, batch on {batch.device}: both must be on the current device")
