@@ -35,7 +35,7 @@ constexpr int kChunkRows = 128, kChunkKeys = 64;
 
 // Waves per SIMD that a build's registers are for, and with that workgroups to a CU.  Single tokens' rows of 4 bits fit three; chunks of such rows at
 // d = 64 do not without spills, which the exponentials of a cap hide (2 x 2048 tokens of 16384, 32 / 8 heads: 663 us with three, 634 with two, with a cap 907
-// and 943; of 8 bits, where three spill less, 660 and 658, 907 and 945).  Cut chunks were not compared: they are planned for the places there are.
+// and 943; of 8 bits, whose three spill 8 to 17 registers, 660 and 658, 907 and 945).  Cut chunks were not compared: they are planned for the places there are.
 __host__ __device__ constexpr int chunk_waves(int D, int bits, bool capped) { return D == 64 && (bits != 4 || capped) ? 3 : 2; }
 __host__ __device__ constexpr int waves_of(int D, int MODE, int KIND, int BITS) {
   return KIND == 2 ? (D == 64 || BITS == 4 ? 3 : 2) : chunk_waves(D, BITS, MODE & 5);
