@@ -53,6 +53,9 @@ def test_refusals_of_the_hook():
         with pytest.raises(A.ArkvError):
             cut(**kw)
     assert P.load().arkv_debug_attention_cut(None, None, None, None, 8, None) == A.EINVAL
+    with pytest.raises(A.ArkvError) as e:               # 2^27 workgroups
+        cut([1] * (1 << 14), [5] * (1 << 14), 16, 16, 128, 8, max_kv=1 << 20)
+    assert e.value.code == A.EUNSUPPORTED
     with pytest.raises(ValueError):
         P.arkv_debug_attention_cut([0, 1], [3, 4], 1, 1, 4, 8, 2, 64, 8)
 
